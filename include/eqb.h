@@ -419,6 +419,123 @@ eqb_status eqb_router_layer_step(const eqb_bf16 *x, const eqb_bf16 *W_r, int64_t
                                  float eta, float c, void *workspace, size_t workspace_bytes,
                                  int32_t *err_flag, void *stream);
 
+/* Balance loss and per-expert counts, with the gradient (the auxiliary loss
+ * alpha sum_e F_e P_e of Sec. 2 as a whole, where gshard_inject_grad adds the
+ * gradient of one form of it).  For microbatch l with n valid tokens (all of
+ * them, or those with a non-zero mask byte):
+ *   f_{l,e} = entries of the valid tokens' lists that name expert e (an entry
+ *             outside [0, E), such as -1, names none),  F_e = f_{l,e} / (K n),
+ *   p_t     = softmax(z_t), or sigmoid(z_t) divided by its sum over the experts,
+ *   loss[l] = (alpha sum_e F_e P_e,  zeta mean_t lse_t^2),
+ *             P_e = mean_t p_{t,e}, lse_t = log sum_e exp(z_{t,e}),
+ * and, F being a constant, the gradient of grad_scale * (the two summed over
+ * the microbatches) with respect to z:
+ *   d_{t,j} = p_j (alpha / n (F_j - sum_e p_e F_e) + 2 zeta / n lse_t)   (softmax)
+ *   d_{t,j} = p_j (1 - s_j) alpha / n (F_j - sum_e p_e F_e)              (sigmoid)
+ * written as grad_out = grad_in + d (grad_out = d without grad_in).  A token
+ * that is masked out contributes nothing, its d is 0 and its row of z is not
+ * read.  A logit of -inf closes its expert to the token (p = 0); a row that is
+ * -inf throughout has p = 0, lse = 0 and d = 0 and still counts in n.  An empty
+ * microbatch has loss 0 and P = 0.
+ * The arithmetic is fp32 (p and lse; the exponentials within a few ulps), F in
+ * whole numbers and fp64; sums over tokens are formed in a fixed order, so the
+ * same call gives the same bits.  The counts need no z, so one pass over it
+ * gives loss and gradient.
+ *   z          device bf16 [T,E], or fp32 with z_fp32 != 0; 16-byte aligned
+ *   topk_idx   device int32 [T,K], e.g. from eqb_route_topk
+ *   mask       device uint8 [T] (nullable)
+ *   score      0 softmax, 1 normalised sigmoid (zeta must then be 0)
+ *   grad_in    device fp32 [T,E], 16-byte aligned (nullable)
+ *   grad_out   device fp32 [T,E], or bf16 with grad_out_bf16 != 0 (rounded to
+ *              nearest even: the operand of eqb_router_grad); 16-byte aligned
+ *              (nullable: no gradient).  May be grad_in where both are fp32.
+ *   grad_scale device fp32 [1] (nullable: 1): a loss scale
+ *   counts     device int32 [M,E] (out, overwritten): f
+ *   prob       device fp32 [M,E] (out, nullable): P
+ *   loss       device fp32 [M,2] (out, nullable)
+ *   workspace  device buffer of eqb_balance_loss_workspace_bytes(T, E, M)
+ *              bytes, 256-byte aligned, needed unless prob, loss and mask are
+ *              all NULL; nothing in it is kept between calls
+ *   err_flag   EQB_ERR_NONFINITE for a NaN (softmax: or +inf) logit of a
+ *              token that counts
+ * Supported: E a multiple of 8 up to 1024, 1 <= K < E, K <= 31, T as above,
+ * 1 <= M <= 2^20. */
+size_t eqb_balance_loss_workspace_bytes(int64_t T, int32_t E, int32_t M);
+eqb_status eqb_balance_loss(const void *z, int32_t z_fp32, const int32_t *topk_idx, int64_t T,
+                            int32_t E, int32_t K, const int64_t *mb_offsets, int32_t M,
+                            const uint8_t *mask, int32_t score, double alpha, double zeta,
+                            const float *grad_in, void *grad_out, int32_t grad_out_bf16,
+                            const float *grad_scale, int32_t *counts, float *prob, float *loss,
+                            void *workspace, size_t workspace_bytes, int32_t *err_flag,
+                            void *stream);
+
+/* Gradients of the router projection z = x W_r^T (eqb_router_logits):
+ *   dx[t, j] = sum_e dz[t, e] W_r[e, j]      (bf16)
+ *   dW[e, j] = sum_t dz[t, e] x[t, j]        (fp32)
+ * from bf16 inputs with fp32 accumulation on the tensor cores (tcgen05).  With
+ * accumulate_dx or accumulate_dW the result is added to what the output holds
+ * (in fp32, dx rounded once).  Either output may be NULL; then it is not
+ * computed.  dW's tokens are summed in parts that depend on T, d, E and the SM
+ * count and the parts in a fixed order: the same call gives the same bits.
+ *   dz         device bf16 [T,E], 16-byte aligned, e.g. from eqb_balance_loss
+ *   x          device bf16 [T,d], 16-byte aligned (not read without dW)
+ *   W_r        device bf16 [E,d], 16-byte aligned (not read without dx)
+ *   dx         device bf16 [T,d], 16-byte aligned
+ *   dW         device fp32 [E,d], 16-byte aligned
+ *   workspace  device buffer of eqb_router_grad_workspace_bytes(T, d, E)
+ *              bytes, 256-byte aligned (dW only; may be NULL where that is 0)
+ *   err_flag   EQB_ERR_CUDA if a kernel's pipeline stalled and it gave up
+ * Supported: d and E as in eqb_router_logits.  T = 0: dx is empty, dW is 0 (or
+ * left as it is with accumulate_dW). */
+size_t eqb_router_grad_workspace_bytes(int64_t T, int32_t d, int32_t E);
+eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16 *W_r, int64_t T,
+                           int32_t d, int32_t E, eqb_bf16 *dx, int32_t accumulate_dx, float *dW,
+                           int32_t accumulate_dW, void *workspace, size_t workspace_bytes,
+                           int32_t *err_flag, void *stream);
+
+/* One AdamW step over many tensors (no counterpart in the paper: it is what
+ * takes the gradients above back into the router and the experts).  For every
+ * element, with g the gradient times grad_scale:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - lr weight_decay) p
+ *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
+ * The arithmetic is fp32, the factors are formed in fp64.  A bf16 parameter is
+ * rounded to nearest once a step (an update below half its last place is
+ * lost: keep an fp32 parameter with a bf16 copy where that matters).
+ * state_bits 32: exp_avg holds m and exp_avg_sq holds v, fp32 [n].
+ * state_bits 8:  exp_avg holds m and exp_avg_sq holds sqrt(v) (whose range is
+ *   half as many powers of two) in e4m3, one byte an element, each block of 256
+ *   consecutive elements with an fp32 scale: the value is code * scale, scale =
+ *   largest magnitude / 448, rounded to nearest even; a root that is not zero
+ *   is not rounded to zero.  avg_scale, sq_scale: fp32 [ceil(n / 256)].  A block
+ *   whose scale would be below 2^-126 is stored as zeros.
+ * Zeroed states (and scales) are those of a first step.
+ *   tensors    host array [count]; read before the call returns.  n >= 0; an
+ *              entry with n = 0 or grad = NULL is left as it is.  Tensors must
+ *              not overlap.  Any element alignment; 16-byte alignment of fp32,
+ *              8 of bf16 and 4 of 8-bit arrays is the fast path.
+ *   grad_scale device fp32 [1] (nullable: 1): a clipping factor or the inverse
+ *              of a loss scale, formed on the device
+ *   err_flag   EQB_ERR_NONFINITE if a parameter or second moment became
+ *              non-finite
+ * Up to 400 tensors share a launch. */
+typedef struct eqb_adamw_tensor {
+  void *param;      /* fp32 or bf16 [n], updated */
+  const void *grad; /* fp32 or bf16 [n] */
+  void *exp_avg;
+  void *exp_avg_sq;
+  float *avg_scale; /* state_bits 8 */
+  float *sq_scale;
+  eqb_bf16 *copy;   /* nullable, with an fp32 param: bf16 [n], the new param rounded */
+  int64_t n;
+  int32_t param_bf16;
+  int32_t grad_bf16;
+} eqb_adamw_tensor;
+eqb_status eqb_adamw_step(const eqb_adamw_tensor *tensors, int32_t count, int32_t state_bits,
+                          double lr, int64_t step, double beta1, double beta2, double eps,
+                          double weight_decay, const float *grad_scale, int32_t *err_flag,
+                          void *stream);
+
 /* Self-test of failure detection (no GPU fault involved): every wait in the
  * library's kernels is a bounded poll of a shared-memory mbarrier, and a
  * kernel whose pipeline stalls gives up, writes EQB_ERR_CUDA to its error

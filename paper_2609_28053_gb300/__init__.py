@@ -25,7 +25,7 @@ import ctypes
 
 import torch
 
-from ._lib import STATUS, EqbError, load
+from ._lib import STATUS, AdamwTensor, EqbError, load
 
 __all__ = [
     "EqbError", "STATUS", "load", "eqb_target_rank", "eqb_route_topk", "eqb_margin_hist_pass1",
@@ -34,7 +34,8 @@ __all__ = [
     "eqb_layer_step", "eqb_layer_step_noalloc", "eqb_router_route", "eqb_router_layer_step",
     "eqb_maxvio", "gshard_inject_grad", "eqb_rank_averaged_bias", "eqb_fixed_hist_bias",
     "eqb_rank_averaged_workspace_bytes", "eqb_selftest_stalled_wait", "lei_coefficients",
-    "eqb_margin_hist_lei",
+    "eqb_margin_hist_lei", "eqb_balance_loss", "eqb_balance_loss_workspace_bytes", "eqb_router_grad",
+    "eqb_router_grad_workspace_bytes", "EqbAdamW",
 ]
 
 
@@ -518,3 +519,178 @@ def eqb_layer_forward(z, b, K, mb_offsets, ws: EqbWorkspace, topk_idx, tau, load
     eqb_margin_hist_pass2(z, tau, ws.u, ws.hist_lo, stream)
     eqb_select_quantile(ws.hist_lo, 2, r, ws.u, ws.rho, ws.q_hat, ws.err, stream)
     eqb_bias_update(ws.q_hat, b_next, stream)
+
+
+def eqb_balance_loss_workspace_bytes(T: int, E: int, M: int) -> int:
+    return int(load().eqb_balance_loss_workspace_bytes(T, E, M))
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def eqb_balance_loss(z, topk_idx, mb_offsets, alpha, zeta=0.0, score="softmax", mask=None, grad_in=None, grad_out=None,
+                     grad_scale=None, counts=None, prob=None, loss=None, workspace=None, err_flag=None, stream=None):
+    """Balance loss, z-loss and per-expert counts of every microbatch, and
+    their gradient, from one pass over z (see eqb.h).  z bf16 or fp32 [T,E];
+    topk_idx int32 [T,K]; mask bool or uint8 [T].  With grad_out (fp32 or bf16
+    [T,E]) the gradient is written as grad_in + grad_scale * d, or without
+    grad_in as grad_scale * d; grad_out may be grad_in.  prob (fp32 [M,E])
+    takes the mean probabilities when given.  Returns (loss fp32 [M,2]: balance
+    loss and z-loss; counts int32 [M,E])."""
+    T, E = z.shape
+    _need(z, torch.float32 if z.dtype is torch.float32 else torch.bfloat16, "z")
+    K = topk_idx.shape[1] if topk_idx.dim() == 2 else 0
+    _need(topk_idx, torch.int32, "topk_idx", (T, K))
+    _need(mb_offsets, torch.int64, "mb_offsets")
+    M = mb_offsets.numel() - 1
+    if score not in _SCORES:
+        raise ValueError(f"score must be one of {sorted(_SCORES)}, got {score!r}")
+    if mask is not None:
+        _need(mask, torch.bool if mask.dtype is torch.bool else torch.uint8, "mask", (T,))
+    _need(grad_in, torch.float32, "grad_in", (T, E))
+    if grad_out is not None:
+        _need(grad_out, torch.bfloat16 if grad_out.dtype is torch.bfloat16 else torch.float32, "grad_out", (T, E))
+    _need(grad_scale, torch.float32, "grad_scale", (1,))
+    if counts is None:
+        counts = torch.empty((M, E), dtype=torch.int32, device=z.device)
+    if loss is None:
+        loss = torch.empty((M, 2), dtype=torch.float32, device=z.device)
+    _need(counts, torch.int32, "counts", (M, E))
+    _need(loss, torch.float32, "loss", (M, 2))
+    _need(prob, torch.float32, "prob", (M, E))
+    if workspace is None:
+        workspace = torch.empty(eqb_balance_loss_workspace_bytes(T, E, M), dtype=torch.uint8, device=z.device)
+    _need(workspace, torch.uint8, "workspace")
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_balance_loss(_p(z), z.dtype is torch.float32, _p(topk_idx), T, E, K, _p(mb_offsets), M, _p(mask),
+                                 _SCORES[score], float(alpha), float(zeta), _p(grad_in), _p(grad_out),
+                                 grad_out is not None and grad_out.dtype is torch.bfloat16, _p(grad_scale), _p(counts),
+                                 _p(prob), _p(loss), _p(workspace), workspace.numel(), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_balance_loss")
+    return loss, counts
+
+
+def eqb_router_grad_workspace_bytes(T: int, d: int, E: int) -> int:
+    return int(load().eqb_router_grad_workspace_bytes(T, d, E))
+
+
+def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulate_dW=False, workspace=None,
+                    err_flag=None, stream=None):
+    """Gradients of eqb_router_logits from dz bf16 [T,E]: dx = dz W_r into dx
+    bf16 [T,d] and dW = dz^T x into dW fp32 [E,d], each where it is given (or
+    added to it, with accumulate_*).  Returns (dx, dW)."""
+    T, E = dz.shape
+    d = W_r.shape[1]
+    _need(dz, torch.bfloat16, "dz")
+    _need(x, torch.bfloat16, "x", (T, d))
+    _need(W_r, torch.bfloat16, "W_r", (E, d))
+    _need(dx, torch.bfloat16, "dx", (T, d))
+    _need(dW, torch.float32, "dW", (E, d))
+    need = eqb_router_grad_workspace_bytes(T, d, E) if dW is not None else 0
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dz.device)
+    _need(workspace, torch.uint8, "workspace")
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_router_grad(_p(dz), _p(x), _p(W_r), T, d, E, _p(dx), bool(accumulate_dx), _p(dW), bool(accumulate_dW),
+                                _p(workspace), 0 if workspace is None else workspace.numel(), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_router_grad")
+    return dx, dW
+
+
+class EqbAdamW:
+    """AdamW over a list of tensors, one launch for up to 400 of them (see
+    eqb_adamw_step in eqb.h).
+
+    params  fp32 or bf16 tensors, contiguous, on one GPU
+    state_bits  32: exp_avg, exp_avg_sq fp32.  8: exp_avg (m) and exp_avg_sq
+            (the root of the second moment) torch.float8_e4m3fn, with an fp32
+            scale for every 256 elements in avg_scale and sq_scale.
+    exp_avg, exp_avg_sq, avg_scale, sq_scale  lists of tensors to keep the
+            states in (continued from a checkpoint, say); zeros when not given
+    copies  bf16 tensors (or None) that receive the new value of the fp32
+            parameter beside them, rounded, e.g. the W_r that the projection
+            reads
+
+    The object holds the tensors; their storage must stay where it is."""
+
+    BLOCK = 256
+
+    def __init__(self, params, state_bits=32, exp_avg=None, exp_avg_sq=None, avg_scale=None, sq_scale=None, copies=None):
+        self.params = list(params)
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.state_bits = state_bits
+        kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        for i, p in enumerate(self.params):
+            if not isinstance(p, torch.Tensor):
+                raise TypeError(f"params[{i}] must be a torch.Tensor")
+            if p.dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError(f"params[{i}] must be torch.float32 or torch.bfloat16, got {p.dtype}")
+            _need(p, p.dtype, f"params[{i}]")
+
+        def own(given, name, shapes, dtype):
+            if given is None:
+                return [torch.zeros(s, dtype=dtype, device=p.device) for p, s in zip(self.params, shapes)]
+            given = list(given)
+            if len(given) != len(self.params):
+                raise ValueError(f"{name} must have {len(self.params)} tensors, got {len(given)}")
+            for i, (t, s) in enumerate(zip(given, shapes)):
+                if t is None:
+                    raise TypeError(f"{name}[{i}] must be a torch.Tensor")
+                _need(t, dtype, f"{name}[{i}]", s)
+            return given
+
+        shapes = [p.shape for p in self.params]
+        self.exp_avg = own(exp_avg, "exp_avg", shapes, kind)
+        self.exp_avg_sq = own(exp_avg_sq, "exp_avg_sq", shapes, kind)
+        self.avg_scale = self.sq_scale = None
+        if state_bits == 8:
+            blocks = [((p.numel() + self.BLOCK - 1) // self.BLOCK,) for p in self.params]
+            self.avg_scale = own(avg_scale, "avg_scale", blocks, torch.float32)
+            self.sq_scale = own(sq_scale, "sq_scale", blocks, torch.float32)
+        elif avg_scale is not None or sq_scale is not None:
+            raise ValueError("avg_scale and sq_scale belong to state_bits=8")
+        self.copies = [None] * len(self.params) if copies is None else list(copies)
+        if len(self.copies) != len(self.params):
+            raise ValueError(f"copies must have {len(self.params)} entries, got {len(self.copies)}")
+        for i, (c, p) in enumerate(zip(self.copies, self.params)):
+            if c is not None and p.dtype is not torch.float32:
+                raise TypeError(f"copies[{i}] is given but params[{i}] is not torch.float32")
+            _need(c, torch.bfloat16, f"copies[{i}]", p.shape)
+        self._held = [t for ts in (self.params, self.exp_avg, self.exp_avg_sq, self.avg_scale or [], self.sq_scale or [],
+                                   [c for c in self.copies if c is not None]) for t in ts]
+        if len({t.device for t in self._held}) > 1:
+            raise ValueError("all tensors must be on one device")
+        self._where = [t.data_ptr() for t in self._held]
+        self._table = (AdamwTensor * len(self.params))()
+        for i, (e, p) in enumerate(zip(self._table, self.params)):
+            e.param, e.n, e.param_bf16 = p.data_ptr(), p.numel(), p.dtype is torch.bfloat16
+            e.exp_avg, e.exp_avg_sq = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
+            if state_bits == 8:
+                e.avg_scale, e.sq_scale = self.avg_scale[i].data_ptr(), self.sq_scale[i].data_ptr()
+            e.copy = _p(self.copies[i])
+
+    def step(self, grads, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, grad_scale=None, err_flag=None,
+             stream=None):
+        """One step (step = 1 for the first) with `grads`, a list of fp32 or
+        bf16 tensors of the parameters' shapes; a parameter whose entry is
+        None is left as it is.  grad_scale: fp32 CUDA tensor [1] that every
+        gradient is multiplied by."""
+        if len(grads) != len(self.params):
+            raise ValueError(f"grads must have {len(self.params)} entries, got {len(grads)}")
+        if [t.data_ptr() for t in self._held] != self._where:
+            raise ValueError("a parameter or state tensor has moved to another storage: make a new EqbAdamW")
+        for i, (e, g, p) in enumerate(zip(self._table, grads, self.params)):
+            if g is None:
+                e.grad = None
+                continue
+            bf16 = g.dtype is torch.bfloat16
+            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]", p.shape)
+            if g.device != p.device:
+                raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
+            e.grad, e.grad_bf16 = g.data_ptr(), bf16
+        _need(grad_scale, torch.float32, "grad_scale", (1,))
+        _need(err_flag, torch.int32, "err_flag")
+        _check(load().eqb_adamw_step(self._table, len(self.params), self.state_bits, float(lr), int(step), float(beta1),
+                                     float(beta2), float(eps), float(weight_decay), _p(grad_scale), _p(err_flag),
+                                     _stream(stream)), "eqb_adamw_step")

@@ -20,10 +20,20 @@ EXPORTS = (
     "eqb_router_layer_step", "eqb_maxvio", "gshard_inject_grad",
     "eqb_rank_averaged_bias", "eqb_fixed_hist_bias", "eqb_rank_averaged_workspace_bytes",
     "eqb_selftest_stalled_wait", "lei_coefficients", "eqb_margin_hist_lei", "eqb_route_hist_fused",
+    "eqb_balance_loss_workspace_bytes", "eqb_balance_loss", "eqb_router_grad_workspace_bytes",
+    "eqb_router_grad", "eqb_adamw_step",
 )
 
 STATUS = {0: "EQB_OK", 1: "EQB_ERR_INVALID_ARG", 2: "EQB_ERR_UNSUPPORTED", 3: "EQB_ERR_CUDA",
           4: "EQB_ERR_NONFINITE", 5: "EQB_ERR_RANK"}
+
+class AdamwTensor(ctypes.Structure):
+    """eqb_adamw_tensor of eqb.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("avg_scale", ctypes.c_void_p), ("sq_scale", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("n", ctypes.c_int64), ("param_bf16", ctypes.c_int32),
+                ("grad_bf16", ctypes.c_int32)]
+
 
 _lock = threading.Lock()
 _lib = None
@@ -49,6 +59,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
                 "(python -m paper_2609_28053_gb300.build); there is no CPU fallback")
         lib = ctypes.CDLL(p)
         P, i64, i32, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
+        f64, size = ctypes.c_double, ctypes.c_size_t
         sigs = {
             "eqb_route_topk": [P, P, i64, i32, i32, P, i32, P, P, P, P, P, P],
             "eqb_margin_hist_pass1": [P, P, i64, i32, P, P, P],
@@ -72,6 +83,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                ctypes.c_size_t, P, P],
             "eqb_layer_step_noalloc": [P, P, i64, i32, i32, P, P, i32, i64, P, P, P, P, P, f32,
                                        f32, P, P],
+            "eqb_balance_loss": [P, i32, P, i64, i32, i32, P, i32, P, i32, f64, f64, P, P, i32, P, P, P, P,
+                                 P, size, P, P],
+            "eqb_router_grad": [P, P, P, i64, i32, i32, P, i32, P, i32, P, size, P, P],
+            "eqb_adamw_step": [P, i32, i32, f64, i64, f64, f64, f64, f64, P, P, P],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -85,6 +100,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eqb_layer_workspace_bytes.restype = ctypes.c_size_t
         lib.eqb_rank_averaged_workspace_bytes.argtypes = [i32, i32]
         lib.eqb_rank_averaged_workspace_bytes.restype = ctypes.c_size_t
+        lib.eqb_balance_loss_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.eqb_balance_loss_workspace_bytes.restype = size
+        lib.eqb_router_grad_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.eqb_router_grad_workspace_bytes.restype = size
         lib.eqb_target_rank.argtypes = [i64, i32, i32]
         lib.eqb_target_rank.restype = i64
         if path is None:

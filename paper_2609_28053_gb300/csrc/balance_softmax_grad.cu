@@ -1,0 +1,8 @@
+// balance_softmax_grad.cu -- instances of the balance loss's pass over z.
+#include "balance.cuh"
+
+namespace eqb {
+
+int launch_balance_softmax_grad(const BalanceArgs& a, int64_t tpc, cudaStream_t s) { return launch_bal_type<false, true>(a, tpc, s); }
+
+}  // namespace eqb

@@ -208,4 +208,79 @@ int launch_router_route(const uint16_t* x, const uint16_t* W, int64_t T, int d, 
                         const int64_t* off, int M, uint16_t* z, int32_t* idx, float* tau, int32_t* loads,
                         int32_t* hist, int32_t* err, bool split, cudaStream_t s);
 
+// The balance loss (balance.cu, balance.cuh).
+struct BalanceArgs {
+  const void* z;  // bf16, or fp32 with z_fp32
+  int z_fp32;
+  const int32_t* idx;
+  int64_t T;
+  int E, K;
+  const int64_t* off;
+  int M;
+  const uint8_t* mask;  // nullable: all tokens count
+  int sigmoid;
+  double alpha, zeta;
+  const float* grad_in;  // nullable
+  void* grad_out;        // nullable; fp32, or bf16 with grad_bf16
+  int grad_bf16;
+  const float* grad_scale;  // nullable: 1
+  int32_t* counts;
+  float* prob;  // nullable
+  float* loss;  // nullable
+  float* part;  // rows of a block's sums (loss or prob): sum of p.R, of lse^2, rows alive, unused, then E of p
+  int row;      // floats in a row: E + 4
+  int32_t* valid;  // [M]: valid tokens (mask)
+  int32_t* err;
+};
+constexpr int kBalMaxGrid = 2048;  // most blocks of the pass over z
+constexpr size_t balance_part_bytes(int E, int M) {
+  return carve_round((static_cast<size_t>(kBalMaxGrid) + static_cast<size_t>(M)) * (static_cast<size_t>(E) + 4) * 4);
+}
+int launch_balance(BalanceArgs a, cudaStream_t s);
+// the pass over z, its instances each in their own file
+int launch_balance_softmax_value(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
+int launch_balance_softmax_grad(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
+int launch_balance_sigmoid_value(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
+int launch_balance_sigmoid_grad(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
+
+// One tensor of an AdamW step (adamw.cu).
+struct AdamwTensor {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;    // the second moment, in 8 bits its root
+  float* ms;  // scales of m and v (8 bits)
+  float* vs;
+  uint16_t* copy;  // nullable: bf16 copy of an fp32 p
+  int64_t n;
+  int32_t flags;  // 1: p is bf16, 2: g is bf16, 4: every pointer is aligned for the wide loads
+};
+struct AdamwScalars {
+  float b1, c1, b2, c2;  // beta1, 1 - beta1, beta2, 1 - beta2
+  float rbc2, eps, decay, step;
+  const float* grad_scale;  // nullable: 1
+  int32_t* err;
+};
+// Tensors of a launch: its parameters, 32,764 bytes at most, hold 76 a tensor.
+constexpr int kAdamwBatch = 400;
+int launch_adamw(const AdamwTensor* t, int count, int bits, const AdamwScalars& sc, cudaStream_t s);
+
+// The projection's gradients (router_grad.cu); workspace of
+// router_grad_workspace(T, d, E) bytes.
+struct RouterGradArgs {
+  const uint16_t* dz;
+  const uint16_t* x;
+  const uint16_t* W;
+  int64_t T;
+  int d, E;
+  uint16_t* dx;  // nullable
+  int add_dx;
+  float* dW;  // nullable
+  int add_dW;
+  float* part;
+  int32_t* err;
+};
+size_t router_grad_workspace(int64_t T, int d, int E);
+int launch_router_grad(const RouterGradArgs& a, cudaStream_t s);
+
 }  // namespace eqb

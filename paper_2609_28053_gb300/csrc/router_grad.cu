@@ -1,0 +1,535 @@
+// router_grad.cu -- the gradients of the router projection z = x W_r^T:
+//   dx = dz W_r   [T,d] bf16,      dW = dz^T x   [E,d] fp32,
+// on the tensor cores (tcgen05, fp32 accumulators in tensor memory).
+//
+// Both products are as large as the forward one (2 T d E flops beside T d
+// bf16 values read or written): at E = 256 the tensor cores and the memory need
+// about the same time, below that memory bounds them.  W_r, x and, for dW, dz
+// are stored with the dimension that is summed over as the slow one, so they
+// enter the MMAs as MN-major operands: a tile of 64 columns (one 128-byte
+// swizzle atom) x R rows as TMA writes it, its 8-row groups 1 KiB apart, the
+// next 64 columns one tile further.
+//
+// dx: a block keeps a slab of W_r (all E rows, N columns) in shared memory and
+// runs over tiles of 128 tokens; dz streams through a ring of [128 x 64]
+// stages, two accumulators alternate, and four warps round the accumulators to
+// bf16 into swizzled staging tiles that TMA stores as whole lines.
+// dW: a block has all experts x N columns of d and a part of the tokens; dz and
+// x stream through one ring, 64 tokens a stage, and x is read by one block only.
+// With several parts of the tokens their sums are added in order by a second
+// kernel.
+//
+// Roles, bounded waits and the way out of a stall are those of the forward
+// projection: warp 0 loads, warp 1 issues the MMAs, warps 2 to 5 take the
+// accumulators out.
+#include "tcgen05.cuh"
+
+namespace eqb {
+
+namespace {
+
+constexpr int kGradThreads = 192;
+constexpr int kGradCtas = 152;            // blocks of a dW grid: one an SM
+constexpr uint32_t kTile64 = 64 * 128;    // bytes of 64 rows of 64 bf16
+constexpr uint32_t kDzStage = 128 * 128;  // dx: 128 tokens x 64 experts
+constexpr uint32_t kStaging = 32 * 128;   // dx: a warp's 32 rows x 64 columns
+
+// Shared-memory descriptor of an MN-major operand in 128-byte swizzled rows:
+// `lead` bytes between tiles of 64 columns, 1 KiB between groups of 8 rows.
+__device__ __forceinline__ uint64_t mn128_desc(uint32_t saddr, uint32_t lead) {
+  uint64_t d = static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(lead >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;
+  return d;
+}
+constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: A, B are MN-major
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(src), "r"(c0), "r"(c1)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+struct DxArgs {
+  int T, d, E, N, slabs, ntiles, S;
+  uint16_t* dx;  // read where add
+  int add;
+  int32_t* err;
+};
+
+__global__ void __launch_bounds__(kGradThreads, 1)
+    router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
+                     const __grid_constant__ CUtensorMap tmo, DxArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  const int S = a.S, E = a.E, KC = (E + 63) / 64;
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* sm = smem_raw + (base - raw);
+  const uint32_t wtile = static_cast<uint32_t>(E) * 128u;  // bytes of W's E rows x 64 columns
+  const uint32_t wbytes = wtile * static_cast<uint32_t>(a.N / 64);
+  const uint32_t ring = base + wbytes;
+  const uint32_t stag = ring + static_cast<uint32_t>(S) * kDzStage;
+  const uint32_t bars = stag + 8u * kStaging;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (S + s); };
+  auto accf = [&](int b) { return bars + 8u * (2 * S + b); };
+  auto acce = [&](int b) { return bars + 8u * (2 * S + 2 + b); };
+  const uint32_t wfull = bars + 8u * (2 * S + 4), wempty = wfull + 8u, drain = wfull + 16u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8u * (2 * S + 7));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  int* issued = reinterpret_cast<int*>(tmem_holder + 2);  // loads of dz, of W
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf(b), 1);
+      mbar_init(acce(b), 128);
+    }
+    mbar_init(wfull, 1);
+    mbar_init(wempty, 1);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    issued[0] = issued[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  griddep_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  // items (slab, tile), slab-major; a block has a contiguous range of them
+  const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
+  const int64_t i0 = items * blockIdx.x / gridDim.x, i1 = items * (blockIdx.x + 1) / gridDim.x;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0, n = 0, nw = 0, slab = -1;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int64_t i = i0; i < i1 && ok; ++i) {
+        const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+        if (sl != slab) {
+          slab = sl;
+          if (!mbar_wait(wempty, (static_cast<uint32_t>(nw) & 1u) ^ 1u, abort_flag)) break;
+          const int chunks = min(a.N, a.d - sl * a.N) / 64;
+          mbar_expect_tx(wfull, wtile * static_cast<uint32_t>(chunks));
+          for (int c = 0; c < chunks; ++c)
+            tma_load_2d(base + wtile * static_cast<uint32_t>(c), &tmw, wfull, sl * a.N + c * 64, 0);
+          ++nw;
+        }
+        for (int kc = 0; kc < KC; ++kc, ++n) {
+          if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+          mbar_expect_tx(full(stage), kDzStage);
+          tma_load_2d(ring + static_cast<uint32_t>(stage) * kDzStage, &tmz, full(stage), kc * 64, tile * kBM);
+          if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
+      }
+      issued[0] = n;
+      issued[1] = nw;
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int stage = 0, nw = 0, slab = -1, it = 0;
+      uint32_t phase = 0, idesc = 0;
+      bool ok = true;
+      for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
+        const int sl = static_cast<int>(i / a.ntiles);
+        if (sl != slab) {
+          if (slab >= 0) umma_commit(wempty);  // the slab may be replaced once its MMAs are done
+          slab = sl;
+          if (!mbar_wait(wfull, static_cast<uint32_t>(nw) & 1u, abort_flag)) break;
+          tc_fence_after();
+          ++nw;
+          idesc = umma_idesc_bf16(kBM, min(a.N, a.d - sl * a.N)) | kMnB;
+        }
+        const int buf = it & 1;
+        if (!mbar_wait(acce(buf), (static_cast<uint32_t>(it >> 1) & 1u) ^ 1u, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t dt = tmem + static_cast<uint32_t>(buf * 256);
+        for (int kc = 0; kc < KC; ++kc) {
+          if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t ad = sw128_desc(ring + static_cast<uint32_t>(stage) * kDzStage);
+          const int steps = min(4, (E - kc * 64) / 16);
+          for (int kk = 0; kk < steps; ++kk)
+            umma_bf16(dt, ad + 2u * kk, mn128_desc(base + static_cast<uint32_t>(kc * 64 + kk * 16) * 128u, wtile), idesc,
+                      (kc | kk) != 0 ? 1u : 0u);
+          umma_commit(empty(stage));
+          if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        umma_commit(accf(buf));
+      }
+      umma_commit(drain);
+      for (uint32_t i = 0; i < kSpinLimit; ++i)
+        if (mbar_try_wait(drain, 0u)) break;
+    }
+  } else {
+    const int q = warp & 3;
+    const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
+    const uint32_t mine = stag + static_cast<uint32_t>(q) * 2u * kStaging;
+    const uint32_t swz = static_cast<uint32_t>(lane & 7);
+    int it = 0, nstore = 0;
+    // the output's old values, two chunks of 64 columns ahead
+    uint4 old[2][8];
+    auto fetch = [&](int64_t i, int c, uint4 (&o)[8]) {
+      const int sl = static_cast<int>(i / a.ntiles), row = static_cast<int>(i % a.ntiles) * kBM + q * 32 + lane;
+      if (row < a.T) {
+        const uint4* src = reinterpret_cast<const uint4*>(a.dx + static_cast<size_t>(row) * a.d + sl * a.N + c * 64);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) o[v] = __ldcs(src + v);
+      }
+    };
+    int64_t have = -1;  // the item whose first two chunks are in `old`
+    for (int64_t i = i0; i < i1; ++i, ++it) {
+      const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+      const int chunks = min(a.N, a.d - sl * a.N) / 64;
+      const int row0 = tile * kBM + q * 32;
+      if (a.add && have != i) {
+        fetch(i, 0, old[0]);
+        if (chunks > 1) fetch(i, 1, old[1]);
+      }
+      const bool ahead = a.add && chunks % 2 == 0 && i + 1 < i1 && static_cast<int>((i + 1) / a.ntiles) == sl;
+      const int buf = it & 1;
+      if (!__all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag))) break;
+      tc_fence_after();
+      for (int c0 = 0; c0 < chunks; c0 += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = c0 + h;
+          if (c >= chunks) break;
+          uint32_t p[32];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t r[32];
+            tmem_ld32(tmem + lane_base + static_cast<uint32_t>(buf * 256 + c * 64 + half * 32), r);
+            if (a.add) {
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                const uint32_t w[4] = {old[h][4 * half + v].x, old[h][4 * half + v].y, old[h][4 * half + v].z,
+                                       old[h][4 * half + v].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  r[8 * v + 2 * k] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k]) + bf16_lo(w[k]));
+                  r[8 * v + 2 * k + 1] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k + 1]) + bf16_hi(w[k]));
+                }
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              p[16 * half + k] = pack_bf16x2_rn(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+          }
+          if (a.add) {
+            if (c + 2 < chunks) fetch(i, c + 2, old[h]);
+            else if (ahead) fetch(i + 1, h, old[h]);
+          }
+          if (c == chunks - 1) {  // the accumulator is read
+            tc_fence_before();
+            mbar_arrive(acce(buf));
+          }
+          // the store that used this staging tile two stores ago has read it
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          __syncwarp();
+          const uint32_t dst = mine + static_cast<uint32_t>(nstore & 1) * kStaging;
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + static_cast<uint32_t>(lane) * 128u +
+                                                                          ((static_cast<uint32_t>(v) ^ swz) << 4)),
+                         "r"(p[4 * v]), "r"(p[4 * v + 1]), "r"(p[4 * v + 2]), "r"(p[4 * v + 3])
+                         : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
+          ++nstore;
+        }
+      }
+      if (ahead) have = i + 1;
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) {
+    drain_loads(issued[0], S, full);
+    drain_loads(issued[1], 1, [&](int) { return wfull; });
+    raise_flag(a.err, kErrCuda);
+  }
+}
+
+struct DwArgs {
+  int T, d, E, N, tiles, parts, S;
+  int64_t stages;  // of 64 tokens, in all
+  float* out;      // dW, or the parts' sums [parts, E, d]
+  int add;         // one part only: out += (dW)
+  int32_t* err;
+};
+
+__global__ void __launch_bounds__(kGradThreads, 1)
+    router_dw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmx, DwArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  const int S = a.S, MT = a.E > 128 ? 2 : 1;
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* sm = smem_raw + (base - raw);
+  const uint32_t a_bytes = static_cast<uint32_t>(2 * MT) * kTile64;
+  const uint32_t stage_bytes = a_bytes + static_cast<uint32_t>(a.N / 64) * kTile64;
+  const uint32_t bars = base + static_cast<uint32_t>(S) * stage_bytes;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (S + s); };
+  const uint32_t accf = bars + 8u * (2 * S), drain = accf + 8u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8u * (2 * S + 2));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  int* issued = reinterpret_cast<int*>(tmem_holder + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    mbar_init(accf, 1);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    *issued = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  griddep_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  const int tile = static_cast<int>(blockIdx.x) % a.tiles, part = static_cast<int>(blockIdx.x) / a.tiles;
+  const int64_t s0 = a.stages * part / a.parts, s1 = a.stages * (part + 1) / a.parts;
+  const int j0 = tile * a.N, nn = min(a.N, a.d - j0);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0, n = 0;
+      uint32_t phase = 0;
+      const uint32_t bytes = a_bytes + static_cast<uint32_t>(nn / 64) * kTile64;
+      for (int64_t k = s0; k < s1; ++k, ++n) {
+        if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) break;
+        const uint32_t dst = base + static_cast<uint32_t>(stage) * stage_bytes;
+        const int t = static_cast<int>(k * 64);
+        mbar_expect_tx(full(stage), bytes);
+        // experts past E (and tokens past T) are filled with zeros
+        for (int c = 0; c < 2 * MT; ++c) tma_load_2d(dst + static_cast<uint32_t>(c) * kTile64, &tmz, full(stage), c * 64, t);
+        for (int c = 0; c < nn / 64; ++c)
+          tma_load_2d(dst + a_bytes + static_cast<uint32_t>(c) * kTile64, &tmx, full(stage), j0 + c * 64, t);
+        if (++stage == S) { stage = 0; phase ^= 1u; }
+      }
+      *issued = n;
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_bf16(kBM, nn) | kMnA | kMnB;
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int64_t k = s0; k < s1; ++k) {
+        if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sa = base + static_cast<uint32_t>(stage) * stage_bytes;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)  // 16 tokens per MMA
+          for (int m = 0; m < MT; ++m)
+            umma_bf16(tmem + static_cast<uint32_t>(m * a.N),
+                      mn128_desc(sa + static_cast<uint32_t>(m) * 2u * kTile64 + kk * 2048u, kTile64),
+                      mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k > s0 || kk > 0 ? 1u : 0u);
+        umma_commit(empty(stage));
+        if (++stage == S) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) umma_commit(accf);
+      umma_commit(drain);
+      for (uint32_t i = 0; i < kSpinLimit; ++i)
+        if (mbar_try_wait(drain, 0u)) break;
+    }
+  } else {
+    const int q = warp & 3;
+    if (__all_sync(0xffffffffu, mbar_wait(accf, 0u, abort_flag))) {
+      tc_fence_after();
+      for (int m = 0; m < MT; ++m) {
+        const int e = m * 128 + q * 32 + lane;
+        float* out = a.out + (static_cast<size_t>(part) * a.E + e) * a.d + j0;
+        for (int c = 0; c < nn; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(m * a.N + c), r);
+          if (e < a.E) {
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+              float4 o = make_float4(__uint_as_float(r[4 * v]), __uint_as_float(r[4 * v + 1]), __uint_as_float(r[4 * v + 2]),
+                                     __uint_as_float(r[4 * v + 3]));
+              float4* dst = reinterpret_cast<float4*>(out + c) + v;
+              if (a.add) {
+                const float4 w = *dst;
+                o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w;
+              }
+              *dst = o;
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) {
+    drain_loads(*issued, S, full);
+    raise_flag(a.err, kErrCuda);
+  }
+}
+
+// dW (+)= the parts' sums, in ascending order; n a multiple of 4.
+__global__ void __launch_bounds__(256) router_dw_sum_kernel(const float* part, int parts, int64_t n, float* dW, int add) {
+  griddep_wait();
+  const int64_t n4 = n / 4;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n4; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const float4* p = reinterpret_cast<const float4*>(part) + i;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+      const float4 w = __ldcg(p + k * n4);
+      s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
+    }
+    float4* o = reinterpret_cast<float4*>(dW) + i;
+    if (add) {
+      const float4 w = *o;
+      s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
+    }
+    *o = s;
+  }
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(float* p, int64_t n) {
+  griddep_wait();
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256)
+    p[i] = 0.f;
+}
+
+struct DwPlan {
+  int N, tiles, parts;
+  int64_t stages;
+};
+
+// Columns of a dW tile and parts of the tokens: the widest tile that gives
+// every SM a block with at least four stages.
+DwPlan plan_dw(int64_t T, int d, int E) {
+  DwPlan p;
+  p.stages = (T + 63) / 64;
+  const int64_t most = (p.stages + 3) / 4;  // parts
+  for (p.N = 256;; p.N /= 2) {
+    p.tiles = (d + p.N - 1) / p.N;
+    int64_t parts = kGradCtas / p.tiles;
+    if (parts > most) parts = most;
+    p.parts = parts < 1 ? 1 : static_cast<int>(parts);
+    if (p.N == 64 || p.tiles * p.parts >= 120) return p;
+  }
+}
+
+int launch_dx(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
+  if (!allow_smem(router_dx_kernel, di.max_smem_optin)) return kErrCuda;
+  DxArgs a{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, g.dx, g.add_dx, g.err};
+  // narrower slabs while the tiles leave SMs without work
+  for (;; a.N /= 2) {
+    a.slabs = (g.d + a.N - 1) / a.N;
+    if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= di.sm_count) break;
+  }
+  const int extra = 1024 + 8 * kStaging + 8 * (2 * 8 + 7) + 16;
+  const int wbytes = a.E * 128 * (a.N / 64);
+  a.S = (di.max_smem_optin - extra - wbytes) / static_cast<int>(kDzStage);
+  if (a.S > 8) a.S = 8;
+  if (a.S < 2) return kErrUnsupported;
+  CUtensorMap tmz, tmw, tmo;
+  if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
+      !make_map(&tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
+      !make_map(&tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32))
+    return kErrCuda;
+  const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
+  const int grid = items < di.sm_count ? static_cast<int>(items) : di.sm_count;
+  return launch_dependent(router_dx_kernel, dim3(grid), dim3(kGradThreads), wbytes + a.S * kDzStage + extra, s, tmz, tmw, tmo,
+                          a) == cudaSuccess
+             ? kOk
+             : kErrCuda;
+}
+
+int launch_dw(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
+  const int64_t n = static_cast<int64_t>(g.E) * g.d;
+  if (g.T == 0) {
+    if (g.add_dW) return kOk;
+    return launch_dependent(zero_kernel, dim3(static_cast<unsigned>((n + 1023) / 1024)), dim3(256), 0, s, g.dW, n) == cudaSuccess
+               ? kOk
+               : kErrCuda;
+  }
+  if (!allow_smem(router_dw_kernel, di.max_smem_optin)) return kErrCuda;
+  const DwPlan p = plan_dw(g.T, g.d, g.E);
+  DwArgs a{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
+           p.parts > 1 ? 0 : g.add_dW, g.err};
+  const int extra = 1024 + 8 * (2 * 8 + 2) + 16;
+  const int stage_bytes = static_cast<int>(kTile64) * ((g.E > 128 ? 4 : 2) + p.N / 64);
+  a.S = (di.max_smem_optin - extra) / stage_bytes;
+  if (a.S > 8) a.S = 8;
+  if (a.S < 2) return kErrUnsupported;
+  CUtensorMap tmz, tmx;
+  if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), 64) ||
+      !make_map(&tmx, g.x, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 64))
+    return kErrCuda;
+  if (launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), a.S * stage_bytes + extra, s, tmz, tmx,
+                       a) != cudaSuccess)
+    return kErrCuda;
+  if (p.parts == 1) return kOk;
+  int64_t grid = (n / 4 + 255) / 256;
+  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
+  return launch_dependent(router_dw_sum_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, g.part, p.parts, n, g.dW,
+                          g.add_dW) == cudaSuccess
+             ? kOk
+             : kErrCuda;
+}
+
+}  // namespace
+
+size_t router_grad_workspace(int64_t T, int d, int E) {
+  const DwPlan p = plan_dw(T, d, E);
+  return p.parts > 1 ? static_cast<size_t>(p.parts) * E * d * 4 : 0;
+}
+
+int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
+  DeviceInfo di;
+  if (int rc = device_info(&di)) return rc;
+  if (g.dx && g.T > 0)
+    if (int rc = launch_dx(g, di, s)) return rc;
+  if (g.dW)
+    if (int rc = launch_dw(g, di, s)) return rc;
+  return kOk;
+}
+
+}  // namespace eqb
