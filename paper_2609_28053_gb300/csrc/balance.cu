@@ -132,18 +132,15 @@ int launch_balance(BalanceArgs a, cudaStream_t s) {
   }
   if (!a.prob && !a.loss && !a.grad_out) return kOk;
   if (!a.prob && !a.loss) a.part = nullptr;
-  int64_t grid = (a.T + 63) / 64;
-  const int64_t most = di.sm_count * 8 < kBalMaxGrid ? di.sm_count * 8 : kBalMaxGrid;
-  if (grid > most) grid = most;
-  const int64_t tpc = a.T > 0 ? (a.T + grid - 1) / grid : 1;
+  BalanceRun run{1};
   if (a.T > 0) {
-    const int rc = a.sigmoid ? (a.grad_out ? launch_balance_sigmoid_grad(a, tpc, s) : launch_balance_sigmoid_value(a, tpc, s))
-                             : (a.grad_out ? launch_balance_softmax_grad(a, tpc, s) : launch_balance_softmax_value(a, tpc, s));
+    const int rc = a.sigmoid ? (a.grad_out ? launch_balance_sigmoid_grad(a, &run, s) : launch_balance_sigmoid_value(a, &run, s))
+                             : (a.grad_out ? launch_balance_softmax_grad(a, &run, s) : launch_balance_softmax_value(a, &run, s));
     if (rc) return rc;
   }
   if (!a.part) return kOk;
   const dim3 fin(static_cast<unsigned>((a.E + 31) / 32), static_cast<unsigned>(a.M < 4096 ? a.M : 4096));
-  return launch_dependent(balance_finish_kernel, fin, dim3(256), 0, s, a, tpc) == cudaSuccess ? kOk : kErrCuda;
+  return launch_dependent(balance_finish_kernel, fin, dim3(256), 0, s, a, run.tokens_per_cta) == cudaSuccess ? kOk : kErrCuda;
 }
 
 }  // namespace eqb

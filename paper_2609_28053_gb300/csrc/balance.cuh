@@ -1,4 +1,4 @@
-// balance.cuh -- the balance loss with its gradient: what its kernels share.
+// balance.cuh -- the balance loss with its gradient: the pass over z.
 //
 // For the n valid tokens of a microbatch (a token may be masked out) and the
 // counts f_e of its experts' lists, F_e = f_e / (K n):
@@ -10,9 +10,16 @@
 // once they are there a single pass over z gives the loss and the gradient.
 // R_e = F_e - 1/E takes the place of F_e: p.F = p.R + 1/E, and R is formed from
 // an exact whole number, so that balanced counts give exactly 0.
+//
+// The pass is a stream.  Rows lie one after the other, so each warp fetches its
+// groups of up to 32 tokens (z and grad_in) by bulk copies into a ring of its
+// own in shared memory: what is in flight does not depend on registers.  LPT
+// lanes share a token, C chunks of four experts a lane, chunk k at LPT k + sub,
+// so that fp32 and bf16 rows are both read and written in whole lines.
 #pragma once
 
 #include "eqb_device.cuh"
+#include "mbarrier.cuh"
 
 namespace eqb {
 
@@ -20,6 +27,7 @@ namespace {
 
 constexpr int kBalThreads = 256;
 constexpr int kBalWarps = kBalThreads / 32;
+constexpr int kBalMaxStages = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -33,37 +41,129 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return r;
 }
 
+// fp32 min that propagates NaN.
+__device__ __forceinline__ float fmin_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Two fp32 values in one instruction.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float lo2(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v)); }
+__device__ __forceinline__ float hi2(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v >> 32)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 // Sum over the lanes that share `lane & (step - 1)` (step a power of two).
 __device__ __forceinline__ float sum_slots(float x, int step) {
   for (int m = step; m < 32; m <<= 1) x += __shfl_xor_sync(kFull, x, m);
   return x;
 }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// A launch's cut: tokens a block, tokens a group, stages of a warp's ring.
+struct BalanceCut {
+  int64_t tokens_per_cta;
+  int group, stages;
+};
+
+// Blocks an SM holds, by their registers.
+constexpr int bal_blocks(bool sig_grad, int C) { return C <= 2 || (C == 3 && !sig_grad) ? 3 : C <= 4 ? 2 : 1; }
+
+// Shared memory: R [EM], the warps' column sums [8, EM], the rings, the barriers.
+__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM + 4 * kBalWarps * EM; }
+__host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bool gin) {
+  return group * E * ((f32 ? 4 : 2) + (gin ? 4 : 0));
+}
+
 // One block takes a contiguous range of tokens and walks the microbatches in
-// it.  LPT lanes share a token, eight experts a lane and chunk (CPL chunks a
-// lane where E > 256); U tokens a lane are in flight.  The sums of a
-// microbatch's tokens go to the row blockIdx + microbatch of a.part, which no
-// other pair of the two has, and are added up in ascending order by
-// balance_finish: no atomics, so the same call gives the same bits.
-template <bool SIG, bool GRAD, bool F32, int LPT, int CPL>
-__global__ void __launch_bounds__(kBalThreads) balance_kernel(BalanceArgs a, int64_t tokens_per_cta) {
-  constexpr int TPW = 32 / LPT;  // tokens a warp takes at a time
-  constexpr int U = CPL > 1 ? 1 : 2;
-  constexpr int EM = LPT * CPL * 8;  // experts the lanes hold
-  __shared__ __align__(16) float Rs[EM];
-  __shared__ __align__(16) float colsum[kBalWarps][EM];
+// it.  The sums of a microbatch's tokens go to the row blockIdx + microbatch of
+// a.part, which no other pair of the two has, and balance_finish adds them up
+// in ascending order: no atomics, so the same call gives the same bits.
+template <bool SIG, bool GRAD, bool F32, int LPT, int C>
+__global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balance_kernel(BalanceArgs a, BalanceCut cut) {
+  constexpr int TPW = 32 / LPT;    // tokens a warp takes at a time
+  constexpr int EM = LPT * C * 4;  // experts the lanes hold
+  constexpr bool RREG = C <= 4;    // R in registers
+  extern __shared__ __align__(128) uint8_t sm[];
   __shared__ float sums[kBalWarps][3];
+  __shared__ __align__(8) uint64_t bars[kBalWarps * kBalMaxStages];
   __shared__ double inv;  // 1 / (K n E)
   __shared__ float cs[2];
-  const int E = a.E, nch = E >> 3;
-  griddep_wait();
-  const int64_t tb = static_cast<int64_t>(blockIdx.x) * tokens_per_cta;
-  const int64_t te = min(tb + tokens_per_cta, a.T);
-  if (tb >= te) return;
+  __shared__ int aborted;
+  float* Rs = reinterpret_cast<float*>(sm);
+  float* colsum = Rs + EM;
+  const int E = a.E, nch = E >> 2, G = cut.group, D = cut.stages;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int sub = lane & (LPT - 1), slot = lane / LPT;
+  const bool gin = GRAD && a.grad_in;
+  const uint32_t zrow = static_cast<uint32_t>(E) * (F32 ? 4u : 2u), grow = gin ? static_cast<uint32_t>(E) * 4u : 0u;
+  const uint32_t stage_bytes = static_cast<uint32_t>(G) * (zrow + grow);
+  uint8_t* ring = sm + bal_fixed_bytes(EM) + static_cast<size_t>(wid) * D * stage_bytes;
+  const uint32_t ring_s = smem_u32(ring), bar0 = smem_u32(bars + wid * kBalMaxStages);
+  if (lane == 0) {
+    for (int s = 0; s < D; ++s) mbar_init(bar0 + 8u * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (threadIdx.x == 0) aborted = 0;
+  griddep_wait();
+  const int64_t tb = static_cast<int64_t>(blockIdx.x) * cut.tokens_per_cta;
+  const int64_t te = min(tb + cut.tokens_per_cta, a.T);
+  __syncthreads();
+  if (tb >= te) return;
+  // this warp's groups: number j holds the tokens tb + (8 j + wid) G ..
+  const int ngroups = static_cast<int>((te - tb + G - 1) / G);
+  const int nj = ngroups > wid ? (ngroups - wid + kBalWarps - 1) / kBalWarps : 0;
+  auto start = [&](int j) { return tb + (static_cast<int64_t>(j) * kBalWarps + wid) * G; };
+  auto issue = [&](int j, int stage) {
+    if (lane == 0) {
+      const int64_t t0 = start(j);
+      const uint32_t cnt = static_cast<uint32_t>(min(static_cast<int64_t>(G), te - t0));
+      const uint32_t dst = ring_s + static_cast<uint32_t>(stage) * stage_bytes, bar = bar0 + 8u * stage;
+      mbar_expect_tx(bar, cnt * (zrow + grow));
+      bulk_load(dst, static_cast<const uint8_t*>(a.z) + t0 * zrow, cnt * zrow, bar);
+      if (gin) bulk_load(dst + static_cast<uint32_t>(G) * zrow, a.grad_in + t0 * E, cnt * grow, bar);
+    }
+  };
+  for (int j = 0; j < D && j < nj; ++j) issue(j, j);
   const float gs = GRAD && a.grad_scale ? *a.grad_scale : 1.0f;
+  auto mask_of = [&](int j) -> uint32_t {  // of the group's tokens, one bit each
+    if (!a.mask || j >= nj) return kFull;
+    const int64_t tok = start(j) + lane;
+    return __ballot_sync(kFull, lane < G && tok < te && a.mask[tok]);
+  };
+  uint32_t mbits = mask_of(0), mnext = mask_of(1);
 
+  int j = 0, stage = 0, waited = -1;
+  uint32_t phase = 0;
+  bool dead = false;  // a wait of this warp ran out
   int64_t t = tb;
   while (t < te) {
     const int l = microbatch_of(a.off, a.M, t);
@@ -87,82 +187,103 @@ __global__ void __launch_bounds__(kBalThreads) balance_kernel(BalanceArgs a, int
       Rs[e] = r;
     }
     __syncthreads();
-    float r[CPL][8], acc[CPL][8];
+    F2 r[RREG ? C : 1][2], acc[C][2];
+    auto load_r = [&](int k, F2 (&o)[2]) {
+      const float4 w = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
+      o[0] = f2(w.x, w.y);
+      o[1] = f2(w.z, w.w);
+    };
 #pragma unroll
-    for (int k = 0; k < CPL; ++k) {
-      const float4 r0 = reinterpret_cast<const float4*>(Rs)[2 * (sub + k * LPT)];
-      const float4 r1 = reinterpret_cast<const float4*>(Rs)[2 * (sub + k * LPT) + 1];
-      r[k][0] = r0.x; r[k][1] = r0.y; r[k][2] = r0.z; r[k][3] = r0.w;
-      r[k][4] = r1.x; r[k][5] = r1.y; r[k][6] = r1.z; r[k][7] = r1.w;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[k][i] = 0.f;
+    for (int k = 0; k < C; ++k) {
+      if constexpr (RREG) load_r(k, r[k]);
+      acc[k][0] = acc[k][1] = f2(0.f, 0.f);
     }
     const float ca = cs[0], cz = cs[1];
     float hsum = 0.f, zsum = 0.f, alive_n = 0.f;
 
-    const int64_t stride = kBalWarps * TPW;
-    for (int64_t base = t + static_cast<int64_t>(wid) * TPW; base < seg_end; base += U * stride) {
-      float z[U][CPL][8];
-      bool ok[U];  // a token of the range that counts
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t tok = base + u * stride + slot;
-        ok[u] = tok < seg_end && (!a.mask || a.mask[tok]);
-#pragma unroll
-        for (int k = 0; k < CPL; ++k) {
-          const int c = sub + k * LPT;
-          const bool have = ok[u] && c < nch;
-          if constexpr (F32) {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.z) + tok * E) + 2 * c;
-            const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            const float4 w0 = have ? __ldcs(p) : none, w1 = have ? __ldcs(p + 1) : none;
-            z[u][k][0] = w0.x; z[u][k][1] = w0.y; z[u][k][2] = w0.z; z[u][k][3] = w0.w;
-            z[u][k][4] = w1.x; z[u][k][5] = w1.y; z[u][k][6] = w1.z; z[u][k][7] = w1.w;
-          } else {
-            const uint32_t none = 0xff80ff80u;  // -inf
-            const uint4 w = have ? __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.z) + tok * E) + c)
-                                 : make_uint4(none, none, none, none);
-            z[u][k][0] = bf16_lo(w.x); z[u][k][1] = bf16_hi(w.x);
-            z[u][k][2] = bf16_lo(w.y); z[u][k][3] = bf16_hi(w.y);
-            z[u][k][4] = bf16_lo(w.z); z[u][k][5] = bf16_hi(w.z);
-            z[u][k][6] = bf16_lo(w.w); z[u][k][7] = bf16_hi(w.w);
-          }
-        }
+    while (j < nj && !dead) {
+      const int64_t g0 = start(j);
+      if (g0 >= seg_end) break;
+      if (waited != j) {
+        waited = j;
+        dead = !__all_sync(kFull, mbar_wait(bar0 + 8u * stage, phase, &aborted));
+        if (dead) break;
       }
+      const uint8_t* zs = ring + static_cast<uint32_t>(stage) * stage_bytes;
+      const uint8_t* gsrc = zs + static_cast<uint32_t>(G) * zrow;
+      // the group's tokens of this microbatch, counted from g0
+      const int from = t > g0 ? static_cast<int>(t - g0) : 0;
+      const int to = static_cast<int>(min(seg_end - g0, static_cast<int64_t>(G)));
+      for (int i0 = from / TPW * TPW; i0 < to; i0 += TPW) {
+        const int i = i0 + slot;
+        const bool in = i >= from && i < to;
+        const bool ok = in && (mbits >> i & 1u);
+        F2 e[C][2];
+        float top;
+        if constexpr (F32) {
+          top = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t tok = base + u * stride + slot;
-        float top = -INFINITY;
+          for (int k = 0; k < C; ++k) {
+            const int c = sub + k * LPT;
+            float4 w = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (ok && c < nch) w = reinterpret_cast<const float4*>(zs + static_cast<uint32_t>(i) * zrow)[c];
+            top = fmaxf(fmaxf(top, fmaxf(w.x, w.y)), fmaxf(w.z, w.w));
+            e[k][0] = f2(w.x, w.y);
+            e[k][1] = f2(w.z, w.w);
+          }
 #pragma unroll
-        for (int k = 0; k < CPL; ++k)
+          for (int m = 1; m < LPT; m <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, m));
+        } else {
+          uint32_t top2 = 0xff80ff80u;  // -inf
 #pragma unroll
-          for (int i = 0; i < 8; ++i) top = fmaxf(top, z[u][k][i]);
+          for (int k = 0; k < C; ++k) {
+            const int c = sub + k * LPT;
+            uint2 w = make_uint2(0xff80ff80u, 0xff80ff80u);
+            if (ok && c < nch) w = reinterpret_cast<const uint2*>(zs + static_cast<uint32_t>(i) * zrow)[c];
+            top2 = hmax2_bf16(top2, hmax2_bf16(w.x, w.y));
+            e[k][0] = f2(bf16_lo(w.x), bf16_hi(w.x));
+            e[k][1] = f2(bf16_lo(w.y), bf16_hi(w.y));
+          }
 #pragma unroll
-        for (int m = 1; m < LPT; m <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, m));
+          for (int m = 1; m < LPT; m <<= 1) top2 = hmax2_bf16(top2, __shfl_xor_sync(kFull, top2, m));
+          top = fmaxf(bf16_lo(top2), bf16_hi(top2));
+        }
         // a row without a finite logit has no probabilities (nor has a masked one)
-        const bool alive = ok[u] && top > -INFINITY;
+        const bool alive = ok && top > -INFINITY;
         // sigmoids are taken relative to e^top where all are far below 0.5:
         // s e^-top = 1 / (e^top + e^(top - z))
         const float ref = !alive ? 0.f : SIG ? fminf(top, 0.f) : top;
         const float m2 = ref * kLog2e;
+        const F2 mul = f2(SIG ? -kLog2e : kLog2e, SIG ? -kLog2e : kLog2e), shift = f2(SIG ? m2 : -m2, SIG ? m2 : -m2);
         const float em = SIG ? ex2_approx(m2) : 0.f;
-        float w[CPL][8];  // 1 - s (sigmoid with gradient)
-        float d = 0.f, h = 0.f;
+        F2 w[SIG && GRAD ? C : 1][2];  // 1 - s
+        F2 d2 = f2(0.f, 0.f), h2 = f2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < CPL; ++k)
+        for (int k = 0; k < C; ++k) {
+          F2 rk[2];
+          if constexpr (!RREG) load_r(k, rk);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int q = 0; q < 2; ++q) {
+            const F2 x = fma2(e[k][q], mul, shift);
             if constexpr (SIG) {
-              const float x = ex2_approx(__fmaf_rn(z[u][k][i], -kLog2e, m2));
-              const float s = rcp_approx(em + x);
-              if constexpr (GRAD) w[k][i] = fminf(x, 0x1p120f) * s;
-              z[u][k][i] = s;
+              // one reciprocal for two: beyond 2^60 of the row's reference a
+              // sigmoid counts as zero, so that the product stays finite
+              constexpr float kFar = 0x1p60f;
+              const float x0 = ex2_approx(lo2(x)), x1 = ex2_approx(hi2(x));
+              const F2 xc = f2(fmin_nan(x0, kFar), fmin_nan(x1, kFar));
+              const F2 y = add2(f2(em, em), xc);
+              const float rr = rcp_approx(lo2(y) * hi2(y));
+              const F2 s = mul2(f2(rr, rr), f2(hi2(y), lo2(y)));
+              if constexpr (GRAD) w[k][q] = mul2(xc, s);
+              e[k][q] = f2(x0 > kFar ? 0.f : lo2(s), x1 > kFar ? 0.f : hi2(s));
             } else {
-              z[u][k][i] = ex2_approx(__fmaf_rn(z[u][k][i], kLog2e, -m2));
+              e[k][q] = f2(ex2_approx(lo2(x)), ex2_approx(hi2(x)));
             }
-            d += z[u][k][i];
-            h = __fmaf_rn(z[u][k][i], r[k][i], h);
+            d2 = add2(d2, e[k][q]);
+            h2 = fma2(e[k][q], RREG ? r[RREG ? k : 0][q] : rk[q], h2);
           }
+        }
+        float d = lo2(d2) + hi2(d2), h = lo2(h2) + hi2(h2);
 #pragma unroll
         for (int m = 1; m < LPT; m <<= 1) {
           d += __shfl_xor_sync(kFull, d, m);
@@ -178,53 +299,62 @@ __global__ void __launch_bounds__(kBalThreads) balance_kernel(BalanceArgs a, int
           zsum = __fmaf_rn(lse, lse, zsum);
           alive_n += alive ? 1.f : 0.f;
         }
-        const float cl = cz * lse;
+        const F2 id2 = f2(id, id);
+        if constexpr (!GRAD) {
 #pragma unroll
-        for (int k = 0; k < CPL; ++k) {
-          const int c = sub + k * LPT;
-          float gr[8];
+          for (int k = 0; k < C; ++k)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float p = z[u][k][i] * id;
-            acc[k][i] += p;
-            if constexpr (GRAD) {
-              float q = __fmaf_rn(ca, r[k][i] - h, cl);
-              if constexpr (SIG) q *= w[k][i];
-              gr[i] = p * q;
+            for (int q = 0; q < 2; ++q) acc[k][q] = fma2(e[k][q], id2, acc[k][q]);
+        } else {
+          const float kk = __fmaf_rn(-ca, h, cz * lse);
+          const F2 ca2 = f2(ca, ca), k2 = f2(kk, kk);
+          const int64_t tok = g0 + i;
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            const int c = sub + k * LPT;
+            F2 rk[2], g[2];
+            if constexpr (!RREG) load_r(k, rk);
+            const bool have = in && c < nch;
+            float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (gin && have) old = reinterpret_cast<const float4*>(gsrc + static_cast<uint32_t>(i) * grow)[c];
+            g[0] = f2(old.x, old.y);
+            g[1] = f2(old.z, old.w);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const F2 p = mul2(e[k][q], id2);
+              acc[k][q] = fma2(e[k][q], id2, acc[k][q]);  // as without a gradient
+              F2 v = fma2(ca2, RREG ? r[RREG ? k : 0][q] : rk[q], k2);
+              if constexpr (SIG) v = mul2(v, w[k][q]);
+              g[q] = fma2(p, v, g[q]);
             }
-          }
-          if constexpr (GRAD) {
-            if (tok >= seg_end || c >= nch) continue;
-            if (a.grad_in) {
-              const float4* gp = reinterpret_cast<const float4*>(a.grad_in + tok * E) + 2 * c;
-              const float4 g0 = __ldcs(gp), g1 = __ldcs(gp + 1);
-              gr[0] += g0.x; gr[1] += g0.y; gr[2] += g0.z; gr[3] += g0.w;
-              gr[4] += g1.x; gr[5] += g1.y; gr[6] += g1.z; gr[7] += g1.w;
-            }
-            if (a.grad_bf16) {
-              __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.grad_out) + tok * E) + c,
-                     make_uint4(pack_bf16x2_rn(gr[0], gr[1]), pack_bf16x2_rn(gr[2], gr[3]), pack_bf16x2_rn(gr[4], gr[5]),
-                                pack_bf16x2_rn(gr[6], gr[7])));
-            } else {
-              float4* op = reinterpret_cast<float4*>(static_cast<float*>(a.grad_out) + tok * E) + 2 * c;
-              __stcs(op, make_float4(gr[0], gr[1], gr[2], gr[3]));
-              __stcs(op + 1, make_float4(gr[4], gr[5], gr[6], gr[7]));
-            }
+            if (!have) continue;
+            if (a.grad_bf16)
+              __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.grad_out) + tok * E) + c,
+                     make_uint2(pack_bf16x2_rn(lo2(g[0]), hi2(g[0])), pack_bf16x2_rn(lo2(g[1]), hi2(g[1]))));
+            else
+              __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.grad_out) + tok * E) + c,
+                     make_float4(lo2(g[0]), hi2(g[0]), lo2(g[1]), hi2(g[1])));
           }
         }
       }
+      if (g0 + G > seg_end && seg_end < te) break;  // the rest is the next microbatch's
+      __syncwarp();
+      if (j + D < nj) issue(j + D, stage);
+      ++j;
+      mbits = mnext;
+      mnext = mask_of(j + 1);
+      if (++stage == D) { stage = 0; phase ^= 1u; }
     }
 
     // the block's sums of this microbatch
     if (a.part) {
       float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;
 #pragma unroll
-      for (int k = 0; k < CPL; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float v = sum_slots(acc[k][i], LPT);
-          if (slot == 0) colsum[wid][(sub + k * LPT) * 8 + i] = v;
-        }
+      for (int k = 0; k < C; ++k) {
+        const float4 v = make_float4(sum_slots(lo2(acc[k][0]), LPT), sum_slots(hi2(acc[k][0]), LPT),
+                                     sum_slots(lo2(acc[k][1]), LPT), sum_slots(hi2(acc[k][1]), LPT));
+        if (slot == 0) reinterpret_cast<float4*>(colsum + wid * EM)[sub + k * LPT] = v;
+      }
       hsum = sum_slots(hsum, 1);
       zsum = sum_slots(zsum, 1);
       alive_n = sum_slots(alive_n, 1);
@@ -237,7 +367,7 @@ __global__ void __launch_bounds__(kBalThreads) balance_kernel(BalanceArgs a, int
       for (int e = threadIdx.x; e < E; e += kBalThreads) {
         float v = 0.f;
 #pragma unroll
-        for (int q = 0; q < kBalWarps; ++q) v += colsum[q][e];
+        for (int q = 0; q < kBalWarps; ++q) v += colsum[q * EM + e];
         row[4 + e] = v;
       }
       if (threadIdx.x < 3) {
@@ -249,36 +379,61 @@ __global__ void __launch_bounds__(kBalThreads) balance_kernel(BalanceArgs a, int
     }
     t = seg_end;
   }
+  if (dead && lane == 0) {  // the copies in flight must land before the block leaves
+    drain_loads(min(nj, j + D), D, [&](int s) { return bar0 + 8u * s; });
+    raise_flag(a.err, kErrCuda);
+  }
 }
 
-template <bool SIG, bool GRAD, bool F32, int LPT, int CPL>
-int launch_bal(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s) {
-  const int64_t grid = (a.T + tokens_per_cta - 1) / tokens_per_cta;
-  return launch_dependent(balance_kernel<SIG, GRAD, F32, LPT, CPL>, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), 0,
-                          s, a, tokens_per_cta) == cudaSuccess
-             ? kOk
-             : kErrCuda;
+template <bool SIG, bool GRAD, bool F32, int LPT, int C>
+int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
+  constexpr int TPW = 32 / LPT, EM = LPT * C * 4;
+  DeviceInfo di;
+  if (int rc = device_info(&di)) return rc;
+  const bool gin = GRAD && a.grad_in;
+  // a ring as deep as the blocks of an SM leave room for, its groups of up to 2 KB
+  BalanceCut cut;
+  cut.group = TPW;
+  while (cut.group * 2 <= 32 && bal_stage_bytes(a.E, cut.group * 2, F32, gin) <= 2048) cut.group *= 2;
+  // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
+  const int room = di.max_smem_optin / bal_blocks(SIG && GRAD, C) - 2048 - bal_fixed_bytes(EM);
+  cut.stages = room / (kBalWarps * bal_stage_bytes(a.E, cut.group, F32, gin));
+  if (cut.stages > kBalMaxStages) cut.stages = kBalMaxStages;
+  if (cut.stages < 1) return kErrUnsupported;
+  int64_t grid = (a.T + kBalWarps * TPW - 1) / (kBalWarps * TPW);
+  const int64_t most = di.sm_count * bal_blocks(SIG && GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(SIG && GRAD, C) : kBalMaxGrid;
+  if (grid > most) grid = most;
+  cut.tokens_per_cta = (a.T + grid - 1) / grid;
+  run->tokens_per_cta = cut.tokens_per_cta;
+  grid = (a.T + cut.tokens_per_cta - 1) / cut.tokens_per_cta;
+  const int smem = bal_fixed_bytes(EM) + kBalWarps * cut.stages * bal_stage_bytes(a.E, cut.group, F32, gin);
+  const auto kern = balance_kernel<SIG, GRAD, F32, LPT, C>;
+  if (!allow_smem(kern, di.max_smem_optin - 2048)) return kErrCuda;
+  return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), smem, s, a, cut) == cudaSuccess ? kOk
+                                                                                                                     : kErrCuda;
 }
 
 template <bool SIG, bool GRAD, bool F32>
-int launch_bal_width(const BalanceArgs& a, int64_t tpc, cudaStream_t s) {
-  const int nch = a.E >> 3;
-  if (nch <= 1) return launch_bal<SIG, GRAD, F32, 1, 1>(a, tpc, s);
-  if (nch <= 2) return launch_bal<SIG, GRAD, F32, 2, 1>(a, tpc, s);
-  if (nch <= 4) return launch_bal<SIG, GRAD, F32, 4, 1>(a, tpc, s);
-  if (nch <= 8) return launch_bal<SIG, GRAD, F32, 8, 1>(a, tpc, s);
-  if (nch <= 16) return launch_bal<SIG, GRAD, F32, 16, 1>(a, tpc, s);
-  if (nch <= 32) return launch_bal<SIG, GRAD, F32, 32, 1>(a, tpc, s);
-  if (nch <= 48) return launch_bal<SIG, GRAD, F32, 16, 3>(a, tpc, s);
-  if (nch <= 64) return launch_bal<SIG, GRAD, F32, 32, 2>(a, tpc, s);
-  if (nch <= 96) return launch_bal<SIG, GRAD, F32, 32, 3>(a, tpc, s);
-  if (nch <= 128) return launch_bal<SIG, GRAD, F32, 32, 4>(a, tpc, s);
+int launch_bal_width(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
+  if (a.E <= 8) return launch_bal<SIG, GRAD, F32, 1, 2>(a, run, s);
+  if (a.E <= 16) return launch_bal<SIG, GRAD, F32, 2, 2>(a, run, s);
+  if (a.E <= 32) return launch_bal<SIG, GRAD, F32, 4, 2>(a, run, s);
+  if (a.E <= 48) return launch_bal<SIG, GRAD, F32, 4, 3>(a, run, s);
+  if (a.E <= 64) return launch_bal<SIG, GRAD, F32, 8, 2>(a, run, s);
+  if (a.E <= 96) return launch_bal<SIG, GRAD, F32, 8, 3>(a, run, s);
+  if (a.E <= 128) return launch_bal<SIG, GRAD, F32, 16, 2>(a, run, s);
+  if (a.E <= 192) return launch_bal<SIG, GRAD, F32, 16, 3>(a, run, s);
+  if (a.E <= 256) return launch_bal<SIG, GRAD, F32, 32, 2>(a, run, s);
+  if (a.E <= 384) return launch_bal<SIG, GRAD, F32, 32, 3>(a, run, s);
+  if (a.E <= 512) return launch_bal<SIG, GRAD, F32, 32, 4>(a, run, s);
+  if (a.E <= 768) return launch_bal<SIG, GRAD, F32, 32, 6>(a, run, s);
+  if (a.E <= 1024) return launch_bal<SIG, GRAD, F32, 32, 8>(a, run, s);
   return kErrUnsupported;
 }
 
 template <bool SIG, bool GRAD>
-int launch_bal_type(const BalanceArgs& a, int64_t tpc, cudaStream_t s) {
-  return a.z_fp32 ? launch_bal_width<SIG, GRAD, true>(a, tpc, s) : launch_bal_width<SIG, GRAD, false>(a, tpc, s);
+int launch_bal_type(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
+  return a.z_fp32 ? launch_bal_width<SIG, GRAD, true>(a, run, s) : launch_bal_width<SIG, GRAD, false>(a, run, s);
 }
 
 }  // namespace

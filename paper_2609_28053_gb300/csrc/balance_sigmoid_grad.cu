@@ -3,6 +3,8 @@
 
 namespace eqb {
 
-int launch_balance_sigmoid_grad(const BalanceArgs& a, int64_t tpc, cudaStream_t s) { return launch_bal_type<true, true>(a, tpc, s); }
+int launch_balance_sigmoid_grad(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
+  return launch_bal_type<true, true>(a, run, s);
+}
 
 }  // namespace eqb

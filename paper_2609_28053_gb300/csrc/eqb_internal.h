@@ -232,16 +232,19 @@ struct BalanceArgs {
   int32_t* valid;  // [M]: valid tokens (mask)
   int32_t* err;
 };
-constexpr int kBalMaxGrid = 2048;  // most blocks of the pass over z
+constexpr int kBalMaxGrid = 512;  // most blocks of the pass over z
 constexpr size_t balance_part_bytes(int E, int M) {
   return carve_round((static_cast<size_t>(kBalMaxGrid) + static_cast<size_t>(M)) * (static_cast<size_t>(E) + 4) * 4);
 }
 int launch_balance(BalanceArgs a, cudaStream_t s);
-// the pass over z, its instances each in their own file
-int launch_balance_softmax_value(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
-int launch_balance_softmax_grad(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
-int launch_balance_sigmoid_value(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
-int launch_balance_sigmoid_grad(const BalanceArgs& a, int64_t tokens_per_cta, cudaStream_t s);
+// The pass over z, its instances in files of their own; says how it was cut.
+struct BalanceRun {
+  int64_t tokens_per_cta;
+};
+int launch_balance_softmax_value(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
+int launch_balance_softmax_grad(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
+int launch_balance_sigmoid_value(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
+int launch_balance_sigmoid_grad(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
 
 // One tensor of an AdamW step (adamw.cu).
 struct AdamwTensor {

@@ -37,7 +37,7 @@ eqb_status eqb_balance_loss(const void* z, int32_t z_fp32, const int32_t* topk_i
   if (M > (1 << 20)) return EQB_ERR_UNSUPPORTED;
   if (!mb_offsets || !counts) return EQB_ERR_INVALID_ARG;
   if (T > 0 && (!topk_idx || (!z && (prob || loss || grad_out)))) return EQB_ERR_INVALID_ARG;
-  if ((grad_in || grad_scale) && !grad_out) return EQB_ERR_INVALID_ARG;
+  if (grad_in && !grad_out) return EQB_ERR_INVALID_ARG;
   if (grad_out_bf16 && grad_out && grad_out == static_cast<const void*>(grad_in)) return EQB_ERR_INVALID_ARG;
   if (!aligned(z, 16) || !aligned(topk_idx, 4) || !aligned(mb_offsets, 8) || !aligned(grad_in, 16) || !aligned(grad_out, 16) ||
       !aligned(grad_scale, 4) || !aligned(counts, 4) || !aligned(prob, 4) || !aligned(loss, 4) || !aligned(err_flag, 4))

@@ -20,7 +20,7 @@
 // kernel.
 //
 // Roles, bounded waits and the way out of a stall are those of the forward
-// projection: warp 0 loads, warp 1 issues the MMAs, warps 2 to 5 take the
+// projection: warp 0 loads, warp 1 issues the MMAs, the others take the
 // accumulators out.
 #include "tcgen05.cuh"
 
@@ -275,6 +275,16 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   }
 }
 
+// dW's accumulators.  The tensor cores cut their fp32 sums off instead of
+// rounding them, which draws every sum toward zero: 1.0e-9 of it a token (d =
+// 38,912, E = 128, one sum over 512, 4,096 and 16,384 tokens: off by 4.7e-7,
+// 4.4e-6 and 1.9e-5; the same sums rounded to nearest by 1.6e-7 to 1.5e-6).  So
+// 512 tokens are summed in tensor memory at a time, in two accumulators that
+// alternate, and eight warps add each to the sums that they hold in registers
+// (128 a thread, which bounds a block to 128 x 256 or 256 x 128 sums).
+constexpr int kDwStages = 8;      // stages of 64 tokens between two of these additions
+constexpr int kDwThreads = 320;   // two warps beside the eight
+
 struct DwArgs {
   int T, d, E, N, tiles, parts, S;
   int64_t stages;  // of 64 tokens, in all
@@ -283,7 +293,7 @@ struct DwArgs {
   int32_t* err;
 };
 
-__global__ void __launch_bounds__(kGradThreads, 1)
+__global__ void __launch_bounds__(kDwThreads, 1)
     router_dw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmx, DwArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const int S = a.S, MT = a.E > 128 ? 2 : 1;
@@ -295,8 +305,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   const uint32_t bars = base + static_cast<uint32_t>(S) * stage_bytes;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (S + s); };
-  const uint32_t accf = bars + 8u * (2 * S), drain = accf + 8u;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8u * (2 * S + 2));
+  auto accf = [&](int b) { return bars + 8u * (2 * S + b); };
+  auto acce = [&](int b) { return bars + 8u * (2 * S + 2 + b); };
+  const uint32_t drain = bars + 8u * (2 * S + 4);
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8u * (2 * S + 5));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   int* issued = reinterpret_cast<int*>(tmem_holder + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -306,7 +318,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    mbar_init(accf, 1);
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf(b), 1);
+      mbar_init(acce(b), 256);
+    }
     mbar_init(drain, 1);
     *abort_flag = 0;
     *issued = 0;
@@ -325,7 +340,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
   const int tile = static_cast<int>(blockIdx.x) % a.tiles, part = static_cast<int>(blockIdx.x) / a.tiles;
-  const int64_t s0 = a.stages * part / a.parts, s1 = a.stages * (part + 1) / a.parts;
+  const int64_t s0 = a.stages * part / a.parts;
+  const int ns = static_cast<int>(a.stages * (part + 1) / a.parts - s0);
   const int j0 = tile * a.N, nn = min(a.N, a.d - j0);
 
   if (warp == 0) {
@@ -333,10 +349,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       int stage = 0, n = 0;
       uint32_t phase = 0;
       const uint32_t bytes = a_bytes + static_cast<uint32_t>(nn / 64) * kTile64;
-      for (int64_t k = s0; k < s1; ++k, ++n) {
+      for (int k = 0; k < ns; ++k, ++n) {
         if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) break;
         const uint32_t dst = base + static_cast<uint32_t>(stage) * stage_bytes;
-        const int t = static_cast<int>(k * 64);
+        const int t = static_cast<int>((s0 + k) * 64);
         mbar_expect_tx(full(stage), bytes);
         // experts past E (and tokens past T) are filled with zeros
         for (int c = 0; c < 2 * MT; ++c) tma_load_2d(dst + static_cast<uint32_t>(c) * kTile64, &tmz, full(stage), c * 64, t);
@@ -351,50 +367,73 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       const uint32_t idesc = umma_idesc_bf16(kBM, nn) | kMnA | kMnB;
       int stage = 0;
       uint32_t phase = 0;
-      bool ok = true;
-      for (int64_t k = s0; k < s1; ++k) {
-        if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
+      for (int k = 0; k < ns; ++k) {
+        const int chunk = k / kDwStages, buf = chunk & 1;
+        if (k % kDwStages == 0) {
+          if (!mbar_wait(acce(buf), (static_cast<uint32_t>(chunk >> 1) & 1u) ^ 1u, abort_flag)) break;
+          tc_fence_after();
+        }
+        if (!mbar_wait(full(stage), phase, abort_flag)) break;
         tc_fence_after();
         const uint32_t sa = base + static_cast<uint32_t>(stage) * stage_bytes;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)  // 16 tokens per MMA
           for (int m = 0; m < MT; ++m)
-            umma_bf16(tmem + static_cast<uint32_t>(m * a.N),
+            umma_bf16(tmem + static_cast<uint32_t>(buf * 256 + m * a.N),
                       mn128_desc(sa + static_cast<uint32_t>(m) * 2u * kTile64 + kk * 2048u, kTile64),
-                      mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k > s0 || kk > 0 ? 1u : 0u);
+                      mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k % kDwStages != 0 || kk > 0 ? 1u : 0u);
         umma_commit(empty(stage));
+        if (k % kDwStages == kDwStages - 1 || k == ns - 1) umma_commit(accf(buf));
         if (++stage == S) { stage = 0; phase ^= 1u; }
       }
-      if (ok) umma_commit(accf);
       umma_commit(drain);
       for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(drain, 0u)) break;
     }
   } else {
-    const int q = warp & 3;
-    if (__all_sync(0xffffffffu, mbar_wait(accf, 0u, abort_flag))) {
-      tc_fence_after();
-      for (int m = 0; m < MT; ++m) {
-        const int e = m * 128 + q * 32 + lane;
-        float* out = a.out + (static_cast<size_t>(part) * a.E + e) * a.d + j0;
-        for (int c = 0; c < nn; c += 32) {
-          uint32_t r[32];
-          tmem_ld32(tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(m * a.N + c), r);
-          if (e < a.E) {
+    // warps 2..5 and 6..9 take the two halves of an accumulator's MT * N columns
+    const int q = warp & 3, h = (warp - 2) >> 2, cw = MT * a.N / 2;
+    const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * cw);
+    float acc[4][32];
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-              float4 o = make_float4(__uint_as_float(r[4 * v]), __uint_as_float(r[4 * v + 1]), __uint_as_float(r[4 * v + 2]),
-                                     __uint_as_float(r[4 * v + 3]));
-              float4* dst = reinterpret_cast<float4*>(out + c) + v;
-              if (a.add) {
-                const float4 w = *dst;
-                o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w;
-              }
-              *dst = o;
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[g][i] = 0.f;
+    const int chunks = (ns + kDwStages - 1) / kDwStages;
+    bool ok = true;
+    for (int c = 0; c < chunks; ++c) {
+      const int buf = c & 1;
+      ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(c >> 1) & 1u, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (g * 32 < cw) {
+          uint32_t r[32];
+          tmem_ld32(mine + static_cast<uint32_t>(buf * 256 + g * 32), r);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[g][i] = __fadd_rn(acc[g][i], __uint_as_float(r[i]));
+        }
+      tc_fence_before();
+      mbar_arrive(acce(buf));
+    }
+    const int e = (MT == 2 ? h * 128 : 0) + q * 32 + lane, c0 = MT == 2 ? 0 : h * cw;
+    if (ok && e < a.E) {
+      float* out = a.out + (static_cast<size_t>(part) * a.E + e) * a.d + j0 + c0;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (g * 32 < cw && c0 + g * 32 < nn) {
+#pragma unroll
+          for (int v = 0; v < 8; ++v) {
+            float4 o = make_float4(acc[g][4 * v], acc[g][4 * v + 1], acc[g][4 * v + 2], acc[g][4 * v + 3]);
+            float4* dst = reinterpret_cast<float4*>(out + g * 32) + v;
+            if (a.add) {
+              const float4 w = *dst;
+              o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w;
             }
+            *dst = o;
           }
         }
-      }
     }
   }
   tc_fence_before();
@@ -447,7 +486,7 @@ DwPlan plan_dw(int64_t T, int d, int E) {
   DwPlan p;
   p.stages = (T + 63) / 64;
   const int64_t most = (p.stages + 3) / 4;  // parts
-  for (p.N = 256;; p.N /= 2) {
+  for (p.N = E > 128 ? 128 : 256;; p.N /= 2) {
     p.tiles = (d + p.N - 1) / p.N;
     int64_t parts = kGradCtas / p.tiles;
     if (parts > most) parts = most;
@@ -494,7 +533,7 @@ int launch_dw(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
   const DwPlan p = plan_dw(g.T, g.d, g.E);
   DwArgs a{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
            p.parts > 1 ? 0 : g.add_dW, g.err};
-  const int extra = 1024 + 8 * (2 * 8 + 2) + 16;
+  const int extra = 1024 + 8 * (2 * 8 + 5) + 16;
   const int stage_bytes = static_cast<int>(kTile64) * ((g.E > 128 ? 4 : 2) + p.N / 64);
   a.S = (di.max_smem_optin - extra) / stage_bytes;
   if (a.S > 8) a.S = 8;
@@ -503,7 +542,7 @@ int launch_dw(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
   if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), 64) ||
       !make_map(&tmx, g.x, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 64))
     return kErrCuda;
-  if (launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), a.S * stage_bytes + extra, s, tmz, tmx,
+  if (launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kDwThreads), a.S * stage_bytes + extra, s, tmz, tmx,
                        a) != cudaSuccess)
     return kErrCuda;
   if (p.parts == 1) return kOk;
