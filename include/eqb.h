@@ -499,7 +499,8 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   p = (1 - lr weight_decay) p
  *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
- * The arithmetic is fp32, the factors are formed in fp64.  A bf16 parameter is
+ * The arithmetic is fp32 (root and quotient within 2 ulps, a second moment
+ * below 2^-126 counts as 0 in the root), the factors are formed in fp64.  A bf16 parameter is
  * rounded to nearest once a step (an update below half its last place is
  * lost: keep an fp32 parameter with a bf16 copy where that matters).
  * state_bits 32: exp_avg holds m and exp_avg_sq holds v, fp32 [n].
@@ -512,12 +513,12 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  * Zeroed states (and scales) are those of a first step.
  *   tensors    host array [count]; read before the call returns.  n >= 0; an
  *              entry with n = 0 or grad = NULL is left as it is.  Tensors must
- *              not overlap.  Any element alignment; 16-byte alignment of fp32,
- *              8 of bf16 and 4 of 8-bit arrays is the fast path.
+ *              not overlap.  Any element alignment; 16-byte alignment
+ *              (8 of 8-bit arrays) is the fast path.
  *   grad_scale device fp32 [1] (nullable: 1): a clipping factor or the inverse
  *              of a loss scale, formed on the device
- *   err_flag   EQB_ERR_NONFINITE if a parameter or second moment became
- *              non-finite
+ *   err_flag   EQB_ERR_NONFINITE if a moment became non-finite (a gradient
+ *              was, or its square is beyond fp32)
  * Up to 400 tensors share a launch. */
 typedef struct eqb_adamw_tensor {
   void *param;      /* fp32 or bf16 [n], updated */

@@ -22,6 +22,7 @@ z_t = W_r x_t) on the tensor cores.
 from __future__ import annotations
 
 import ctypes
+from array import array
 
 import torch
 
@@ -586,15 +587,18 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
     _need(W_r, torch.bfloat16, "W_r", (E, d))
     _need(dx, torch.bfloat16, "dx", (T, d))
     _need(dW, torch.float32, "dW", (E, d))
-    need = eqb_router_grad_workspace_bytes(T, d, E) if dW is not None else 0
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dz.device)
+    if workspace is None and dW is not None:
+        need = eqb_router_grad_workspace_bytes(T, d, E)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dz.device) if need else None
     _need(workspace, torch.uint8, "workspace")
     _need(err_flag, torch.int32, "err_flag")
     rc = load().eqb_router_grad(_p(dz), _p(x), _p(W_r), T, d, E, _p(dx), bool(accumulate_dx), _p(dW), bool(accumulate_dW),
                                 _p(workspace), 0 if workspace is None else workspace.numel(), _p(err_flag), _stream(stream))
     _check(rc, "eqb_router_grad")
     return dx, dW
+
+
+_data_ptr, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 
 class EqbAdamW:
@@ -611,7 +615,9 @@ class EqbAdamW:
             parameter beside them, rounded, e.g. the W_r that the projection
             reads
 
-    The object holds the tensors; their storage must stay where it is."""
+    The object holds the tensors.  A parameter that has moved to another
+    storage is refused by step(); states and copies that are moved away from
+    their storage are not followed."""
 
     BLOCK = 256
 
@@ -657,18 +663,49 @@ class EqbAdamW:
             if c is not None and p.dtype is not torch.float32:
                 raise TypeError(f"copies[{i}] is given but params[{i}] is not torch.float32")
             _need(c, torch.bfloat16, f"copies[{i}]", p.shape)
-        self._held = [t for ts in (self.params, self.exp_avg, self.exp_avg_sq, self.avg_scale or [], self.sq_scale or [],
-                                   [c for c in self.copies if c is not None]) for t in ts]
-        if len({t.device for t in self._held}) > 1:
+        states = self.exp_avg + self.exp_avg_sq + (self.avg_scale or []) + (self.sq_scale or []) + [
+            c for c in self.copies if c is not None]
+        if len({t.device for t in self.params + states}) > 1:
             raise ValueError("all tensors must be on one device")
-        self._where = [t.data_ptr() for t in self._held]
+        # aliases: what the table points to stays allocated whatever becomes of the tensors above
+        self._held = [t.detach() for t in self.params + states]
+        self._ptrs = [p.data_ptr() for p in self.params]
+        self._shapes = [p.shape for p in self.params]
+        self._device = [p.get_device() for p in self.params]
+        self._dtypes = None  # of the last step's gradients: the table's grad_bf16
+        self._whole = [True] * len(self.params)
         self._table = (AdamwTensor * len(self.params))()
+        # the grad field of every entry, as one strided row
+        words = ctypes.sizeof(AdamwTensor) // 8
+        self._grad_words = memoryview(self._table).cast("B").cast("Q")[AdamwTensor.grad.offset // 8::words]
         for i, (e, p) in enumerate(zip(self._table, self.params)):
             e.param, e.n, e.param_bf16 = p.data_ptr(), p.numel(), p.dtype is torch.bfloat16
             e.exp_avg, e.exp_avg_sq = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
             if state_bits == 8:
                 e.avg_scale, e.sq_scale = self.avg_scale[i].data_ptr(), self.sq_scale[i].data_ptr()
             e.copy = _p(self.copies[i])
+
+    def _point_to(self, grads):
+        """The gradients' addresses into the table, after their checks."""
+        try:  # the checks of all of them at once: hundreds of tensors take longer one by one than their step
+            ptrs = list(map(_data_ptr, grads))
+            fits = (list(map(_get_device, grads)) == self._device and list(map(_is_contiguous, grads)) == self._whole and
+                    [g.shape for g in grads] == self._shapes and [g.dtype for g in grads] == self._dtypes)
+        except (TypeError, AttributeError):
+            fits = False
+        if fits:
+            self._grad_words[:] = memoryview(array("Q", ptrs))
+            return
+        for i, (e, g, p) in enumerate(zip(self._table, grads, self.params)):
+            if g is None:
+                e.grad = None
+                continue
+            bf16 = isinstance(g, torch.Tensor) and g.dtype is torch.bfloat16
+            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]", p.shape)
+            if g.device != p.device:
+                raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
+            e.grad, e.grad_bf16 = g.data_ptr(), bf16
+        self._dtypes = None if any(g is None for g in grads) else [g.dtype for g in grads]
 
     def step(self, grads, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, grad_scale=None, err_flag=None,
              stream=None):
@@ -678,17 +715,9 @@ class EqbAdamW:
         gradient is multiplied by."""
         if len(grads) != len(self.params):
             raise ValueError(f"grads must have {len(self.params)} entries, got {len(grads)}")
-        if [t.data_ptr() for t in self._held] != self._where:
-            raise ValueError("a parameter or state tensor has moved to another storage: make a new EqbAdamW")
-        for i, (e, g, p) in enumerate(zip(self._table, grads, self.params)):
-            if g is None:
-                e.grad = None
-                continue
-            bf16 = g.dtype is torch.bfloat16
-            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]", p.shape)
-            if g.device != p.device:
-                raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
-            e.grad, e.grad_bf16 = g.data_ptr(), bf16
+        if list(map(_data_ptr, self.params)) != self._ptrs:
+            raise ValueError("a parameter has moved to another storage: make a new EqbAdamW")
+        self._point_to(grads)
         _need(grad_scale, torch.float32, "grad_scale", (1,))
         _need(err_flag, torch.int32, "err_flag")
         _check(load().eqb_adamw_step(self._table, len(self.params), self.state_bits, float(lr), int(step), float(beta1),

@@ -14,6 +14,7 @@
 // nearest by itself, so that the 8-bit codes do not depend on how the compiler
 // fuses them.
 #include "eqb_device.cuh"
+#include "f32x2.cuh"
 
 namespace eqb {
 
@@ -35,191 +36,231 @@ struct AdamwTable {
   AdamwScalars s;
 };
 
-// Root and quotient of the update, within 2 ulps: the rounded-to-nearest ones
-// take about twenty instructions of the sixty an element has time for.
-__device__ __forceinline__ float sqrt_approx(float x) {
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-// two e4m3 codes -> fp32, and back (nearest even, NaN stays NaN)
-__device__ __forceinline__ void e4m3x2_to_f32(uint32_t c, float& lo, float& hi) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(h) : "r"(c));
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}"
+// Two e4m3 codes -> fp32, and back (nearest even, NaN stays NaN).
+__device__ __forceinline__ F2 e4m3x2_to_f32(uint32_t c) {
+  float lo, hi;
+  asm("{\n\t.reg .b16 t, a, b;\n\t.reg .b32 h;\n\tcvt.u16.u32 t, %2;\n\tcvt.rn.f16x2.e4m3x2 h, t;\n\t"
+      "mov.b32 {a, b}, h;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}"
       : "=f"(lo), "=f"(hi)
-      : "r"(h));
+      : "r"(c));
+  return f2(lo, hi);
 }
-__device__ __forceinline__ uint32_t f32_to_e4m3x2(float lo, float hi) {
+__device__ __forceinline__ uint32_t f32_to_e4m3x2(F2 x) {
   uint32_t r;
   asm("{\n\t.reg .b16 t;\n\tcvt.rn.satfinite.e4m3x2.f32 t, %2, %1;\n\tcvt.u32.u16 %0, t;\n\t}"
       : "=r"(r)
-      : "f"(lo), "f"(hi));
+      : "f"(lo2(x)), "f"(hi2(x)));
   return r;
 }
 
-// Element j (0..7) of a lane: two groups of four neighbours where the unit is
-// whole and aligned, else one of every 32.
-template <bool VEC>
-__device__ __forceinline__ int place(int j, int lane) {
-  return VEC ? (j >> 2) * 128 + lane * 4 + (j & 3) : j * 32 + lane;
-}
+// Where a lane's eight elements lie in its unit, in pairs: neighbours
+// (Run, for rows of 2- and 1-byte elements), two groups of four neighbours
+// (Quads, where 4-byte elements are among them), or one of every 32 (Single:
+// arrays that are not aligned, and a tensor's last unit).
+enum Layout { Run, Quads, Single };
 
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void load8(const void* src, int64_t base, int left, int lane, float (&x)[8]) {
-  if constexpr (VEC && BF16) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint2 w = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(src) + base + h * 128) + lane);
-      x[4 * h] = bf16_lo(w.x); x[4 * h + 1] = bf16_hi(w.x);
-      x[4 * h + 2] = bf16_lo(w.y); x[4 * h + 3] = bf16_hi(w.y);
-    }
-  } else if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float4 w = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(src) + base + h * 128) + lane);
-      x[4 * h] = w.x; x[4 * h + 1] = w.y; x[4 * h + 2] = w.z; x[4 * h + 3] = w.w;
-    }
-  } else {
+template <bool BF16, Layout L>
+__device__ __forceinline__ void load8(const void* src, int64_t base, int left, int lane, F2 (&x)[4]) {
+  if constexpr (L == Single) {
+    float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int i = place<false>(j, lane);
-      x[j] = i >= left ? 0.f
+      const int i = j * 32 + lane;
+      v[j] = i >= left ? 0.f
              : BF16    ? bf16_bits_to_f32(static_cast<const uint16_t*>(src)[base + i])
                        : static_cast<const float*>(src)[base + i];
     }
-  }
-}
-
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void store8(void* dst, int64_t base, int left, int lane, const float (&x)[8]) {
-  if constexpr (VEC && BF16) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(dst) + base + h * 128) + lane,
-             make_uint2(pack_bf16x2_rn(x[4 * h], x[4 * h + 1]), pack_bf16x2_rn(x[4 * h + 2], x[4 * h + 3])));
-  } else if constexpr (VEC) {
+    for (int j = 0; j < 4; ++j) x[j] = f2(v[2 * j], v[2 * j + 1]);
+  } else if constexpr (BF16 && L == Run) {
+    const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(src) + base) + lane);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      __stcs(reinterpret_cast<float4*>(static_cast<float*>(dst) + base + h * 128) + lane,
-             make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = place<false>(j, lane);
-      if (i >= left) continue;
-      if (BF16) static_cast<uint16_t*>(dst)[base + i] = static_cast<uint16_t>(pack_bf16x2_rn(x[j], 0.f));
-      else static_cast<float*>(dst)[base + i] = x[j];
-    }
-  }
-}
-
-template <bool VEC>
-__device__ __forceinline__ void load8_e4m3(const void* src, int64_t base, int left, int lane, float scale,
-                                           float (&x)[8]) {
-  const uint8_t* c = static_cast<const uint8_t*>(src) + base;
-  if constexpr (VEC) {
+    for (int j = 0; j < 4; ++j) x[j] = f2(bf16_lo(u[j]), bf16_hi(u[j]));
+  } else if constexpr (BF16) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t w = __ldcs(reinterpret_cast<const uint32_t*>(c + h * 128) + lane);
-      e4m3x2_to_f32(w & 0xffffu, x[4 * h], x[4 * h + 1]);
-      e4m3x2_to_f32(w >> 16, x[4 * h + 2], x[4 * h + 3]);
+      const uint2 w = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(src) + base + h * 128) + lane);
+      x[2 * h] = f2(bf16_lo(w.x), bf16_hi(w.x));
+      x[2 * h + 1] = f2(bf16_lo(w.y), bf16_hi(w.y));
     }
   } else {
 #pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(src) + base);
+      const float4 w = __ldcs(p + (L == Run ? 2 * lane + h : 32 * h + lane));
+      x[2 * h] = f2(w.x, w.y);
+      x[2 * h + 1] = f2(w.z, w.w);
+    }
+  }
+}
+
+template <bool BF16, Layout L>
+__device__ __forceinline__ void store8(void* dst, int64_t base, int left, int lane, const F2 (&x)[4]) {
+  if constexpr (L == Single) {
+#pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int i = place<false>(j, lane);
-      float none;
-      e4m3x2_to_f32(i < left ? c[i] : 0u, x[j], none);
+      const int i = j * 32 + lane;
+      const float v = j & 1 ? hi2(x[j >> 1]) : lo2(x[j >> 1]);
+      if (i >= left) continue;
+      if (BF16) static_cast<uint16_t*>(dst)[base + i] = static_cast<uint16_t>(pack_bf16x2_rn(v, 0.f));
+      else static_cast<float*>(dst)[base + i] = v;
+    }
+  } else if constexpr (BF16) {
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = pack_bf16x2_rn(lo2(x[j]), hi2(x[j]));
+    if constexpr (L == Run) {
+      __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(dst) + base) + lane, make_uint4(u[0], u[1], u[2], u[3]));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(dst) + base + h * 128) + lane, make_uint2(u[2 * h], u[2 * h + 1]));
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float4* p = reinterpret_cast<float4*>(static_cast<float*>(dst) + base);
+      __stcs(p + (L == Run ? 2 * lane + h : 32 * h + lane),
+             make_float4(lo2(x[2 * h]), hi2(x[2 * h]), lo2(x[2 * h + 1]), hi2(x[2 * h + 1])));
+    }
+  }
+}
+
+template <Layout L>
+__device__ __forceinline__ void load8_e4m3(const void* src, int64_t base, int left, int lane, float scale, F2 (&x)[4]) {
+  const uint8_t* c = static_cast<const uint8_t*>(src) + base;
+  if constexpr (L == Single) {
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j * 32 + lane < left ? c[j * 32 + lane] : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = e4m3x2_to_f32(v[2 * j] | v[2 * j + 1] << 8);
+  } else {
+    uint32_t w[2];
+    if constexpr (L == Run) {
+      const uint2 u = __ldcs(reinterpret_cast<const uint2*>(c) + lane);
+      w[0] = u.x;
+      w[1] = u.y;
+    } else {
+      w[0] = __ldcs(reinterpret_cast<const uint32_t*>(c) + lane);
+      w[1] = __ldcs(reinterpret_cast<const uint32_t*>(c + 128) + lane);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x[2 * h] = e4m3x2_to_f32(w[h] & 0xffffu);
+      x[2 * h + 1] = e4m3x2_to_f32(w[h] >> 16);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], scale);
+  for (int j = 0; j < 4; ++j) x[j] = mul2(x[j], splat2(scale));
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store8_e4m3(void* dst, int64_t base, int left, int lane, const float (&x)[8]) {
+template <Layout L>
+__device__ __forceinline__ void store8_e4m3(void* dst, int64_t base, int left, int lane, const F2 (&x)[4]) {
   uint8_t* c = static_cast<uint8_t*>(dst) + base;
-  if constexpr (VEC) {
+  uint32_t p[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      __stcs(reinterpret_cast<uint32_t*>(c + h * 128) + lane,
-             f32_to_e4m3x2(x[4 * h], x[4 * h + 1]) | f32_to_e4m3x2(x[4 * h + 2], x[4 * h + 3]) << 16);
+  for (int j = 0; j < 4; ++j) p[j] = f32_to_e4m3x2(x[j]);
+  if constexpr (L == Single) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j * 32 + lane < left) c[j * 32 + lane] = static_cast<uint8_t>(j & 1 ? p[j >> 1] >> 8 : p[j >> 1]);
+  } else if constexpr (L == Run) {
+    __stcs(reinterpret_cast<uint2*>(c) + lane, make_uint2(p[0] | p[1] << 16, p[2] | p[3] << 16));
   } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = place<false>(j, lane);
-      if (i < left) c[i] = static_cast<uint8_t>(f32_to_e4m3x2(x[j], 0.f));
-    }
+    __stcs(reinterpret_cast<uint32_t*>(c) + lane, p[0] | p[1] << 16);
+    __stcs(reinterpret_cast<uint32_t*>(c + 128) + lane, p[2] | p[3] << 16);
   }
 }
 
 // The scale of a unit and its reciprocal, from the largest magnitude of the
 // warp's elements (a NaN is larger than all, so it stays visible).  A unit
-// below the normal numbers is stored as zeros.
-__device__ __forceinline__ void unit_scale(const float (&x)[8], float& scale, float& inv) {
+// below the normal numbers is stored as zeros.  False if it is not finite.
+__device__ __forceinline__ bool unit_scale(const F2 (&x)[4], float& scale, float& inv) {
   uint32_t a = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) a = max(a, __float_as_uint(x[j]) & 0x7fffffffu);
-  scale = __fmul_rn(__uint_as_float(__reduce_max_sync(kFull, a)), 1.0f / kTop);
+  for (int j = 0; j < 4; ++j)
+    a = max(a, max(__float_as_uint(lo2(x[j])) & 0x7fffffffu, __float_as_uint(hi2(x[j])) & 0x7fffffffu));
+  a = __reduce_max_sync(kFull, a);
+  scale = __fmul_rn(__uint_as_float(a), 1.0f / kTop);
   if (scale < kMinNormal) scale = 0.f;
   inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  return a < 0x7f800000u;
 }
 
-// One unit of a tensor: `left` elements from `base` on (256 where VEC).
-template <int BITS, bool PB, bool GB, bool VEC>
+// One unit of a tensor: `left` elements from `base` on (256 unless Single).
+// The update's root and quotient are within 2 ulps: rounded to nearest they take
+// about twenty instructions of the fifty-five that an 8-bit element has time for.
+template <int BITS, bool PB, bool GB, Layout L>
 __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t base, int left,
                                            int lane) {
-  float p[8], g[8], m[8], v[8];
-  load8<PB, VEC>(t.p, base, left, lane, p);
-  load8<GB, VEC>(t.g, base, left, lane, g);
+  F2 p[4], g[4], m[4], v[4];
   const int64_t unit = base / kUnit;
+  float ms = 0.f, vs = 0.f;
+  if constexpr (BITS == 8) {
+    ms = t.ms[unit];
+    vs = t.vs[unit];
+  }
+  load8<PB, L>(t.p, base, left, lane, p);
+  load8<GB, L>(t.g, base, left, lane, g);
   if constexpr (BITS == 32) {
-    load8<false, VEC>(t.m, base, left, lane, m);
-    load8<false, VEC>(t.v, base, left, lane, v);
+    load8<false, L>(t.m, base, left, lane, m);
+    load8<false, L>(t.v, base, left, lane, v);
   } else {
-    load8_e4m3<VEC>(t.m, base, left, lane, t.ms[unit], m);
-    load8_e4m3<VEC>(t.v, base, left, lane, t.vs[unit], v);
+    load8_e4m3<L>(t.m, base, left, lane, ms, m);
+    load8_e4m3<L>(t.v, base, left, lane, vs, v);
   }
   bool bad = false;
-  float root[8];
+  F2 root[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float gj = __fmul_rn(g[j], gs);
-    if constexpr (BITS == 8) v[j] = __fmul_rn(v[j], v[j]);  // the root is what 8 bits hold
-    m[j] = __fadd_rn(__fmul_rn(m[j], s.b1), __fmul_rn(gj, s.c1));
-    v[j] = __fadd_rn(__fmul_rn(v[j], s.b2), __fmul_rn(__fmul_rn(gj, s.c2), gj));
-    root[j] = sqrt_approx(v[j]);
-    const float den = __fadd_rn(__fmul_rn(root[j], s.rbc2), s.eps);
-    p[j] = __fsub_rn(__fmul_rn(p[j], s.decay), __fmul_rn(__fdividef(m[j], den), s.step));
-    bad |= !(fabsf(p[j]) < INFINITY) || !(v[j] < INFINITY);
+  for (int j = 0; j < 4; ++j) {
+    const F2 gj = mul2(g[j], splat2(gs));
+    if constexpr (BITS == 8) v[j] = mul2(v[j], v[j]);  // the root is what 8 bits hold
+    m[j] = add2(mul2(m[j], splat2(s.b1)), mul2(gj, splat2(s.c1)));
+    v[j] = add2(mul2(v[j], splat2(s.b2)), mul2(mul2(gj, splat2(s.c2)), gj));
+    root[j] = f2(sqrt_approx(lo2(v[j])), sqrt_approx(hi2(v[j])));
+    const F2 den = add2(mul2(root[j], splat2(s.rbc2)), splat2(s.eps));
+    const F2 q = mul2(m[j], f2(rcp_approx(lo2(den)), rcp_approx(hi2(den))));
+    p[j] = sub2(mul2(p[j], splat2(s.decay)), mul2(q, splat2(s.step)));
+    if constexpr (BITS == 32)
+      bad |= !(fabsf(lo2(m[j])) < INFINITY) || !(fabsf(hi2(m[j])) < INFINITY) || !(lo2(v[j]) < INFINITY) ||
+             !(hi2(v[j]) < INFINITY);
   }
-  store8<PB, VEC>(t.p, base, left, lane, p);
-  if (!PB && t.copy) store8<true, VEC>(t.copy, base, left, lane, p);
+  store8<PB, L>(t.p, base, left, lane, p);
+  if (!PB && t.copy) store8<true, L>(t.copy, base, left, lane, p);
   if constexpr (BITS == 32) {
-    store8<false, VEC>(t.m, base, left, lane, m);
-    store8<false, VEC>(t.v, base, left, lane, v);
+    store8<false, L>(t.m, base, left, lane, m);
+    store8<false, L>(t.v, base, left, lane, v);
   } else {
-    float ms, mi, vs, vi;
-    unit_scale(m, ms, mi);
-    unit_scale(root, vs, vi);
+    float mi, vi;
+    bad = !unit_scale(m, ms, mi);
+    bad |= !unit_scale(root, vs, vi);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      m[j] = __fmul_rn(m[j], mi);
-      const float u = __fmul_rn(root[j], vi);
+    for (int j = 0; j < 4; ++j) {
+      m[j] = mul2(m[j], splat2(mi));
+      const F2 u = mul2(root[j], splat2(vi));
       // a root that is not zero stays so: eps alone in the denominator would
-      // make a step out of what is left in m
-      root[j] = vi > 0.f && root[j] > 0.f ? fmaxf(u, kLeast) : u;
+      // make a step out of what is left in m.  (fmaxf would drop a NaN.)
+      root[j] = f2(lo2(root[j]) > 0.f && lo2(u) < kLeast && vi > 0.f ? kLeast : lo2(u),
+                   hi2(root[j]) > 0.f && hi2(u) < kLeast && vi > 0.f ? kLeast : hi2(u));
     }
-    store8_e4m3<VEC>(t.m, base, left, lane, m);
-    store8_e4m3<VEC>(t.v, base, left, lane, root);
+    store8_e4m3<L>(t.m, base, left, lane, m);
+    store8_e4m3<L>(t.v, base, left, lane, root);
     if (lane == 0) {
       t.ms[unit] = ms;
       t.vs[unit] = vs;
     }
   }
   return bad;
+}
+
+template <int BITS, bool PB, bool GB>
+__device__ __forceinline__ bool adamw_any(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t base, int left,
+                                          int lane) {
+  constexpr Layout wide = BITS == 8 && PB ? Run : Quads;
+  if ((t.flags & 4) && left == kUnit) return adamw_unit<BITS, PB, GB, wide>(t, s, gs, base, left, lane);
+  return adamw_unit<BITS, PB, GB, Single>(t, s, gs, base, left, lane);
 }
 
 template <int CAP, int BITS>
@@ -240,17 +281,10 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     if (base >= t.n) break;
     const int left = t.n - base < kUnit ? static_cast<int>(t.n - base) : kUnit;
     const int kind = t.flags & 3;  // uniform in the block
-    if ((t.flags & 4) && left == kUnit) {
-      if (kind == 0) bad |= adamw_unit<BITS, false, false, true>(t, tab.s, gs, base, left, lane);
-      else if (kind == 1) bad |= adamw_unit<BITS, true, false, true>(t, tab.s, gs, base, left, lane);
-      else if (kind == 2) bad |= adamw_unit<BITS, false, true, true>(t, tab.s, gs, base, left, lane);
-      else bad |= adamw_unit<BITS, true, true, true>(t, tab.s, gs, base, left, lane);
-    } else {
-      if (kind == 0) bad |= adamw_unit<BITS, false, false, false>(t, tab.s, gs, base, left, lane);
-      else if (kind == 1) bad |= adamw_unit<BITS, true, false, false>(t, tab.s, gs, base, left, lane);
-      else if (kind == 2) bad |= adamw_unit<BITS, false, true, false>(t, tab.s, gs, base, left, lane);
-      else bad |= adamw_unit<BITS, true, true, false>(t, tab.s, gs, base, left, lane);
-    }
+    if (kind == 0) bad |= adamw_any<BITS, false, false>(t, tab.s, gs, base, left, lane);
+    else if (kind == 1) bad |= adamw_any<BITS, true, false>(t, tab.s, gs, base, left, lane);
+    else if (kind == 2) bad |= adamw_any<BITS, false, true>(t, tab.s, gs, base, left, lane);
+    else bad |= adamw_any<BITS, true, true>(t, tab.s, gs, base, left, lane);
   }
   if (bad) raise_flag(tab.s.err, kErrNonfinite);
 }
@@ -262,7 +296,12 @@ int launch_adamw_cap(const AdamwTensor* t, int count, int bits, const AdamwScala
   AdamwTable<CAP> tab;
   tab.s = sc;
   tab.count = 0;
-  tab.units = 4 * kAdamWarps;
+  // a block takes 32 units, or as few as 8 where the blocks would be too few to
+  // fill the SMs four times (each with four blocks)
+  int64_t units = 0;
+  for (int i = 0; i < count; ++i) units += (t[i].n + kUnit - 1) / kUnit;
+  int64_t per_warp = units / (static_cast<int64_t>(kAdamWarps) * di.sm_count * 16);
+  tab.units = kAdamWarps * static_cast<int>(per_warp < 1 ? 1 : per_warp > 4 ? 4 : per_warp);
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     tab.t[tab.count] = t[i];

@@ -15,10 +15,15 @@
 // groups of up to 32 tokens (z and grad_in) by bulk copies into a ring of its
 // own in shared memory: what is in flight does not depend on registers.  LPT
 // lanes share a token, C chunks of four experts a lane, chunk k at LPT k + sub,
-// so that fp32 and bf16 rows are both read and written in whole lines.
+// so that fp32 and bf16 rows are both written in whole sectors.  Few lanes with
+// many experts each (32 at E = 256), because what a token costs beside its
+// experts -- three reductions over its lanes, a reciprocal, a logarithm -- is
+// paid once for the tokens of a warp: with 32 lanes a token and 8 experts a
+// lane E = 256 took 480 instructions a token, and issue slots bounded the pass.
 #pragma once
 
 #include "eqb_device.cuh"
+#include "f32x2.cuh"
 #include "mbarrier.cuh"
 
 namespace eqb {
@@ -28,52 +33,7 @@ namespace {
 constexpr int kBalThreads = 256;
 constexpr int kBalWarps = kBalThreads / 32;
 constexpr int kBalMaxStages = 4;
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float ex2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ float rcp_approx(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-// fp32 min that propagates NaN.
-__device__ __forceinline__ float fmin_nan(float a, float b) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
-// Two fp32 values in one instruction.
-struct F2 {
-  uint64_t v;
-};
-__device__ __forceinline__ F2 f2(float a, float b) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float lo2(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v)); }
-__device__ __forceinline__ float hi2(F2 a) { return __uint_as_float(static_cast<uint32_t>(a.v >> 32)); }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Sum over the lanes that share `lane & (step - 1)` (step a power of two).
 __device__ __forceinline__ float sum_slots(float x, int step) {
@@ -94,10 +54,14 @@ struct BalanceCut {
 };
 
 // Blocks an SM holds, by their registers.
-constexpr int bal_blocks(bool sig_grad, int C) { return C <= 2 || (C == 3 && !sig_grad) ? 3 : C <= 4 ? 2 : 1; }
+constexpr int bal_blocks(bool grad, int C) { return C <= 3 || (C == 4 && !grad) ? 3 : 2; }
 
-// Shared memory: R [EM], the warps' column sums [8, EM], the rings, the barriers.
-__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM + 4 * kBalWarps * EM; }
+// Rows of the block's column sums in shared memory: the warps add theirs in
+// rounds where 8 rows would take much of it.
+constexpr int bal_rows(int EM) { return EM <= 256 ? kBalWarps : 2; }
+
+// Shared memory: R [EM], the warps' column sums [bal_rows, EM], the rings.
+__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM + 4 * bal_rows(EM) * EM; }
 __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bool gin) {
   return group * E * ((f32 ? 4 : 2) + (gin ? 4 : 0));
 }
@@ -107,10 +71,9 @@ __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bo
 // a.part, which no other pair of the two has, and balance_finish adds them up
 // in ascending order: no atomics, so the same call gives the same bits.
 template <bool SIG, bool GRAD, bool F32, int LPT, int C>
-__global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balance_kernel(BalanceArgs a, BalanceCut cut) {
+__global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kernel(BalanceArgs a, BalanceCut cut) {
   constexpr int TPW = 32 / LPT;    // tokens a warp takes at a time
   constexpr int EM = LPT * C * 4;  // experts the lanes hold
-  constexpr bool RREG = C <= 4;    // R in registers
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ float sums[kBalWarps][3];
   __shared__ __align__(8) uint64_t bars[kBalWarps * kBalMaxStages];
@@ -187,17 +150,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balan
       Rs[e] = r;
     }
     __syncthreads();
-    F2 r[RREG ? C : 1][2], acc[C][2];
-    auto load_r = [&](int k, F2 (&o)[2]) {
-      const float4 w = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
-      o[0] = f2(w.x, w.y);
-      o[1] = f2(w.z, w.w);
-    };
+    F2 acc[C][2];
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-      if constexpr (RREG) load_r(k, r[k]);
-      acc[k][0] = acc[k][1] = f2(0.f, 0.f);
-    }
+    for (int k = 0; k < C; ++k) acc[k][0] = acc[k][1] = f2(0.f, 0.f);
     const float ca = cs[0], cz = cs[1];
     float hsum = 0.f, zsum = 0.f, alive_n = 0.f;
 
@@ -218,69 +173,85 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balan
         const int i = i0 + slot;
         const bool in = i >= from && i < to;
         const bool ok = in && (mbits >> i & 1u);
+        // a row that does not count is read as zeros: finite, and its p becomes 0
         F2 e[C][2];
-        float top;
+        float top, low;
         if constexpr (F32) {
+          const float4* zr = reinterpret_cast<const float4*>(zs + static_cast<uint32_t>(i) * zrow) + sub;
           top = -INFINITY;
+          low = INFINITY;
 #pragma unroll
           for (int k = 0; k < C; ++k) {
-            const int c = sub + k * LPT;
-            float4 w = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            if (ok && c < nch) w = reinterpret_cast<const float4*>(zs + static_cast<uint32_t>(i) * zrow)[c];
-            top = fmaxf(fmaxf(top, fmaxf(w.x, w.y)), fmaxf(w.z, w.w));
+            float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (sub + k * LPT < nch) {
+              if (ok) w = zr[k * LPT];
+              top = fmaxf(fmaxf(top, fmaxf(w.x, w.y)), fmaxf(w.z, w.w));
+              if constexpr (SIG) low = fminf(fminf(low, fminf(w.x, w.y)), fminf(w.z, w.w));
+            }
             e[k][0] = f2(w.x, w.y);
             e[k][1] = f2(w.z, w.w);
           }
 #pragma unroll
           for (int m = 1; m < LPT; m <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, m));
         } else {
-          uint32_t top2 = 0xff80ff80u;  // -inf
+          const uint2* zr = reinterpret_cast<const uint2*>(zs + static_cast<uint32_t>(i) * zrow) + sub;
+          uint32_t top2 = 0xff80ff80u, low2 = 0x7f807f80u;  // -inf, inf
 #pragma unroll
           for (int k = 0; k < C; ++k) {
-            const int c = sub + k * LPT;
-            uint2 w = make_uint2(0xff80ff80u, 0xff80ff80u);
-            if (ok && c < nch) w = reinterpret_cast<const uint2*>(zs + static_cast<uint32_t>(i) * zrow)[c];
-            top2 = hmax2_bf16(top2, hmax2_bf16(w.x, w.y));
+            uint2 w = make_uint2(0u, 0u);
+            if (sub + k * LPT < nch) {
+              if (ok) w = zr[k * LPT];
+              top2 = hmax2_bf16(top2, hmax2_bf16(w.x, w.y));
+              if constexpr (SIG) low2 = hmin2_bf16(low2, hmin2_bf16(w.x, w.y));
+            }
             e[k][0] = f2(bf16_lo(w.x), bf16_hi(w.x));
             e[k][1] = f2(bf16_lo(w.y), bf16_hi(w.y));
           }
 #pragma unroll
           for (int m = 1; m < LPT; m <<= 1) top2 = hmax2_bf16(top2, __shfl_xor_sync(kFull, top2, m));
           top = fmaxf(bf16_lo(top2), bf16_hi(top2));
+          low = fminf(bf16_lo(low2), bf16_hi(low2));
         }
         // a row without a finite logit has no probabilities (nor has a masked one)
         const bool alive = ok && top > -INFINITY;
         // sigmoids are taken relative to e^top where all are far below 0.5:
         // s e^-top = 1 / (e^top + e^(top - z))
-        const float ref = !alive ? 0.f : SIG ? fminf(top, 0.f) : top;
+        const float ref = !(top > -INFINITY) ? 0.f : SIG ? fminf(top, 0.f) : top;
         const float m2 = ref * kLog2e;
-        const F2 mul = f2(SIG ? -kLog2e : kLog2e, SIG ? -kLog2e : kLog2e), shift = f2(SIG ? m2 : -m2, SIG ? m2 : -m2);
+        const F2 mul = splat2(SIG ? -kLog2e : kLog2e), shift = splat2(SIG ? m2 : -m2);
         const float em = SIG ? ex2_approx(m2) : 0.f;
-        F2 w[SIG && GRAD ? C : 1][2];  // 1 - s
+        const F2 em2 = splat2(em);
+        // one reciprocal serves two sigmoids as long as the product of the two
+        // denominators is finite; beyond 2^60 of the row's reference (-inf
+        // among them) a sigmoid counts as zero.  Most rows are nearer than that.
+        constexpr float kFar = 0x1p60f;
+        const bool far = SIG && __any_sync(kFull, low < ref - 40.f);
+        auto sigmoids = [&](F2 x) {
+          const F2 xc = far ? f2(fmin_nan(lo2(x), kFar), fmin_nan(hi2(x), kFar)) : x;
+          const F2 y = add2(em2, xc);
+          const F2 sg = mul2(splat2(rcp_approx(lo2(y) * hi2(y))), f2(hi2(y), lo2(y)));
+          return far ? f2(lo2(x) > kFar ? 0.f : lo2(sg), hi2(x) > kFar ? 0.f : hi2(sg)) : sg;
+        };
         F2 d2 = f2(0.f, 0.f), h2 = f2(0.f, 0.f);
+        {
 #pragma unroll
-        for (int k = 0; k < C; ++k) {
-          F2 rk[2];
-          if constexpr (!RREG) load_r(k, rk);
+          for (int k = 0; k < C; ++k) {
+            if (sub + k * LPT < nch) {
+              const float4 rw = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
+              const F2 rk[2] = {f2(rw.x, rw.y), f2(rw.z, rw.w)};
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const F2 x = fma2(e[k][q], mul, shift);
-            if constexpr (SIG) {
-              // one reciprocal for two: beyond 2^60 of the row's reference a
-              // sigmoid counts as zero, so that the product stays finite
-              constexpr float kFar = 0x1p60f;
-              const float x0 = ex2_approx(lo2(x)), x1 = ex2_approx(hi2(x));
-              const F2 xc = f2(fmin_nan(x0, kFar), fmin_nan(x1, kFar));
-              const F2 y = add2(f2(em, em), xc);
-              const float rr = rcp_approx(lo2(y) * hi2(y));
-              const F2 s = mul2(f2(rr, rr), f2(hi2(y), lo2(y)));
-              if constexpr (GRAD) w[k][q] = mul2(xc, s);
-              e[k][q] = f2(x0 > kFar ? 0.f : lo2(s), x1 > kFar ? 0.f : hi2(s));
+              for (int q = 0; q < 2; ++q) {
+                F2 x = fma2(e[k][q], mul, shift);
+                x = f2(ex2_approx(lo2(x)), ex2_approx(hi2(x)));
+                const F2 sg = SIG ? sigmoids(x) : x;
+                // with a gradient the sigmoid is formed again from x, which 1 - s needs too
+                e[k][q] = SIG && GRAD ? x : sg;
+                d2 = add2(d2, sg);
+                h2 = fma2(sg, rk[q], h2);
+              }
             } else {
-              e[k][q] = f2(ex2_approx(lo2(x)), ex2_approx(hi2(x)));
+              e[k][0] = e[k][1] = f2(0.f, 0.f);
             }
-            d2 = add2(d2, e[k][q]);
-            h2 = fma2(e[k][q], RREG ? r[RREG ? k : 0][q] : rk[q], h2);
           }
         }
         float d = lo2(d2) + hi2(d2), h = lo2(h2) + hi2(h2);
@@ -290,50 +261,51 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balan
           h += __shfl_xor_sync(kFull, h, m);
         }
         if (alive && !(d < INFINITY)) raise_flag(a.err, kErrNonfinite);
-        const float id = alive ? __frcp_rn(d) : 0.f;
+        float id = rcp_approx(d);
+        id = alive ? __fmaf_rn(id, __fmaf_rn(-d, id, 1.0f), id) : 0.f;
         h *= id;
         float lse = 0.f;
-        if (!SIG && a.zeta != 0.0) lse = alive ? top + logf(d) : 0.f;
+        if (!SIG && a.zeta != 0.0) lse = alive ? __fmaf_rn(lg2_approx(d), kLn2, top) : 0.f;
         if (sub == 0) {
           hsum += h;
           zsum = __fmaf_rn(lse, lse, zsum);
           alive_n += alive ? 1.f : 0.f;
         }
-        const F2 id2 = f2(id, id);
+        const F2 id2 = splat2(id);
         if constexpr (!GRAD) {
 #pragma unroll
           for (int k = 0; k < C; ++k)
 #pragma unroll
             for (int q = 0; q < 2; ++q) acc[k][q] = fma2(e[k][q], id2, acc[k][q]);
         } else {
-          const float kk = __fmaf_rn(-ca, h, cz * lse);
-          const F2 ca2 = f2(ca, ca), k2 = f2(kk, kk);
-          const int64_t tok = g0 + i;
+          const F2 ca2 = splat2(ca), k2 = splat2(__fmaf_rn(-ca, h, cz * lse));
+          const float4* gr = reinterpret_cast<const float4*>(gsrc + static_cast<uint32_t>(i) * grow) + sub;
+          const int64_t at = (g0 + i) * nch + sub;  // chunk of the output
 #pragma unroll
           for (int k = 0; k < C; ++k) {
-            const int c = sub + k * LPT;
-            F2 rk[2], g[2];
-            if constexpr (!RREG) load_r(k, rk);
-            const bool have = in && c < nch;
+            if (sub + k * LPT >= nch) continue;
+            const float4 rw = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
+            const F2 rk[2] = {f2(rw.x, rw.y), f2(rw.z, rw.w)};
             float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (gin && have) old = reinterpret_cast<const float4*>(gsrc + static_cast<uint32_t>(i) * grow)[c];
-            g[0] = f2(old.x, old.y);
-            g[1] = f2(old.z, old.w);
+            if (gin) old = gr[k * LPT];
+            F2 g[2] = {f2(old.x, old.y), f2(old.z, old.w)};
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              const F2 p = mul2(e[k][q], id2);
-              acc[k][q] = fma2(e[k][q], id2, acc[k][q]);  // as without a gradient
-              F2 v = fma2(ca2, RREG ? r[RREG ? k : 0][q] : rk[q], k2);
-              if constexpr (SIG) v = mul2(v, w[k][q]);
-              g[q] = fma2(p, v, g[q]);
+              const F2 sg = SIG ? sigmoids(e[k][q]) : e[k][q];
+              acc[k][q] = fma2(sg, id2, acc[k][q]);
+              F2 v = fma2(ca2, rk[q], k2);
+              if constexpr (SIG) {
+                const F2 xc = far ? f2(fmin_nan(lo2(e[k][q]), kFar), fmin_nan(hi2(e[k][q]), kFar)) : e[k][q];
+                v = mul2(v, mul2(xc, sg));
+              }
+              g[q] = fma2(mul2(sg, id2), v, g[q]);
             }
-            if (!have) continue;
+            if (!in) continue;
             if (a.grad_bf16)
-              __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.grad_out) + tok * E) + c,
+              __stcs(static_cast<uint2*>(a.grad_out) + at + k * LPT,
                      make_uint2(pack_bf16x2_rn(lo2(g[0]), hi2(g[0])), pack_bf16x2_rn(lo2(g[1]), hi2(g[1]))));
             else
-              __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.grad_out) + tok * E) + c,
-                     make_float4(lo2(g[0]), hi2(g[0]), lo2(g[1]), hi2(g[1])));
+              __stcs(static_cast<float4*>(a.grad_out) + at + k * LPT, make_float4(lo2(g[0]), hi2(g[0]), lo2(g[1]), hi2(g[1])));
           }
         }
       }
@@ -349,11 +321,22 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balan
     // the block's sums of this microbatch
     if (a.part) {
       float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;
+      constexpr int ROWS = bal_rows(EM);
+      for (int round = 0; round < kBalWarps / ROWS; ++round) {
+        if (round) __syncthreads();
+        if (wid / ROWS != round) continue;
 #pragma unroll
-      for (int k = 0; k < C; ++k) {
-        const float4 v = make_float4(sum_slots(lo2(acc[k][0]), LPT), sum_slots(hi2(acc[k][0]), LPT),
-                                     sum_slots(lo2(acc[k][1]), LPT), sum_slots(hi2(acc[k][1]), LPT));
-        if (slot == 0) reinterpret_cast<float4*>(colsum + wid * EM)[sub + k * LPT] = v;
+        for (int k = 0; k < C; ++k) {
+          float4 v = make_float4(sum_slots(lo2(acc[k][0]), LPT), sum_slots(hi2(acc[k][0]), LPT),
+                                 sum_slots(lo2(acc[k][1]), LPT), sum_slots(hi2(acc[k][1]), LPT));
+          float4* col = reinterpret_cast<float4*>(colsum + wid % ROWS * EM) + sub + k * LPT;
+          if (round) {
+            const float4 w = *col;
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+          }
+          __syncwarp();
+          if (slot == 0) *col = v;
+        }
       }
       hsum = sum_slots(hsum, 1);
       zsum = sum_slots(zsum, 1);
@@ -367,7 +350,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(SIG && GRAD, C)) balan
       for (int e = threadIdx.x; e < E; e += kBalThreads) {
         float v = 0.f;
 #pragma unroll
-        for (int q = 0; q < kBalWarps; ++q) v += colsum[q * EM + e];
+        for (int q = 0; q < bal_rows(EM); ++q) v += colsum[q * EM + e];
         row[4 + e] = v;
       }
       if (threadIdx.x < 3) {
@@ -396,12 +379,12 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   cut.group = TPW;
   while (cut.group * 2 <= 32 && bal_stage_bytes(a.E, cut.group * 2, F32, gin) <= 2048) cut.group *= 2;
   // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
-  const int room = di.max_smem_optin / bal_blocks(SIG && GRAD, C) - 2048 - bal_fixed_bytes(EM);
+  const int room = di.max_smem_optin / bal_blocks(GRAD, C) - 2048 - bal_fixed_bytes(EM);
   cut.stages = room / (kBalWarps * bal_stage_bytes(a.E, cut.group, F32, gin));
   if (cut.stages > kBalMaxStages) cut.stages = kBalMaxStages;
   if (cut.stages < 1) return kErrUnsupported;
   int64_t grid = (a.T + kBalWarps * TPW - 1) / (kBalWarps * TPW);
-  const int64_t most = di.sm_count * bal_blocks(SIG && GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(SIG && GRAD, C) : kBalMaxGrid;
+  const int64_t most = di.sm_count * bal_blocks(GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(GRAD, C) : kBalMaxGrid;
   if (grid > most) grid = most;
   cut.tokens_per_cta = (a.T + grid - 1) / grid;
   run->tokens_per_cta = cut.tokens_per_cta;
@@ -419,13 +402,13 @@ int launch_bal_width(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   if (a.E <= 16) return launch_bal<SIG, GRAD, F32, 2, 2>(a, run, s);
   if (a.E <= 32) return launch_bal<SIG, GRAD, F32, 4, 2>(a, run, s);
   if (a.E <= 48) return launch_bal<SIG, GRAD, F32, 4, 3>(a, run, s);
-  if (a.E <= 64) return launch_bal<SIG, GRAD, F32, 8, 2>(a, run, s);
+  if (a.E <= 64) return launch_bal<SIG, GRAD, F32, 4, 4>(a, run, s);
   if (a.E <= 96) return launch_bal<SIG, GRAD, F32, 8, 3>(a, run, s);
-  if (a.E <= 128) return launch_bal<SIG, GRAD, F32, 16, 2>(a, run, s);
-  if (a.E <= 192) return launch_bal<SIG, GRAD, F32, 16, 3>(a, run, s);
-  if (a.E <= 256) return launch_bal<SIG, GRAD, F32, 32, 2>(a, run, s);
-  if (a.E <= 384) return launch_bal<SIG, GRAD, F32, 32, 3>(a, run, s);
-  if (a.E <= 512) return launch_bal<SIG, GRAD, F32, 32, 4>(a, run, s);
+  if (a.E <= 128) return launch_bal<SIG, GRAD, F32, 8, 4>(a, run, s);
+  if (a.E <= 192) return launch_bal<SIG, GRAD, F32, 8, 6>(a, run, s);
+  if (a.E <= 256) return launch_bal<SIG, GRAD, F32, 8, 8>(a, run, s);
+  if (a.E <= 384) return launch_bal<SIG, GRAD, F32, 16, 6>(a, run, s);
+  if (a.E <= 512) return launch_bal<SIG, GRAD, F32, 16, 8>(a, run, s);
   if (a.E <= 768) return launch_bal<SIG, GRAD, F32, 32, 6>(a, run, s);
   if (a.E <= 1024) return launch_bal<SIG, GRAD, F32, 32, 8>(a, run, s);
   return kErrUnsupported;
