@@ -513,8 +513,8 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  * Zeroed states (and scales) are those of a first step.
  *   tensors    host array [count]; read before the call returns.  n >= 0; an
  *              entry with n = 0 or grad = NULL is left as it is.  Tensors must
- *              not overlap.  Any element alignment; 16-byte alignment
- *              (8 of 8-bit arrays) is the fast path.
+ *              not overlap.  Any element alignment; arrays aligned to 16
+ *              bytes are the fast path.
  *   grad_scale device fp32 [1] (nullable: 1): a clipping factor or the inverse
  *              of a loss scale, formed on the device
  *   err_flag   EQB_ERR_NONFINITE if a moment became non-finite (a gradient

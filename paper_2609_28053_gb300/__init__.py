@@ -598,7 +598,8 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
     return dx, dW
 
 
-_data_ptr, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.get_device, torch.Tensor.is_contiguous
+_data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
+_get_device, _is_contiguous = torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 
 class EqbAdamW:
@@ -670,7 +671,7 @@ class EqbAdamW:
         # aliases: what the table points to stays allocated whatever becomes of the tensors above
         self._held = [t.detach() for t in self.params + states]
         self._ptrs = [p.data_ptr() for p in self.params]
-        self._shapes = [p.shape for p in self.params]
+        self._numels = [p.numel() for p in self.params]
         self._device = [p.get_device() for p in self.params]
         self._dtypes = None  # of the last step's gradients: the table's grad_bf16
         self._whole = [True] * len(self.params)
@@ -690,7 +691,7 @@ class EqbAdamW:
         try:  # the checks of all of them at once: hundreds of tensors take longer one by one than their step
             ptrs = list(map(_data_ptr, grads))
             fits = (list(map(_get_device, grads)) == self._device and list(map(_is_contiguous, grads)) == self._whole and
-                    [g.shape for g in grads] == self._shapes and [g.dtype for g in grads] == self._dtypes)
+                    list(map(_numel, grads)) == self._numels and [g.dtype for g in grads] == self._dtypes)
         except (TypeError, AttributeError):
             fits = False
         if fits:
@@ -701,7 +702,9 @@ class EqbAdamW:
                 e.grad = None
                 continue
             bf16 = isinstance(g, torch.Tensor) and g.dtype is torch.bfloat16
-            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]", p.shape)
+            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]")
+            if g.numel() != p.numel():
+                raise ValueError(f"grads[{i}] must have shape {tuple(p.shape)} or as many elements, got {tuple(g.shape)}")
             if g.device != p.device:
                 raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
             e.grad, e.grad_bf16 = g.data_ptr(), bf16
@@ -710,8 +713,8 @@ class EqbAdamW:
     def step(self, grads, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, grad_scale=None, err_flag=None,
              stream=None):
         """One step (step = 1 for the first) with `grads`, a list of fp32 or
-        bf16 tensors of the parameters' shapes; a parameter whose entry is
-        None is left as it is.  grad_scale: fp32 CUDA tensor [1] that every
+        bf16 tensors of the parameters' shapes (or flat); a parameter whose
+        entry is None is left as it is.  grad_scale: fp32 CUDA tensor [1] that every
         gradient is multiplied by."""
         if len(grads) != len(self.params):
             raise ValueError(f"grads must have {len(self.params)} entries, got {len(grads)}")

@@ -10,11 +10,14 @@
 // nothing to copy, to own or to keep), a block finds its tensor by bisection,
 // and a warp takes 256 consecutive elements at a time, eight a lane: the elements
 // of one 8-bit scale, whose largest magnitude is then one reduction within the
-// warp.  Every operation up to the moments and their scales is rounded to
+// warp.  With 8-bit states a lane reads 48 bytes a unit, too few to hide a
+// load's latency behind the warps of an SM, so there each warp fetches its units
+// by bulk copies into a ring of its own in shared memory.  Every operation up to the moments and their scales is rounded to
 // nearest by itself, so that the 8-bit codes do not depend on how the compiler
 // fuses them.
 #include "eqb_device.cuh"
 #include "f32x2.cuh"
+#include "mbarrier.cuh"
 
 namespace eqb {
 
@@ -33,6 +36,7 @@ struct AdamwTable {
   int32_t first[CAP];  // the first block of each tensor
   int32_t count;
   int32_t units;       // units a block takes
+  int32_t stage;       // bytes of a stage of a warp's ring (8 bits)
   AdamwScalars s;
 };
 
@@ -59,39 +63,67 @@ __device__ __forceinline__ uint32_t f32_to_e4m3x2(F2 x) {
 // arrays that are not aligned, and a tensor's last unit).
 enum Layout { Run, Quads, Single };
 
-template <bool BF16, Layout L>
-__device__ __forceinline__ void load8(const void* src, int64_t base, int left, int lane, F2 (&x)[4]) {
+// Eight elements of a lane as they lie in memory: W words for elements of
+// 4 W / 8 bytes (single ones of 1 and 2 bytes are packed as the wide loads
+// have them).
+template <int W, Layout L>
+__device__ __forceinline__ void load_words(const void* src, int64_t base, int left, int lane, uint32_t (&w)[W]) {
+  constexpr int B = W / 2;  // bytes an element
+  const uint8_t* p = static_cast<const uint8_t*>(src) + base * B;
   if constexpr (L == Single) {
-    float v[8];
+    uint32_t v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int i = j * 32 + lane;
-      v[j] = i >= left ? 0.f
-             : BF16    ? bf16_bits_to_f32(static_cast<const uint16_t*>(src)[base + i])
-                       : static_cast<const float*>(src)[base + i];
+      v[j] = 0;
+      if (i < left)
+        v[j] = B == 4 ? reinterpret_cast<const uint32_t*>(p)[i] : B == 2 ? reinterpret_cast<const uint16_t*>(p)[i] : p[i];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = f2(v[2 * j], v[2 * j + 1]);
-  } else if constexpr (BF16 && L == Run) {
-    const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(src) + base) + lane);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    for (int k = 0; k < W; ++k) {
+      if constexpr (B == 4) w[k] = v[k];
+      else if constexpr (B == 2) w[k] = v[2 * k] | v[2 * k + 1] << 16;
+      else w[k] = v[4 * k] | v[4 * k + 1] << 8 | v[4 * k + 2] << 16 | v[4 * k + 3] << 24;
+    }
+  } else if constexpr (L == Run && W == 2) {
+    const uint2 u = __ldcs(reinterpret_cast<const uint2*>(p) + lane);
+    w[0] = u.x; w[1] = u.y;
+  } else if constexpr (L == Run) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = f2(bf16_lo(u[j]), bf16_hi(u[j]));
-  } else if constexpr (BF16) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint2 w = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(src) + base + h * 128) + lane);
-      x[2 * h] = f2(bf16_lo(w.x), bf16_hi(w.x));
-      x[2 * h + 1] = f2(bf16_lo(w.y), bf16_hi(w.y));
+    for (int h = 0; h < W / 4; ++h) {
+      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p) + W / 4 * lane + h);
+      w[4 * h] = u.x; w[4 * h + 1] = u.y; w[4 * h + 2] = u.z; w[4 * h + 3] = u.w;
     }
   } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(src) + base);
-      const float4 w = __ldcs(p + (L == Run ? 2 * lane + h : 32 * h + lane));
-      x[2 * h] = f2(w.x, w.y);
-      x[2 * h + 1] = f2(w.z, w.w);
+      if constexpr (W == 8) {
+        const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p) + 32 * h + lane);
+        w[4 * h] = u.x; w[4 * h + 1] = u.y; w[4 * h + 2] = u.z; w[4 * h + 3] = u.w;
+      } else if constexpr (W == 4) {
+        const uint2 u = __ldcs(reinterpret_cast<const uint2*>(p) + 32 * h + lane);
+        w[2 * h] = u.x; w[2 * h + 1] = u.y;
+      } else {
+        w[h] = __ldcs(reinterpret_cast<const uint32_t*>(p) + 32 * h + lane);
+      }
     }
+  }
+}
+
+// The words' values, in pairs.
+__device__ __forceinline__ void values_of(const uint32_t (&w)[8], F2 (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = f2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+}
+__device__ __forceinline__ void values_of(const uint32_t (&w)[4], F2 (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = f2(bf16_lo(w[j]), bf16_hi(w[j]));
+}
+__device__ __forceinline__ void values_of(const uint32_t (&w)[2], F2 (&x)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    x[2 * h] = e4m3x2_to_f32(w[h] & 0xffffu);
+    x[2 * h + 1] = e4m3x2_to_f32(w[h] >> 16);
   }
 }
 
@@ -128,35 +160,6 @@ __device__ __forceinline__ void store8(void* dst, int64_t base, int left, int la
 }
 
 template <Layout L>
-__device__ __forceinline__ void load8_e4m3(const void* src, int64_t base, int left, int lane, float scale, F2 (&x)[4]) {
-  const uint8_t* c = static_cast<const uint8_t*>(src) + base;
-  if constexpr (L == Single) {
-    uint32_t v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j * 32 + lane < left ? c[j * 32 + lane] : 0u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = e4m3x2_to_f32(v[2 * j] | v[2 * j + 1] << 8);
-  } else {
-    uint32_t w[2];
-    if constexpr (L == Run) {
-      const uint2 u = __ldcs(reinterpret_cast<const uint2*>(c) + lane);
-      w[0] = u.x;
-      w[1] = u.y;
-    } else {
-      w[0] = __ldcs(reinterpret_cast<const uint32_t*>(c) + lane);
-      w[1] = __ldcs(reinterpret_cast<const uint32_t*>(c + 128) + lane);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      x[2 * h] = e4m3x2_to_f32(w[h] & 0xffffu);
-      x[2 * h + 1] = e4m3x2_to_f32(w[h] >> 16);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = mul2(x[j], splat2(scale));
-}
-
-template <Layout L>
 __device__ __forceinline__ void store8_e4m3(void* dst, int64_t base, int left, int lane, const F2 (&x)[4]) {
   uint8_t* c = static_cast<uint8_t*>(dst) + base;
   uint32_t p[4];
@@ -174,49 +177,65 @@ __device__ __forceinline__ void store8_e4m3(void* dst, int64_t base, int left, i
   }
 }
 
+// fp32 max of a and |b| that propagates NaN.
+__device__ __forceinline__ float max_abs(float a, float b) { return fmax_nan(a, fabsf(b)); }
+
 // The scale of a unit and its reciprocal, from the largest magnitude of the
-// warp's elements (a NaN is larger than all, so it stays visible).  A unit
-// below the normal numbers is stored as zeros.  False if it is not finite.
+// warp's elements.  A unit below the normal numbers is stored as zeros.  False
+// if it is not finite.
 __device__ __forceinline__ bool unit_scale(const F2 (&x)[4], float& scale, float& inv) {
-  uint32_t a = 0;
+  float a = 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    a = max(a, max(__float_as_uint(lo2(x[j])) & 0x7fffffffu, __float_as_uint(hi2(x[j])) & 0x7fffffffu));
-  a = __reduce_max_sync(kFull, a);
-  scale = __fmul_rn(__uint_as_float(a), 1.0f / kTop);
+  for (int j = 0; j < 4; ++j) a = max_abs(max_abs(a, lo2(x[j])), hi2(x[j]));
+  // bit patterns of magnitudes are in their order, NaN above all
+  const uint32_t u = __reduce_max_sync(kFull, __float_as_uint(a));
+  scale = __fmul_rn(__uint_as_float(u), 1.0f / kTop);
   if (scale < kMinNormal) scale = 0.f;
-  inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
-  return a < 0x7f800000u;
+  const float r = rcp_approx(scale);
+  inv = scale > 0.f ? __fmaf_rn(r, __fmaf_rn(-scale, r, 1.0f), r) : 0.f;
+  return u < 0x7f800000u;
 }
 
-// One unit of a tensor: `left` elements from `base` on (256 unless Single).
+// What a lane reads of one unit of a tensor: `left` elements from `base` on
+// (256 unless Single).
+template <int BITS, bool PB, bool GB>
+struct UnitWords {
+  uint32_t p[PB ? 4 : 8], g[GB ? 4 : 8], m[BITS / 4], v[BITS / 4];
+  float ms, vs;
+};
+template <int BITS, bool PB, bool GB, Layout L>
+__device__ __forceinline__ void load_unit(const AdamwTensor& t, int64_t base, int left, int lane, UnitWords<BITS, PB, GB>& w) {
+  load_words<PB ? 4 : 8, L>(t.p, base, left, lane, w.p);
+  load_words<GB ? 4 : 8, L>(t.g, base, left, lane, w.g);
+  load_words<BITS / 4, L>(t.m, base, left, lane, w.m);
+  load_words<BITS / 4, L>(t.v, base, left, lane, w.v);
+  if constexpr (BITS == 8) {
+    w.ms = t.ms[base / kUnit];
+    w.vs = t.vs[base / kUnit];
+  }
+}
+
 // The update's root and quotient are within 2 ulps: rounded to nearest they take
 // about twenty instructions of the fifty-five that an 8-bit element has time for.
 template <int BITS, bool PB, bool GB, Layout L>
 __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t base, int left,
-                                           int lane) {
+                                           int lane, const UnitWords<BITS, PB, GB>& w) {
   F2 p[4], g[4], m[4], v[4];
   const int64_t unit = base / kUnit;
-  float ms = 0.f, vs = 0.f;
-  if constexpr (BITS == 8) {
-    ms = t.ms[unit];
-    vs = t.vs[unit];
-  }
-  load8<PB, L>(t.p, base, left, lane, p);
-  load8<GB, L>(t.g, base, left, lane, g);
-  if constexpr (BITS == 32) {
-    load8<false, L>(t.m, base, left, lane, m);
-    load8<false, L>(t.v, base, left, lane, v);
-  } else {
-    load8_e4m3<L>(t.m, base, left, lane, ms, m);
-    load8_e4m3<L>(t.v, base, left, lane, vs, v);
-  }
+  values_of(w.p, p);
+  values_of(w.g, g);
+  values_of(w.m, m);
+  values_of(w.v, v);
   bool bad = false;
   F2 root[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const F2 gj = mul2(g[j], splat2(gs));
-    if constexpr (BITS == 8) v[j] = mul2(v[j], v[j]);  // the root is what 8 bits hold
+    if constexpr (BITS == 8) {
+      m[j] = mul2(m[j], splat2(w.ms));
+      v[j] = mul2(v[j], splat2(w.vs));
+      v[j] = mul2(v[j], v[j]);  // the root is what 8 bits hold
+    }
     m[j] = add2(mul2(m[j], splat2(s.b1)), mul2(gj, splat2(s.c1)));
     v[j] = add2(mul2(v[j], splat2(s.b2)), mul2(mul2(gj, splat2(s.c2)), gj));
     root[j] = f2(sqrt_approx(lo2(v[j])), sqrt_approx(hi2(v[j])));
@@ -233,17 +252,23 @@ __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScal
     store8<false, L>(t.m, base, left, lane, m);
     store8<false, L>(t.v, base, left, lane, v);
   } else {
-    float mi, vi;
+    float ms, vs, mi, vi;
     bad = !unit_scale(m, ms, mi);
     bad |= !unit_scale(root, vs, vi);
+    float low = INFINITY;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m[j] = mul2(m[j], splat2(mi));
-      const F2 u = mul2(root[j], splat2(vi));
-      // a root that is not zero stays so: eps alone in the denominator would
-      // make a step out of what is left in m.  (fmaxf would drop a NaN.)
-      root[j] = f2(lo2(root[j]) > 0.f && lo2(u) < kLeast && vi > 0.f ? kLeast : lo2(u),
-                   hi2(root[j]) > 0.f && hi2(u) < kLeast && vi > 0.f ? kLeast : hi2(u));
+      root[j] = mul2(root[j], splat2(vi));
+      low = fminf(low, fminf(lo2(root[j]), hi2(root[j])));
+    }
+    // a root that is not zero stays so: eps alone in the denominator would make
+    // a step out of what is left in m
+    if (low < kLeast && vi > 0.f) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        root[j] = f2(lo2(v[j]) > 0.f && lo2(root[j]) < kLeast ? kLeast : lo2(root[j]),
+                     hi2(v[j]) > 0.f && hi2(root[j]) < kLeast ? kLeast : hi2(root[j]));
     }
     store8_e4m3<L>(t.m, base, left, lane, m);
     store8_e4m3<L>(t.v, base, left, lane, root);
@@ -255,16 +280,148 @@ __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScal
   return bad;
 }
 
+// A warp's units of a block's chunk, numbers warp, warp + 8, ... of `units`;
+// with 32-bit states the next one's loads are issued before the current one's
+// arithmetic (403M fp32 parameters with bf16 gradients and copies 1,640 -> 1,618 us).
+template <int BITS, bool PB, bool GB, Layout L>
+__device__ __forceinline__ bool adamw_units(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t first, int units,
+                                            int warp, int lane) {
+  UnitWords<BITS, PB, GB> w, next;
+  constexpr bool AHEAD = BITS == 32 && L != Single;
+  bool bad = false;
+  auto left_of = [&](int k) {
+    const int64_t n = t.n - (first + k) * kUnit;
+    return n < kUnit ? static_cast<int>(n) : kUnit;
+  };
+  if (AHEAD && warp < units) load_unit<BITS, PB, GB, L>(t, (first + warp) * kUnit, left_of(warp), lane, w);
+  for (int k = warp; k < units; k += kAdamWarps) {
+    if (!AHEAD)
+      load_unit<BITS, PB, GB, L>(t, (first + k) * kUnit, left_of(k), lane, w);
+    else if (k + kAdamWarps < units)
+      load_unit<BITS, PB, GB, L>(t, (first + k + kAdamWarps) * kUnit, left_of(k + kAdamWarps), lane, next);
+    bad |= adamw_unit<BITS, PB, GB, L>(t, s, gs, (first + k) * kUnit, left_of(k), lane, w);
+    if (AHEAD) w = next;
+  }
+  return bad;
+}
+
+// A warp's ring: stages of two units (p, g, m and v one after the other, as far
+// as the chunk goes), and where it stands.
+struct AdamwRing {
+  uint8_t* at;
+  uint32_t bar;  // kRing barriers
+  uint32_t bytes;
+};
+constexpr int kRing = 2;
+
+// The whole units of a chunk with 8-bit states, through the ring: numbers
+// 16 j + 2 warp and the one after it.  `stalled`: a wait ran out.
+template <bool PB, bool GB>
+__device__ __forceinline__ bool adamw_stream(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t first, int units,
+                                             int warp, int lane, const AdamwRing& ring, volatile int* stalled) {
+  constexpr uint32_t PE = PB ? 2 : 4, GE = GB ? 2 : 4, U = kUnit;
+  const int nj = (units - 2 * warp + 2 * kAdamWarps - 1) / (2 * kAdamWarps);  // may be 0 or less
+  auto unit_of = [&](int j) { return first + 2 * (j * kAdamWarps + warp); };
+  auto count_of = [&](int j) { return min(2, units - 2 * (j * kAdamWarps + warp)); };
+  auto issue = [&](int j) {
+    if (lane == 0) {
+      const int64_t u = unit_of(j);
+      const uint32_t n = static_cast<uint32_t>(count_of(j)) * U, dst = smem_u32(ring.at) + (j & 1) * ring.bytes;
+      const uint32_t bar = ring.bar + 8u * (j & 1);
+      mbar_expect_tx(bar, n * (PE + GE + 2));
+      bulk_load(dst, static_cast<const uint8_t*>(t.p) + u * U * PE, n * PE, bar);
+      bulk_load(dst + 2 * U * PE, static_cast<const uint8_t*>(t.g) + u * U * GE, n * GE, bar);
+      bulk_load(dst + 2 * U * (PE + GE), static_cast<const uint8_t*>(t.m) + u * U, n, bar);
+      bulk_load(dst + 2 * U * (PE + GE + 1), static_cast<const uint8_t*>(t.v) + u * U, n, bar);
+    }
+  };
+  // lanes 0, 1: the scales of m of the two units, lanes 2, 3: of v
+  auto scale_of = [&](int j) {
+    const int64_t u = unit_of(j) + (lane & 1);
+    return lane < 4 && (lane & 1) < count_of(j) ? (lane < 2 ? t.ms : t.vs)[u] : 0.f;
+  };
+  for (int j = 0; j < kRing && j < nj; ++j) issue(j);
+  float scale = nj > 0 ? scale_of(0) : 0.f;
+  bool bad = false;
+  for (int j = 0; j < nj; ++j) {
+    const float next = j + 1 < nj ? scale_of(j + 1) : 0.f;
+    if (!__all_sync(kFull, mbar_wait(ring.bar + 8u * (j & 1), (j >> 1) & 1u, stalled))) {
+      if (lane == 0) drain_loads(min(nj, j + kRing), kRing, [&](int k) { return ring.bar + 8u * k; });
+      return bad;
+    }
+    const uint8_t* src = ring.at + (j & 1) * ring.bytes;
+    const int n = count_of(j);
+    for (int i = 0; i < n; ++i) {
+      UnitWords<8, PB, GB> w;
+      auto take = [&](uint32_t off, auto& x) {
+        constexpr int W = sizeof(x) / 4;
+        if constexpr (W == 2) {
+          const uint2 v = reinterpret_cast<const uint2*>(src + off)[lane + 32 * i];
+          x[0] = v.x; x[1] = v.y;
+        } else {
+#pragma unroll
+          for (int h = 0; h < W / 4; ++h) {
+            // Run: a lane's eight elements are neighbours; Quads: two groups of four
+            const int c = PB ? W / 4 * lane + h : 32 * h + lane;
+            const uint4 v = reinterpret_cast<const uint4*>(src + off)[c + 32 * (W / 4) * i];
+            x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+          }
+        }
+      };
+      auto take_quads = [&](uint32_t off, auto& x) {  // the same of 2- and 1-byte elements in the layout Quads
+        constexpr int W = sizeof(x) / 4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if constexpr (W == 4) {
+            const uint2 v = reinterpret_cast<const uint2*>(src + off)[64 * i + 32 * h + lane];
+            x[2 * h] = v.x; x[2 * h + 1] = v.y;
+          } else {
+            x[h] = reinterpret_cast<const uint32_t*>(src + off)[64 * i + 32 * h + lane];
+          }
+        }
+      };
+      take(0, w.p);
+      if constexpr (!PB && GB) take_quads(2 * U * PE, w.g);
+      else take(2 * U * PE, w.g);
+      if constexpr (PB) {
+        take(2 * U * (PE + GE), w.m);
+        take(2 * U * (PE + GE + 1), w.v);
+      } else {
+        take_quads(2 * U * (PE + GE), w.m);
+        take_quads(2 * U * (PE + GE + 1), w.v);
+      }
+      w.ms = __shfl_sync(kFull, scale, i);
+      w.vs = __shfl_sync(kFull, scale, 2 + i);
+      bad |= adamw_unit<8, PB, GB, PB ? Run : Quads>(t, s, gs, (unit_of(j) + i) * U, kUnit, lane, w);
+    }
+    scale = next;
+    __syncwarp();
+    if (j + kRing < nj) issue(j + kRing);
+  }
+  return bad;
+}
+
+// The chunk of `units` units from number `first` of a tensor on, as far as the
+// tensor goes.
 template <int BITS, bool PB, bool GB>
-__device__ __forceinline__ bool adamw_any(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t base, int left,
-                                          int lane) {
-  constexpr Layout wide = BITS == 8 && PB ? Run : Quads;
-  if ((t.flags & 4) && left == kUnit) return adamw_unit<BITS, PB, GB, wide>(t, s, gs, base, left, lane);
-  return adamw_unit<BITS, PB, GB, Single>(t, s, gs, base, left, lane);
+__device__ __forceinline__ bool adamw_chunk(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t first, int units,
+                                            int warp, int lane, const AdamwRing& ring, volatile int* stalled) {
+  const int64_t whole = t.n / kUnit - first;  // whole units left
+  const int all = static_cast<int>(min(static_cast<int64_t>(units), (t.n + kUnit - 1) / kUnit - first));
+  if (!(t.flags & 4)) return adamw_units<BITS, PB, GB, Single>(t, s, gs, first, all, warp, lane);
+  bool bad;
+  const int n = whole < units ? static_cast<int>(whole) : units;
+  if constexpr (BITS == 8) bad = adamw_stream<PB, GB>(t, s, gs, first, n, warp, lane, ring, stalled);
+  else bad = adamw_units<BITS, PB, GB, Quads>(t, s, gs, first, n, warp, lane);
+  if (whole < all && warp == 0) bad |= adamw_units<BITS, PB, GB, Single>(t, s, gs, first + whole, 1, 0, lane);
+  return bad;
 }
 
 template <int CAP, int BITS>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
+__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 4 : 2) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ __align__(8) uint64_t bars[kAdamWarps * kRing];
+  __shared__ int stalled;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int lo = 0, hi = tab.count - 1;
   while (lo < hi) {
@@ -273,20 +430,28 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   }
   const AdamwTensor& t = tab.t[lo];
   const int64_t chunk = static_cast<int64_t>(blockIdx.x) - tab.first[lo];
+  AdamwRing ring{sm + static_cast<size_t>(warp) * kRing * tab.stage, smem_u32(bars + warp * kRing),
+                 static_cast<uint32_t>(tab.stage)};
+  if constexpr (BITS == 8) {
+    if (lane == 0) {
+      for (int k = 0; k < kRing; ++k) mbar_init(ring.bar + 8u * k, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (threadIdx.x == 0) stalled = 0;
+    __syncthreads();
+  }
   griddep_wait();
   const float gs = tab.s.grad_scale ? *tab.s.grad_scale : 1.0f;
-  bool bad = false;
-  for (int k = warp; k < tab.units; k += kAdamWarps) {
-    const int64_t base = (chunk * tab.units + k) * kUnit;
-    if (base >= t.n) break;
-    const int left = t.n - base < kUnit ? static_cast<int>(t.n - base) : kUnit;
-    const int kind = t.flags & 3;  // uniform in the block
-    if (kind == 0) bad |= adamw_any<BITS, false, false>(t, tab.s, gs, base, left, lane);
-    else if (kind == 1) bad |= adamw_any<BITS, true, false>(t, tab.s, gs, base, left, lane);
-    else if (kind == 2) bad |= adamw_any<BITS, false, true>(t, tab.s, gs, base, left, lane);
-    else bad |= adamw_any<BITS, true, true>(t, tab.s, gs, base, left, lane);
-  }
+  const int kind = t.flags & 3;  // uniform in the block
+  const int64_t first = chunk * tab.units;
+  bool bad;
+  if (kind == 0) bad = adamw_chunk<BITS, false, false>(t, tab.s, gs, first, tab.units, warp, lane, ring, &stalled);
+  else if (kind == 1) bad = adamw_chunk<BITS, true, false>(t, tab.s, gs, first, tab.units, warp, lane, ring, &stalled);
+  else if (kind == 2) bad = adamw_chunk<BITS, false, true>(t, tab.s, gs, first, tab.units, warp, lane, ring, &stalled);
+  else bad = adamw_chunk<BITS, true, true>(t, tab.s, gs, first, tab.units, warp, lane, ring, &stalled);
   if (bad) raise_flag(tab.s.err, kErrNonfinite);
+  if (BITS == 8 && lane == 0 && *static_cast<volatile int*>(&stalled)) raise_flag(tab.s.err, kErrCuda);
 }
 
 template <int CAP>
@@ -310,10 +475,18 @@ int launch_adamw_cap(const AdamwTensor* t, int count, int bits, const AdamwScala
     blocks += (t[i].n + per - 1) / per;
     if (blocks > INT32_MAX) return kErrUnsupported;
   }
+  // the widest element of p and g among the tensors sets the ring's stage
+  int wide = 4;
+  for (int i = 0; i < count; ++i) {
+    const int w = (t[i].flags & 1 ? 2 : 4) + (t[i].flags & 2 ? 2 : 4);
+    if (w > wide) wide = w;
+  }
+  tab.stage = bits == 8 ? 2 * kUnit * (wide + 2) : 0;
+  const int smem = kAdamWarps * kRing * tab.stage;
   const auto kern = bits == 8 ? adamw_kernel<CAP, 8> : adamw_kernel<CAP, 32>;
-  return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(kAdamThreads), 0, s, tab) == cudaSuccess
-             ? kOk
-             : kErrCuda;
+  if (smem && !allow_smem(kern, kAdamWarps * kRing * 2 * kUnit * 10)) return kErrCuda;
+  return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(kAdamThreads), smem, s, tab) == cudaSuccess ? kOk
+                                                                                                                   : kErrCuda;
 }
 
 }  // namespace

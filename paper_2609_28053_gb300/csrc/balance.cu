@@ -40,9 +40,30 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
     // below 2^31: a block has at most T / grid tokens of at most 31 entries, or 64
     const int m = static_cast<int>((seg_end - t) * K);
     const int32_t* idx = a.idx + t * K;
-    for (int i = threadIdx.x; i < m; i += kCountThreads) {
-      const int e = __ldcs(idx + i);
-      if (static_cast<unsigned>(e) < static_cast<unsigned>(E) && (!a.mask || a.mask[t + i / K])) atomicAdd(mine + e, 1);
+    auto count = [&](int e) {
+      if (static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(mine + e, 1);
+    };
+    if (a.mask) {
+      for (int i = threadIdx.x; i < m; i += kCountThreads) {
+        const int e = __ldcs(idx + i);
+        if (a.mask[t + i / K]) count(e);
+      }
+    } else {
+      // four entries a load, two loads in flight; single ones up to the first
+      // 16-byte boundary and at the end
+      const int head = min(m, static_cast<int>((16u - (reinterpret_cast<uintptr_t>(idx) & 15u)) & 15u) / 4);
+      const int quads = (m - head) / 4;
+      const int4* q4 = reinterpret_cast<const int4*>(idx + head);
+      for (int i = threadIdx.x; i < quads; i += 2 * kCountThreads) {
+        const bool two = i + kCountThreads < quads;
+        const int4 w0 = __ldcs(q4 + i);
+        const int4 w1 = two ? __ldcs(q4 + i + kCountThreads) : make_int4(-1, -1, -1, -1);
+        count(w0.x); count(w0.y); count(w0.z); count(w0.w);
+        count(w1.x); count(w1.y); count(w1.z); count(w1.w);
+      }
+      if (static_cast<int>(threadIdx.x) < head) count(idx[threadIdx.x]);
+      const int end = head + 4 * quads + static_cast<int>(threadIdx.x);
+      if (end < m) count(idx[end]);
     }
     if (a.mask) {
       int v = 0;
@@ -64,46 +85,53 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
 }
 
 // prob and loss of microbatch blockIdx.y from its rows of a.part, which the
-// blocks of its tokens wrote: 32 experts a block, a warp every 8th row.
-__global__ void __launch_bounds__(256) balance_finish_kernel(BalanceArgs a, int64_t tokens_per_cta) {
-  __shared__ float col[8][32];
-  __shared__ double tot[8][3];
+// blocks of its tokens wrote: 32 experts a block, its warps every W-th row.
+template <int W>
+__global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, uint32_t tokens_per_cta) {
+  __shared__ float col[W][32];
+  __shared__ double tot[W][3];
   griddep_wait();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   for (int l = blockIdx.y; l < a.M; l += gridDim.y) {
     const int64_t lo = __ldg(a.off + l), hi = min(__ldg(a.off + l + 1), a.T);
     const int64_t n = a.mask ? a.valid[l] : hi - lo;
-    const int64_t first = lo / tokens_per_cta, rows = hi > lo ? (hi - 1) / tokens_per_cta - first + 1 : 0;
-    const float* p = a.part + (first + l) * a.row;
+    // tokens are fewer than 2^31
+    const uint32_t first = static_cast<uint32_t>(lo) / tokens_per_cta;
+    const int rows = hi > lo ? static_cast<int>(static_cast<uint32_t>(hi - 1) / tokens_per_cta - first) + 1 : 0;
+    const float* p = a.part + (static_cast<int64_t>(first) + l) * a.row;
     const int e = blockIdx.x * 32 + lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (e < a.E)
-      for (int64_t q = wid; q < rows; q += 32) {
+    if (e < a.E && a.prob)
+      for (int q = wid; q < rows; q += 4 * W) {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (q + 8 * u < rows) v[u] += __ldcg(p + (q + 8 * u) * a.row + 4 + e);
+          if (q + W * u < rows) v[u] += __ldcg(p + static_cast<int64_t>(q + W * u) * a.row + 4 + e);
       }
-    col[wid][lane] = (v[0] + v[1]) + (v[2] + v[3]);
-    double s = 0.0;
-    if (blockIdx.x == 0 && lane < 3)
-      for (int64_t q = wid; q < rows; q += 8) s += static_cast<double>(__ldcg(p + q * a.row + lane));
-    if (lane < 3) tot[wid][lane] = s;
+    if (W > 1) col[wid][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    const bool sums = blockIdx.x == 0 && a.loss;
+    if (sums && lane < 3) {
+      double s = 0.0;
+      for (int q = wid; q < rows; q += W) s += static_cast<double>(__ldcg(p + static_cast<int64_t>(q) * a.row + lane));
+      tot[wid][lane] = s;
+    }
     __syncthreads();
     if (wid == 0 && e < a.E && a.prob) {
-      float x = 0.f;
+      float x = (v[0] + v[1]) + (v[2] + v[3]);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) x += col[q][lane];
+      for (int q = 1; q < W; ++q) x += col[q][lane];
       a.prob[static_cast<int64_t>(l) * a.E + e] = n > 0 ? x / static_cast<float>(n) : 0.f;
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.loss) {
+    if (sums && threadIdx.x == 0) {
       double h = 0.0, zz = 0.0, alive = 0.0;
-      for (int q = 0; q < 8; ++q) {
+#pragma unroll
+      for (int q = 0; q < W; ++q) {
         h += tot[q][0];
         zz += tot[q][1];
         alive += tot[q][2];
       }
-      a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha * (h + alive / a.E) / static_cast<double>(n)) : 0.f;
-      a.loss[2 * l + 1] = n > 0 ? static_cast<float>(a.zeta * zz / static_cast<double>(n)) : 0.f;
+      const double r = n > 0 ? 1.0 / static_cast<double>(n) : 0.0;
+      a.loss[2 * l] = static_cast<float>(a.alpha * (h + alive / a.E) * r);
+      a.loss[2 * l + 1] = static_cast<float>(a.zeta * zz * r);
     }
     __syncthreads();
   }
@@ -140,7 +168,12 @@ int launch_balance(BalanceArgs a, cudaStream_t s) {
   }
   if (!a.part) return kOk;
   const dim3 fin(static_cast<unsigned>((a.E + 31) / 32), static_cast<unsigned>(a.M < 4096 ? a.M : 4096));
-  return launch_dependent(balance_finish_kernel, fin, dim3(256), 0, s, a, run.tokens_per_cta) == cudaSuccess ? kOk : kErrCuda;
+  // a warp a block where a microbatch has a few rows
+  const bool few = a.T / run.tokens_per_cta <= 16 * static_cast<int64_t>(a.M);
+  const auto kern = few ? balance_finish_kernel<1> : balance_finish_kernel<8>;
+  return launch_dependent(kern, fin, dim3(few ? 32 : 256), 0, s, a, static_cast<uint32_t>(run.tokens_per_cta)) == cudaSuccess
+             ? kOk
+             : kErrCuda;
 }
 
 }  // namespace eqb

@@ -41,11 +41,13 @@ __device__ __forceinline__ float sum_slots(float x, int step) {
   return x;
 }
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
+// A choice made once for a step, as a constant of the code below it.
+struct Yes {
+  __device__ constexpr operator bool() const { return true; }
+};
+struct No {
+  __device__ constexpr operator bool() const { return false; }
+};
 
 // A launch's cut: tokens a block, tokens a group, stages of a warp's ring.
 struct BalanceCut {
@@ -69,11 +71,16 @@ __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bo
 // One block takes a contiguous range of tokens and walks the microbatches in
 // it.  The sums of a microbatch's tokens go to the row blockIdx + microbatch of
 // a.part, which no other pair of the two has, and balance_finish adds them up
-// in ascending order: no atomics, so the same call gives the same bits.
-template <bool SIG, bool GRAD, bool F32, int LPT, int C>
+// in ascending order: no atomics, so the same call gives the same bits.  The
+// first CMIN chunks of every lane lie within E for all widths of an instance.
+template <bool SIG, bool GRAD, bool F32, int LPT, int C, int CMIN>
 __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kernel(BalanceArgs a, BalanceCut cut) {
   constexpr int TPW = 32 / LPT;    // tokens a warp takes at a time
   constexpr int EM = LPT * C * 4;  // experts the lanes hold
+  // chunks that need no test.  Not with a gradient and many chunks: without the
+  // branches between them the loads and stores of a row crowd together, and
+  // E = 256 takes 1,037 us where it took 665 (E = 128's value 69 with, 74 without)
+  constexpr int SURE = GRAD && C > 4 ? 0 : CMIN;
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ float sums[kBalWarps][3];
   __shared__ __align__(8) uint64_t bars[kBalWarps * kBalMaxStages];
@@ -173,7 +180,8 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         const int i = i0 + slot;
         const bool in = i >= from && i < to;
         const bool ok = in && (mbits >> i & 1u);
-        // a row that does not count is read as zeros: finite, and its p becomes 0
+        // a row that does not count is taken as zeros: finite, and its p becomes 0
+        const bool whole = __all_sync(kFull, ok);
         F2 e[C][2];
         float top, low;
         if constexpr (F32) {
@@ -183,8 +191,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
 #pragma unroll
           for (int k = 0; k < C; ++k) {
             float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (sub + k * LPT < nch) {
-              if (ok) w = zr[k * LPT];
+            if (k < SURE || sub + k * LPT < nch) {
+              w = zr[k * LPT];
+              if (!whole && !ok) w = make_float4(0.f, 0.f, 0.f, 0.f);
               top = fmaxf(fmaxf(top, fmaxf(w.x, w.y)), fmaxf(w.z, w.w));
               if constexpr (SIG) low = fminf(fminf(low, fminf(w.x, w.y)), fminf(w.z, w.w));
             }
@@ -199,8 +208,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
 #pragma unroll
           for (int k = 0; k < C; ++k) {
             uint2 w = make_uint2(0u, 0u);
-            if (sub + k * LPT < nch) {
-              if (ok) w = zr[k * LPT];
+            if (k < SURE || sub + k * LPT < nch) {
+              w = zr[k * LPT];
+              if (!whole && !ok) w = make_uint2(0u, 0u);
               top2 = hmax2_bf16(top2, hmax2_bf16(w.x, w.y));
               if constexpr (SIG) low2 = hmin2_bf16(low2, hmin2_bf16(w.x, w.y));
             }
@@ -226,24 +236,24 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         // among them) a sigmoid counts as zero.  Most rows are nearer than that.
         constexpr float kFar = 0x1p60f;
         const bool far = SIG && __any_sync(kFull, low < ref - 40.f);
-        auto sigmoids = [&](F2 x) {
-          const F2 xc = far ? f2(fmin_nan(lo2(x), kFar), fmin_nan(hi2(x), kFar)) : x;
+        auto sigmoids = [&](auto FAR, F2 x) {
+          const F2 xc = FAR ? f2(fmin_nan(lo2(x), kFar), fmin_nan(hi2(x), kFar)) : x;
           const F2 y = add2(em2, xc);
           const F2 sg = mul2(splat2(rcp_approx(lo2(y) * hi2(y))), f2(hi2(y), lo2(y)));
-          return far ? f2(lo2(x) > kFar ? 0.f : lo2(sg), hi2(x) > kFar ? 0.f : hi2(sg)) : sg;
+          return FAR ? f2(lo2(x) > kFar ? 0.f : lo2(sg), hi2(x) > kFar ? 0.f : hi2(sg)) : sg;
         };
         F2 d2 = f2(0.f, 0.f), h2 = f2(0.f, 0.f);
-        {
+        auto sums_of = [&](auto FAR) {
 #pragma unroll
           for (int k = 0; k < C; ++k) {
-            if (sub + k * LPT < nch) {
+            if (k < SURE || sub + k * LPT < nch) {
               const float4 rw = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
               const F2 rk[2] = {f2(rw.x, rw.y), f2(rw.z, rw.w)};
 #pragma unroll
               for (int q = 0; q < 2; ++q) {
                 F2 x = fma2(e[k][q], mul, shift);
                 x = f2(ex2_approx(lo2(x)), ex2_approx(hi2(x)));
-                const F2 sg = SIG ? sigmoids(x) : x;
+                const F2 sg = SIG ? sigmoids(FAR, x) : x;
                 // with a gradient the sigmoid is formed again from x, which 1 - s needs too
                 e[k][q] = SIG && GRAD ? x : sg;
                 d2 = add2(d2, sg);
@@ -253,7 +263,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
               e[k][0] = e[k][1] = f2(0.f, 0.f);
             }
           }
-        }
+        };
+        if (far) sums_of(Yes{});
+        else sums_of(No{});
         float d = lo2(d2) + hi2(d2), h = lo2(h2) + hi2(h2);
 #pragma unroll
         for (int m = 1; m < LPT; m <<= 1) {
@@ -281,9 +293,10 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
           const F2 ca2 = splat2(ca), k2 = splat2(__fmaf_rn(-ca, h, cz * lse));
           const float4* gr = reinterpret_cast<const float4*>(gsrc + static_cast<uint32_t>(i) * grow) + sub;
           const int64_t at = (g0 + i) * nch + sub;  // chunk of the output
+          auto gradients = [&](auto FAR) {
 #pragma unroll
           for (int k = 0; k < C; ++k) {
-            if (sub + k * LPT >= nch) continue;
+            if (k >= SURE && sub + k * LPT >= nch) continue;
             const float4 rw = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
             const F2 rk[2] = {f2(rw.x, rw.y), f2(rw.z, rw.w)};
             float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -291,11 +304,11 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
             F2 g[2] = {f2(old.x, old.y), f2(old.z, old.w)};
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              const F2 sg = SIG ? sigmoids(e[k][q]) : e[k][q];
+              const F2 sg = SIG ? sigmoids(FAR, e[k][q]) : e[k][q];
               acc[k][q] = fma2(sg, id2, acc[k][q]);
               F2 v = fma2(ca2, rk[q], k2);
               if constexpr (SIG) {
-                const F2 xc = far ? f2(fmin_nan(lo2(e[k][q]), kFar), fmin_nan(hi2(e[k][q]), kFar)) : e[k][q];
+                const F2 xc = FAR ? f2(fmin_nan(lo2(e[k][q]), kFar), fmin_nan(hi2(e[k][q]), kFar)) : e[k][q];
                 v = mul2(v, mul2(xc, sg));
               }
               g[q] = fma2(mul2(sg, id2), v, g[q]);
@@ -307,6 +320,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
             else
               __stcs(static_cast<float4*>(a.grad_out) + at + k * LPT, make_float4(lo2(g[0]), hi2(g[0]), lo2(g[1]), hi2(g[1])));
           }
+          };
+          if (far) gradients(Yes{});
+          else gradients(No{});
         }
       }
       if (g0 + G > seg_end && seg_end < te) break;  // the rest is the next microbatch's
@@ -368,7 +384,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   }
 }
 
-template <bool SIG, bool GRAD, bool F32, int LPT, int C>
+template <bool SIG, bool GRAD, bool F32, int LPT, int C, int CMIN>
 int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   constexpr int TPW = 32 / LPT, EM = LPT * C * 4;
   DeviceInfo di;
@@ -390,7 +406,7 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   run->tokens_per_cta = cut.tokens_per_cta;
   grid = (a.T + cut.tokens_per_cta - 1) / cut.tokens_per_cta;
   const int smem = bal_fixed_bytes(EM) + kBalWarps * cut.stages * bal_stage_bytes(a.E, cut.group, F32, gin);
-  const auto kern = balance_kernel<SIG, GRAD, F32, LPT, C>;
+  const auto kern = balance_kernel<SIG, GRAD, F32, LPT, C, CMIN>;
   if (!allow_smem(kern, di.max_smem_optin - 2048)) return kErrCuda;
   return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), smem, s, a, cut) == cudaSuccess ? kOk
                                                                                                                      : kErrCuda;
@@ -398,19 +414,19 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
 
 template <bool SIG, bool GRAD, bool F32>
 int launch_bal_width(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
-  if (a.E <= 8) return launch_bal<SIG, GRAD, F32, 1, 2>(a, run, s);
-  if (a.E <= 16) return launch_bal<SIG, GRAD, F32, 2, 2>(a, run, s);
-  if (a.E <= 32) return launch_bal<SIG, GRAD, F32, 4, 2>(a, run, s);
-  if (a.E <= 48) return launch_bal<SIG, GRAD, F32, 4, 3>(a, run, s);
-  if (a.E <= 64) return launch_bal<SIG, GRAD, F32, 4, 4>(a, run, s);
-  if (a.E <= 96) return launch_bal<SIG, GRAD, F32, 8, 3>(a, run, s);
-  if (a.E <= 128) return launch_bal<SIG, GRAD, F32, 8, 4>(a, run, s);
-  if (a.E <= 192) return launch_bal<SIG, GRAD, F32, 8, 6>(a, run, s);
-  if (a.E <= 256) return launch_bal<SIG, GRAD, F32, 8, 8>(a, run, s);
-  if (a.E <= 384) return launch_bal<SIG, GRAD, F32, 16, 6>(a, run, s);
-  if (a.E <= 512) return launch_bal<SIG, GRAD, F32, 16, 8>(a, run, s);
-  if (a.E <= 768) return launch_bal<SIG, GRAD, F32, 32, 6>(a, run, s);
-  if (a.E <= 1024) return launch_bal<SIG, GRAD, F32, 32, 8>(a, run, s);
+  if (a.E <= 8) return launch_bal<SIG, GRAD, F32, 1, 2, 2>(a, run, s);
+  if (a.E <= 16) return launch_bal<SIG, GRAD, F32, 2, 2, 2>(a, run, s);
+  if (a.E <= 32) return launch_bal<SIG, GRAD, F32, 4, 2, 1>(a, run, s);
+  if (a.E <= 48) return launch_bal<SIG, GRAD, F32, 4, 3, 2>(a, run, s);
+  if (a.E <= 64) return launch_bal<SIG, GRAD, F32, 4, 4, 3>(a, run, s);
+  if (a.E <= 96) return launch_bal<SIG, GRAD, F32, 8, 3, 2>(a, run, s);
+  if (a.E <= 128) return launch_bal<SIG, GRAD, F32, 8, 4, 3>(a, run, s);
+  if (a.E <= 192) return launch_bal<SIG, GRAD, F32, 8, 6, 4>(a, run, s);
+  if (a.E <= 256) return launch_bal<SIG, GRAD, F32, 8, 8, 6>(a, run, s);
+  if (a.E <= 384) return launch_bal<SIG, GRAD, F32, 16, 6, 4>(a, run, s);
+  if (a.E <= 512) return launch_bal<SIG, GRAD, F32, 16, 8, 6>(a, run, s);
+  if (a.E <= 768) return launch_bal<SIG, GRAD, F32, 32, 6, 4>(a, run, s);
+  if (a.E <= 1024) return launch_bal<SIG, GRAD, F32, 32, 8, 6>(a, run, s);
   return kErrUnsupported;
 }
 

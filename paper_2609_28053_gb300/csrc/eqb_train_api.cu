@@ -111,9 +111,8 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t count, int32_
   for (int32_t i = 0; i < count; ++i) {
     const eqb_adamw_tensor& t = tensors[i];
     if (t.n > 0 && t.grad) {
-      const uintptr_t sa = bits8 ? 8 : 16;
-      const bool wide = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.exp_avg, sa) && aligned(t.exp_avg_sq, sa) &&
-                        aligned(t.copy, 8);
+      const bool wide = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.exp_avg, 16) && aligned(t.exp_avg_sq, 16) &&
+                        aligned(t.copy, 16);
       batch[n++] = eqb::AdamwTensor{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.copy, t.n,
                                     (t.param_bf16 ? 1 : 0) | (t.grad_bf16 ? 2 : 0) | (wide ? 4 : 0)};
     }

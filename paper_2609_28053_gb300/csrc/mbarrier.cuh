@@ -59,6 +59,14 @@ __device__ __forceinline__ void drain_loads(int issued, int S, Barrier barrier) 
     while (left > 0u && !mbar_try_wait(barrier(i % S), static_cast<uint32_t>(i / S) & 1u)) --left;
 }
 
+// An untiled copy into shared memory, counted by a barrier: addresses and size
+// are multiples of 16 bytes.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 }  // namespace
 
 }  // namespace eqb
