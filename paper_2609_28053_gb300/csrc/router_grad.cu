@@ -13,7 +13,8 @@
 // dx: a block keeps a slab of W_r (all E rows, N columns) in shared memory and
 // runs over tiles of 128 tokens; dz streams through a ring of [128 x 64]
 // stages, two accumulators alternate, and four warps round the accumulators to
-// bf16 into swizzled staging tiles that TMA stores as whole lines.
+// bf16 into swizzled tiles of a second ring that TMA stores as whole lines; where
+// dx is added to, a further warp loads the old values into that ring ahead.
 // dW: a block has all experts x N columns of d and a part of the tokens; dz and
 // x stream through one ring, 64 tokens a stage, and x is read by one block only.
 // With several parts of the tokens their sums are added in order by a second
@@ -28,11 +29,10 @@ namespace eqb {
 
 namespace {
 
-constexpr int kGradThreads = 192;
+constexpr int kDxThreads = 224;
 constexpr int kGradCtas = 152;            // blocks of a dW grid: one an SM
 constexpr uint32_t kTile64 = 64 * 128;    // bytes of 64 rows of 64 bf16
-constexpr uint32_t kDzStage = 128 * 128;  // dx: 128 tokens x 64 experts
-constexpr uint32_t kStaging = 32 * 128;   // dx: a warp's 32 rows x 64 columns
+constexpr uint32_t kDxStage = 128 * 128;  // dx: 128 tokens x 64 experts of dz or columns of dx
 
 // Shared-memory descriptor of an MN-major operand in 128-byte swizzled rows:
 // `lead` bytes between tiles of 64 columns, 1 KiB between groups of 8 rows.
@@ -51,43 +51,48 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                    reinterpret_cast<uint64_t>(map)),
                "r"(src), "r"(c0), "r"(c1)
                : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 struct DxArgs {
-  int T, d, E, N, slabs, ntiles, S;
-  uint16_t* dx;  // read where add
+  int T, d, E, N, slabs, ntiles;
+  int S, SO;  // stages of dz, and of the output
   int add;
   int32_t* err;
 };
 
-__global__ void __launch_bounds__(kGradThreads, 1)
+__global__ void __launch_bounds__(kDxThreads, 1)
     router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
-                     const __grid_constant__ CUtensorMap tmo, DxArgs a) {
+                     const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi, DxArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  const int S = a.S, E = a.E, KC = (E + 63) / 64;
+  const int S = a.S, SO = a.SO, E = a.E, KC = (E + 63) / 64;
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* sm = smem_raw + (base - raw);
   const uint32_t wtile = static_cast<uint32_t>(E) * 128u;  // bytes of W's E rows x 64 columns
-  const uint32_t wbytes = wtile * static_cast<uint32_t>(a.N / 64);
-  const uint32_t ring = base + wbytes;
-  const uint32_t stag = ring + static_cast<uint32_t>(S) * kDzStage;
-  const uint32_t bars = stag + 8u * kStaging;
+  const uint32_t ring = base + wtile * static_cast<uint32_t>(a.N / 64);
+  const uint32_t stag = ring + static_cast<uint32_t>(S) * kDxStage;
+  const uint32_t bars = stag + static_cast<uint32_t>(SO) * kDxStage;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (S + s); };
-  auto accf = [&](int b) { return bars + 8u * (2 * S + b); };
-  auto acce = [&](int b) { return bars + 8u * (2 * S + 2 + b); };
-  const uint32_t wfull = bars + 8u * (2 * S + 4), wempty = wfull + 8u, drain = wfull + 16u;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (bars - base) + 8u * (2 * S + 7));
+  auto ofull = [&](int s) { return bars + 8u * (2 * S + s); };
+  auto oempty = [&](int s) { return bars + 8u * (2 * S + SO + s); };
+  const uint32_t rest = bars + 8u * (2 * S + 2 * SO);
+  auto accf = [&](int b) { return rest + 8u * b; };
+  auto acce = [&](int b) { return rest + 8u * (2 + b); };
+  const uint32_t wfull = rest + 32u, wempty = rest + 40u, drain = rest + 48u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(sm + (rest - base) + 56u);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  int* issued = reinterpret_cast<int*>(tmem_holder + 2);  // loads of dz, of W
+  int* issued = reinterpret_cast<int*>(tmem_holder + 2);  // loads of dz, of W, of the output's old values
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
+    }
+    for (int s = 0; s < SO; ++s) {
+      mbar_init(ofull(s), 1);
+      mbar_init(oempty(s), 4);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf(b), 1);
@@ -97,7 +102,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     mbar_init(wempty, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
-    issued[0] = issued[1] = 0;
+    issued[0] = issued[1] = issued[2] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -134,13 +139,30 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         for (int kc = 0; kc < KC; ++kc, ++n) {
           if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-          mbar_expect_tx(full(stage), kDzStage);
-          tma_load_2d(ring + static_cast<uint32_t>(stage) * kDzStage, &tmz, full(stage), kc * 64, tile * kBM);
+          mbar_expect_tx(full(stage), kDxStage);
+          tma_load_2d(ring + static_cast<uint32_t>(stage) * kDxStage, &tmz, full(stage), kc * 64, tile * kBM);
           if (++stage == S) { stage = 0; phase ^= 1u; }
         }
       }
       issued[0] = n;
       issued[1] = nw;
+    }
+  } else if (warp == 6) {
+    if (lane == 0 && a.add) {  // the output's old values, as far ahead as its ring goes
+      int stage = 0, n = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int64_t i = i0; i < i1 && ok; ++i) {
+        const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+        const int chunks = min(a.N, a.d - sl * a.N) / 64;
+        for (int c = 0; c < chunks; ++c, ++n) {
+          if (!mbar_wait(oempty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+          mbar_expect_tx(ofull(stage), kDxStage);
+          tma_load_2d(stag + static_cast<uint32_t>(stage) * kDxStage, &tmi, ofull(stage), sl * a.N + c * 64, tile * kBM);
+          if (++stage == SO) { stage = 0; phase ^= 1u; }
+        }
+      }
+      issued[2] = n;
     }
   } else if (warp == 1) {
     if (lane == 0) {
@@ -164,7 +186,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         for (int kc = 0; kc < KC; ++kc) {
           if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint64_t ad = sw128_desc(ring + static_cast<uint32_t>(stage) * kDzStage);
+          const uint64_t ad = sw128_desc(ring + static_cast<uint32_t>(stage) * kDxStage);
           const int steps = min(4, (E - kc * 64) / 16);
           for (int kk = 0; kk < steps; ++kk)
             umma_bf16(dt, ad + 2u * kk, mn128_desc(base + static_cast<uint32_t>(kc * 64 + kk * 16) * 128u, wtile), idesc,
@@ -182,83 +204,67 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   } else {
     const int q = warp & 3;
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
-    const uint32_t mine = stag + static_cast<uint32_t>(q) * 2u * kStaging;
     const uint32_t swz = static_cast<uint32_t>(lane & 7);
-    int it = 0, nstore = 0;
-    // the output's old values, two chunks of 64 columns ahead
-    uint4 old[2][8];
-    auto fetch = [&](int64_t i, int c, uint4 (&o)[8]) {
-      const int sl = static_cast<int>(i / a.ntiles), row = static_cast<int>(i % a.ntiles) * kBM + q * 32 + lane;
-      if (row < a.T) {
-        const uint4* src = reinterpret_cast<const uint4*>(a.dx + static_cast<size_t>(row) * a.d + sl * a.N + c * 64);
-#pragma unroll
-        for (int v = 0; v < 8; ++v) o[v] = __ldcs(src + v);
-      }
-    };
-    int64_t have = -1;  // the item whose first two chunks are in `old`
-    for (int64_t i = i0; i < i1; ++i, ++it) {
+    int it = 0, stage = 0, last = -1;  // last: the stage that the store before this one reads
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
       const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
       const int chunks = min(a.N, a.d - sl * a.N) / 64;
       const int row0 = tile * kBM + q * 32;
-      if (a.add && have != i) {
-        fetch(i, 0, old[0]);
-        if (chunks > 1) fetch(i, 1, old[1]);
-      }
-      const bool ahead = a.add && chunks % 2 == 0 && i + 1 < i1 && static_cast<int>((i + 1) / a.ntiles) == sl;
       const int buf = it & 1;
-      if (!__all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag))) break;
+      ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag));
+      if (!ok) break;
       tc_fence_after();
-      for (int c0 = 0; c0 < chunks; c0 += 2) {
+      for (int c = 0; c < chunks; ++c) {
+        // the stage is free, or holds the old values
+        ok = __all_sync(0xffffffffu, a.add ? mbar_wait(ofull(stage), phase, abort_flag)
+                                           : mbar_wait(oempty(stage), phase ^ 1u, abort_flag));
+        if (!ok) break;
+        const uint32_t dst = stag + static_cast<uint32_t>(stage) * kDxStage + static_cast<uint32_t>(q * 32 + lane) * 128u;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int c = c0 + h;
-          if (c >= chunks) break;
-          uint32_t p[32];
+        for (int half = 0; half < 2; ++half) {
+          uint32_t r[32];
+          tmem_ld32(tmem + lane_base + static_cast<uint32_t>(buf * 256 + c * 64 + half * 32), r);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t r[32];
-            tmem_ld32(tmem + lane_base + static_cast<uint32_t>(buf * 256 + c * 64 + half * 32), r);
+          for (int v = 0; v < 4; ++v) {
+            const uint32_t at = dst + ((static_cast<uint32_t>(4 * half + v) ^ swz) << 4);
             if (a.add) {
+              uint32_t w[4];
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                           : "r"(at)
+                           : "memory");
 #pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const uint32_t w[4] = {old[h][4 * half + v].x, old[h][4 * half + v].y, old[h][4 * half + v].z,
-                                       old[h][4 * half + v].w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  r[8 * v + 2 * k] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k]) + bf16_lo(w[k]));
-                  r[8 * v + 2 * k + 1] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k + 1]) + bf16_hi(w[k]));
-                }
+              for (int k = 0; k < 4; ++k) {
+                r[8 * v + 2 * k] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k]) + bf16_lo(w[k]));
+                r[8 * v + 2 * k + 1] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k + 1]) + bf16_hi(w[k]));
               }
             }
+            uint32_t p[4];
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-              p[16 * half + k] = pack_bf16x2_rn(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
-          }
-          if (a.add) {
-            if (c + 2 < chunks) fetch(i, c + 2, old[h]);
-            else if (ahead) fetch(i + 1, h, old[h]);
-          }
-          if (c == chunks - 1) {  // the accumulator is read
-            tc_fence_before();
-            mbar_arrive(acce(buf));
-          }
-          // the store that used this staging tile two stores ago has read it
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          __syncwarp();
-          const uint32_t dst = mine + static_cast<uint32_t>(nstore & 1) * kStaging;
-#pragma unroll
-          for (int v = 0; v < 8; ++v)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + static_cast<uint32_t>(lane) * 128u +
-                                                                          ((static_cast<uint32_t>(v) ^ swz) << 4)),
-                         "r"(p[4 * v]), "r"(p[4 * v + 1]), "r"(p[4 * v + 2]), "r"(p[4 * v + 3])
+            for (int k = 0; k < 4; ++k)
+              p[k] = pack_bf16x2_rn(__uint_as_float(r[8 * v + 2 * k]), __uint_as_float(r[8 * v + 2 * k + 1]));
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3])
                          : "memory");
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0 && row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
-          ++nstore;
+          }
         }
+        if (c == chunks - 1) {  // the accumulator is read
+          tc_fence_before();
+          mbar_arrive(acce(buf));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          // the store before this one has read its stage
+          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          if (last >= 0) mbar_arrive(oempty(last));
+        }
+        last = stage;
+        if (++stage == SO) { stage = 0; phase ^= 1u; }
       }
-      if (ahead) have = i + 1;
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
@@ -271,6 +277,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   if (threadIdx.x == 0 && *abort_flag) {
     drain_loads(issued[0], S, full);
     drain_loads(issued[1], 1, [&](int) { return wfull; });
+    drain_loads(issued[2], SO, ofull);
     raise_flag(a.err, kErrCuda);
   }
 }
@@ -497,26 +504,30 @@ DwPlan plan_dw(int64_t T, int d, int E) {
 
 int launch_dx(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
   if (!allow_smem(router_dx_kernel, di.max_smem_optin)) return kErrCuda;
-  DxArgs a{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, g.dx, g.add_dx, g.err};
+  DxArgs a{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, 0, g.add_dx, g.err};
   // narrower slabs while the tiles leave SMs without work
   for (;; a.N /= 2) {
     a.slabs = (g.d + a.N - 1) / a.N;
     if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= di.sm_count) break;
   }
-  const int extra = 1024 + 8 * kStaging + 8 * (2 * 8 + 7) + 16;
+  // what W_r's slab leaves, half for the output (its old values are on their way
+  // there with add_dx) and half for dz
+  const int extra = 1024 + 8 * (4 * 8 + 7) + 20;
   const int wbytes = a.E * 128 * (a.N / 64);
-  a.S = (di.max_smem_optin - extra - wbytes) / static_cast<int>(kDzStage);
-  if (a.S > 8) a.S = 8;
-  if (a.S < 2) return kErrUnsupported;
-  CUtensorMap tmz, tmw, tmo;
+  const int stages = (di.max_smem_optin - extra - wbytes) / static_cast<int>(kDxStage);
+  a.SO = stages / 2 < 8 ? stages / 2 : 8;
+  a.S = stages - a.SO < 8 ? stages - a.SO : 8;
+  if (a.SO < 2) return kErrUnsupported;
+  CUtensorMap tmz, tmw, tmo, tmi;
   if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
       !make_map(&tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
-      !make_map(&tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32))
+      !make_map(&tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32) ||
+      !make_map(&tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
     return kErrCuda;
   const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
   const int grid = items < di.sm_count ? static_cast<int>(items) : di.sm_count;
-  return launch_dependent(router_dx_kernel, dim3(grid), dim3(kGradThreads), wbytes + a.S * kDzStage + extra, s, tmz, tmw, tmo,
-                          a) == cudaSuccess
+  const int smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
+  return launch_dependent(router_dx_kernel, dim3(grid), dim3(kDxThreads), smem, s, tmz, tmw, tmo, tmi, a) == cudaSuccess
              ? kOk
              : kErrCuda;
 }
