@@ -29,7 +29,7 @@ namespace eqb {
 
 namespace {
 
-constexpr int kDxThreads = 224;
+constexpr int kGradThreads = 352;         // two warps, the eight that take accumulators out, and one more for dx
 constexpr int kGradCtas = 152;            // blocks of a dW grid: one an SM
 constexpr uint32_t kTile64 = 64 * 128;    // bytes of 64 rows of 64 bf16
 constexpr uint32_t kDxStage = 128 * 128;  // dx: 128 tokens x 64 experts of dz or columns of dx
@@ -60,10 +60,10 @@ struct DxArgs {
   int32_t* err;
 };
 
-__global__ void __launch_bounds__(kDxThreads, 1)
-    router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
-                     const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi, DxArgs a) {
-  extern __shared__ uint8_t smem_raw[];
+// dx of the items of block `block` of `blocks`.
+__device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& tmz, const CUtensorMap& tmw,
+                                         const CUtensorMap& tmo, const CUtensorMap& tmi, const DxArgs& a, int block,
+                                         int blocks) {
   const int S = a.S, SO = a.SO, E = a.E, KC = (E + 63) / 64;
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf(b), 1);
-      mbar_init(acce(b), 128);
+      mbar_init(acce(b), 256);
     }
     mbar_init(wfull, 1);
     mbar_init(wempty, 1);
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   const uint32_t tmem = *tmem_holder;
   // items (slab, tile), slab-major; a block has a contiguous range of them
   const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
-  const int64_t i0 = items * blockIdx.x / gridDim.x, i1 = items * (blockIdx.x + 1) / gridDim.x;
+  const int64_t i0 = items * block / blocks, i1 = items * (block + 1) / blocks;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
       issued[0] = n;
       issued[1] = nw;
     }
-  } else if (warp == 6) {
+  } else if (warp == 10) {
     if (lane == 0 && a.add) {  // the output's old values, as far ahead as its ring goes
       int stage = 0, n = 0;
       uint32_t phase = 0;
@@ -202,10 +202,11 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         if (mbar_try_wait(drain, 0u)) break;
     }
   } else {
-    const int q = warp & 3;
+    // warps 2..5 take the even chunks of 64 columns, 6..9 the odd ones
+    const int q = warp & 3, odd = (warp - 2) >> 2;
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
     const uint32_t swz = static_cast<uint32_t>(lane & 7);
-    int it = 0, stage = 0, last = -1;  // last: the stage that the store before this one reads
+    int it = 0, stage = 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
@@ -216,7 +217,13 @@ __global__ void __launch_bounds__(kDxThreads, 1)
       ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      for (int c = 0; c < chunks; ++c) {
+      const int mine = chunks - 1 - ((chunks - 1 - odd) & 1);  // this warp's last chunk, -1 if it has none
+      if (mine < 0) {
+        tc_fence_before();
+        mbar_arrive(acce(buf));
+      }
+      for (int c = 0; c < chunks; ++c, stage = stage + 1 == SO ? 0 : stage + 1, phase ^= stage == 0 ? 1u : 0u) {
+        if ((c & 1) != odd) continue;
         // the stage is free, or holds the old values
         ok = __all_sync(0xffffffffu, a.add ? mbar_wait(ofull(stage), phase, abort_flag)
                                            : mbar_wait(oempty(stage), phase ^ 1u, abort_flag));
@@ -249,7 +256,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
                          : "memory");
           }
         }
-        if (c == chunks - 1) {  // the accumulator is read
+        if (c == mine) {  // this warp's share of the accumulator is read
           tc_fence_before();
           mbar_arrive(acce(buf));
         }
@@ -258,12 +265,9 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         if (lane == 0) {
           if (row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          // the store before this one has read its stage
-          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          if (last >= 0) mbar_arrive(oempty(last));
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          mbar_arrive(oempty(stage));
         }
-        last = stage;
-        if (++stage == SO) { stage = 0; phase ^= 1u; }
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -290,7 +294,6 @@ __global__ void __launch_bounds__(kDxThreads, 1)
 // alternate, and eight warps add each to the sums that they hold in registers
 // (128 a thread, which bounds a block to 128 x 256 or 256 x 128 sums).
 constexpr int kDwStages = 8;      // stages of 64 tokens between two of these additions
-constexpr int kDwThreads = 320;   // two warps beside the eight
 
 struct DwArgs {
   int T, d, E, N, tiles, parts, S;
@@ -300,9 +303,9 @@ struct DwArgs {
   int32_t* err;
 };
 
-__global__ void __launch_bounds__(kDwThreads, 1)
-    router_dw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmx, DwArgs a) {
-  extern __shared__ uint8_t smem_raw[];
+// The sums of block `block`: one tile of dW over one part of the tokens.
+__device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& tmz, const CUtensorMap& tmx, const DwArgs& a,
+                                         int block) {
   const int S = a.S, MT = a.E > 128 ? 2 : 1;
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(kDwThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  const int tile = static_cast<int>(blockIdx.x) % a.tiles, part = static_cast<int>(blockIdx.x) / a.tiles;
+  const int tile = block % a.tiles, part = block / a.tiles;
   const int64_t s0 = a.stages * part / a.parts;
   const int ns = static_cast<int>(a.stages * (part + 1) / a.parts - s0);
   const int j0 = tile * a.N, nn = min(a.N, a.d - j0);
@@ -397,7 +400,7 @@ __global__ void __launch_bounds__(kDwThreads, 1)
       for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(drain, 0u)) break;
     }
-  } else {
+  } else if (warp < 10) {
     // warps 2..5 and 6..9 take the two halves of an accumulator's MT * N columns
     const int q = warp & 3, h = (warp - 2) >> 2, cw = MT * a.N / 2;
     const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * cw);
@@ -455,6 +458,32 @@ __global__ void __launch_bounds__(kDwThreads, 1)
   }
 }
 
+__global__ void __launch_bounds__(kGradThreads, 1)
+    router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
+                     const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi, DxArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  dx_block(smem_raw, tmz, tmw, tmo, tmi, a, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+}
+
+__global__ void __launch_bounds__(kGradThreads, 1)
+    router_dw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmx, DwArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  dw_block(smem_raw, tmz, tmx, a, static_cast<int>(blockIdx.x));
+}
+
+// Few tokens: both gradients in one launch, the first blocks dW's (a tile each,
+// over all tokens), the others dx's.
+__global__ void __launch_bounds__(kGradThreads, 1)
+    router_dxdw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
+                       const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi,
+                       const __grid_constant__ CUtensorMap tmz64, const __grid_constant__ CUtensorMap tmx, DxArgs a,
+                       DwArgs w) {
+  extern __shared__ uint8_t smem_raw[];
+  const int block = static_cast<int>(blockIdx.x);
+  if (block < w.tiles) dw_block(smem_raw, tmz64, tmx, w, block);
+  else dx_block(smem_raw, tmz, tmw, tmo, tmi, a, block - w.tiles, static_cast<int>(gridDim.x) - w.tiles);
+}
+
 // dW (+)= the parts' sums, in ascending order; n a multiple of 4.
 __global__ void __launch_bounds__(256) router_dw_sum_kernel(const float* part, int parts, int64_t n, float* dW, int add) {
   griddep_wait();
@@ -487,13 +516,26 @@ struct DwPlan {
   int64_t stages;
 };
 
+// Up to this many tokens dW's tiles are narrow and take all tokens, and both
+// gradients share a launch.
+constexpr int64_t kFewTokens = 1024;
+
 // Columns of a dW tile and parts of the tokens: the widest tile that gives
-// every SM a block with at least four stages.
+// every SM a block with at least four stages; of few tokens the narrowest one
+// that needs no more than a wave of blocks.
 DwPlan plan_dw(int64_t T, int d, int E) {
   DwPlan p;
+  const int widest = E > 128 ? 128 : 256;
   p.stages = (T + 63) / 64;
+  if (T <= kFewTokens) {
+    p.N = 64;
+    while (p.N < widest && (d + p.N - 1) / p.N > kGradCtas) p.N *= 2;
+    p.tiles = (d + p.N - 1) / p.N;
+    p.parts = 1;
+    return p;
+  }
   const int64_t most = (p.stages + 3) / 4;  // parts
-  for (p.N = E > 128 ? 128 : 256;; p.N /= 2) {
+  for (p.N = widest;; p.N /= 2) {
     p.tiles = (d + p.N - 1) / p.N;
     int64_t parts = kGradCtas / p.tiles;
     if (parts > most) parts = most;
@@ -502,13 +544,20 @@ DwPlan plan_dw(int64_t T, int d, int E) {
   }
 }
 
-int launch_dx(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
-  if (!allow_smem(router_dx_kernel, di.max_smem_optin)) return kErrCuda;
-  DxArgs a{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, 0, g.add_dx, g.err};
+struct DxLaunch {
+  DxArgs a;
+  CUtensorMap tmz, tmw, tmo, tmi;
+  int smem;
+  int64_t items;
+};
+// dx on up to `sms` blocks.
+int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l) {
+  DxArgs& a = l->a;
+  a = DxArgs{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, 0, g.add_dx, g.err};
   // narrower slabs while the tiles leave SMs without work
   for (;; a.N /= 2) {
     a.slabs = (g.d + a.N - 1) / a.N;
-    if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= di.sm_count) break;
+    if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= sms) break;
   }
   // what W_r's slab leaves, half for the output (its old values are on their way
   // there with add_dx) and half for dz
@@ -518,52 +567,37 @@ int launch_dx(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
   a.SO = stages / 2 < 8 ? stages / 2 : 8;
   a.S = stages - a.SO < 8 ? stages - a.SO : 8;
   if (a.SO < 2) return kErrUnsupported;
-  CUtensorMap tmz, tmw, tmo, tmi;
-  if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
-      !make_map(&tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
-      !make_map(&tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32) ||
-      !make_map(&tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
+  if (!make_map(&l->tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
+      !make_map(&l->tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
+      !make_map(&l->tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32) ||
+      !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
     return kErrCuda;
-  const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
-  const int grid = items < di.sm_count ? static_cast<int>(items) : di.sm_count;
-  const int smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
-  return launch_dependent(router_dx_kernel, dim3(grid), dim3(kDxThreads), smem, s, tmz, tmw, tmo, tmi, a) == cudaSuccess
-             ? kOk
-             : kErrCuda;
+  l->items = static_cast<int64_t>(a.slabs) * a.ntiles;
+  l->smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
+  return kOk;
 }
 
-int launch_dw(const RouterGradArgs& g, const DeviceInfo& di, cudaStream_t s) {
-  const int64_t n = static_cast<int64_t>(g.E) * g.d;
-  if (g.T == 0) {
-    if (g.add_dW) return kOk;
-    return launch_dependent(zero_kernel, dim3(static_cast<unsigned>((n + 1023) / 1024)), dim3(256), 0, s, g.dW, n) == cudaSuccess
-               ? kOk
-               : kErrCuda;
-  }
-  if (!allow_smem(router_dw_kernel, di.max_smem_optin)) return kErrCuda;
-  const DwPlan p = plan_dw(g.T, g.d, g.E);
-  DwArgs a{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
-           p.parts > 1 ? 0 : g.add_dW, g.err};
+struct DwLaunch {
+  DwArgs a;
+  CUtensorMap tmz, tmx;
+  int smem;
+};
+int plan_dw_launch(const RouterGradArgs& g, const DeviceInfo& di, const DwPlan& p, DwLaunch* l) {
+  l->a = DwArgs{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
+                p.parts > 1 ? 0 : g.add_dW, g.err};
   const int extra = 1024 + 8 * (2 * 8 + 5) + 16;
   const int stage_bytes = static_cast<int>(kTile64) * ((g.E > 128 ? 4 : 2) + p.N / 64);
-  a.S = (di.max_smem_optin - extra) / stage_bytes;
-  if (a.S > 8) a.S = 8;
-  if (a.S < 2) return kErrUnsupported;
-  CUtensorMap tmz, tmx;
-  if (!make_map(&tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), 64) ||
-      !make_map(&tmx, g.x, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 64))
+  l->a.S = (di.max_smem_optin - extra) / stage_bytes;
+  if (l->a.S > 8) l->a.S = 8;
+  if (l->a.S < 2) return kErrUnsupported;
+  if (!make_map(&l->tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), 64) ||
+      !make_map(&l->tmx, g.x, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 64))
     return kErrCuda;
-  if (launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kDwThreads), a.S * stage_bytes + extra, s, tmz, tmx,
-                       a) != cudaSuccess)
-    return kErrCuda;
-  if (p.parts == 1) return kOk;
-  int64_t grid = (n / 4 + 255) / 256;
-  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
-  return launch_dependent(router_dw_sum_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, g.part, p.parts, n, g.dW,
-                          g.add_dW) == cudaSuccess
-             ? kOk
-             : kErrCuda;
+  l->smem = l->a.S * stage_bytes + extra;
+  return kOk;
 }
+
+int status_of(cudaError_t e) { return e == cudaSuccess ? kOk : kErrCuda; }
 
 }  // namespace
 
@@ -575,11 +609,42 @@ size_t router_grad_workspace(int64_t T, int d, int E) {
 int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  if (g.dx && g.T > 0)
-    if (int rc = launch_dx(g, di, s)) return rc;
+  const int64_t n = static_cast<int64_t>(g.E) * g.d;
+  if (g.T == 0) {
+    if (!g.dW || g.add_dW) return kOk;
+    return status_of(launch_dependent(zero_kernel, dim3(static_cast<unsigned>((n + 1023) / 1024)), dim3(256), 0, s, g.dW, n));
+  }
+  // before the maps: encoding them needs a context, which a thread's first runtime call makes current
+  if (!allow_smem(router_dx_kernel, di.max_smem_optin) || !allow_smem(router_dw_kernel, di.max_smem_optin) ||
+      !allow_smem(router_dxdw_kernel, di.max_smem_optin))
+    return kErrCuda;
+  DxLaunch x;
+  DwLaunch w;
+  const DwPlan p = plan_dw(g.T, g.d, g.E);
   if (g.dW)
-    if (int rc = launch_dw(g, di, s)) return rc;
-  return kOk;
+    if (int rc = plan_dw_launch(g, di, p, &w)) return rc;
+  const bool one = g.dx && g.dW && g.T <= kFewTokens && p.tiles < di.sm_count;
+  // beside dW's tiles, but at least half of the SMs
+  const int sms = !one ? di.sm_count : di.sm_count - p.tiles > di.sm_count / 2 ? di.sm_count - p.tiles : di.sm_count / 2;
+  if (g.dx)
+    if (int rc = plan_dx(g, di, sms, &x)) return rc;
+  const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
+  if (one)
+    return status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles), dim3(kGradThreads),
+                                      x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmo, x.tmi, w.tmz, w.tmx, x.a, w.a));
+  if (g.dx)
+    if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kGradThreads), x.smem, s, x.tmz, x.tmw, x.tmo, x.tmi,
+                                            x.a)))
+      return rc;
+  if (!g.dW) return kOk;
+  if (int rc = status_of(launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), w.smem, s, w.tmz, w.tmx,
+                                          w.a)))
+    return rc;
+  if (p.parts == 1) return kOk;
+  int64_t grid = (n / 4 + 255) / 256;
+  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
+  return status_of(launch_dependent(router_dw_sum_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, g.part, p.parts, n,
+                                    g.dW, g.add_dW));
 }
 
 }  // namespace eqb
