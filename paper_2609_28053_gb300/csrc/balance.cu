@@ -31,9 +31,11 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
   griddep_wait();
   const int64_t tb = static_cast<int64_t>(blockIdx.x) * tokens_per_cta;
   const int64_t te = min(tb + tokens_per_cta, a.T);
+  if (tb >= te) return;
+  int l = microbatch_of_warp(a.off, a.M, tb, threadIdx.x & 31);
   int64_t t = tb;
   while (t < te) {
-    const int l = microbatch_of(a.off, a.M, t);
+    while (__ldg(a.off + l + 1) <= t && l + 1 < a.M) ++l;  // the next one that is not empty
     const int64_t hi = __ldg(a.off + l + 1);
     const int64_t seg_end = hi > t ? min(te, hi) : te;
     __syncthreads();
@@ -139,34 +141,38 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
 
 }  // namespace
 
-int launch_balance(BalanceArgs a, cudaStream_t s) {
+// counts (and valid, with a mask) of the whole batch.
+int launch_balance_counts(const BalanceArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
   const int64_t cells = static_cast<int64_t>(a.M) * a.E;
-  {
-    const int64_t grid = (cells + 1023) / 1024;
-    if (launch_dependent(balance_clear_kernel, dim3(static_cast<unsigned>(grid < 1024 ? grid : 1024)), dim3(256), 0, s,
-                         a.counts, cells, a.mask ? a.valid : nullptr, a.M) != cudaSuccess)
-      return kErrCuda;
-  }
-  if (a.T > 0) {
-    int64_t grid = (a.T + 63) / 64;
-    if (grid > di.sm_count * 8) grid = di.sm_count * 8;
-    const int64_t tpc = (a.T + grid - 1) / grid;
-    const int copies = a.E <= 512 ? kCountWarps : kCountWarps / 2;
-    if (launch_dependent(balance_count_kernel, dim3(static_cast<unsigned>((a.T + tpc - 1) / tpc)), dim3(kCountThreads),
-                         static_cast<size_t>(copies) * a.E * 4, s, a, tpc, copies) != cudaSuccess)
-      return kErrCuda;
-  }
-  if (!a.prob && !a.loss && !a.grad_out) return kOk;
-  if (!a.prob && !a.loss) a.part = nullptr;
-  BalanceRun run{1};
-  if (a.T > 0) {
+  const int64_t cgrid = (cells + 1023) / 1024;
+  if (launch_dependent(balance_clear_kernel, dim3(static_cast<unsigned>(cgrid < 1024 ? cgrid : 1024)), dim3(256), 0, s, a.counts,
+                       cells, a.mask ? a.valid : nullptr, a.M) != cudaSuccess)
+    return kErrCuda;
+  if (a.T == 0) return kOk;
+  int64_t grid = (a.T + 63) / 64;
+  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
+  const int64_t tpc = (a.T + grid - 1) / grid;
+  const int copies = a.E <= 512 ? kCountWarps : kCountWarps / 2;
+  return launch_dependent(balance_count_kernel, dim3(static_cast<unsigned>((a.T + tpc - 1) / tpc)), dim3(kCountThreads),
+                          static_cast<size_t>(copies) * a.E * 4, s, a, tpc, copies) == cudaSuccess
+             ? kOk
+             : kErrCuda;
+}
+
+int launch_balance(BalanceArgs a, cudaStream_t s) {
+  const bool sums = a.prob || a.loss;
+  if (!sums) a.part = nullptr;
+  BalanceRun run{1, 1, 0};
+  if (a.T > 0 && (sums || a.grad_out)) {
     const int rc = a.sigmoid ? (a.grad_out ? launch_balance_sigmoid_grad(a, &run, s) : launch_balance_sigmoid_value(a, &run, s))
                              : (a.grad_out ? launch_balance_softmax_grad(a, &run, s) : launch_balance_softmax_value(a, &run, s));
     if (rc) return rc;
+  } else if (int rc = launch_balance_counts(a, s)) {
+    return rc;
   }
-  if (!a.part) return kOk;
+  if (!sums || run.done) return kOk;
   const dim3 fin(static_cast<unsigned>((a.E + 31) / 32), static_cast<unsigned>(a.M < 4096 ? a.M : 4096));
   // a warp a block where a microbatch has a few rows
   const bool few = a.T / run.tokens_per_cta <= 16 * static_cast<int64_t>(a.M);

@@ -49,10 +49,11 @@ struct No {
   __device__ constexpr operator bool() const { return false; }
 };
 
-// A launch's cut: tokens a block, tokens a group, stages of a warp's ring.
+// A launch's cut: tokens a block (0: a cluster of blocks a microbatch), blocks a
+// cluster, tokens a group, stages of a warp's ring.
 struct BalanceCut {
   int64_t tokens_per_cta;
-  int group, stages;
+  int cluster, group, stages;
 };
 
 // Blocks an SM holds, by their registers.
@@ -62,17 +63,31 @@ constexpr int bal_blocks(bool grad, int C) { return C <= 3 || (C == 4 && !grad) 
 // rounds where 8 rows would take much of it.
 constexpr int bal_rows(int EM) { return EM <= 256 ? kBalWarps : 2; }
 
-// Shared memory: R [EM], the warps' column sums [bal_rows, EM], the rings.
-__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM + 4 * bal_rows(EM) * EM; }
+// Shared memory: R [EM], a cluster's counts [EM], the warps' column sums
+// [bal_rows, EM], the rings.
+__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM * (2 + bal_rows(EM)); }
 __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bool gin) {
   return group * E * ((f32 ? 4 : 2) + (gin ? 4 : 0));
 }
 
+// A word of the same place in another block's shared memory.
+__device__ __forceinline__ uint32_t peer_word(const void* p, uint32_t rank) {
+  uint32_t at, v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float peer_float(const void* p, uint32_t rank) { return __uint_as_float(peer_word(p, rank)); }
+
 // One block takes a contiguous range of tokens and walks the microbatches in
 // it.  The sums of a microbatch's tokens go to the row blockIdx + microbatch of
 // a.part, which no other pair of the two has, and balance_finish adds them up
-// in ascending order: no atomics, so the same call gives the same bits.  The
-// first CMIN chunks of every lane lie within E for all widths of an instance.
+// in ascending order: no atomics, so the same call gives the same bits.
+// Of few tokens a cluster takes each microbatch, a slice a block, and does all
+// of the call: the blocks count their lists, add up the cluster's counts, pass
+// over z, and add up the cluster's sums, so that one launch takes the place of
+// four.  The first CMIN chunks of every lane lie within E for all widths of an
+// instance.
 template <bool SIG, bool GRAD, bool F32, int LPT, int C, int CMIN>
 __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kernel(BalanceArgs a, BalanceCut cut) {
   constexpr int TPW = 32 / LPT;    // tokens a warp takes at a time
@@ -84,11 +99,11 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ float sums[kBalWarps][3];
   __shared__ __align__(8) uint64_t bars[kBalWarps * kBalMaxStages];
-  __shared__ double inv;  // 1 / (K n E)
-  __shared__ float cs[2];
-  __shared__ int aborted;
+  __shared__ float tot[3];
+  __shared__ int valid_n, aborted;
   float* Rs = reinterpret_cast<float*>(sm);
-  float* colsum = Rs + EM;
+  int* hist = reinterpret_cast<int*>(Rs + EM);
+  float* colsum = Rs + 2 * EM;
   const int E = a.E, nch = E >> 2, G = cut.group, D = cut.stages;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int sub = lane & (LPT - 1), slot = lane / LPT;
@@ -102,57 +117,105 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (threadIdx.x == 0) aborted = 0;
+  if (threadIdx.x == 0) valid_n = aborted = 0;
+  if (cut.cluster)
+    for (int e = threadIdx.x; e < EM; e += kBalThreads) hist[e] = 0;
   griddep_wait();
-  const int64_t tb = static_cast<int64_t>(blockIdx.x) * cut.tokens_per_cta;
-  const int64_t te = min(tb + cut.tokens_per_cta, a.T);
+  int l = 0;
+  uint32_t rank = 0;
+  int64_t tb, te;
+  if (cut.cluster) {
+    l = static_cast<int>(blockIdx.x) / cut.cluster;
+    rank = blockIdx.x % static_cast<unsigned>(cut.cluster);
+    const int64_t lo = __ldg(a.off + l), n = __ldg(a.off + l + 1) - lo;
+    tb = lo + n * rank / cut.cluster;
+    te = lo + n * (rank + 1) / cut.cluster;
+  } else {
+    tb = static_cast<int64_t>(blockIdx.x) * cut.tokens_per_cta;
+    te = min(tb + cut.tokens_per_cta, a.T);
+    if (tb >= te) return;
+    l = microbatch_of_warp(a.off, a.M, tb, lane);
+  }
+  // tokens are counted from tb on from here
+  const int nt = static_cast<int>(te - tb);
+  const uint8_t* zb = static_cast<const uint8_t*>(a.z) + tb * zrow;
+  const float* gb = gin ? a.grad_in + tb * E : nullptr;
+  const uint8_t* mb = a.mask ? a.mask + tb : nullptr;
   __syncthreads();
-  if (tb >= te) return;
-  // this warp's groups: number j holds the tokens tb + (8 j + wid) G ..
-  const int ngroups = static_cast<int>((te - tb + G - 1) / G);
-  const int nj = ngroups > wid ? (ngroups - wid + kBalWarps - 1) / kBalWarps : 0;
-  auto start = [&](int j) { return tb + (static_cast<int64_t>(j) * kBalWarps + wid) * G; };
-  auto issue = [&](int j, int stage) {
-    if (lane == 0) {
-      const int64_t t0 = start(j);
-      const uint32_t cnt = static_cast<uint32_t>(min(static_cast<int64_t>(G), te - t0));
+  // this warp's groups start at wid G, (wid + 8) G, ...
+  const int gstep = kBalWarps * G;
+  int g0 = wid * G;
+  auto issue = [&](int at, int stage) {
+    if (lane == 0 && at < nt) {
+      const uint32_t cnt = static_cast<uint32_t>(min(G, nt - at));
       const uint32_t dst = ring_s + static_cast<uint32_t>(stage) * stage_bytes, bar = bar0 + 8u * stage;
       mbar_expect_tx(bar, cnt * (zrow + grow));
-      bulk_load(dst, static_cast<const uint8_t*>(a.z) + t0 * zrow, cnt * zrow, bar);
-      if (gin) bulk_load(dst + static_cast<uint32_t>(G) * zrow, a.grad_in + t0 * E, cnt * grow, bar);
+      bulk_load(dst, zb + static_cast<int64_t>(at) * zrow, cnt * zrow, bar);
+      if (gin) bulk_load(dst + static_cast<uint32_t>(G) * zrow, gb + static_cast<int64_t>(at) * E, cnt * grow, bar);
     }
   };
-  for (int j = 0; j < D && j < nj; ++j) issue(j, j);
+  for (int s = 0; s < D; ++s) issue(g0 + s * gstep, s);
   const float gs = GRAD && a.grad_scale ? *a.grad_scale : 1.0f;
-  auto mask_of = [&](int j) -> uint32_t {  // of the group's tokens, one bit each
-    if (!a.mask || j >= nj) return kFull;
-    const int64_t tok = start(j) + lane;
-    return __ballot_sync(kFull, lane < G && tok < te && a.mask[tok]);
+  auto mask_of = [&](int at) -> uint32_t {  // of a group's tokens, one bit each
+    if (!mb || at >= nt) return kFull;
+    return __ballot_sync(kFull, lane < G && at + lane < nt && mb[at + lane]);
   };
-  uint32_t mbits = mask_of(0), mnext = mask_of(1);
+  uint32_t mbits = mask_of(g0), mnext = mask_of(g0 + gstep);
 
-  int j = 0, stage = 0, waited = -1;
+  if (cut.cluster) {  // the lists' counts, this block's and then the cluster's
+    const int32_t* idx = a.idx + tb * a.K;
+    for (int i = threadIdx.x; i < nt * a.K; i += kBalThreads) {
+      const int e = idx[i];
+      if (static_cast<unsigned>(e) < static_cast<unsigned>(E) && (!mb || mb[i / a.K])) atomicAdd(hist + e, 1);
+    }
+    if (mb) {
+      int v = 0;
+      for (int i = threadIdx.x; i < nt; i += kBalThreads) v += mb[i] != 0;
+      v = __reduce_add_sync(kFull, v);
+      if (lane == 0 && v) atomicAdd(&valid_n, v);
+    }
+    cluster_sync();
+  }
+
+  int stage = 0, waited = -1;
   uint32_t phase = 0;
   bool dead = false;  // a wait of this warp ran out
-  int64_t t = tb;
-  while (t < te) {
-    const int l = microbatch_of(a.off, a.M, t);
-    const int64_t lo = __ldg(a.off + l), hi = __ldg(a.off + l + 1);
-    // malformed offsets must not stall the loop
-    const int64_t seg_end = hi > t ? min(te, hi) : te;
-    const int64_t n = a.mask ? a.valid[l] : hi - lo;
-    __syncthreads();  // the previous microbatch is done with the shared values
-    if (threadIdx.x == 0) {
-      inv = n > 0 ? 1.0 / (static_cast<double>(a.K) * static_cast<double>(n) * static_cast<double>(E)) : 0.0;
-      cs[0] = n > 0 ? gs * __double2float_rn(a.alpha / static_cast<double>(n)) : 0.f;
-      cs[1] = n > 0 ? gs * __double2float_rn(2.0 * a.zeta / static_cast<double>(n)) : 0.f;
+  int t = 0;
+  do {
+    int64_t n;
+    int seg_end = nt;
+    if (cut.cluster) {
+      n = __ldg(a.off + l + 1) - __ldg(a.off + l);
+      if (mb) {
+        n = 0;
+        for (int q = 0; q < cut.cluster; ++q) n += peer_word(&valid_n, q);
+      }
+    } else {
+      // malformed offsets must not stall the loop
+      int64_t lo = __ldg(a.off + l), hi = __ldg(a.off + l + 1);
+      while (hi <= tb + t && l + 1 < a.M) {  // the next one that is not empty
+        ++l;
+        lo = hi;
+        hi = __ldg(a.off + l + 1);
+      }
+      if (hi > tb + t && hi < te) seg_end = static_cast<int>(hi - tb);
+      n = a.mask ? a.valid[l] : hi - lo;
+      __syncthreads();  // the previous microbatch is done with the shared values
     }
-    __syncthreads();
+    // R from an exact whole number, so that balanced counts give 0
+    const float rn = n > 0 ? __frcp_rn(static_cast<float>(n)) : 0.f;
+    const float rkne = rn / static_cast<float>(a.K * E);
     for (int e = threadIdx.x; e < EM; e += kBalThreads) {
       float r = 0.f;
       if (e < E) {
-        const int64_t f = a.counts[static_cast<int64_t>(l) * E + e];
-        r = __double2float_rn(static_cast<double>(f * E - static_cast<int64_t>(a.K) * n) * inv);
+        int64_t f = 0;
+        if (cut.cluster) {
+          for (int q = 0; q < cut.cluster; ++q) f += peer_word(hist + e, q);
+          if (rank == 0) a.counts[static_cast<int64_t>(l) * E + e] = static_cast<int32_t>(f);
+        } else {
+          f = a.counts[static_cast<int64_t>(l) * E + e];
+        }
+        r = __ll2float_rn(f * E - a.K * n) * rkne;
       }
       Rs[e] = r;
     }
@@ -160,22 +223,19 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     F2 acc[C][2];
 #pragma unroll
     for (int k = 0; k < C; ++k) acc[k][0] = acc[k][1] = f2(0.f, 0.f);
-    const float ca = cs[0], cz = cs[1];
+    const float ca = gs * (static_cast<float>(a.alpha) * rn), cz = gs * (2.0f * static_cast<float>(a.zeta) * rn);
     float hsum = 0.f, zsum = 0.f, alive_n = 0.f;
 
-    while (j < nj && !dead) {
-      const int64_t g0 = start(j);
-      if (g0 >= seg_end) break;
-      if (waited != j) {
-        waited = j;
+    while (g0 < seg_end && !dead) {
+      if (waited != g0) {
+        waited = g0;
         dead = !__all_sync(kFull, mbar_wait(bar0 + 8u * stage, phase, &aborted));
         if (dead) break;
       }
       const uint8_t* zs = ring + static_cast<uint32_t>(stage) * stage_bytes;
       const uint8_t* gsrc = zs + static_cast<uint32_t>(G) * zrow;
       // the group's tokens of this microbatch, counted from g0
-      const int from = t > g0 ? static_cast<int>(t - g0) : 0;
-      const int to = static_cast<int>(min(seg_end - g0, static_cast<int64_t>(G)));
+      const int from = max(t - g0, 0), to = min(seg_end - g0, G);
       for (int i0 = from / TPW * TPW; i0 < to; i0 += TPW) {
         const int i = i0 + slot;
         const bool in = i >= from && i < to;
@@ -292,7 +352,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         } else {
           const F2 ca2 = splat2(ca), k2 = splat2(__fmaf_rn(-ca, h, cz * lse));
           const float4* gr = reinterpret_cast<const float4*>(gsrc + static_cast<uint32_t>(i) * grow) + sub;
-          const int64_t at = (g0 + i) * nch + sub;  // chunk of the output
+          const int64_t at = (tb + g0 + i) * nch + sub;  // chunk of the output
           auto gradients = [&](auto FAR) {
 #pragma unroll
           for (int k = 0; k < C; ++k) {
@@ -325,18 +385,18 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
           else gradients(No{});
         }
       }
-      if (g0 + G > seg_end && seg_end < te) break;  // the rest is the next microbatch's
+      if (g0 + G > seg_end && seg_end < nt) break;  // the rest is the next microbatch's
       __syncwarp();
-      if (j + D < nj) issue(j + D, stage);
-      ++j;
+      issue(g0 + D * gstep, stage);
+      g0 += gstep;
       mbits = mnext;
-      mnext = mask_of(j + 1);
+      mnext = mask_of(g0 + gstep);
       if (++stage == D) { stage = 0; phase ^= 1u; }
     }
 
     // the block's sums of this microbatch
-    if (a.part) {
-      float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;
+    if (a.part || cut.cluster) {
+      float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;  // not used by a cluster
       constexpr int ROWS = bal_rows(EM);
       for (int round = 0; round < kBalWarps / ROWS; ++round) {
         if (round) __syncthreads();
@@ -367,19 +427,42 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         float v = 0.f;
 #pragma unroll
         for (int q = 0; q < bal_rows(EM); ++q) v += colsum[q * EM + e];
-        row[4 + e] = v;
+        if (cut.cluster) colsum[e] = v;
+        else row[4 + e] = v;
       }
       if (threadIdx.x < 3) {
         float v = 0.f;
 #pragma unroll
         for (int q = 0; q < kBalWarps; ++q) v += sums[q][threadIdx.x];
-        row[threadIdx.x] = v;
+        if (cut.cluster) tot[threadIdx.x] = v;
+        else row[threadIdx.x] = v;
       }
     }
+    if (cut.cluster) {
+      cluster_sync();
+      const float n1 = static_cast<float>(n);
+      if (a.prob)
+        for (int e = rank * kBalThreads + threadIdx.x; e < E; e += cut.cluster * kBalThreads) {
+          float v = 0.f;
+          for (int q = 0; q < cut.cluster; ++q) v += peer_float(colsum + e, q);
+          a.prob[static_cast<int64_t>(l) * E + e] = n > 0 ? v / n1 : 0.f;
+        }
+      if (a.loss && rank == 0 && threadIdx.x == 0) {
+        float v[3] = {0.f, 0.f, 0.f};
+        for (int q = 0; q < cut.cluster; ++q)
+#pragma unroll
+          for (int i = 0; i < 3; ++i) v[i] += peer_float(tot + i, q);
+        a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * ((v[0] + v[2] / static_cast<float>(E)) / n1) : 0.f;
+        a.loss[2 * l + 1] = n > 0 ? static_cast<float>(a.zeta) * (v[1] / n1) : 0.f;
+      }
+      cluster_sync();  // no block leaves while another reads its sums
+    }
     t = seg_end;
-  }
+  } while (t < nt);
   if (dead && lane == 0) {  // the copies in flight must land before the block leaves
-    drain_loads(min(nj, j + D), D, [&](int s) { return bar0 + 8u * s; });
+    const int j = g0 / gstep;
+    const int sent = min((nt - wid * G + gstep - 1) / gstep, j + D);
+    drain_loads(sent, D, [&](int s) { return bar0 + 8u * s; });
     raise_flag(a.err, kErrCuda);
   }
 }
@@ -390,26 +473,48 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
   const bool gin = GRAD && a.grad_in;
-  // a ring as deep as the blocks of an SM leave room for, its groups of up to 2 KB
+  // Few tokens: a cluster a microbatch.  The host does not know how long the
+  // microbatches are, so the limit is on what one of them could hold: 2^17
+  // elements a block, some 10 us.
   BalanceCut cut;
+  cut.cluster = 0;
+  if (run->may_cluster) {
+    const int cl = a.M >= di.sm_count ? 1 : a.M >= 64 ? 2 : a.M >= 32 ? 4 : 8;
+    if (a.T * a.E <= (int64_t(1) << 17) * cl) cut.cluster = cl;
+  }
+  int64_t grid;
+  if (cut.cluster) {
+    grid = static_cast<int64_t>(a.M) * cut.cluster;
+    cut.tokens_per_cta = (a.T + grid - 1) / grid;
+  } else {
+    grid = (a.T + kBalWarps * TPW - 1) / (kBalWarps * TPW);
+    const int64_t most = di.sm_count * bal_blocks(GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(GRAD, C) : kBalMaxGrid;
+    if (grid > most) grid = most;
+    cut.tokens_per_cta = (a.T + grid - 1) / grid;
+    grid = (a.T + cut.tokens_per_cta - 1) / cut.tokens_per_cta;
+  }
+  // groups of up to 4 KB, two of them for every warp where there are as many
+  // tokens, and a ring as deep as the blocks of an SM leave room for
   cut.group = TPW;
-  while (cut.group * 2 <= 32 && bal_stage_bytes(a.E, cut.group * 2, F32, gin) <= 2048) cut.group *= 2;
+  while (cut.group * 2 <= 32 && bal_stage_bytes(a.E, cut.group * 2, F32, gin) <= 4096 &&
+         cut.group * 4 * kBalWarps <= cut.tokens_per_cta)
+    cut.group *= 2;
   // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
   const int room = di.max_smem_optin / bal_blocks(GRAD, C) - 2048 - bal_fixed_bytes(EM);
   cut.stages = room / (kBalWarps * bal_stage_bytes(a.E, cut.group, F32, gin));
   if (cut.stages > kBalMaxStages) cut.stages = kBalMaxStages;
   if (cut.stages < 1) return kErrUnsupported;
-  int64_t grid = (a.T + kBalWarps * TPW - 1) / (kBalWarps * TPW);
-  const int64_t most = di.sm_count * bal_blocks(GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(GRAD, C) : kBalMaxGrid;
-  if (grid > most) grid = most;
-  cut.tokens_per_cta = (a.T + grid - 1) / grid;
   run->tokens_per_cta = cut.tokens_per_cta;
-  grid = (a.T + cut.tokens_per_cta - 1) / cut.tokens_per_cta;
+  run->done = cut.cluster != 0;
   const int smem = bal_fixed_bytes(EM) + kBalWarps * cut.stages * bal_stage_bytes(a.E, cut.group, F32, gin);
   const auto kern = balance_kernel<SIG, GRAD, F32, LPT, C, CMIN>;
   if (!allow_smem(kern, di.max_smem_optin - 2048)) return kErrCuda;
-  return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), smem, s, a, cut) == cudaSuccess ? kOk
-                                                                                                                     : kErrCuda;
+  if (cut.cluster == 0) {
+    if (int rc = launch_balance_counts(a, s)) return rc;
+  }
+  return launch_clusters(kern, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), smem, s, cut.cluster, a, cut) == cudaSuccess
+             ? kOk
+             : kErrCuda;
 }
 
 template <bool SIG, bool GRAD, bool F32>

@@ -60,6 +60,28 @@ inline int resident_blocks(void (*kern)(KArgs...), int threads, size_t smem, int
   return n;
 }
 
+// Launch `kern` as a programmatic dependent of the previous work in `s`, its
+// blocks in clusters of `cluster` (0: none).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                                    cudaStream_t s, int cluster, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 // Launch `kern` as a programmatic dependent of the previous work in `s`.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
@@ -149,6 +171,19 @@ __device__ __forceinline__ int microbatch_of(const int64_t* __restrict__ off, in
     if (__ldg(off + mid) <= t) lo = mid; else hi = mid - 1;
   }
   return lo;
+}
+
+// The microbatch of token t, by all lanes of a warp: 32 boundaries at a time.
+__device__ __forceinline__ int microbatch_of_warp(const int64_t* __restrict__ off, int M, int64_t t, int lane) {
+  int l = 0, span = M;  // off[l] <= t, and the answer is below l + span
+  while (span > 1) {
+    const int step = (span + 31) / 32, i = l + lane * step;
+    const bool below = lane == 0 || (lane * step < span && __ldg(off + i) <= t);
+    const int k = 31 - __clz(__ballot_sync(kFull, below));
+    l += k * step;
+    span = min(step, span - k * step);
+  }
+  return l;
 }
 
 __device__ __forceinline__ void raise_flag(int32_t* err, int code) {

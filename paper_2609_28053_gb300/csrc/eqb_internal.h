@@ -237,10 +237,14 @@ constexpr size_t balance_part_bytes(int E, int M) {
   return carve_round((static_cast<size_t>(kBalMaxGrid) + static_cast<size_t>(M)) * (static_cast<size_t>(E) + 4) * 4);
 }
 int launch_balance(BalanceArgs a, cudaStream_t s);
-// The pass over z, its instances in files of their own; says how it was cut.
+// The pass over z, its instances in files of their own, after the counts
+// (launch_balance_counts) where it does not form them itself.
 struct BalanceRun {
-  int64_t tokens_per_cta;
+  int may_cluster;         // loss and counts may be formed by a cluster a microbatch
+  int64_t tokens_per_cta;  // out: how it was cut
+  int done;                // out: prob and loss are complete
 };
+int launch_balance_counts(const BalanceArgs& a, cudaStream_t s);
 int launch_balance_softmax_value(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
 int launch_balance_softmax_grad(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);
 int launch_balance_sigmoid_value(const BalanceArgs& a, BalanceRun* run, cudaStream_t s);

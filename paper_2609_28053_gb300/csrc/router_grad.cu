@@ -29,7 +29,8 @@ namespace eqb {
 
 namespace {
 
-constexpr int kGradThreads = 352;         // two warps, the eight that take accumulators out, and one more for dx
+constexpr int kDxThreads = 224;    // two warps, four that take accumulators out, one that loads old values
+constexpr int kGradThreads = 320;  // dW: two warps, eight that take accumulators out
 constexpr int kGradCtas = 152;            // blocks of a dW grid: one an SM
 constexpr uint32_t kTile64 = 64 * 128;    // bytes of 64 rows of 64 bf16
 constexpr uint32_t kDxStage = 128 * 128;  // dx: 128 tokens x 64 experts of dz or columns of dx
@@ -96,7 +97,7 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf(b), 1);
-      mbar_init(acce(b), 256);
+      mbar_init(acce(b), 128);
     }
     mbar_init(wfull, 1);
     mbar_init(wempty, 1);
@@ -147,7 +148,7 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
       issued[0] = n;
       issued[1] = nw;
     }
-  } else if (warp == 10) {
+  } else if (warp == 6) {
     if (lane == 0 && a.add) {  // the output's old values, as far ahead as its ring goes
       int stage = 0, n = 0;
       uint32_t phase = 0;
@@ -201,12 +202,11 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
       for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(drain, 0u)) break;
     }
-  } else {
-    // warps 2..5 take the even chunks of 64 columns, 6..9 the odd ones
-    const int q = warp & 3, odd = (warp - 2) >> 2;
+  } else if (warp < 6) {
+    const int q = warp & 3;
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
     const uint32_t swz = static_cast<uint32_t>(lane & 7);
-    int it = 0, stage = 0;
+    int it = 0, stage = 0, last = -1;  // last: the stage that the store before this one reads
     uint32_t phase = 0;
     bool ok = true;
     for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
@@ -217,13 +217,7 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
       ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const int mine = chunks - 1 - ((chunks - 1 - odd) & 1);  // this warp's last chunk, -1 if it has none
-      if (mine < 0) {
-        tc_fence_before();
-        mbar_arrive(acce(buf));
-      }
-      for (int c = 0; c < chunks; ++c, stage = stage + 1 == SO ? 0 : stage + 1, phase ^= stage == 0 ? 1u : 0u) {
-        if ((c & 1) != odd) continue;
+      for (int c = 0; c < chunks; ++c) {
         // the stage is free, or holds the old values
         ok = __all_sync(0xffffffffu, a.add ? mbar_wait(ofull(stage), phase, abort_flag)
                                            : mbar_wait(oempty(stage), phase ^ 1u, abort_flag));
@@ -256,7 +250,7 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
                          : "memory");
           }
         }
-        if (c == mine) {  // this warp's share of the accumulator is read
+        if (c == chunks - 1) {  // the accumulator is read
           tc_fence_before();
           mbar_arrive(acce(buf));
         }
@@ -265,9 +259,12 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
         if (lane == 0) {
           if (row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-          mbar_arrive(oempty(stage));
+          // the store before this one has read its stage
+          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          if (last >= 0) mbar_arrive(oempty(last));
         }
+        last = stage;
+        if (++stage == SO) { stage = 0; phase ^= 1u; }
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -400,7 +397,7 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
       for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(drain, 0u)) break;
     }
-  } else if (warp < 10) {
+  } else {
     // warps 2..5 and 6..9 take the two halves of an accumulator's MT * N columns
     const int q = warp & 3, h = (warp - 2) >> 2, cw = MT * a.N / 2;
     const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * cw);
@@ -458,7 +455,7 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
   }
 }
 
-__global__ void __launch_bounds__(kGradThreads, 1)
+__global__ void __launch_bounds__(kDxThreads, 1)
     router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
                      const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi, DxArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -633,7 +630,7 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     return status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles), dim3(kGradThreads),
                                       x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmo, x.tmi, w.tmz, w.tmx, x.a, w.a));
   if (g.dx)
-    if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kGradThreads), x.smem, s, x.tmz, x.tmw, x.tmo, x.tmi,
+    if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kDxThreads), x.smem, s, x.tmz, x.tmw, x.tmo, x.tmi,
                                             x.a)))
       return rc;
   if (!g.dW) return kOk;
