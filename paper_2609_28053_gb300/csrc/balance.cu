@@ -7,7 +7,6 @@ namespace eqb {
 namespace {
 
 constexpr int kCountThreads = 256;
-constexpr int kCountWarps = kCountThreads / 32;
 
 __global__ void balance_clear_kernel(int32_t* counts, int64_t n, int32_t* valid, int M) {
   griddep_wait();
@@ -25,9 +24,9 @@ __global__ void balance_clear_kernel(int32_t* counts, int64_t n, int32_t* valid,
 // of its own in shared memory, so that only lanes of a warp meet on a hot expert.
 __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArgs a, int64_t tokens_per_cta, int copies) {
   extern __shared__ int32_t hist[];
-  const int E = a.E, K = a.K;
+  const int E = a.E, K = a.K, threads = static_cast<int>(blockDim.x);
   int32_t* mine = hist + static_cast<int>((threadIdx.x >> 5) % copies) * E;
-  for (int i = threadIdx.x; i < copies * E; i += kCountThreads) hist[i] = 0;
+  for (int i = threadIdx.x; i < copies * E; i += threads) hist[i] = 0;
   griddep_wait();
   const int64_t tb = static_cast<int64_t>(blockIdx.x) * tokens_per_cta;
   const int64_t te = min(tb + tokens_per_cta, a.T);
@@ -46,9 +45,18 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
       if (static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(mine + e, 1);
     };
     if (a.mask) {
-      for (int i = threadIdx.x; i < m; i += kCountThreads) {
-        const int e = __ldcs(idx + i);
-        if (a.mask[t + i / K]) count(e);
+      for (int i = threadIdx.x; i < m; i += 4 * threads) {  // four entries in flight
+        int e[4];
+        uint8_t ok[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int j = i + u * threads;
+          e[u] = j < m ? __ldcs(idx + j) : -1;
+          ok[u] = j < m ? a.mask[t + j / K] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (ok[u]) count(e[u]);
       }
     } else {
       // four entries a load, two loads in flight; single ones up to the first
@@ -56,10 +64,10 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
       const int head = min(m, static_cast<int>((16u - (reinterpret_cast<uintptr_t>(idx) & 15u)) & 15u) / 4);
       const int quads = (m - head) / 4;
       const int4* q4 = reinterpret_cast<const int4*>(idx + head);
-      for (int i = threadIdx.x; i < quads; i += 2 * kCountThreads) {
-        const bool two = i + kCountThreads < quads;
+      for (int i = threadIdx.x; i < quads; i += 2 * threads) {
+        const bool two = i + threads < quads;
         const int4 w0 = __ldcs(q4 + i);
-        const int4 w1 = two ? __ldcs(q4 + i + kCountThreads) : make_int4(-1, -1, -1, -1);
+        const int4 w1 = two ? __ldcs(q4 + i + threads) : make_int4(-1, -1, -1, -1);
         count(w0.x); count(w0.y); count(w0.z); count(w0.w);
         count(w1.x); count(w1.y); count(w1.z); count(w1.w);
       }
@@ -69,12 +77,12 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
     }
     if (a.mask) {
       int v = 0;
-      for (int64_t i = t + threadIdx.x; i < seg_end; i += kCountThreads) v += a.mask[i] != 0;
+      for (int64_t i = t + threadIdx.x; i < seg_end; i += threads) v += a.mask[i] != 0;
       v = __reduce_add_sync(kFull, v);
       if ((threadIdx.x & 31) == 0 && v) atomicAdd(a.valid + l, v);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += kCountThreads) {
+    for (int e = threadIdx.x; e < E; e += threads) {
       int c = 0;
       for (int q = 0; q < copies; ++q) {
         c += hist[q * E + e];
@@ -104,17 +112,27 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
     const int e = blockIdx.x * 32 + lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (e < a.E && a.prob)
-      for (int q = wid; q < rows; q += 4 * W) {
+      for (int q = wid; q < rows; q += 8 * W) {  // eight loads in flight
+        float w[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (q + W * u < rows) v[u] += __ldcg(p + static_cast<int64_t>(q + W * u) * a.row + 4 + e);
+        for (int u = 0; u < 8; ++u) w[u] = q + W * u < rows ? __ldcg(p + static_cast<int64_t>(q + W * u) * a.row + 4 + e) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u & 3] += w[u];
       }
     if (W > 1) col[wid][lane] = (v[0] + v[1]) + (v[2] + v[3]);
     const bool sums = blockIdx.x == 0 && a.loss;
-    if (sums && lane < 3) {
-      double s = 0.0;
-      for (int q = wid; q < rows; q += W) s += static_cast<double>(__ldcg(p + static_cast<int64_t>(q) * a.row + lane));
-      tot[wid][lane] = s;
+    double t3[3] = {0.0, 0.0, 0.0};
+    if (sums) {
+      for (int q = threadIdx.x; q < rows; q += 32 * W) {
+        const float4 w = __ldcg(reinterpret_cast<const float4*>(p + static_cast<int64_t>(q) * a.row));
+        t3[0] += w.x; t3[1] += w.y; t3[2] += w.z;
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) t3[i] += __shfl_xor_sync(kFull, t3[i], m);
+        if (lane == 0) tot[wid][i] = t3[i];
+      }
     }
     __syncthreads();
     if (wid == 0 && e < a.E && a.prob) {
@@ -131,9 +149,9 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
         zz += tot[q][1];
         alive += tot[q][2];
       }
-      const double r = n > 0 ? 1.0 / static_cast<double>(n) : 0.0;
-      a.loss[2 * l] = static_cast<float>(a.alpha * (h + alive / a.E) * r);
-      a.loss[2 * l + 1] = static_cast<float>(a.zeta * zz * r);
+      const float n1 = static_cast<float>(n);
+      a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * (static_cast<float>(h + alive * (1.0 / a.E)) / n1) : 0.f;
+      a.loss[2 * l + 1] = n > 0 ? static_cast<float>(a.zeta) * (static_cast<float>(zz) / n1) : 0.f;
     }
     __syncthreads();
   }
@@ -151,11 +169,23 @@ int launch_balance_counts(const BalanceArgs& a, cudaStream_t s) {
                        cells, a.mask ? a.valid : nullptr, a.M) != cudaSuccess)
     return kErrCuda;
   if (a.T == 0) return kOk;
-  int64_t grid = (a.T + 63) / 64;
-  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
+  // fewer threads a block where a microbatch's lists are shorter than four
+  // entries for each of 256, and more blocks
+  const int64_t mean = a.T / a.M * a.K;
+  int threads = kCountThreads;
+  while (threads > 32 && threads * 4 > mean) threads /= 2;
+  // a block a microbatch of mean length, or 4,096 entries of a longer one where
+  // that leaves every SM a block: its counts then go to global memory once
+  int64_t least = a.K * (a.T / a.M) < 4096 ? a.T / a.M : 4096 / a.K;
+  if (least > a.T / di.sm_count) least = a.T / di.sm_count;
+  if (least < threads / 4) least = threads / 4;
+  const int64_t most = di.sm_count * 8 * (kCountThreads / threads);
+  int64_t grid = (a.T + least - 1) / least;
+  if (grid > most) grid = most;
   const int64_t tpc = (a.T + grid - 1) / grid;
-  const int copies = a.E <= 512 ? kCountWarps : kCountWarps / 2;
-  return launch_dependent(balance_count_kernel, dim3(static_cast<unsigned>((a.T + tpc - 1) / tpc)), dim3(kCountThreads),
+  int copies = threads / 32;
+  if (a.E > 512 && copies > 4) copies = 4;
+  return launch_dependent(balance_count_kernel, dim3(static_cast<unsigned>((a.T + tpc - 1) / tpc)), dim3(threads),
                           static_cast<size_t>(copies) * a.E * 4, s, a, tpc, copies) == cudaSuccess
              ? kOk
              : kErrCuda;

@@ -60,12 +60,12 @@ struct BalanceCut {
 constexpr int bal_blocks(bool grad, int C) { return C <= 3 || (C == 4 && !grad) ? 3 : 2; }
 
 // Rows of the block's column sums in shared memory: the warps add theirs in
-// rounds where 8 rows would take much of it.
-constexpr int bal_rows(int EM) { return EM <= 256 ? kBalWarps : 2; }
+// rounds where a row each would take much of it.
+__host__ __device__ constexpr int bal_rows(int EM, int warps) { return EM <= 256 || warps < 2 ? warps : 2; }
 
 // Shared memory: R [EM], a cluster's counts [EM], the warps' column sums
 // [bal_rows, EM], the rings.
-__host__ __device__ constexpr int bal_fixed_bytes(int EM) { return 4 * EM * (2 + bal_rows(EM)); }
+__host__ __device__ constexpr int bal_fixed_bytes(int EM, int warps) { return 4 * EM * (2 + bal_rows(EM, warps)); }
 __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bool gin) {
   return group * E * ((f32 ? 4 : 2) + (gin ? 4 : 0));
 }
@@ -105,12 +105,13 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   int* hist = reinterpret_cast<int*>(Rs + EM);
   float* colsum = Rs + 2 * EM;
   const int E = a.E, nch = E >> 2, G = cut.group, D = cut.stages;
+  const int threads = static_cast<int>(blockDim.x), warps = threads >> 5;  // 8, or fewer for short microbatches
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int sub = lane & (LPT - 1), slot = lane / LPT;
   const bool gin = GRAD && a.grad_in;
   const uint32_t zrow = static_cast<uint32_t>(E) * (F32 ? 4u : 2u), grow = gin ? static_cast<uint32_t>(E) * 4u : 0u;
   const uint32_t stage_bytes = static_cast<uint32_t>(G) * (zrow + grow);
-  uint8_t* ring = sm + bal_fixed_bytes(EM) + static_cast<size_t>(wid) * D * stage_bytes;
+  uint8_t* ring = sm + bal_fixed_bytes(EM, warps) + static_cast<size_t>(wid) * D * stage_bytes;
   const uint32_t ring_s = smem_u32(ring), bar0 = smem_u32(bars + wid * kBalMaxStages);
   if (lane == 0) {
     for (int s = 0; s < D; ++s) mbar_init(bar0 + 8u * s, 1);
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   }
   if (threadIdx.x == 0) valid_n = aborted = 0;
   if (cut.cluster)
-    for (int e = threadIdx.x; e < EM; e += kBalThreads) hist[e] = 0;
+    for (int e = threadIdx.x; e < EM; e += threads) hist[e] = 0;
   griddep_wait();
   int l = 0;
   uint32_t rank = 0;
@@ -142,8 +143,8 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   const float* gb = gin ? a.grad_in + tb * E : nullptr;
   const uint8_t* mb = a.mask ? a.mask + tb : nullptr;
   __syncthreads();
-  // this warp's groups start at wid G, (wid + 8) G, ...
-  const int gstep = kBalWarps * G;
+  // this warp's groups start at wid G, (wid + warps) G, ...
+  const int gstep = warps * G;
   int g0 = wid * G;
   auto issue = [&](int at, int stage) {
     if (lane == 0 && at < nt) {
@@ -164,13 +165,13 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
 
   if (cut.cluster) {  // the lists' counts, this block's and then the cluster's
     const int32_t* idx = a.idx + tb * a.K;
-    for (int i = threadIdx.x; i < nt * a.K; i += kBalThreads) {
+    for (int i = threadIdx.x; i < nt * a.K; i += threads) {
       const int e = idx[i];
       if (static_cast<unsigned>(e) < static_cast<unsigned>(E) && (!mb || mb[i / a.K])) atomicAdd(hist + e, 1);
     }
     if (mb) {
       int v = 0;
-      for (int i = threadIdx.x; i < nt; i += kBalThreads) v += mb[i] != 0;
+      for (int i = threadIdx.x; i < nt; i += threads) v += mb[i] != 0;
       v = __reduce_add_sync(kFull, v);
       if (lane == 0 && v) atomicAdd(&valid_n, v);
     }
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     // R from an exact whole number, so that balanced counts give 0
     const float rn = n > 0 ? __frcp_rn(static_cast<float>(n)) : 0.f;
     const float rkne = rn / static_cast<float>(a.K * E);
-    for (int e = threadIdx.x; e < EM; e += kBalThreads) {
+    for (int e = threadIdx.x; e < EM; e += threads) {
       float r = 0.f;
       if (e < E) {
         int64_t f = 0;
@@ -397,8 +398,8 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     // the block's sums of this microbatch
     if (a.part || cut.cluster) {
       float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;  // not used by a cluster
-      constexpr int ROWS = bal_rows(EM);
-      for (int round = 0; round < kBalWarps / ROWS; ++round) {
+      const int ROWS = bal_rows(EM, warps);
+      for (int round = 0; round < warps / ROWS; ++round) {
         if (round) __syncthreads();
         if (wid / ROWS != round) continue;
 #pragma unroll
@@ -423,17 +424,15 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         sums[wid][2] = alive_n;
       }
       __syncthreads();
-      for (int e = threadIdx.x; e < E; e += kBalThreads) {
+      for (int e = threadIdx.x; e < E; e += threads) {
         float v = 0.f;
-#pragma unroll
-        for (int q = 0; q < bal_rows(EM); ++q) v += colsum[q * EM + e];
+        for (int q = 0; q < ROWS; ++q) v += colsum[q * EM + e];
         if (cut.cluster) colsum[e] = v;
         else row[4 + e] = v;
       }
       if (threadIdx.x < 3) {
         float v = 0.f;
-#pragma unroll
-        for (int q = 0; q < kBalWarps; ++q) v += sums[q][threadIdx.x];
+        for (int q = 0; q < warps; ++q) v += sums[q][threadIdx.x];
         if (cut.cluster) tot[threadIdx.x] = v;
         else row[threadIdx.x] = v;
       }
@@ -442,7 +441,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
       cluster_sync();
       const float n1 = static_cast<float>(n);
       if (a.prob)
-        for (int e = rank * kBalThreads + threadIdx.x; e < E; e += cut.cluster * kBalThreads) {
+        for (int e = rank * threads + threadIdx.x; e < E; e += cut.cluster * threads) {
           float v = 0.f;
           for (int q = 0; q < cut.cluster; ++q) v += peer_float(colsum + e, q);
           a.prob[static_cast<int64_t>(l) * E + e] = n > 0 ? v / n1 : 0.f;
@@ -473,22 +472,41 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
   const bool gin = GRAD && a.grad_in;
-  // Few tokens: a cluster a microbatch.  The host does not know how long the
-  // microbatches are, so the limit is on what one of them could hold: 2^17
-  // elements a block, some 10 us.
+  // Few tokens: a cluster a microbatch.  A block passes over 3,000 elements a
+  // microsecond, the four launches take 17 us (M = 1, T = 8,000, E = 128 by one
+  // cluster 44 us, by four launches TIME).  The host does not know how long the
+  // microbatches are: the limit is 2^15 elements a block if the longest has twice
+  // the mean, and eight times that if one has all the tokens.
   BalanceCut cut;
   cut.cluster = 0;
   if (run->may_cluster) {
     const int cl = a.M >= di.sm_count ? 1 : a.M >= 64 ? 2 : a.M >= 32 ? 4 : 8;
-    if (a.T * a.E <= (int64_t(1) << 17) * cl) cut.cluster = cl;
+    const int even = a.M >= 8 ? 4 : a.M >= 2 ? (a.M + 1) / 2 : 1;
+    if (a.T * a.E <= (int64_t(1) << 15) * cl * even) cut.cluster = cl;
   }
+  // Warps of a block: no more than a microbatch of mean length keeps busy
+  // for a round (50,000 tokens in 1,900 microbatches, E = 64: this pass 16 us with
+  // one warp a block, 22 with four, 21 with eight; 4,370 in 470, E = 256 with a
+  // sigmoid's gradient: 53 with one, 31 with four).
+  const int64_t mean = a.T / a.M / (cut.cluster ? cut.cluster : 1);
+  int warps = kBalWarps;
+  while (warps > 1 && warps * TPW > mean && !(cut.cluster && warps * 64 <= EM)) warps /= 2;
+  const int stage1 = bal_stage_bytes(a.E, TPW, F32, gin);
+  // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
+  int blocks = bal_blocks(GRAD, C) * kBalWarps / warps;
+  const int fixed = bal_fixed_bytes(EM, warps), two = fixed + 2 * warps * stage1 + 2048;
+  if (warps < kBalWarps && blocks > di.max_smem_optin / two) blocks = di.max_smem_optin / two;
+  const int room = di.max_smem_optin / blocks - 2048 - fixed;
   int64_t grid;
   if (cut.cluster) {
     grid = static_cast<int64_t>(a.M) * cut.cluster;
     cut.tokens_per_cta = (a.T + grid - 1) / grid;
   } else {
-    grid = (a.T + kBalWarps * TPW - 1) / (kBalWarps * TPW);
-    const int64_t most = di.sm_count * bal_blocks(GRAD, C) < kBalMaxGrid ? di.sm_count * bal_blocks(GRAD, C) : kBalMaxGrid;
+    // at least a round of the block's warps, and of short microbatches a whole one
+    int64_t least = warps * TPW;
+    if (warps < kBalWarps && least < mean) least = mean;
+    grid = (a.T + least - 1) / least;
+    const int64_t most = di.sm_count * blocks < kBalMaxGrid ? di.sm_count * blocks : kBalMaxGrid;
     if (grid > most) grid = most;
     cut.tokens_per_cta = (a.T + grid - 1) / grid;
     grid = (a.T + cut.tokens_per_cta - 1) / cut.tokens_per_cta;
@@ -497,22 +515,20 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   // tokens, and a ring as deep as the blocks of an SM leave room for
   cut.group = TPW;
   while (cut.group * 2 <= 32 && bal_stage_bytes(a.E, cut.group * 2, F32, gin) <= 4096 &&
-         cut.group * 4 * kBalWarps <= cut.tokens_per_cta)
+         cut.group * 4 * warps <= cut.tokens_per_cta && 4 * warps * bal_stage_bytes(a.E, cut.group, F32, gin) <= room)
     cut.group *= 2;
-  // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
-  const int room = di.max_smem_optin / bal_blocks(GRAD, C) - 2048 - bal_fixed_bytes(EM);
-  cut.stages = room / (kBalWarps * bal_stage_bytes(a.E, cut.group, F32, gin));
+  cut.stages = room / (warps * bal_stage_bytes(a.E, cut.group, F32, gin));
   if (cut.stages > kBalMaxStages) cut.stages = kBalMaxStages;
   if (cut.stages < 1) return kErrUnsupported;
   run->tokens_per_cta = cut.tokens_per_cta;
   run->done = cut.cluster != 0;
-  const int smem = bal_fixed_bytes(EM) + kBalWarps * cut.stages * bal_stage_bytes(a.E, cut.group, F32, gin);
+  const int smem = fixed + warps * cut.stages * bal_stage_bytes(a.E, cut.group, F32, gin);
   const auto kern = balance_kernel<SIG, GRAD, F32, LPT, C, CMIN>;
   if (!allow_smem(kern, di.max_smem_optin - 2048)) return kErrCuda;
   if (cut.cluster == 0) {
     if (int rc = launch_balance_counts(a, s)) return rc;
   }
-  return launch_clusters(kern, dim3(static_cast<unsigned>(grid)), dim3(kBalThreads), smem, s, cut.cluster, a, cut) == cudaSuccess
+  return launch_clusters(kern, dim3(static_cast<unsigned>(grid)), dim3(32 * warps), smem, s, cut.cluster, a, cut) == cudaSuccess
              ? kOk
              : kErrCuda;
 }

@@ -232,7 +232,7 @@ struct BalanceArgs {
   int32_t* valid;  // [M]: valid tokens (mask)
   int32_t* err;
 };
-constexpr int kBalMaxGrid = 512;  // most blocks of the pass over z
+constexpr int kBalMaxGrid = 2432;  // most blocks of the pass over z
 constexpr size_t balance_part_bytes(int E, int M) {
   return carve_round((static_cast<size_t>(kBalMaxGrid) + static_cast<size_t>(M)) * (static_cast<size_t>(E) + 4) * 4);
 }

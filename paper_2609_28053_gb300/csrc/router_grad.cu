@@ -468,8 +468,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   dw_block(smem_raw, tmz, tmx, a, static_cast<int>(blockIdx.x));
 }
 
-// Few tokens: both gradients in one launch, the first blocks dW's (a tile each,
-// over all tokens), the others dx's.
+// Both gradients in one launch, the first blocks dW's, the others dx's.
 __global__ void __launch_bounds__(kGradThreads, 1)
     router_dxdw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
                        const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi,
@@ -477,8 +476,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                        DwArgs w) {
   extern __shared__ uint8_t smem_raw[];
   const int block = static_cast<int>(blockIdx.x);
-  if (block < w.tiles) dw_block(smem_raw, tmz64, tmx, w, block);
-  else dx_block(smem_raw, tmz, tmw, tmo, tmi, a, block - w.tiles, static_cast<int>(gridDim.x) - w.tiles);
+  const int nw = w.tiles * w.parts;
+  if (block < nw) dw_block(smem_raw, tmz64, tmx, w, block);
+  else dx_block(smem_raw, tmz, tmw, tmo, tmi, a, block - nw, static_cast<int>(gridDim.x) - nw);
 }
 
 // dW (+)= the parts' sums, in ascending order; n a multiple of 4.
@@ -513,9 +513,14 @@ struct DwPlan {
   int64_t stages;
 };
 
-// Up to this many tokens dW's tiles are narrow and take all tokens, and both
-// gradients share a launch.
+// Up to this many tokens dW's tiles are narrow and take all tokens: a sum of
+// parts would cost a launch.
 constexpr int64_t kFewTokens = 1024;
+
+// Up to this many elements of x both gradients share a launch, each on a part
+// of the SMs: of two launches each has its start and its end.  Beyond it the
+// uneven split costs more.
+constexpr int64_t kSharedElements = int64_t(1) << 26;
 
 // Columns of a dW tile and parts of the tokens: the widest tile that gives
 // every SM a block with at least four stages; of few tokens the narrowest one
@@ -617,26 +622,41 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     return kErrCuda;
   DxLaunch x;
   DwLaunch w;
-  const DwPlan p = plan_dw(g.T, g.d, g.E);
+  DwPlan p = plan_dw(g.T, g.d, g.E);
+  // SMs of dx where both share a launch: by what each has to move, dW's in
+  // whole parts and at most three quarters of them
+  int sms = di.sm_count;
+  bool one = false;
+  if (g.dx && g.dW && g.T * g.d <= kSharedElements && 4 * p.tiles <= 3 * di.sm_count) {
+    const double dz = 2.0 * g.T * g.E, row = 2.0 * g.T * g.d;
+    const double bx = (1 + g.add_dx) * row + dz * ((g.d + 255) / 256), bw = row + dz * p.tiles;
+    const int want = static_cast<int>(di.sm_count * bw / (bx + bw) / p.tiles + 0.5);
+    int parts = p.parts < want ? p.parts : want;
+    while (parts > 1 && 4 * parts * p.tiles > 3 * di.sm_count) --parts;
+    p.parts = parts < 1 ? 1 : parts;
+    sms = di.sm_count - p.parts * p.tiles;
+    one = true;
+  }
   if (g.dW)
     if (int rc = plan_dw_launch(g, di, p, &w)) return rc;
-  const bool one = g.dx && g.dW && g.T <= kFewTokens && p.tiles < di.sm_count;
-  // beside dW's tiles, but at least half of the SMs
-  const int sms = !one ? di.sm_count : di.sm_count - p.tiles > di.sm_count / 2 ? di.sm_count - p.tiles : di.sm_count / 2;
   if (g.dx)
     if (int rc = plan_dx(g, di, sms, &x)) return rc;
   const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
-  if (one)
-    return status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles), dim3(kGradThreads),
-                                      x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmo, x.tmi, w.tmz, w.tmx, x.a, w.a));
-  if (g.dx)
+  if (one) {
+    if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles * p.parts), dim3(kGradThreads),
+                                            x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmo, x.tmi, w.tmz, w.tmx, x.a,
+                                            w.a)))
+      return rc;
+  } else if (g.dx) {
     if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kDxThreads), x.smem, s, x.tmz, x.tmw, x.tmo, x.tmi,
                                             x.a)))
       return rc;
+  }
   if (!g.dW) return kOk;
-  if (int rc = status_of(launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), w.smem, s, w.tmz, w.tmx,
-                                          w.a)))
-    return rc;
+  if (!one)
+    if (int rc = status_of(launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), w.smem, s, w.tmz, w.tmx,
+                                            w.a)))
+      return rc;
   if (p.parts == 1) return kOk;
   int64_t grid = (n / 4 + 255) / 256;
   if (grid > di.sm_count * 8) grid = di.sm_count * 8;
