@@ -13,8 +13,8 @@
 // dx: a block keeps a slab of W_r (all E rows, N columns) in shared memory and
 // runs over tiles of 128 tokens; dz streams through a ring of [128 x 64]
 // stages, two accumulators alternate, and four warps round the accumulators to
-// bf16 into swizzled tiles of a second ring that TMA stores as whole lines; where
-// dx is added to, a further warp loads the old values into that ring ahead.
+// bf16 and store 32 bytes a lane, a whole sector; where dx is added to, a further
+// warp loads the old values into a second ring ahead.
 // dW: a block has all experts x N columns of d and a part of the tokens; dz and
 // x stream through one ring, 64 tokens a stage, and x is read by one block only.
 // With several parts of the tokens their sums are added in order by a second
@@ -47,24 +47,24 @@ __device__ __forceinline__ uint64_t mn128_desc(uint32_t saddr, uint32_t lead) {
 }
 constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: A, B are MN-major
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(map)),
-               "r"(src), "r"(c0), "r"(c1)
+// 32 bytes: one whole sector a lane.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                : "memory");
 }
 
 struct DxArgs {
   int T, d, E, N, slabs, ntiles;
-  int S, SO;  // stages of dz, and of the output
+  int S, SO;  // stages of dz, and of the output's old values (add)
+  uint16_t* dx;
   int add;
   int32_t* err;
 };
 
 // dx of the items of block `block` of `blocks`.
 __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& tmz, const CUtensorMap& tmw,
-                                         const CUtensorMap& tmo, const CUtensorMap& tmi, const DxArgs& a, int block,
-                                         int blocks) {
+                                         const CUtensorMap& tmi, const DxArgs& a, int block, int blocks) {
   const int S = a.S, SO = a.SO, E = a.E, KC = (E + 63) / 64;
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -120,15 +120,23 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
   const uint32_t tmem = *tmem_holder;
   // items (slab, tile), slab-major; a block has a contiguous range of them
   const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
-  const int64_t i0 = items * block / blocks, i1 = items * (block + 1) / blocks;
+  const int64_t i0 = items * block / blocks;
+  const int64_t mine = items * (block + 1) / blocks - i0;
+  const int sl0 = static_cast<int>(i0 / a.ntiles), tile0 = static_cast<int>(i0 % a.ntiles);
+  // the item after (sl, tile); a division an item and role would take as long as its MMAs
+  auto advance = [&](int& sl, int& tile) {
+    if (++tile == a.ntiles) {
+      tile = 0;
+      ++sl;
+    }
+  };
 
   if (warp == 0) {
     if (lane == 0) {
-      int stage = 0, n = 0, nw = 0, slab = -1;
+      int stage = 0, n = 0, nw = 0, slab = -1, sl = sl0, tile = tile0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int64_t i = i0; i < i1 && ok; ++i) {
-        const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+      for (int64_t i = 0; i < mine && ok; ++i, advance(sl, tile)) {
         if (sl != slab) {
           slab = sl;
           if (!mbar_wait(wempty, (static_cast<uint32_t>(nw) & 1u) ^ 1u, abort_flag)) break;
@@ -150,11 +158,10 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
     }
   } else if (warp == 6) {
     if (lane == 0 && a.add) {  // the output's old values, as far ahead as its ring goes
-      int stage = 0, n = 0;
+      int stage = 0, n = 0, sl = sl0, tile = tile0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int64_t i = i0; i < i1 && ok; ++i) {
-        const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+      for (int64_t i = 0; i < mine && ok; ++i, advance(sl, tile)) {
         const int chunks = min(a.N, a.d - sl * a.N) / 64;
         for (int c = 0; c < chunks; ++c, ++n) {
           if (!mbar_wait(oempty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
@@ -167,11 +174,10 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      int stage = 0, nw = 0, slab = -1, it = 0;
+      int stage = 0, nw = 0, slab = -1, it = 0, sl = sl0, tile = tile0;
       uint32_t phase = 0, idesc = 0;
       bool ok = true;
-      for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
-        const int sl = static_cast<int>(i / a.ntiles);
+      for (int64_t i = 0; i < mine && ok; ++i, ++it, advance(sl, tile)) {
         if (sl != slab) {
           if (slab >= 0) umma_commit(wempty);  // the slab may be replaced once its MMAs are done
           slab = sl;
@@ -206,35 +212,36 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
     const int q = warp & 3;
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
     const uint32_t swz = static_cast<uint32_t>(lane & 7);
-    int it = 0, stage = 0, last = -1;  // last: the stage that the store before this one reads
+    int it = 0, stage = 0;
+    int sl = sl0, tile = tile0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int64_t i = i0; i < i1 && ok; ++i, ++it) {
-      const int sl = static_cast<int>(i / a.ntiles), tile = static_cast<int>(i % a.ntiles);
+    for (int64_t i = 0; i < mine && ok; ++i, ++it, advance(sl, tile)) {
       const int chunks = min(a.N, a.d - sl * a.N) / 64;
-      const int row0 = tile * kBM + q * 32;
+      const int row = tile * kBM + q * 32 + lane;
+      uint16_t* out = a.dx + static_cast<int64_t>(row) * a.d + sl * a.N;
       const int buf = it & 1;
       ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
       for (int c = 0; c < chunks; ++c) {
-        // the stage is free, or holds the old values
-        ok = __all_sync(0xffffffffu, a.add ? mbar_wait(ofull(stage), phase, abort_flag)
-                                           : mbar_wait(oempty(stage), phase ^ 1u, abort_flag));
-        if (!ok) break;
-        const uint32_t dst = stag + static_cast<uint32_t>(stage) * kDxStage + static_cast<uint32_t>(q * 32 + lane) * 128u;
+        if (a.add) {
+          ok = __all_sync(0xffffffffu, mbar_wait(ofull(stage), phase, abort_flag));
+          if (!ok) break;
+        }
+        const uint32_t old = stag + static_cast<uint32_t>(stage) * kDxStage + static_cast<uint32_t>(q * 32 + lane) * 128u;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t r[32];
           tmem_ld32(tmem + lane_base + static_cast<uint32_t>(buf * 256 + c * 64 + half * 32), r);
+          uint32_t p[2][8];
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const uint32_t at = dst + ((static_cast<uint32_t>(4 * half + v) ^ swz) << 4);
             if (a.add) {
               uint32_t w[4];
               asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                            : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                           : "r"(at)
+                           : "r"(old + ((static_cast<uint32_t>(4 * half + v) ^ swz) << 4))
                            : "memory");
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
@@ -242,32 +249,26 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
                 r[8 * v + 2 * k + 1] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k + 1]) + bf16_hi(w[k]));
               }
             }
-            uint32_t p[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              p[k] = pack_bf16x2_rn(__uint_as_float(r[8 * v + 2 * k]), __uint_as_float(r[8 * v + 2 * k + 1]));
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3])
-                         : "memory");
+              p[v >> 1][4 * (v & 1) + k] = pack_bf16x2_rn(__uint_as_float(r[8 * v + 2 * k]), __uint_as_float(r[8 * v + 2 * k + 1]));
+          }
+          if (row < a.T) {
+            store_sector(out + c * 64 + half * 32, p[0]);
+            store_sector(out + c * 64 + half * 32 + 16, p[1]);
           }
         }
         if (c == chunks - 1) {  // the accumulator is read
           tc_fence_before();
           mbar_arrive(acce(buf));
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          if (row0 < a.T) tma_store_2d(&tmo, dst, sl * a.N + c * 64, row0);
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          // the store before this one has read its stage
-          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          if (last >= 0) mbar_arrive(oempty(last));
+        if (a.add) {
+          __syncwarp();  // the old values are read
+          if (lane == 0) mbar_arrive(oempty(stage));
+          if (++stage == SO) { stage = 0; phase ^= 1u; }
         }
-        last = stage;
-        if (++stage == SO) { stage = 0; phase ^= 1u; }
       }
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -457,9 +458,9 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
 
 __global__ void __launch_bounds__(kDxThreads, 1)
     router_dx_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
-                     const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi, DxArgs a) {
+                     const __grid_constant__ CUtensorMap tmi, DxArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  dx_block(smem_raw, tmz, tmw, tmo, tmi, a, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+  dx_block(smem_raw, tmz, tmw, tmi, a, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
 }
 
 __global__ void __launch_bounds__(kGradThreads, 1)
@@ -471,14 +472,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 // Both gradients in one launch, the first blocks dW's, the others dx's.
 __global__ void __launch_bounds__(kGradThreads, 1)
     router_dxdw_kernel(const __grid_constant__ CUtensorMap tmz, const __grid_constant__ CUtensorMap tmw,
-                       const __grid_constant__ CUtensorMap tmo, const __grid_constant__ CUtensorMap tmi,
-                       const __grid_constant__ CUtensorMap tmz64, const __grid_constant__ CUtensorMap tmx, DxArgs a,
+                       const __grid_constant__ CUtensorMap tmi, const __grid_constant__ CUtensorMap tmz64, const __grid_constant__ CUtensorMap tmx, DxArgs a,
                        DwArgs w) {
   extern __shared__ uint8_t smem_raw[];
   const int block = static_cast<int>(blockIdx.x);
   const int nw = w.tiles * w.parts;
   if (block < nw) dw_block(smem_raw, tmz64, tmx, w, block);
-  else dx_block(smem_raw, tmz, tmw, tmo, tmi, a, block - nw, static_cast<int>(gridDim.x) - nw);
+  else dx_block(smem_raw, tmz, tmw, tmi, a, block - nw, static_cast<int>(gridDim.x) - nw);
 }
 
 // dW (+)= the parts' sums, in ascending order; n a multiple of 4.
@@ -548,30 +548,28 @@ DwPlan plan_dw(int64_t T, int d, int E) {
 
 struct DxLaunch {
   DxArgs a;
-  CUtensorMap tmz, tmw, tmo, tmi;
+  CUtensorMap tmz, tmw, tmi;
   int smem;
   int64_t items;
 };
 // dx on up to `sms` blocks.
 int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l) {
   DxArgs& a = l->a;
-  a = DxArgs{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, 0, g.add_dx, g.err};
+  a = DxArgs{static_cast<int>(g.T), g.d, g.E, 256, 0, static_cast<int>((g.T + kBM - 1) / kBM), 0, 0, g.dx, g.add_dx, g.err};
   // narrower slabs while the tiles leave SMs without work
   for (;; a.N /= 2) {
     a.slabs = (g.d + a.N - 1) / a.N;
     if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= sms) break;
   }
-  // what W_r's slab leaves, half for the output (its old values are on their way
-  // there with add_dx) and half for dz
+  // what W_r's slab leaves: dz's, with add_dx half of it for the old values
   const int extra = 1024 + 8 * (4 * 8 + 7) + 20;
   const int wbytes = a.E * 128 * (a.N / 64);
   const int stages = (di.max_smem_optin - extra - wbytes) / static_cast<int>(kDxStage);
-  a.SO = stages / 2 < 8 ? stages / 2 : 8;
+  a.SO = !g.add_dx ? 0 : stages / 2 < 8 ? stages / 2 : 8;
   a.S = stages - a.SO < 8 ? stages - a.SO : 8;
-  if (a.SO < 2) return kErrUnsupported;
+  if (a.S < 2) return kErrUnsupported;
   if (!make_map(&l->tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
       !make_map(&l->tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
-      !make_map(&l->tmo, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), 32) ||
       !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
     return kErrCuda;
   l->items = static_cast<int64_t>(a.slabs) * a.ntiles;
@@ -644,11 +642,11 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
   if (one) {
     if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles * p.parts), dim3(kGradThreads),
-                                            x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmo, x.tmi, w.tmz, w.tmx, x.a,
+                                            x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmi, w.tmz, w.tmx, x.a,
                                             w.a)))
       return rc;
   } else if (g.dx) {
-    if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kDxThreads), x.smem, s, x.tmz, x.tmw, x.tmo, x.tmi,
+    if (int rc = status_of(launch_dependent(router_dx_kernel, dim3(nx), dim3(kDxThreads), x.smem, s, x.tmz, x.tmw, x.tmi,
                                             x.a)))
       return rc;
   }
