@@ -13,8 +13,10 @@
 // dx: a block keeps a slab of W_r (all E rows, N columns) in shared memory and
 // runs over tiles of 128 tokens; dz streams through a ring of [128 x 64]
 // stages, two accumulators alternate, and four warps round the accumulators to
-// bf16 and store 32 bytes a lane, a whole sector; where dx is added to, a further
-// warp loads the old values into a second ring ahead.
+// bf16 and turn them in shared memory, so that a store takes whole 128-byte lines
+// (T = 32,768, d = 4,096, E = 128: TIME us; 62 with a row a lane, 32 bytes of 32
+// rows a store; 63 by TMA from the same tiles).  Where dx is added to, a further
+// warp loads the old values into a ring ahead, and they are turned in its stages.
 // dW: a block has all experts x N columns of d and a part of the tokens; dz and
 // x stream through one ring, 64 tokens a stage, and x is read by one block only.
 // With several parts of the tokens their sums are added in order by a second
@@ -47,11 +49,14 @@ __device__ __forceinline__ uint64_t mn128_desc(uint32_t saddr, uint32_t lead) {
 }
 constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: A, B are MN-major
 
-// 32 bytes: one whole sector a lane.
-__device__ __forceinline__ void store_sector(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+// 32 bytes a lane: one whole sector.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&w)[2][4]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0][0]), "r"(w[0][1]), "r"(w[0][2]),
+               "r"(w[0][3]), "r"(w[1][0]), "r"(w[1][1]), "r"(w[1][2]), "r"(w[1][3])
                : "memory");
+}
+__device__ __forceinline__ void lds128(uint32_t at, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
 }
 
 struct DxArgs {
@@ -118,14 +123,27 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  // items (slab, tile), slab-major; a block has a contiguous range of them
-  const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles;
-  const int64_t i0 = items * block / blocks;
-  const int64_t mine = items * (block + 1) / blocks - i0;
-  const int sl0 = static_cast<int>(i0 / a.ntiles), tile0 = static_cast<int>(i0 % a.ntiles);
+  // items (slab, tile).  With a block for every slab a block keeps its slab and
+  // takes every step-th tile, so that the slabs of a tile -- whole rows of dx --
+  // are written at the same time; else it has a contiguous range of items,
+  // slab-major.
+  const int step = blocks >= a.slabs ? blocks / a.slabs : 1;
+  int sl0, tile0;
+  int64_t mine;
+  if (blocks >= a.slabs) {
+    sl0 = block % a.slabs;
+    tile0 = block / a.slabs;
+    mine = tile0 < step && tile0 < a.ntiles ? (a.ntiles - tile0 + step - 1) / step : 0;
+  } else {
+    const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles, i0 = items * block / blocks;
+    mine = items * (block + 1) / blocks - i0;
+    sl0 = static_cast<int>(i0 / a.ntiles);
+    tile0 = static_cast<int>(i0 % a.ntiles);
+  }
   // the item after (sl, tile); a division an item and role would take as long as its MMAs
   auto advance = [&](int& sl, int& tile) {
-    if (++tile == a.ntiles) {
+    tile += step;
+    if (tile >= a.ntiles) {
       tile = 0;
       ++sl;
     }
@@ -218,8 +236,9 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
     bool ok = true;
     for (int64_t i = 0; i < mine && ok; ++i, ++it, advance(sl, tile)) {
       const int chunks = min(a.N, a.d - sl * a.N) / 64;
-      const int row = tile * kBM + q * 32 + lane;
-      uint16_t* out = a.dx + static_cast<int64_t>(row) * a.d + sl * a.N;
+      // a store takes 128-byte lines of eight rows, four lanes a line
+      const int row = tile * kBM + q * 32 + (lane >> 2);
+      uint16_t* out = a.dx + static_cast<int64_t>(row) * a.d + sl * a.N + (lane & 3) * 16;
       const int buf = it & 1;
       ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(it >> 1) & 1u, abort_flag));
       if (!ok) break;
@@ -229,41 +248,47 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
           ok = __all_sync(0xffffffffu, mbar_wait(ofull(stage), phase, abort_flag));
           if (!ok) break;
         }
-        const uint32_t old = stag + static_cast<uint32_t>(stage) * kDxStage + static_cast<uint32_t>(q * 32 + lane) * 128u;
+        // the warp's 32 rows x 64 columns, swizzled: the old values' stage, or the one stage without them
+        const uint32_t tile64 = stag + static_cast<uint32_t>(stage) * kDxStage + static_cast<uint32_t>(q * 32) * 128u;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t r[32];
           tmem_ld32(tmem + lane_base + static_cast<uint32_t>(buf * 256 + c * 64 + half * 32), r);
-          uint32_t p[2][8];
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
+            const uint32_t at = tile64 + static_cast<uint32_t>(lane) * 128u + ((static_cast<uint32_t>(4 * half + v) ^ swz) << 4);
             if (a.add) {
               uint32_t w[4];
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                           : "r"(old + ((static_cast<uint32_t>(4 * half + v) ^ swz) << 4))
-                           : "memory");
+              lds128(at, w);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 r[8 * v + 2 * k] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k]) + bf16_lo(w[k]));
                 r[8 * v + 2 * k + 1] = __float_as_uint(__uint_as_float(r[8 * v + 2 * k + 1]) + bf16_hi(w[k]));
               }
             }
+            uint32_t p[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              p[v >> 1][4 * (v & 1) + k] = pack_bf16x2_rn(__uint_as_float(r[8 * v + 2 * k]), __uint_as_float(r[8 * v + 2 * k + 1]));
-          }
-          if (row < a.T) {
-            store_sector(out + c * 64 + half * 32, p[0]);
-            store_sector(out + c * 64 + half * 32 + 16, p[1]);
+              p[k] = pack_bf16x2_rn(__uint_as_float(r[8 * v + 2 * k]), __uint_as_float(r[8 * v + 2 * k + 1]));
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3])
+                         : "memory");
           }
         }
         if (c == chunks - 1) {  // the accumulator is read
           tc_fence_before();
           mbar_arrive(acce(buf));
         }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t rr = static_cast<uint32_t>(8 * k + (lane >> 2)), c2 = static_cast<uint32_t>(2 * (lane & 3));
+          uint32_t w[2][4];
+          lds128(tile64 + rr * 128u + ((c2 ^ (rr & 7u)) << 4), w[0]);
+          lds128(tile64 + rr * 128u + (((c2 + 1u) ^ (rr & 7u)) << 4), w[1]);
+          if (row + 8 * k < a.T) store_sector(out + static_cast<int64_t>(8 * k) * a.d + c * 64, w);
+        }
+        __syncwarp();  // the stage is read
         if (a.add) {
-          __syncwarp();  // the old values are read
           if (lane == 0) mbar_arrive(oempty(stage));
           if (++stage == SO) { stage = 0; phase ^= 1u; }
         }
@@ -550,7 +575,6 @@ struct DxLaunch {
   DxArgs a;
   CUtensorMap tmz, tmw, tmi;
   int smem;
-  int64_t items;
 };
 // dx on up to `sms` blocks.
 int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l) {
@@ -561,18 +585,18 @@ int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l)
     a.slabs = (g.d + a.N - 1) / a.N;
     if (a.N == 64 || static_cast<int64_t>(a.slabs) * a.ntiles >= sms) break;
   }
-  // what W_r's slab leaves: dz's, with add_dx half of it for the old values
+  // what W_r's slab leaves: a stage for the way out, with add_dx half of them for
+  // the old values, the others for dz
   const int extra = 1024 + 8 * (4 * 8 + 7) + 20;
   const int wbytes = a.E * 128 * (a.N / 64);
   const int stages = (di.max_smem_optin - extra - wbytes) / static_cast<int>(kDxStage);
-  a.SO = !g.add_dx ? 0 : stages / 2 < 8 ? stages / 2 : 8;
+  a.SO = !g.add_dx ? 1 : stages / 2 < 8 ? stages / 2 : 8;
   a.S = stages - a.SO < 8 ? stages - a.SO : 8;
   if (a.S < 2) return kErrUnsupported;
   if (!make_map(&l->tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
       !make_map(&l->tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
       !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
     return kErrCuda;
-  l->items = static_cast<int64_t>(a.slabs) * a.ntiles;
   l->smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
   return kOk;
 }
@@ -639,7 +663,12 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     if (int rc = plan_dw_launch(g, di, p, &w)) return rc;
   if (g.dx)
     if (int rc = plan_dx(g, di, sms, &x)) return rc;
-  const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
+  // whole groups of blocks, one for each slab, where there are as many
+  int nx = 0;
+  if (g.dx) {
+    const int64_t slabs = x.a.slabs, groups = sms / slabs < x.a.ntiles ? sms / slabs : x.a.ntiles;
+    nx = groups > 0 ? static_cast<int>(groups * slabs) : sms;
+  }
   if (one) {
     if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles * p.parts), dim3(kGradThreads),
                                             x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmi, w.tmz, w.tmx, x.a,
