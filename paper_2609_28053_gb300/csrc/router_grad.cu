@@ -14,11 +14,12 @@
 // runs over tiles of 128 tokens; dz streams through a ring of [128 x 64]
 // stages, two accumulators alternate, and four warps round the accumulators to
 // bf16 and turn them in shared memory, so that a store takes whole 128-byte lines
-// (T = 32,768, d = 4,096, E = 128: TIME us; 62 with a row a lane, 32 bytes of 32
+// (T = 32,768, d = 4,096, E = 128: 50 us; 62 with a row a lane, 32 bytes of 32
 // rows a store; 63 by TMA from the same tiles).  Where dx is added to, a further
 // warp loads the old values into a ring ahead, and they are turned in its stages.
-// dW: a block has all experts x N columns of d and a part of the tokens; dz and
-// x stream through one ring, 64 tokens a stage, and x is read by one block only.
+// dW: a block has 128 experts x N columns of d and a part of the tokens; dz and
+// x stream through one ring, 64 tokens a stage, and x is read from memory once
+// (above 128 experts two neighbouring blocks share it through L2).
 // With several parts of the tokens their sums are added in order by a second
 // kernel.
 //
@@ -123,27 +124,15 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  // items (slab, tile).  With a block for every slab a block keeps its slab and
-  // takes every step-th tile, so that the slabs of a tile -- whole rows of dx --
-  // are written at the same time; else it has a contiguous range of items,
-  // slab-major.
-  const int step = blocks >= a.slabs ? blocks / a.slabs : 1;
-  int sl0, tile0;
-  int64_t mine;
-  if (blocks >= a.slabs) {
-    sl0 = block % a.slabs;
-    tile0 = block / a.slabs;
-    mine = tile0 < step && tile0 < a.ntiles ? (a.ntiles - tile0 + step - 1) / step : 0;
-  } else {
-    const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles, i0 = items * block / blocks;
-    mine = items * (block + 1) / blocks - i0;
-    sl0 = static_cast<int>(i0 / a.ntiles);
-    tile0 = static_cast<int>(i0 % a.ntiles);
-  }
+  // items (slab, tile), slab-major; a block has a contiguous range of them.  (Blocks
+  // that keep a slab and write the slabs of a row at the same time are as fast an
+  // item, but leave SMs over: 63 us for 60 at d = 4,096 with the stores of that time.)
+  const int64_t items = static_cast<int64_t>(a.slabs) * a.ntiles, i0 = items * block / blocks;
+  const int64_t mine = items * (block + 1) / blocks - i0;
+  const int sl0 = static_cast<int>(i0 / a.ntiles), tile0 = static_cast<int>(i0 % a.ntiles);
   // the item after (sl, tile); a division an item and role would take as long as its MMAs
   auto advance = [&](int& sl, int& tile) {
-    tile += step;
-    if (tile >= a.ntiles) {
+    if (++tile == a.ntiles) {
       tile = 0;
       ++sl;
     }
@@ -315,7 +304,7 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
 // 4.4e-6 and 1.9e-5; the same sums rounded to nearest by 1.6e-7 to 1.5e-6).  So
 // 512 tokens are summed in tensor memory at a time, in two accumulators that
 // alternate, and eight warps add each to the sums that they hold in registers
-// (128 a thread, which bounds a block to 128 x 256 or 256 x 128 sums).
+// (128 a thread, which bounds a block to 128 experts x 256 columns).
 constexpr int kDwStages = 8;      // stages of 64 tokens between two of these additions
 
 struct DwArgs {
@@ -329,11 +318,11 @@ struct DwArgs {
 // The sums of block `block`: one tile of dW over one part of the tokens.
 __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& tmz, const CUtensorMap& tmx, const DwArgs& a,
                                          int block) {
-  const int S = a.S, MT = a.E > 128 ? 2 : 1;
+  const int S = a.S;
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* sm = smem_raw + (base - raw);
-  const uint32_t a_bytes = static_cast<uint32_t>(2 * MT) * kTile64;
+  constexpr uint32_t a_bytes = 2u * kTile64;
   const uint32_t stage_bytes = a_bytes + static_cast<uint32_t>(a.N / 64) * kTile64;
   const uint32_t bars = base + static_cast<uint32_t>(S) * stage_bytes;
   auto full = [&](int s) { return bars + 8u * s; };
@@ -373,9 +362,11 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
   const int tile = block % a.tiles, part = block / a.tiles;
+  // neighbours share x where there are two groups of experts
+  const int eg = a.E > 128 ? tile & 1 : 0, e0 = eg * 128;
   const int64_t s0 = a.stages * part / a.parts;
   const int ns = static_cast<int>(a.stages * (part + 1) / a.parts - s0);
-  const int j0 = tile * a.N, nn = min(a.N, a.d - j0);
+  const int j0 = (a.E > 128 ? tile >> 1 : tile) * a.N, nn = min(a.N, a.d - j0);
 
   if (warp == 0) {
     if (lane == 0) {
@@ -388,7 +379,7 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
         const int t = static_cast<int>((s0 + k) * 64);
         mbar_expect_tx(full(stage), bytes);
         // experts past E (and tokens past T) are filled with zeros
-        for (int c = 0; c < 2 * MT; ++c) tma_load_2d(dst + static_cast<uint32_t>(c) * kTile64, &tmz, full(stage), c * 64, t);
+        for (int c = 0; c < 2; ++c) tma_load_2d(dst + static_cast<uint32_t>(c) * kTile64, &tmz, full(stage), e0 + c * 64, t);
         for (int c = 0; c < nn / 64; ++c)
           tma_load_2d(dst + a_bytes + static_cast<uint32_t>(c) * kTile64, &tmx, full(stage), j0 + c * 64, t);
         if (++stage == S) { stage = 0; phase ^= 1u; }
@@ -411,10 +402,8 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
         const uint32_t sa = base + static_cast<uint32_t>(stage) * stage_bytes;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)  // 16 tokens per MMA
-          for (int m = 0; m < MT; ++m)
-            umma_bf16(tmem + static_cast<uint32_t>(buf * 256 + m * a.N),
-                      mn128_desc(sa + static_cast<uint32_t>(m) * 2u * kTile64 + kk * 2048u, kTile64),
-                      mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k % kDwStages != 0 || kk > 0 ? 1u : 0u);
+          umma_bf16(tmem + static_cast<uint32_t>(buf * 256), mn128_desc(sa + kk * 2048u, kTile64),
+                    mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k % kDwStages != 0 || kk > 0 ? 1u : 0u);
         umma_commit(empty(stage));
         if (k % kDwStages == kDwStages - 1 || k == ns - 1) umma_commit(accf(buf));
         if (++stage == S) { stage = 0; phase ^= 1u; }
@@ -424,8 +413,8 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
         if (mbar_try_wait(drain, 0u)) break;
     }
   } else {
-    // warps 2..5 and 6..9 take the two halves of an accumulator's MT * N columns
-    const int q = warp & 3, h = (warp - 2) >> 2, cw = MT * a.N / 2;
+    // warps 2..5 and 6..9 take the two halves of an accumulator's columns
+    const int q = warp & 3, h = (warp - 2) >> 2, cw = a.N / 2;
     const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * cw);
     float acc[4][32];
 #pragma unroll
@@ -450,7 +439,7 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
       tc_fence_before();
       mbar_arrive(acce(buf));
     }
-    const int e = (MT == 2 ? h * 128 : 0) + q * 32 + lane, c0 = MT == 2 ? 0 : h * cw;
+    const int e = e0 + q * 32 + lane, c0 = h * cw;
     if (ok && e < a.E) {
       float* out = a.out + (static_cast<size_t>(part) * a.E + e) * a.d + j0 + c0;
 #pragma unroll
@@ -552,18 +541,18 @@ constexpr int64_t kSharedElements = int64_t(1) << 26;
 // that needs no more than a wave of blocks.
 DwPlan plan_dw(int64_t T, int d, int E) {
   DwPlan p;
-  const int widest = E > 128 ? 128 : 256;
+  const int groups = E > 128 ? 2 : 1;
   p.stages = (T + 63) / 64;
   if (T <= kFewTokens) {
     p.N = 64;
-    while (p.N < widest && (d + p.N - 1) / p.N > kGradCtas) p.N *= 2;
-    p.tiles = (d + p.N - 1) / p.N;
+    while (p.N < 256 && (d + p.N - 1) / p.N * groups > kGradCtas) p.N *= 2;
+    p.tiles = (d + p.N - 1) / p.N * groups;
     p.parts = 1;
     return p;
   }
   const int64_t most = (p.stages + 3) / 4;  // parts
-  for (p.N = widest;; p.N /= 2) {
-    p.tiles = (d + p.N - 1) / p.N;
+  for (p.N = 256;; p.N /= 2) {
+    p.tiles = (d + p.N - 1) / p.N * groups;
     int64_t parts = kGradCtas / p.tiles;
     if (parts > most) parts = most;
     p.parts = parts < 1 ? 1 : static_cast<int>(parts);
@@ -575,6 +564,7 @@ struct DxLaunch {
   DxArgs a;
   CUtensorMap tmz, tmw, tmi;
   int smem;
+  int64_t items;
 };
 // dx on up to `sms` blocks.
 int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l) {
@@ -597,6 +587,7 @@ int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l)
       !make_map(&l->tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
       !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
     return kErrCuda;
+  l->items = static_cast<int64_t>(a.slabs) * a.ntiles;
   l->smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
   return kOk;
 }
@@ -610,7 +601,7 @@ int plan_dw_launch(const RouterGradArgs& g, const DeviceInfo& di, const DwPlan& 
   l->a = DwArgs{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
                 p.parts > 1 ? 0 : g.add_dW, g.err};
   const int extra = 1024 + 8 * (2 * 8 + 5) + 16;
-  const int stage_bytes = static_cast<int>(kTile64) * ((g.E > 128 ? 4 : 2) + p.N / 64);
+  const int stage_bytes = static_cast<int>(kTile64) * (2 + p.N / 64);
   l->a.S = (di.max_smem_optin - extra) / stage_bytes;
   if (l->a.S > 8) l->a.S = 8;
   if (l->a.S < 2) return kErrUnsupported;
@@ -663,12 +654,7 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     if (int rc = plan_dw_launch(g, di, p, &w)) return rc;
   if (g.dx)
     if (int rc = plan_dx(g, di, sms, &x)) return rc;
-  // whole groups of blocks, one for each slab, where there are as many
-  int nx = 0;
-  if (g.dx) {
-    const int64_t slabs = x.a.slabs, groups = sms / slabs < x.a.ntiles ? sms / slabs : x.a.ntiles;
-    nx = groups > 0 ? static_cast<int>(groups * slabs) : sms;
-  }
+  const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
   if (one) {
     if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles * p.parts), dim3(kGradThreads),
                                             x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmi, w.tmz, w.tmx, x.a,
