@@ -300,7 +300,8 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         auto sigmoids = [&](auto FAR, F2 x) {
           const F2 xc = FAR ? f2(fmin_nan(lo2(x), kFar), fmin_nan(hi2(x), kFar)) : x;
           const F2 y = add2(em2, xc);
-          const F2 sg = mul2(splat2(rcp_approx(lo2(y) * hi2(y))), f2(hi2(y), lo2(y)));
+          const float rr = rcp_approx(lo2(y) * hi2(y));
+          const F2 sg = f2(rr * hi2(y), rr * lo2(y));  // two products: a pair would have to be turned and spread
           return FAR ? f2(lo2(x) > kFar ? 0.f : lo2(sg), hi2(x) > kFar ? 0.f : hi2(sg)) : sg;
         };
         F2 d2 = f2(0.f, 0.f), h2 = f2(0.f, 0.f);
