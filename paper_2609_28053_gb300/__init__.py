@@ -539,34 +539,44 @@ def eqb_balance_loss(z, topk_idx, mb_offsets, alpha, zeta=0.0, score="softmax", 
     takes the mean probabilities when given.  Returns (loss fp32 [M,2]: balance
     loss and z-loss; counts int32 [M,E])."""
     T, E = z.shape
-    _need(z, torch.float32 if z.dtype is torch.float32 else torch.bfloat16, "z")
+    fp32 = z.dtype is torch.float32
+    _need(z, torch.float32 if fp32 else torch.bfloat16, "z")
     K = topk_idx.shape[1] if topk_idx.dim() == 2 else 0
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     _need(mb_offsets, torch.int64, "mb_offsets")
     M = mb_offsets.numel() - 1
-    if score not in _SCORES:
+    kind = _SCORES.get(score)
+    if kind is None:
         raise ValueError(f"score must be one of {sorted(_SCORES)}, got {score!r}")
     if mask is not None:
         _need(mask, torch.bool if mask.dtype is torch.bool else torch.uint8, "mask", (T,))
-    _need(grad_in, torch.float32, "grad_in", (T, E))
+    if grad_in is not None:
+        _need(grad_in, torch.float32, "grad_in", (T, E))
+    to_bf16 = grad_out is not None and grad_out.dtype is torch.bfloat16
     if grad_out is not None:
-        _need(grad_out, torch.bfloat16 if grad_out.dtype is torch.bfloat16 else torch.float32, "grad_out", (T, E))
-    _need(grad_scale, torch.float32, "grad_scale", (1,))
+        _need(grad_out, torch.bfloat16 if to_bf16 else torch.float32, "grad_out", (T, E))
+    if grad_scale is not None:
+        _need(grad_scale, torch.float32, "grad_scale", (1,))
     if counts is None:
         counts = torch.empty((M, E), dtype=torch.int32, device=z.device)
+    else:
+        _need(counts, torch.int32, "counts", (M, E))
     if loss is None:
         loss = torch.empty((M, 2), dtype=torch.float32, device=z.device)
-    _need(counts, torch.int32, "counts", (M, E))
-    _need(loss, torch.float32, "loss", (M, 2))
-    _need(prob, torch.float32, "prob", (M, E))
+    else:
+        _need(loss, torch.float32, "loss", (M, 2))
+    if prob is not None:
+        _need(prob, torch.float32, "prob", (M, E))
     if workspace is None:
         workspace = torch.empty(eqb_balance_loss_workspace_bytes(T, E, M), dtype=torch.uint8, device=z.device)
-    _need(workspace, torch.uint8, "workspace")
-    _need(err_flag, torch.int32, "err_flag")
-    rc = load().eqb_balance_loss(_p(z), z.dtype is torch.float32, _p(topk_idx), T, E, K, _p(mb_offsets), M, _p(mask),
-                                 _SCORES[score], float(alpha), float(zeta), _p(grad_in), _p(grad_out),
-                                 grad_out is not None and grad_out.dtype is torch.bfloat16, _p(grad_scale), _p(counts),
-                                 _p(prob), _p(loss), _p(workspace), workspace.numel(), _p(err_flag), _stream(stream))
+    else:
+        _need(workspace, torch.uint8, "workspace")
+    if err_flag is not None:
+        _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_balance_loss(z.data_ptr(), fp32, topk_idx.data_ptr(), T, E, K, mb_offsets.data_ptr(), M, _p(mask), kind,
+                                 alpha, zeta, _p(grad_in), _p(grad_out), to_bf16, _p(grad_scale), counts.data_ptr(),
+                                 _p(prob), loss.data_ptr(), workspace.data_ptr(), workspace.numel(), _p(err_flag),
+                                 _stream(stream))
     _check(rc, "eqb_balance_loss")
     return loss, counts
 

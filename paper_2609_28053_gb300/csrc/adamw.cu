@@ -418,7 +418,7 @@ __device__ __forceinline__ bool adamw_chunk(const AdamwTensor& t, const AdamwSca
 }
 
 template <int CAP, int BITS>
-__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 4 : 2) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
+__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ __align__(8) uint64_t bars[kAdamWarps * kRing];
   __shared__ int stalled;
@@ -461,12 +461,15 @@ int launch_adamw_cap(const AdamwTensor* t, int count, int bits, const AdamwScala
   AdamwTable<CAP> tab;
   tab.s = sc;
   tab.count = 0;
-  // a block takes 32 units, or as few as 8 where the blocks would be too few to
-  // fill the SMs four times (each with four blocks)
+  // units a warp of a block takes: up to 4, with the rings of 8 bits up to 16, or as
+  // few as leave every SM four blocks four times over.  (403M bf16 parameters with
+  // states in 8 bits: 593 us at 16 and three blocks an SM; 928 at 16 and four
+  // blocks of 64 registers, 757 at 4 and four.)
   int64_t units = 0;
   for (int i = 0; i < count; ++i) units += (t[i].n + kUnit - 1) / kUnit;
+  const int64_t most = bits == 8 ? 16 : 4;
   int64_t per_warp = units / (static_cast<int64_t>(kAdamWarps) * di.sm_count * 16);
-  tab.units = kAdamWarps * static_cast<int>(per_warp < 1 ? 1 : per_warp > 4 ? 4 : per_warp);
+  tab.units = kAdamWarps * static_cast<int>(per_warp < 1 ? 1 : per_warp > most ? most : per_warp);
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     tab.t[tab.count] = t[i];
