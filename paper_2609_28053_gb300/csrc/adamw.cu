@@ -12,7 +12,9 @@
 // of one 8-bit scale, whose largest magnitude is then one reduction within the
 // warp.  With 8-bit states a lane reads 48 bytes a unit, too few to hide a
 // load's latency behind the warps of an SM, so there each warp fetches its units
-// by bulk copies into a ring of its own in shared memory.  Every operation up to the moments and their scales is rounded to
+// by bulk copies into a ring of its own in shared memory (192 matrices of 2^21 bf16
+// parameters: 625 us, 6.5 TB/s; 1,148 by loads into registers).  With 32-bit states
+// and bf16 gradients and copies the same take 1,630 us, 6.9 TB/s.  Every operation up to the moments and their scales is rounded to
 // nearest by itself, so that the 8-bit codes do not depend on how the compiler
 // fuses them.
 #include "eqb_device.cuh"
@@ -27,7 +29,8 @@ constexpr int kAdamThreads = 256;
 constexpr int kAdamWarps = kAdamThreads / 32;
 constexpr int kUnit = 256;       // elements a warp takes at a time: the block of an 8-bit scale
 constexpr float kTop = 448.0f;   // largest e4m3 value
-constexpr float kLeast = 0.001953125f;       // 2^-9, the least positive one
+constexpr float kLeast = 0.001953125f;  // 2^-9, the least positive one
+constexpr float kFull8 = 0.015625f;     // 2^-6, from which on all have three places
 constexpr float kMinNormal = 1.17549435e-38f;
 
 template <int CAP>
@@ -177,24 +180,35 @@ __device__ __forceinline__ void store8_e4m3(void* dst, int64_t base, int left, i
   }
 }
 
+// a b + c d, each operation rounded.
+__device__ __forceinline__ float ema(float a, float b, float c, float d) {
+  return __fadd_rn(__fmul_rn(a, b), __fmul_rn(c, d));
+}
+
 // fp32 max of a and |b| that propagates NaN.
 __device__ __forceinline__ float max_abs(float a, float b) { return fmax_nan(a, fabsf(b)); }
 
-// The scale of a unit and its reciprocal, from the largest magnitude of the
-// warp's elements.  A unit below the normal numbers is stored as zeros.  False
-// if it is not finite.
-__device__ __forceinline__ bool unit_scale(const F2 (&x)[4], float& scale, float& inv) {
+// The largest magnitude of the warp's elements.
+__device__ __forceinline__ float largest(const F2 (&x)[4]) {
   float a = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) a = max_abs(max_abs(a, lo2(x[j])), hi2(x[j]));
   // bit patterns of magnitudes are in their order, NaN above all
-  const uint32_t u = __reduce_max_sync(kFull, __float_as_uint(a));
-  scale = __fmul_rn(__uint_as_float(u), 1.0f / kTop);
-  if (scale < kMinNormal) scale = 0.f;
-  const float r = rcp_approx(scale);
-  inv = scale > 0.f ? __fmaf_rn(r, __fmaf_rn(-scale, r, 1.0f), r) : 0.f;
-  return u < 0x7f800000u;
+  return __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(a)));
 }
+
+// The scale of a unit and its reciprocal, from its largest magnitude.  A unit
+// below the normal numbers is stored as zeros.  False if it is not finite.
+__device__ __forceinline__ bool unit_scale(float top, float& scale, float& inv) {
+  scale = __fmul_rn(top, 1.0f / kTop);
+  if (scale < kMinNormal) scale = 0.f;
+  inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
+  return top < INFINITY;
+}
+
+// Whether x, of e4m3's full range, lies within 16 last places of the middle of
+// two of its values.
+__device__ __forceinline__ bool near_middle(float x) { return ((__float_as_uint(x) + 0x80010u) & 0xfffffu) <= 32u; }
 
 // What a lane reads of one unit of a tensor: `left` elements from `base` on
 // (256 unless Single).
@@ -215,8 +229,9 @@ __device__ __forceinline__ void load_unit(const AdamwTensor& t, int64_t base, in
   }
 }
 
-// The update's root and quotient are within 2 ulps: rounded to nearest they take
-// about twenty instructions of the fifty-five that an 8-bit element has time for.
+// The update's quotient is within 2 ulps (and with 32-bit states its root):
+// rounded to nearest it takes about ten of the fifty-five instructions that an
+// 8-bit element has time for.
 template <int BITS, bool PB, bool GB, Layout L>
 __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScalars& s, float gs, int64_t base, int left,
                                            int lane, const UnitWords<BITS, PB, GB>& w) {
@@ -236,8 +251,14 @@ __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScal
       v[j] = mul2(v[j], splat2(w.vs));
       v[j] = mul2(v[j], v[j]);  // the root is what 8 bits hold
     }
-    m[j] = add2(mul2(m[j], splat2(s.b1)), mul2(gj, splat2(s.c1)));
-    v[j] = add2(mul2(v[j], splat2(s.b2)), mul2(mul2(gj, splat2(s.c2)), gj));
+    if constexpr (BITS == 8) {
+      // not in pairs: the assembler fuses those
+      m[j] = f2(ema(lo2(m[j]), s.b1, lo2(gj), s.c1), ema(hi2(m[j]), s.b1, hi2(gj), s.c1));
+      v[j] = f2(ema(lo2(v[j]), s.b2, __fmul_rn(lo2(gj), s.c2), lo2(gj)), ema(hi2(v[j]), s.b2, __fmul_rn(hi2(gj), s.c2), hi2(gj)));
+    } else {
+      m[j] = add2(mul2(m[j], splat2(s.b1)), mul2(gj, splat2(s.c1)));
+      v[j] = add2(mul2(v[j], splat2(s.b2)), mul2(mul2(gj, splat2(s.c2)), gj));
+    }
     root[j] = f2(sqrt_approx(lo2(v[j])), sqrt_approx(hi2(v[j])));
     const F2 den = add2(mul2(root[j], splat2(s.rbc2)), splat2(s.eps));
     const F2 q = mul2(m[j], f2(rcp_approx(lo2(den)), rcp_approx(hi2(den))));
@@ -252,23 +273,35 @@ __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScal
     store8<false, L>(t.m, base, left, lane, m);
     store8<false, L>(t.v, base, left, lane, v);
   } else {
+    // What 8 bits hold is rounded to nearest at every step up to its codes: a
+    // code that falls the other way moves its value by a sixteenth, and the block's
+    // scale with it once that value is the largest.
     float ms, vs, mi, vi;
-    bad = !unit_scale(m, ms, mi);
-    bad |= !unit_scale(root, vs, vi);
+    bad = !unit_scale(largest(m), ms, mi);
+    const float v1 = largest(v);
+    bad |= !(v1 < INFINITY);
+    unit_scale(__fsqrt_rn(v1), vs, vi);
     float low = INFINITY;
+    bool near = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m[j] = mul2(m[j], splat2(mi));
       root[j] = mul2(root[j], splat2(vi));
       low = fminf(low, fminf(lo2(root[j]), hi2(root[j])));
+      near |= near_middle(lo2(root[j])) || near_middle(hi2(root[j]));
     }
-    // a root that is not zero stays so: eps alone in the denominator would make
-    // a step out of what is left in m
-    if (low < kLeast && vi > 0.f) {
+    // Rounding the roots themselves takes ten instructions and a slow path each
+    // (403M parameters 727 us, 625 with this test): only where one is so near the
+    // middle of two codes that its last places decide, or below their full range.
+    // There a root that is not zero does not become zero: eps alone in the
+    // denominator would make a step out of what is left in m.
+    if (near || (low < kFull8 && vi > 0.f)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        root[j] = f2(lo2(v[j]) > 0.f && lo2(root[j]) < kLeast ? kLeast : lo2(root[j]),
-                     hi2(v[j]) > 0.f && hi2(root[j]) < kLeast ? kLeast : hi2(root[j]));
+      for (int j = 0; j < 4; ++j) {
+        const float r0 = __fsqrt_rn(lo2(v[j])), r1 = __fsqrt_rn(hi2(v[j]));
+        const float u0 = __fmul_rn(r0, vi), u1 = __fmul_rn(r1, vi);
+        root[j] = f2(r0 > 0.f && u0 < kLeast && vi > 0.f ? kLeast : u0, r1 > 0.f && u1 < kLeast && vi > 0.f ? kLeast : u1);
+      }
     }
     store8_e4m3<L>(t.m, base, left, lane, m);
     store8_e4m3<L>(t.v, base, left, lane, root);
@@ -326,8 +359,8 @@ __device__ __forceinline__ bool adamw_stream(const AdamwTensor& t, const AdamwSc
   auto issue = [&](int j) {
     if (lane == 0) {
       const int64_t u = unit_of(j);
-      const uint32_t n = static_cast<uint32_t>(count_of(j)) * U, dst = smem_u32(ring.at) + (j & 1) * ring.bytes;
-      const uint32_t bar = ring.bar + 8u * (j & 1);
+      const uint32_t n = static_cast<uint32_t>(count_of(j)) * U, dst = smem_u32(ring.at) + (j & (kRing - 1)) * ring.bytes;
+      const uint32_t bar = ring.bar + 8u * (j & (kRing - 1));
       mbar_expect_tx(bar, n * (PE + GE + 2));
       bulk_load(dst, static_cast<const uint8_t*>(t.p) + u * U * PE, n * PE, bar);
       bulk_load(dst + 2 * U * PE, static_cast<const uint8_t*>(t.g) + u * U * GE, n * GE, bar);
@@ -345,11 +378,11 @@ __device__ __forceinline__ bool adamw_stream(const AdamwTensor& t, const AdamwSc
   bool bad = false;
   for (int j = 0; j < nj; ++j) {
     const float next = j + 1 < nj ? scale_of(j + 1) : 0.f;
-    if (!__all_sync(kFull, mbar_wait(ring.bar + 8u * (j & 1), (j >> 1) & 1u, stalled))) {
+    if (!__all_sync(kFull, mbar_wait(ring.bar + 8u * (j & (kRing - 1)), (j / kRing) & 1u, stalled))) {
       if (lane == 0) drain_loads(min(nj, j + kRing), kRing, [&](int k) { return ring.bar + 8u * k; });
       return bad;
     }
-    const uint8_t* src = ring.at + (j & 1) * ring.bytes;
+    const uint8_t* src = ring.at + (j & (kRing - 1)) * ring.bytes;
     const int n = count_of(j);
     for (int i = 0; i < n; ++i) {
       UnitWords<8, PB, GB> w;
@@ -418,7 +451,7 @@ __device__ __forceinline__ bool adamw_chunk(const AdamwTensor& t, const AdamwSca
 }
 
 template <int CAP, int BITS>
-__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
+__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 4 : 2) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab) {
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ __align__(8) uint64_t bars[kAdamWarps * kRing];
   __shared__ int stalled;
@@ -461,10 +494,9 @@ int launch_adamw_cap(const AdamwTensor* t, int count, int bits, const AdamwScala
   AdamwTable<CAP> tab;
   tab.s = sc;
   tab.count = 0;
-  // units a warp of a block takes: up to 4, with the rings of 8 bits up to 16, or as
-  // few as leave every SM four blocks four times over.  (403M bf16 parameters with
-  // states in 8 bits: 593 us at 16 and three blocks an SM; 928 at 16 and four
-  // blocks of 64 registers, 757 at 4 and four.)
+  // units a warp of a block takes: up to 4, with the rings of 8 bits up to 16 (two
+  // rounds of a ring of two stages leave its start and end uncovered), or as few
+  // as leave every SM four blocks four times over
   int64_t units = 0;
   for (int i = 0; i < count; ++i) units += (t[i].n + kUnit - 1) / kUnit;
   const int64_t most = bits == 8 ? 16 : 4;
