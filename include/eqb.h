@@ -499,11 +499,11 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   p = (1 - lr weight_decay) p
  *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
- * The arithmetic is fp32, the factors are formed in fp64.  m, v and, with 8
- * bits, sqrt(v) and the codes are rounded to nearest operation by operation; the
- * update's quotient is within 2 ulps, and so is its root with 32 bits, where a
- * second moment below 2^-126 counts as 0.  A bf16 parameter is rounded to nearest
- * once a step (an update below half its last place is lost: keep an fp32
+ * The arithmetic is fp32, the factors are formed in fp64.  The update's quotient
+ * is within 2 ulps, and so is its root, where a second moment below 2^-126 counts
+ * as 0.  With 8 bits m, v, sqrt(v), scales and codes are rounded to nearest
+ * operation by operation, without fused ones.  A bf16 parameter is rounded to
+ * nearest once a step (an update below half its last place is lost: keep an fp32
  * parameter with a bf16 copy where that matters).
  * state_bits 32: exp_avg holds m and exp_avg_sq holds v, fp32 [n].
  * state_bits 8:  exp_avg holds m and exp_avg_sq holds sqrt(v) (whose range is

@@ -14,9 +14,9 @@
 // load's latency behind the warps of an SM, so there each warp fetches its units
 // by bulk copies into a ring of its own in shared memory (192 matrices of 2^21 bf16
 // parameters: 625 us, 6.5 TB/s; 1,148 by loads into registers).  With 32-bit states
-// and bf16 gradients and copies the same take 1,630 us, 6.9 TB/s.  Every operation up to the moments and their scales is rounded to
-// nearest by itself, so that the 8-bit codes do not depend on how the compiler
-// fuses them.
+// and bf16 gradients and copies the same take 1,630 us, 6.9 TB/s.  Of 8-bit states
+// every operation up to the moments, their scales and codes is rounded to nearest
+// by itself, so that a code does not depend on how operations are fused.
 #include "eqb_device.cuh"
 #include "f32x2.cuh"
 #include "mbarrier.cuh"
@@ -256,8 +256,8 @@ __device__ __forceinline__ bool adamw_unit(const AdamwTensor& t, const AdamwScal
       m[j] = f2(ema(lo2(m[j]), s.b1, lo2(gj), s.c1), ema(hi2(m[j]), s.b1, hi2(gj), s.c1));
       v[j] = f2(ema(lo2(v[j]), s.b2, __fmul_rn(lo2(gj), s.c2), lo2(gj)), ema(hi2(v[j]), s.b2, __fmul_rn(hi2(gj), s.c2), hi2(gj)));
     } else {
-      m[j] = add2(mul2(m[j], splat2(s.b1)), mul2(gj, splat2(s.c1)));
-      v[j] = add2(mul2(v[j], splat2(s.b2)), mul2(mul2(gj, splat2(s.c2)), gj));
+      m[j] = fma2(m[j], splat2(s.b1), mul2(gj, splat2(s.c1)));
+      v[j] = fma2(v[j], splat2(s.b2), mul2(mul2(gj, splat2(s.c2)), gj));
     }
     root[j] = f2(sqrt_approx(lo2(v[j])), sqrt_approx(hi2(v[j])));
     const F2 den = add2(mul2(root[j], splat2(s.rbc2)), splat2(s.eps));
