@@ -475,12 +475,13 @@ eqb_status eqb_balance_loss(const void *z, int32_t z_fp32, const int32_t *topk_i
  * from bf16 inputs with fp32 accumulation on the tensor cores (tcgen05).  With
  * accumulate_dx or accumulate_dW the result is added to what the output holds
  * (in fp32, dx rounded once).  Either output may be NULL; then it is not
- * computed.  dW's tokens are summed in parts that depend on T, d, E and the SM
- * count and the parts in a fixed order: the same call gives the same bits.
+ * computed.  dW's tokens are summed 512 at a time on the tensor cores, the sums in
+ * parts that depend on T, d, E, the SM count and which outputs are asked for, and
+ * the parts in a fixed order: the same call gives the same bits.
  *   dz         device bf16 [T,E], 16-byte aligned, e.g. from eqb_balance_loss
  *   x          device bf16 [T,d], 16-byte aligned (not read without dW)
  *   W_r        device bf16 [E,d], 16-byte aligned (not read without dx)
- *   dx         device bf16 [T,d], 16-byte aligned
+ *   dx         device bf16 [T,d], 16-byte aligned, not overlapping x
  *   dW         device fp32 [E,d], 16-byte aligned
  *   workspace  device buffer of eqb_router_grad_workspace_bytes(T, d, E)
  *              bytes, 256-byte aligned (dW only; may be NULL where that is 0)

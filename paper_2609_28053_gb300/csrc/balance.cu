@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
   griddep_wait();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   for (int l = blockIdx.y; l < a.M; l += gridDim.y) {
-    const int64_t lo = __ldg(a.off + l), hi = min(__ldg(a.off + l + 1), a.T);
+    const int64_t lo = min(max(__ldg(a.off + l), int64_t(0)), a.T), hi = min(max(__ldg(a.off + l + 1), lo), a.T);
     const int64_t n = a.mask ? a.valid[l] : hi - lo;
     // tokens are fewer than 2^31
     const uint32_t first = static_cast<uint32_t>(lo) / tokens_per_cta;

@@ -124,13 +124,15 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   griddep_wait();
   int l = 0;
   uint32_t rank = 0;
-  int64_t tb, te;
+  int64_t tb, te, len = 0;
   if (cut.cluster) {
     l = static_cast<int>(blockIdx.x) / cut.cluster;
     rank = blockIdx.x % static_cast<unsigned>(cut.cluster);
-    const int64_t lo = __ldg(a.off + l), n = __ldg(a.off + l + 1) - lo;
-    tb = lo + n * rank / cut.cluster;
-    te = lo + n * (rank + 1) / cut.cluster;
+    // within the batch whatever the offsets say
+    const int64_t lo = min(max(__ldg(a.off + l), int64_t(0)), a.T);
+    len = min(max(__ldg(a.off + l + 1), lo), a.T) - lo;
+    tb = lo + len * rank / cut.cluster;
+    te = lo + len * (rank + 1) / cut.cluster;
   } else {
     tb = static_cast<int64_t>(blockIdx.x) * cut.tokens_per_cta;
     te = min(tb + cut.tokens_per_cta, a.T);
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     int64_t n;
     int seg_end = nt;
     if (cut.cluster) {
-      n = __ldg(a.off + l + 1) - __ldg(a.off + l);
+      n = len;
       if (mb) {
         n = 0;
         for (int q = 0; q < cut.cluster; ++q) n += peer_word(&valid_n, q);
