@@ -595,15 +595,20 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
     _need(dz, torch.bfloat16, "dz")
     _need(x, torch.bfloat16, "x", (T, d))
     _need(W_r, torch.bfloat16, "W_r", (E, d))
-    _need(dx, torch.bfloat16, "dx", (T, d))
-    _need(dW, torch.float32, "dW", (E, d))
-    if workspace is None and dW is not None:
+    if dx is not None:
+        _need(dx, torch.bfloat16, "dx", (T, d))
+    if dW is not None:
+        _need(dW, torch.float32, "dW", (E, d))
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    elif dW is not None:
         need = eqb_router_grad_workspace_bytes(T, d, E)
         workspace = torch.empty(need, dtype=torch.uint8, device=dz.device) if need else None
-    _need(workspace, torch.uint8, "workspace")
-    _need(err_flag, torch.int32, "err_flag")
-    rc = load().eqb_router_grad(_p(dz), _p(x), _p(W_r), T, d, E, _p(dx), bool(accumulate_dx), _p(dW), bool(accumulate_dW),
-                                _p(workspace), 0 if workspace is None else workspace.numel(), _p(err_flag), _stream(stream))
+    if err_flag is not None:
+        _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_router_grad(dz.data_ptr(), x.data_ptr(), W_r.data_ptr(), T, d, E, _p(dx), bool(accumulate_dx), _p(dW),
+                                bool(accumulate_dW), _p(workspace), 0 if workspace is None else workspace.numel(),
+                                _p(err_flag), _stream(stream))
     _check(rc, "eqb_router_grad")
     return dx, dW
 

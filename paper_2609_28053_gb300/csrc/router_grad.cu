@@ -586,8 +586,9 @@ int plan_dx(const RouterGradArgs& g, const DeviceInfo& di, int sms, DxLaunch* l)
   if (a.S < 2) return kErrUnsupported;
   if (!make_map(&l->tmz, g.dz, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.E), kBM) ||
       !make_map(&l->tmw, g.W, static_cast<uint64_t>(g.E), static_cast<uint64_t>(g.d), static_cast<uint32_t>(g.E)) ||
-      !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM))
+      (g.add_dx && !make_map(&l->tmi, g.dx, static_cast<uint64_t>(g.T), static_cast<uint64_t>(g.d), kBM)))
     return kErrCuda;
+  if (!g.add_dx) l->tmi = l->tmz;  // not used
   l->items = static_cast<int64_t>(a.slabs) * a.ntiles;
   l->smem = wbytes + (a.S + a.SO) * static_cast<int>(kDxStage) + extra;
   return kOk;
@@ -630,10 +631,6 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     if (!g.dW || g.add_dW) return kOk;
     return status_of(launch_dependent(zero_kernel, dim3(static_cast<unsigned>((n + 1023) / 1024)), dim3(256), 0, s, g.dW, n));
   }
-  // before the maps: encoding them needs a context, which a thread's first runtime call makes current
-  if (!allow_smem(router_dx_kernel, di.max_smem_optin) || !allow_smem(router_dw_kernel, di.max_smem_optin) ||
-      !allow_smem(router_dxdw_kernel, di.max_smem_optin))
-    return kErrCuda;
   DxLaunch x;
   DwLaunch w;
   DwPlan p = plan_dw(g.T, g.d, g.E);
@@ -651,6 +648,11 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     sms = di.sm_count - p.parts * p.tiles;
     one = true;
   }
+  // before the maps: encoding them needs a context, which a thread's first runtime call makes current
+  if (one ? !allow_smem(router_dxdw_kernel, di.max_smem_optin)
+          : (g.dx && !allow_smem(router_dx_kernel, di.max_smem_optin)) ||
+                (g.dW && !allow_smem(router_dw_kernel, di.max_smem_optin)))
+    return kErrCuda;
   if (g.dW)
     if (int rc = plan_dw_launch(g, di, p, &w)) return rc;
   if (g.dx)
