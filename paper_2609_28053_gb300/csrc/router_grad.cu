@@ -534,8 +534,9 @@ constexpr int64_t kFewTokens = 1024;
 // Up to this many elements of x both gradients share a launch, each on a part
 // of the SMs: of two launches each has its start and its end (T = 300, d = 1,024,
 // E = 64 9.3 us for 11.5, 7,520, 1,792, 96 22 for 31, 60,000, 256, 64 32 for 50;
-// from 16,411, 4,096, 128 on 66 for 66: the split is uneven).
-constexpr int64_t kSharedElements = int64_t(1) << 26;
+// 16,411, 4,096, 128 65 for 66, 65,536, 4,096, 128 added to 292 for 274: the split
+// is uneven).
+constexpr int64_t kSharedElements = int64_t(1) << 27;
 
 // Columns of a dW tile and parts of the tokens: the widest tile that gives
 // every SM a block with at least four stages; of few tokens the narrowest one
@@ -634,18 +635,24 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   DxLaunch x;
   DwLaunch w;
   DwPlan p = plan_dw(g.T, g.d, g.E);
-  // SMs of dx where both share a launch: by what each has to move, dW's in
-  // whole parts and at most three quarters of them
+  // SMs of dx where both share a launch, dW's in whole parts.  A tile of 128 tokens
+  // x 256 columns takes an SM 2.0 us of dW and 1.5 + E / 270 of dx, 1.7 times that
+  // where it is added to (T = 32,768, d = 4,096, E = 64, 128 and 256 alone).
   int sms = di.sm_count;
   bool one = false;
   if (g.dx && g.dW && g.T * g.d <= kSharedElements && 4 * p.tiles <= 3 * di.sm_count) {
-    const double dz = 2.0 * g.T * g.E, row = 2.0 * g.T * g.d;
-    const double bx = (1 + g.add_dx) * row + dz * ((g.d + 255) / 256), bw = row + dz * p.tiles;
-    const int want = static_cast<int>(di.sm_count * bw / (bx + bw) / p.tiles + 0.5);
-    int parts = p.parts < want ? p.parts : want;
-    while (parts > 1 && 4 * parts * p.tiles > 3 * di.sm_count) --parts;
-    p.parts = parts < 1 ? 1 : parts;
-    sms = di.sm_count - p.parts * p.tiles;
+    const double dx = (1.5 + g.E / 270.0) * (g.add_dx ? 1.7 : 1.0), dw = 2.0;
+    int best = 1;
+    double least = 1e30;
+    for (int parts = 1; parts <= p.parts && 4 * parts * p.tiles <= 3 * di.sm_count; ++parts) {
+      const double on_x = dx / (di.sm_count - parts * p.tiles), on_w = dw / (parts * p.tiles);
+      if (const double t = on_x > on_w ? on_x : on_w; t < least) {
+        least = t;
+        best = parts;
+      }
+    }
+    p.parts = best;
+    sms = di.sm_count - best * p.tiles;
     one = true;
   }
   // before the maps: encoding them needs a context, which a thread's first runtime call makes current
