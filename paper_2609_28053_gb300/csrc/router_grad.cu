@@ -17,11 +17,10 @@
 // (T = 32,768, d = 4,096, E = 128: 50 us; 62 with a row a lane, 32 bytes of 32
 // rows a store; 63 by TMA from the same tiles).  Where dx is added to, a further
 // warp loads the old values into a ring ahead, and they are turned in its stages.
-// dW: a block has 128 experts x N columns of d and a part of the tokens; dz and
-// x stream through one ring, 64 tokens a stage, and x is read from memory once
-// (above 128 experts two neighbouring blocks share it through L2).
-// With several parts of the tokens their sums are added in order by a second
-// kernel.
+// dW: a block has 128 experts x N columns of d and some of the tokens; dz and x
+// stream through one ring, 64 tokens a stage, and x is read from memory once
+// (above 128 experts two neighbouring blocks share it through L2).  The blocks'
+// sums are added in order by a second kernel.
 //
 // Roles, bounded waits and the way out of a stall are those of the forward
 // projection: warp 0 loads, warp 1 issues the MMAs, the others take the
@@ -307,15 +306,21 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
 // (128 a thread, which bounds a block to 128 experts x 256 columns).
 constexpr int kDwStages = 8;      // stages of 64 tokens between two of these additions
 
+// dW is cut into cols tiles of N columns (and two groups of experts above 128),
+// each over `stages` stages of 64 tokens.  The blocks of a group take equal,
+// contiguous shares of the cols x stages, so that any number of blocks is as
+// good; block c of a group adds what it has of tile t to row c + t of `part`,
+// which no other pair of the two has, and a second kernel adds up the rows of a
+// tile in order.  With a block for every tile (direct) it is dW that they write.
 struct DwArgs {
-  int T, d, E, N, tiles, parts, S;
+  int T, d, E, N, cols, groups, share, S;  // share: blocks of a group
   int64_t stages;  // of 64 tokens, in all
-  float* out;      // dW, or the parts' sums [parts, E, d]
-  int add;         // one part only: out += (dW)
+  float* out;      // dW, or part: rows of groups x [N / 4, 128] x 4 sums
+  int direct, add;
   int32_t* err;
 };
 
-// The sums of block `block`: one tile of dW over one part of the tokens.
+// The sums of block `block`: its share of a group's tiles and stages.
 __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& tmz, const CUtensorMap& tmx, const DwArgs& a,
                                          int block) {
   const int S = a.S;
@@ -361,52 +366,69 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  const int tile = block % a.tiles, part = block / a.tiles;
   // neighbours share x where there are two groups of experts
-  const int eg = a.E > 128 ? tile & 1 : 0, e0 = eg * 128;
-  const int64_t s0 = a.stages * part / a.parts;
-  const int ns = static_cast<int>(a.stages * (part + 1) / a.parts - s0);
-  const int j0 = (a.E > 128 ? tile >> 1 : tile) * a.N, nn = min(a.N, a.d - j0);
+  const int eg = a.groups == 2 ? block & 1 : 0, b = a.groups == 2 ? block >> 1 : block, e0 = eg * 128;
+  // with whole parts of every tile, neighbours take the same tokens of different tiles
+  const int parts = a.share / a.cols, c = parts * a.cols == a.share ? b % a.cols * parts + b / a.cols : b;
+  const int64_t total = a.stages * a.cols, u0 = total * c / a.share, u1 = total * (c + 1) / a.share;
+  const int col0 = static_cast<int>(u0 / a.stages);
+  const int64_t first0 = u0 - col0 * a.stages;
+  // tile `col` from its stage `first` on: `ns` stages, as far as the tile and the share go
+  auto stages_of = [&](int col, int64_t first) {
+    return static_cast<int>(min(a.stages, u1 - static_cast<int64_t>(col) * a.stages) - first);
+  };
 
   if (warp == 0) {
     if (lane == 0) {
-      int stage = 0, n = 0;
+      int stage = 0, n = 0, col = col0;
+      int64_t first = first0;
       uint32_t phase = 0;
-      const uint32_t bytes = a_bytes + static_cast<uint32_t>(nn / 64) * kTile64;
-      for (int k = 0; k < ns; ++k, ++n) {
-        if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) break;
-        const uint32_t dst = base + static_cast<uint32_t>(stage) * stage_bytes;
-        const int t = static_cast<int>((s0 + k) * 64);
-        mbar_expect_tx(full(stage), bytes);
-        // experts past E (and tokens past T) are filled with zeros
-        for (int c = 0; c < 2; ++c) tma_load_2d(dst + static_cast<uint32_t>(c) * kTile64, &tmz, full(stage), e0 + c * 64, t);
-        for (int c = 0; c < nn / 64; ++c)
-          tma_load_2d(dst + a_bytes + static_cast<uint32_t>(c) * kTile64, &tmx, full(stage), j0 + c * 64, t);
-        if (++stage == S) { stage = 0; phase ^= 1u; }
+      bool ok = true;
+      for (int ns; ok && (ns = stages_of(col, first)) > 0; ++col, first = 0) {
+        const int j0 = col * a.N, nn = min(a.N, a.d - j0);
+        const uint32_t bytes = a_bytes + static_cast<uint32_t>(nn / 64) * kTile64;
+        for (int k = 0; k < ns; ++k, ++n) {
+          if (!mbar_wait(empty(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t dst = base + static_cast<uint32_t>(stage) * stage_bytes;
+          const int t = static_cast<int>((first + k) * 64);
+          mbar_expect_tx(full(stage), bytes);
+          // experts past E (and tokens past T) are filled with zeros
+          for (int i = 0; i < 2; ++i) tma_load_2d(dst + static_cast<uint32_t>(i) * kTile64, &tmz, full(stage), e0 + i * 64, t);
+          for (int i = 0; i < nn / 64; ++i)
+            tma_load_2d(dst + a_bytes + static_cast<uint32_t>(i) * kTile64, &tmx, full(stage), j0 + i * 64, t);
+          if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
       }
       *issued = n;
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      const uint32_t idesc = umma_idesc_bf16(kBM, nn) | kMnA | kMnB;
-      int stage = 0;
+      int stage = 0, col = col0, chunk = 0;
+      int64_t first = first0;
       uint32_t phase = 0;
-      for (int k = 0; k < ns; ++k) {
-        const int chunk = k / kDwStages, buf = chunk & 1;
-        if (k % kDwStages == 0) {
-          if (!mbar_wait(acce(buf), (static_cast<uint32_t>(chunk >> 1) & 1u) ^ 1u, abort_flag)) break;
+      bool ok = true;
+      for (int ns; ok && (ns = stages_of(col, first)) > 0; ++col, first = 0) {
+        const uint32_t idesc = umma_idesc_bf16(kBM, min(a.N, a.d - col * a.N)) | kMnA | kMnB;
+        for (int k = 0; k < ns; ++k) {
+          const int buf = chunk & 1;
+          if (k % kDwStages == 0) {
+            if (!mbar_wait(acce(buf), (static_cast<uint32_t>(chunk >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+          }
+          if (!mbar_wait(full(stage), phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
-        }
-        if (!mbar_wait(full(stage), phase, abort_flag)) break;
-        tc_fence_after();
-        const uint32_t sa = base + static_cast<uint32_t>(stage) * stage_bytes;
+          const uint32_t sa = base + static_cast<uint32_t>(stage) * stage_bytes;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)  // 16 tokens per MMA
-          umma_bf16(tmem + static_cast<uint32_t>(buf * 256), mn128_desc(sa + kk * 2048u, kTile64),
-                    mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k % kDwStages != 0 || kk > 0 ? 1u : 0u);
-        umma_commit(empty(stage));
-        if (k % kDwStages == kDwStages - 1 || k == ns - 1) umma_commit(accf(buf));
-        if (++stage == S) { stage = 0; phase ^= 1u; }
+          for (int kk = 0; kk < 4; ++kk)  // 16 tokens per MMA
+            umma_bf16(tmem + static_cast<uint32_t>(buf * 256), mn128_desc(sa + kk * 2048u, kTile64),
+                      mn128_desc(sa + a_bytes + kk * 2048u, kTile64), idesc, k % kDwStages != 0 || kk > 0 ? 1u : 0u);
+          umma_commit(empty(stage));
+          if (k % kDwStages == kDwStages - 1 || k == ns - 1) {
+            umma_commit(accf(buf));
+            ++chunk;
+          }
+          if (++stage == S) { stage = 0; phase ^= 1u; }
+        }
       }
       umma_commit(drain);
       for (uint32_t i = 0; i < kSpinLimit; ++i)
@@ -414,41 +436,49 @@ __device__ __forceinline__ void dw_block(uint8_t* smem_raw, const CUtensorMap& t
     }
   } else {
     // warps 2..5 and 6..9 take the two halves of an accumulator's columns
-    const int q = warp & 3, h = (warp - 2) >> 2, cw = a.N / 2;
-    const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * cw);
-    float acc[4][32];
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int i = 0; i < 32; ++i) acc[g][i] = 0.f;
-    const int chunks = (ns + kDwStages - 1) / kDwStages;
+    const int q = warp & 3, h = (warp - 2) >> 2, cw = a.N / 2, c0 = h * cw;
+    const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(c0);
+    const int row = q * 32 + lane, e = e0 + row;
+    int col = col0, chunk = 0;
+    int64_t first = first0;
     bool ok = true;
-    for (int c = 0; c < chunks; ++c) {
-      const int buf = c & 1;
-      ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(c >> 1) & 1u, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
+    for (int ns; ok && (ns = stages_of(col, first)) > 0; ++col, first = 0) {
+      float acc[4][32];
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        if (g * 32 < cw) {
-          uint32_t r[32];
-          tmem_ld32(mine + static_cast<uint32_t>(buf * 256 + g * 32), r);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[g][i] = __fadd_rn(acc[g][i], __uint_as_float(r[i]));
-        }
-      tc_fence_before();
-      mbar_arrive(acce(buf));
-    }
-    const int e = e0 + q * 32 + lane, c0 = h * cw;
-    if (ok && e < a.E) {
-      float* out = a.out + (static_cast<size_t>(part) * a.E + e) * a.d + j0 + c0;
+        for (int i = 0; i < 32; ++i) acc[g][i] = 0.f;
+      for (int k = 0; k < ns; k += kDwStages, ++chunk) {
+        const int buf = chunk & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(accf(buf), static_cast<uint32_t>(chunk >> 1) & 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          if (g * 32 < cw) {
+            uint32_t r[32];
+            tmem_ld32(mine + static_cast<uint32_t>(buf * 256 + g * 32), r);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[g][i] = __fadd_rn(acc[g][i], __uint_as_float(r[i]));
+          }
+        tc_fence_before();
+        mbar_arrive(acce(buf));
+      }
+      if (!ok || e >= a.E) continue;
+      const int nn = min(a.N, a.d - col * a.N);
+      // in part the rows of four columns lie one after the other, so that a
+      // warp's stores are whole lines
+      float4* out = a.direct ? reinterpret_cast<float4*>(a.out + static_cast<size_t>(e) * a.d + col * a.N + c0)
+                             : reinterpret_cast<float4*>(a.out) +
+                                   ((static_cast<size_t>(c) + col) * a.groups + eg) * (a.N / 4) * 128 + (c0 / 4) * 128 + row;
+      const int next = a.direct ? 1 : 128;
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         if (g * 32 < cw && c0 + g * 32 < nn) {
 #pragma unroll
           for (int v = 0; v < 8; ++v) {
             float4 o = make_float4(acc[g][4 * v], acc[g][4 * v + 1], acc[g][4 * v + 2], acc[g][4 * v + 3]);
-            float4* dst = reinterpret_cast<float4*>(out + g * 32) + v;
+            float4* dst = out + (8 * g + v) * next;
             if (a.add) {
               const float4 w = *dst;
               o.x += w.x; o.y += w.y; o.z += w.z; o.w += w.w;
@@ -490,30 +520,37 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                        DwArgs w) {
   extern __shared__ uint8_t smem_raw[];
   const int block = static_cast<int>(blockIdx.x);
-  const int nw = w.tiles * w.parts;
+  const int nw = w.share * w.groups;
   if (block < nw) dw_block(smem_raw, tmz64, tmx, w, block);
   else dx_block(smem_raw, tmz, tmw, tmi, a, block - nw, static_cast<int>(gridDim.x) - nw);
 }
 
-// dW (+)= the parts' sums, in ascending order; n a multiple of 4.
-__global__ void __launch_bounds__(256) router_dw_sum_kernel(const float* part, int parts, int64_t n, float* dW, int add) {
+// dW (+)= the rows of part that belong to each tile, in ascending order: four
+// columns of an expert a thread.
+__global__ void __launch_bounds__(256) router_dw_sum_kernel(const float4* part, DwArgs a, float* dW) {
+  const int quads = a.N / 4 * 128;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int tile = static_cast<int>(i / quads), at = static_cast<int>(i % quads);  // at = column / 4 * 128 + row
+  const int col = tile / a.groups, eg = tile % a.groups, e = eg * 128 + (at & 127), j = col * a.N + (at >> 7) * 4;
+  const int64_t total = a.stages * a.cols, x0 = a.stages * col, x1 = x0 + a.stages - 1;
+  // the blocks that hold the tile's first and last stages
+  const int first = static_cast<int>(((x0 + 1) * a.share - 1) / total), last = static_cast<int>(((x1 + 1) * a.share - 1) / total);
   griddep_wait();
-  const int64_t n4 = n / 4;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n4; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const float4* p = reinterpret_cast<const float4*>(part) + i;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (col >= a.cols || e >= a.E || j >= a.d) return;
+  const float4* p = part + (static_cast<size_t>(first + col) * a.groups + eg) * quads + at;
+  const size_t row = static_cast<size_t>(a.groups) * quads;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-      const float4 w = __ldcg(p + k * n4);
-      s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
-    }
-    float4* o = reinterpret_cast<float4*>(dW) + i;
-    if (add) {
-      const float4 w = *o;
-      s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
-    }
-    *o = s;
+  for (int c = first; c <= last; ++c, p += row) {
+    const float4 w = __ldcg(p);
+    s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
   }
+  float4* o = reinterpret_cast<float4*>(dW + static_cast<size_t>(e) * a.d + j);
+  if (a.add) {
+    const float4 w = *o;
+    s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
+  }
+  *o = s;
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(float* p, int64_t n) {
@@ -523,8 +560,9 @@ __global__ void __launch_bounds__(256) zero_kernel(float* p, int64_t n) {
 }
 
 struct DwPlan {
-  int N, tiles, parts;
+  int N, cols, groups, share;
   int64_t stages;
+  bool direct;
 };
 
 // Up to this many tokens dW's tiles are narrow and take all tokens: a sum of
@@ -533,33 +571,44 @@ constexpr int64_t kFewTokens = 1024;
 
 // Up to this many elements of x both gradients share a launch, each on a part
 // of the SMs: of two launches each has its start and its end (T = 300, d = 1,024,
-// E = 64 9.3 us for 11.5, 7,520, 1,792, 96 22 for 31, 60,000, 256, 64 32 for 50;
-// 16,411, 4,096, 128 65 for 66, 65,536, 4,096, 128 added to 292 for 274: the split
-// is uneven).
+// E = 64 8.3 us for 11.5, 7,520, 1,792, 96 19 for 31, 60,000, 256, 64 26 for 50;
+// 65,536, 4,096, 128 added to 292 for 274, where the bytes decide).
 constexpr int64_t kSharedElements = int64_t(1) << 27;
 
-// Columns of a dW tile and parts of the tokens: the widest tile that gives
-// every SM a block with at least four stages; of few tokens the narrowest one
-// that needs no more than a wave of blocks.
+// The blocks of a group, of `most`: as many for every tile if that leaves no more
+// than a tenth of them out.  Blocks that take the same tokens at the same time
+// share dz on its way (both gradients of T = 65,536, d = 4,096, E = 128: 274 us with
+// 144 of 152 for dW, 285 with all of them); an uneven share fills the SMs (T =
+// 30,000, d = 1,024, E = 128, each on a part of them: 31 us for 38).
+int even_share(int most, int cols) {
+  const int even = most / cols * cols;
+  return 10 * even >= 9 * most ? even : most;
+}
+
+// Columns of a dW tile and blocks of a group, at most one an SM: the widest tile
+// that leaves most of the SMs a block with at least four stages; of few tokens
+// the narrowest one that needs no more than a wave of blocks.
 DwPlan plan_dw(int64_t T, int d, int E) {
   DwPlan p;
-  const int groups = E > 128 ? 2 : 1;
+  p.groups = E > 128 ? 2 : 1;
   p.stages = (T + 63) / 64;
-  if (T <= kFewTokens) {
+  p.direct = T <= kFewTokens;
+  if (p.direct) {
     p.N = 64;
-    while (p.N < 256 && (d + p.N - 1) / p.N * groups > kGradCtas) p.N *= 2;
-    p.tiles = (d + p.N - 1) / p.N * groups;
-    p.parts = 1;
+    while (p.N < 256 && (d + p.N - 1) / p.N * p.groups > kGradCtas) p.N *= 2;
+    p.cols = p.share = (d + p.N - 1) / p.N;
     return p;
   }
-  const int64_t most = (p.stages + 3) / 4;  // parts
   for (p.N = 256;; p.N /= 2) {
-    p.tiles = (d + p.N - 1) / p.N * groups;
-    int64_t parts = kGradCtas / p.tiles;
-    if (parts > most) parts = most;
-    p.parts = parts < 1 ? 1 : static_cast<int>(parts);
-    if (p.N == 64 || p.tiles * p.parts >= 120) return p;
+    p.cols = (d + p.N - 1) / p.N;
+    const int64_t most = p.stages * p.cols / 4, sms = kGradCtas / p.groups;
+    p.share = even_share(static_cast<int>(most < sms ? most : sms), p.cols);
+    if (p.N == 64 || p.share * p.groups >= 120) break;
   }
+  return p;
+}
+size_t part_bytes(const DwPlan& p) {
+  return p.direct ? 0 : (static_cast<size_t>(p.share) + p.cols) * p.groups * p.N * 128 * 4;
 }
 
 struct DxLaunch {
@@ -601,8 +650,8 @@ struct DwLaunch {
   int smem;
 };
 int plan_dw_launch(const RouterGradArgs& g, const DeviceInfo& di, const DwPlan& p, DwLaunch* l) {
-  l->a = DwArgs{static_cast<int>(g.T), g.d, g.E, p.N, p.tiles, p.parts, 0, p.stages, p.parts > 1 ? g.part : g.dW,
-                p.parts > 1 ? 0 : g.add_dW, g.err};
+  l->a = DwArgs{static_cast<int>(g.T), g.d, g.E, p.N, p.cols, p.groups, p.share, 0, p.stages, p.direct ? g.dW : g.part, p.direct,
+                p.direct ? g.add_dW : 0, g.err};
   const int extra = 1024 + 8 * (2 * 8 + 5) + 16;
   const int stage_bytes = static_cast<int>(kTile64) * (2 + p.N / 64);
   l->a.S = (di.max_smem_optin - extra) / stage_bytes;
@@ -620,8 +669,7 @@ int status_of(cudaError_t e) { return e == cudaSuccess ? kOk : kErrCuda; }
 }  // namespace
 
 size_t router_grad_workspace(int64_t T, int d, int E) {
-  const DwPlan p = plan_dw(T, d, E);
-  return p.parts > 1 ? static_cast<size_t>(p.parts) * E * d * 4 : 0;
+  return part_bytes(plan_dw(T, d, E));
 }
 
 int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
@@ -635,25 +683,18 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   DxLaunch x;
   DwLaunch w;
   DwPlan p = plan_dw(g.T, g.d, g.E);
-  // SMs of dx where both share a launch, dW's in whole parts.  A tile of 128 tokens
-  // x 256 columns takes an SM 2.0 us of dW and 1.5 + E / 270 of dx, 1.7 times that
-  // where it is added to (T = 32,768, d = 4,096, E = 64, 128 and 256 alone).
+  // SMs of dx where both share a launch.  A tile of 128 tokens x 256 columns takes
+  // an SM 2.0 us of dW and 1.5 + E / 270 of dx, 1.7 times that where it is added to
+  // (T = 32,768, d = 4,096, E = 64, 128 and 256 alone).
   int sms = di.sm_count;
-  bool one = false;
-  if (g.dx && g.dW && g.T * g.d <= kSharedElements && 4 * p.tiles <= 3 * di.sm_count) {
-    const double dx = (1.5 + g.E / 270.0) * (g.add_dx ? 1.7 : 1.0), dw = 2.0;
-    int best = 1;
-    double least = 1e30;
-    for (int parts = 1; parts <= p.parts && 4 * parts * p.tiles <= 3 * di.sm_count; ++parts) {
-      const double on_x = dx / (di.sm_count - parts * p.tiles), on_w = dw / (parts * p.tiles);
-      if (const double t = on_x > on_w ? on_x : on_w; t < least) {
-        least = t;
-        best = parts;
-      }
+  const bool one = g.dx && g.dW && g.T * g.d <= kSharedElements && (!p.direct || 4 * p.cols * p.groups <= 3 * di.sm_count);
+  if (one) {
+    if (!p.direct) {
+      const double dx = (1.5 + g.E / 270.0) * (g.add_dx ? 1.7 : 1.0), dw = 2.0;
+      const int want = static_cast<int>(di.sm_count * dw / (dx + dw) / p.groups + 0.5);
+      if (p.share > want) p.share = even_share(want, p.cols);
     }
-    p.parts = best;
-    sms = di.sm_count - best * p.tiles;
-    one = true;
+    sms = di.sm_count - p.share * p.groups;
   }
   // before the maps: encoding them needs a context, which a thread's first runtime call makes current
   if (one ? !allow_smem(router_dxdw_kernel, di.max_smem_optin)
@@ -666,7 +707,7 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
     if (int rc = plan_dx(g, di, sms, &x)) return rc;
   const int nx = g.dx ? static_cast<int>(x.items < sms ? x.items : sms) : 0;
   if (one) {
-    if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.tiles * p.parts), dim3(kGradThreads),
+    if (int rc = status_of(launch_dependent(router_dxdw_kernel, dim3(nx + p.share * p.groups), dim3(kGradThreads),
                                             x.smem > w.smem ? x.smem : w.smem, s, x.tmz, x.tmw, x.tmi, w.tmz, w.tmx, x.a,
                                             w.a)))
       return rc;
@@ -677,14 +718,14 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   }
   if (!g.dW) return kOk;
   if (!one)
-    if (int rc = status_of(launch_dependent(router_dw_kernel, dim3(p.tiles * p.parts), dim3(kGradThreads), w.smem, s, w.tmz, w.tmx,
+    if (int rc = status_of(launch_dependent(router_dw_kernel, dim3(p.share * p.groups), dim3(kGradThreads), w.smem, s, w.tmz, w.tmx,
                                             w.a)))
       return rc;
-  if (p.parts == 1) return kOk;
-  int64_t grid = (n / 4 + 255) / 256;
-  if (grid > di.sm_count * 8) grid = di.sm_count * 8;
-  return status_of(launch_dependent(router_dw_sum_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, g.part, p.parts, n,
-                                    g.dW, g.add_dW));
+  if (p.direct) return kOk;
+  w.a.add = g.add_dW;
+  const int64_t threads = static_cast<int64_t>(p.cols) * p.groups * (p.N / 4) * 128;
+  return status_of(launch_dependent(router_dw_sum_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s,
+                                    reinterpret_cast<const float4*>(g.part), w.a, g.dW));
 }
 
 }  // namespace eqb
