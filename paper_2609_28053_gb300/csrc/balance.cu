@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
   int32_t* mine = hist + static_cast<int>((threadIdx.x >> 5) % copies) * E;
   for (int i = threadIdx.x; i < copies * E; i += threads) hist[i] = 0;
   griddep_wait();
+  griddep_launch();  // the pass over z may start its loads: what came before the call is complete
   const int64_t tb = static_cast<int64_t>(blockIdx.x) * tokens_per_cta;
   const int64_t te = min(tb + tokens_per_cta, a.T);
   if (tb >= te) return;

@@ -121,7 +121,10 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   if (threadIdx.x == 0) valid_n = aborted = 0;
   if (cut.cluster)
     for (int e = threadIdx.x; e < EM; e += threads) hist[e] = 0;
-  griddep_wait();
+  // The counts' kernel lets this one start once what came before the call is
+  // complete, so that z, grad_in, the mask and the offsets may be read; what it
+  // writes is waited for below.
+  if (cut.cluster) griddep_wait();
   int l = 0;
   uint32_t rank = 0;
   int64_t tb, te, len = 0;
@@ -135,8 +138,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     te = lo + len * (rank + 1) / cut.cluster;
   } else {
     tb = static_cast<int64_t>(blockIdx.x) * cut.tokens_per_cta;
-    te = min(tb + cut.tokens_per_cta, a.T);
-    if (tb >= te) return;
+    te = min(tb + cut.tokens_per_cta, a.T);  // beyond tb: the grid is cut to the tokens
     l = microbatch_of_warp(a.off, a.M, tb, lane);
   }
   // tokens are counted from tb on from here
@@ -180,6 +182,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     cluster_sync();
   }
 
+  if (!cut.cluster) griddep_wait();
   int stage = 0, waited = -1;
   uint32_t phase = 0;
   bool dead = false;  // a wait of this warp ran out
