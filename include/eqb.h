@@ -1,7 +1,9 @@
 /*
  * eqb.h -- C ABI of libeqb.so: the per-layer MoE routing-balance path of
  * Exact Quantile Balancing (EQB) and Load-Error Injection (LEI),
- * arXiv 2609.28053, on one NVIDIA GB300 (sm_103a).
+ * arXiv 2609.28053, on one NVIDIA GB300 (sm_103a), and the operators of a
+ * router's training step beside it: the balance loss with its gradient, the
+ * projection's gradients, and AdamW.
  *
  * Notation follows the paper: T tokens, E routed experts, K experts per
  * token, router logits z[T,E], expert bias b[E], cutoff tau_t = the (K+1)st
@@ -55,8 +57,8 @@ typedef enum eqb_status {
   EQB_ERR_INVALID_ARG = 1, /* host-side validation failed; nothing launched */
   EQB_ERR_UNSUPPORTED = 2, /* valid by the paper, outside the sizes the library supports */
   EQB_ERR_CUDA = 3,        /* a CUDA launch or runtime call failed */
-  EQB_ERR_NONFINITE = 4,   /* device flag: non-finite z, b or score, or a
-                              margin of magnitude >= 2^127 */
+  EQB_ERR_NONFINITE = 4,   /* device flag: non-finite z, b or score, a margin
+                              of magnitude >= 2^127, or a moment of AdamW */
   EQB_ERR_RANK = 5         /* device flag: a histogram holds fewer than r
                               margins for some expert */
 } eqb_status;

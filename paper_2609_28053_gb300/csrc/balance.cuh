@@ -480,7 +480,7 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   const bool gin = GRAD && a.grad_in;
   // Few tokens: a cluster a microbatch.  A block passes over 3,000 elements a
   // microsecond, the four launches take 17 us (M = 1, T = 8,000, E = 128 by one
-  // cluster 44 us, by four launches TIME).  The host does not know how long the
+  // cluster 44 us, by four launches 16).  The host does not know how long the
   // microbatches are: the limit is 2^15 elements a block if the longest has twice
   // the mean, and eight times that if one has all the tokens.
   BalanceCut cut;
