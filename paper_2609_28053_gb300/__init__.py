@@ -615,6 +615,7 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
 
 _data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
 _get_device, _is_contiguous = torch.Tensor.get_device, torch.Tensor.is_contiguous
+_GRAD_TYPES = {torch.float32, torch.bfloat16}
 
 
 class EqbAdamW:
@@ -646,9 +647,10 @@ class EqbAdamW:
         for i, p in enumerate(self.params):
             if not isinstance(p, torch.Tensor):
                 raise TypeError(f"params[{i}] must be a torch.Tensor")
-            if p.dtype not in (torch.float32, torch.bfloat16):
+            if p.dtype not in _GRAD_TYPES:
                 raise TypeError(f"params[{i}] must be torch.float32 or torch.bfloat16, got {p.dtype}")
-            _need(p, p.dtype, f"params[{i}]")
+            if not (p.is_cuda and p.is_contiguous()):
+                _need(p, p.dtype, f"params[{i}]")
 
         def own(given, name, shapes, dtype):
             if given is None:
@@ -659,7 +661,8 @@ class EqbAdamW:
             for i, (t, s) in enumerate(zip(given, shapes)):
                 if t is None:
                     raise TypeError(f"{name}[{i}] must be a torch.Tensor")
-                _need(t, dtype, f"{name}[{i}]", s)
+                if not (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == s and t.is_contiguous()):
+                    _need(t, dtype, f"{name}[{i}]", s)
             return given
 
         shapes = [p.shape for p in self.params]
@@ -705,25 +708,27 @@ class EqbAdamW:
         """The gradients' addresses into the table, after their checks."""
         try:  # the checks of all of them at once: hundreds of tensors take longer one by one than their step
             ptrs = list(map(_data_ptr, grads))
+            dtypes = [g.dtype for g in grads]
             fits = (list(map(_get_device, grads)) == self._device and list(map(_is_contiguous, grads)) == self._whole and
-                    list(map(_numel, grads)) == self._numels and [g.dtype for g in grads] == self._dtypes)
+                    list(map(_numel, grads)) == self._numels and (dtypes == self._dtypes or _GRAD_TYPES.issuperset(dtypes)))
         except (TypeError, AttributeError):
             fits = False
-        if fits:
-            self._grad_words[:] = memoryview(array("Q", ptrs))
-            return
-        for i, (e, g, p) in enumerate(zip(self._table, grads, self.params)):
-            if g is None:
-                e.grad = None
-                continue
-            bf16 = isinstance(g, torch.Tensor) and g.dtype is torch.bfloat16
-            _need(g, torch.bfloat16 if bf16 else torch.float32, f"grads[{i}]")
-            if g.numel() != p.numel():
-                raise ValueError(f"grads[{i}] must have shape {tuple(p.shape)} or as many elements, got {tuple(g.shape)}")
-            if g.device != p.device:
-                raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
-            e.grad, e.grad_bf16 = g.data_ptr(), bf16
-        self._dtypes = None if any(g is None for g in grads) else [g.dtype for g in grads]
+        if not fits:  # a gradient is missing, or one that is refused
+            ptrs, dtypes = [], []
+            for i, (g, p) in enumerate(zip(grads, self.params)):
+                if g is not None:
+                    _need(g, g.dtype if getattr(g, "dtype", None) in _GRAD_TYPES else torch.float32, f"grads[{i}]")
+                    if g.numel() != p.numel():
+                        raise ValueError(f"grads[{i}] must have shape {tuple(p.shape)} or as many elements, got {tuple(g.shape)}")
+                    if g.device != p.device:
+                        raise ValueError(f"grads[{i}] is on {g.device}, its parameter on {p.device}")
+                ptrs.append(0 if g is None else g.data_ptr())
+                dtypes.append(torch.float32 if g is None else g.dtype)
+        if dtypes != self._dtypes:
+            for e, t in zip(self._table, dtypes):
+                e.grad_bf16 = t is torch.bfloat16
+            self._dtypes = dtypes
+        self._grad_words[:] = memoryview(array("Q", ptrs))
 
     def step(self, grads, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, grad_scale=None, err_flag=None,
              stream=None):
