@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   int stage = 0, waited = -1;
   uint32_t phase = 0;
   bool dead = false;  // a wait of this warp ran out
-  int t = 0;
+  int t = 0, ahead = -1, ahead_valid = 0;  // the microbatch whose counts are on their way to hist
   do {
     int64_t n = len;
     int seg_end = nt;
@@ -214,11 +214,12 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
           n = 0;
           for (int q = 0; q < cut.cluster; ++q) n += peer_word(&valid_n, q);
         } else {
-          n = a.valid[l];
+          n = l == ahead ? ahead_valid : __ldcg(a.valid + l);
         }
       }
       rn = n > 0 ? __frcp_rn(static_cast<float>(n)) : 0.f;
       const float rkne = rn / static_cast<float>(a.K * E);
+      if (ahead >= 0) asm volatile("cp.async.wait_all;" ::: "memory");
       for (int e = threadIdx.x; e < EM; e += threads) {
         float r = 0.f;
         if (e < E) {
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
             for (int q = 0; q < cut.cluster; ++q) f += peer_word(hist + e, q);
             if (rank == 0) a.counts[static_cast<int64_t>(l) * E + e] = static_cast<int32_t>(f);
           } else {
-            f = __ldcg(a.counts + static_cast<int64_t>(l) * E + e);
+            f = l == ahead ? hist[e] : __ldcg(a.counts + static_cast<int64_t>(l) * E + e);
           }
           r = __ll2float_rn(f * E - a.K * n) * rkne;
         }
@@ -235,7 +236,19 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
       }
       __syncthreads();
     };
-    if constexpr (GRAD) put_r();
+    if constexpr (GRAD) {
+      put_r();
+      if (seg_end < nt && l + 1 < a.M) {
+        // The next one's counts, while this one's tokens are at work (700 sequences
+        // of 286 tokens: 71.5 us for 72.8; 470 of 9, E = 256: 47.6 for 50.3).  Each
+        // thread fetches the words that it reads itself: no barrier is needed.
+        ahead = l + 1;
+        if (mb) ahead_valid = __ldcg(a.valid + ahead);
+        for (int e = threadIdx.x; e < E; e += threads)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;"
+                       :: "r"(smem_u32(hist + e)), "l"(a.counts + static_cast<int64_t>(ahead) * E + e) : "memory");
+      }
+    }
     F2 acc[C][2];
 #pragma unroll
     for (int k = 0; k < C; ++k) acc[k][0] = acc[k][1] = f2(0.f, 0.f);
