@@ -569,15 +569,16 @@ struct DwPlan {
 // parts would cost a launch.
 constexpr int64_t kFewTokens = 1024;
 
-// Up to this many elements of x both gradients share a launch, each on a part
-// of the SMs: of two launches each has its start and its end (T = 300, d = 1,024,
-// E = 64 8.3 us for 11.5, 7,520, 1,792, 96 19 for 31, 60,000, 256, 64 26 for 50;
-// 65,536, 4,096, 128 added to 292 for 274, where the bytes decide).
+// Both gradients share a launch, each on a part of the SMs, where dx is added to,
+// and up to this many elements of x where it is written: of two launches each
+// has its start and its end, and only the shared one reads and writes all along
+// (T = 300, d = 1,024, E = 64 8.3 us for 11.5; 7,520, 1,792, 96 19 for 31; 60,000,
+// 256, 64 26 for 50; 65,536, 4,096, 128 added to 251 for 277, without it 212 for 198).
 constexpr int64_t kSharedElements = int64_t(1) << 27;
 
 // The blocks of a group, of `most`: as many for every tile if that leaves no more
 // than a tenth of them out.  Blocks that take the same tokens at the same time
-// share dz on its way (both gradients of T = 65,536, d = 4,096, E = 128: 274 us with
+// share dz on its way (T = 65,536, d = 4,096, E = 128 by two launches: 274 us with
 // 144 of 152 for dW, 285 with all of them); an uneven share fills the SMs (T =
 // 30,000, d = 1,024, E = 128, each on a part of them: 31 us for 38).
 int even_share(int most, int cols) {
@@ -683,14 +684,18 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   DxLaunch x;
   DwLaunch w;
   DwPlan p = plan_dw(g.T, g.d, g.E);
-  // SMs of dx where both share a launch.  A tile of 128 tokens x 256 columns takes
-  // an SM 2.0 us of dW and 1.5 + E / 270 of dx, 1.7 times that where it is added to
-  // (T = 32,768, d = 4,096, E = 64, 128 and 256 alone).
+  // SMs of dx where both share a launch.  What a tile of 128 tokens x 256 columns
+  // takes an SM of either side beside the other one, from the split that is
+  // fastest: 64 SMs of 152 for dW (E = 32 to 128, d = 512 to 4,096; some GPUs like 56
+  // and others 72 a little better), 48 where dx is added to, 80 and 62 above 128
+  // experts (T = 32,768, d = 4,096, E = 128 added to: 130 us with 48, 142 with 57,
+  // 149 with 64; T = 65,536, d = 2,048, E = 64: 98 to 108 with 64, 100 to 120 with 80).
   int sms = di.sm_count;
-  const bool one = g.dx && g.dW && g.T * g.d <= kSharedElements && (!p.direct || 4 * p.cols * p.groups <= 3 * di.sm_count);
+  const bool one = g.dx && g.dW && (g.add_dx || g.T * g.d <= kSharedElements) &&
+                   (!p.direct || 4 * p.cols * p.groups <= 3 * di.sm_count);
   if (one) {
     if (!p.direct) {
-      const double dx = (1.5 + g.E / 270.0) * (g.add_dx ? 1.7 : 1.0), dw = 2.0;
+      const double dx = g.add_dx ? 4.33 : 2.75, dw = p.groups == 2 ? 3.0 : 2.0;
       const int want = static_cast<int>(di.sm_count * dw / (dx + dw) / p.groups + 0.5);
       if (p.share > want) p.share = even_share(want, p.cols);
     }
