@@ -46,6 +46,9 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
       if (static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(mine + e, 1);
     };
     if (a.mask) {
+      // an entry's token, which goes on by threads / K
+      const int whole = threads / K, part = threads - whole * K;
+      int token = static_cast<int>(threadIdx.x) / K, in = static_cast<int>(threadIdx.x) - token * K;
       for (int i = threadIdx.x; i < m; i += 4 * threads) {  // four entries in flight
         int e[4];
         uint8_t ok[4];
@@ -53,7 +56,13 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
         for (int u = 0; u < 4; ++u) {
           const int j = i + u * threads;
           e[u] = j < m ? __ldcs(idx + j) : -1;
-          ok[u] = j < m ? a.mask[t + j / K] : 0;
+          ok[u] = j < m ? a.mask[t + token] : 0;
+          token += whole;
+          in += part;
+          if (in >= K) {
+            in -= K;
+            ++token;
+          }
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
