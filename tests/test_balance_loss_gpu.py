@@ -235,3 +235,36 @@ def test_long_batch_counts():
         if off[l + 1] > off[l]:
             P = p[off[l]:off[l + 1]].mean(0)
             assert torch.all((prob[l] - P).abs() <= 1e-5 * P)
+
+
+@pytest.mark.parametrize("T,E,M,score,masked,grad", [(20000, 96, 70, "sigmoid", True, True), (20000, 256, 1900, "softmax", True, True),
+                                                     (40000, 128, 5, "softmax", False, True), (300000, 128, 3, "sigmoid", True, False)])
+def test_calls_one_after_the_other_in_the_same_buffers(T, E, M, score, masked, grad):
+    """Calls of different inputs share counts and workspace with nothing between
+    them: each gives the same bits as alone."""
+    dev, sets = "cuda", []
+    for seed in (1, 2, 3):
+        z, idx, off, mask, rng = make(T, E, 6, M, seed, ragged=True)
+        mask = torch.from_numpy(rng.random(T) < 0.2 * seed + 0.2).to(dev) if masked else None
+        sets.append(dict(z=z.to(dev), idx=torch.from_numpy(idx).to(dev), off=torch.from_numpy(off).to(dev), mask=mask,
+                         grad=torch.empty(T, E, device=dev) if grad else None, prob=torch.empty(M, E, device=dev),
+                         loss=torch.empty(M, 2, device=dev)))
+    counts = torch.empty(M, E, dtype=torch.int32, device=dev)
+    ws = torch.empty(eqb.eqb_balance_loss_workspace_bytes(T, E, M), dtype=torch.uint8, device=dev)
+
+    def call(s):
+        eqb.eqb_balance_loss(s["z"], s["idx"], s["off"], 0.1, score=score, mask=s["mask"], grad_out=s["grad"], counts=counts,
+                             prob=s["prob"], loss=s["loss"], workspace=ws)
+
+    alone = []
+    for s in sets:
+        call(s)
+        torch.cuda.synchronize()
+        alone.append([None if s[k] is None else s[k].clone() for k in ("grad", "prob", "loss")])
+    for _ in range(20):
+        for s in sets:
+            call(s)
+    torch.cuda.synchronize()
+    for s, want in zip(sets, alone):
+        for k, w in zip(("grad", "prob", "loss"), want):
+            assert w is None or torch.equal(s[k], w)
