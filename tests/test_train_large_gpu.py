@@ -50,6 +50,27 @@ def test_router_grad_past_2_to_31_elements():
         assert torch.equal(dx[rows], (dz[rows].float() @ W.float()).bfloat16())
 
 
+def test_router_grad_added_past_2_to_31_elements():
+    """The same with both gradients added to: whole numbers below 2^8 in bf16 and
+    below 2^24 in fp32, so exact."""
+    T, d, E = 530_003, 4096, 32
+    dz = torch.randint(-1, 2, (T, E), device="cuda").bfloat16()
+    x, dx = (torch.empty(T, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, dx):
+        for a in range(0, T, 1 << 16):
+            t[a:a + (1 << 16)] = torch.randint(-2, 3, (min(T - a, 1 << 16), d), device="cuda", dtype=torch.int8).bfloat16()
+    W = torch.randint(-2, 3, (E, d), device="cuda").bfloat16()
+    dW = torch.randint(-100, 101, (E, d), device="cuda").float()
+    places = [slice(0, 300), slice(T // 2, T // 2 + 300), slice(T - 300, T)]
+    old, want = [dx[rows].float() for rows in places], dW.double()
+    for a in range(0, T, 1 << 16):
+        want += dz[a:a + (1 << 16)].double().t() @ x[a:a + (1 << 16)].double()
+    eqb.eqb_router_grad(dz, x, W, dx=dx, dW=dW, accumulate_dx=True, accumulate_dW=True)
+    assert torch.equal(dW.double(), want)
+    for rows, o in zip(places, old):
+        assert torch.equal(dx[rows], (o + dz[rows].float() @ W.float()).bfloat16())
+
+
 @pytest.mark.parametrize("bits", [8, 32])
 def test_adamw_past_2_to_31_elements(bits):
     """A tensor of 2^31 + 70,000 elements: its last 2^18 as a tensor of their own give the same bits."""
