@@ -275,6 +275,9 @@ __device__ __forceinline__ void dx_block(uint8_t* smem_raw, const CUtensorMap& t
           lds128(tile64 + rr * 128u + (((c2 + 1u) ^ (rr & 7u)) << 4), w[1]);
           if (row + 8 * k < a.T) store_sector(out + static_cast<int64_t>(8 * k) * a.d + c * 64, w);
         }
+        // the stage was written here by ordinary stores and is refilled by TMA:
+        // every lane orders its own before the arrival that frees the stage
+        if (a.add) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();  // the stage is read
         if (a.add) {
           if (lane == 0) mbar_arrive(oempty(stage));
