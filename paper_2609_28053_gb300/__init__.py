@@ -61,6 +61,18 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _new(shape, dtype, like, stream, make=torch.empty):
+    """A tensor that a call makes itself, on the device of `like`.  It comes from
+    the memory of the stream that the call launches on: torch hands a freed block
+    to the next request of the stream it was taken on, in that stream's order, so
+    memory of another one may still be in use when the call's kernels start, or be
+    in use again before they end."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=like.device)
+
+
 def _need(t, dtype, name, shape=None):
     # one line for a tensor that fits, the reasons below for one that does not:
     # a call checks up to ten tensors, which takes longer than its launches
@@ -106,7 +118,7 @@ def eqb_route_topk(z, b, K, mb_offsets=None, topk_idx=None, tau=None, loads=None
     _need(z, torch.bfloat16, "z")
     _need(b, torch.float32, "b", (E,))
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=z.device)
+        tau = _new(T, torch.float32, z, stream)
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     M = 0
@@ -131,7 +143,7 @@ def eqb_route_hist_fused(z, b, K, mb_offsets=None, topk_idx=None, tau=None, load
     _need(z, torch.bfloat16, "z")
     _need(b, torch.float32, "b", (E,))
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=z.device)
+        tau = _new(T, torch.float32, z, stream)
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     _need(mb_offsets, torch.int64, "mb_offsets")
@@ -202,7 +214,7 @@ def lei_coefficients(loads, mb_offsets, K, eta, c, coef=None, stream=None):
     _need(loads, torch.int32, "loads")
     _need(mb_offsets, torch.int64, "mb_offsets", (M + 1,))
     if coef is None:
-        coef = torch.empty((M, E), dtype=torch.float32, device=loads.device)
+        coef = _new((M, E), torch.float32, loads, stream)
     _need(coef, torch.float32, "coef", (M, E))
     _check(load().lei_coefficients(_p(loads), _p(mb_offsets), M, E, int(K), float(eta), float(c), _p(coef),
                                    _stream(stream)), "lei_coefficients")
@@ -236,7 +248,7 @@ def eqb_router_logits(x, W_r, z=None, err_flag=None, stream=None):
     _need(x, torch.bfloat16, "x")
     _need(W_r, torch.bfloat16, "W_r", (E, d))
     if z is None:
-        z = torch.empty((T, E), dtype=torch.bfloat16, device=x.device)
+        z = _new((T, E), torch.bfloat16, x, stream)
     _need(z, torch.bfloat16, "z", (T, E))
     _need(err_flag, torch.int32, "err_flag")
     _check(load().eqb_router_logits(_p(x), _p(W_r), T, d, E, _p(z), _p(err_flag), _stream(stream)),
@@ -256,9 +268,9 @@ def eqb_router_route(x, W_r, b, K, mb_offsets=None, z=None, topk_idx=None, tau=N
     _need(W_r, torch.bfloat16, "W_r", (E, d))
     _need(b, torch.float32, "b", (E,))
     if z is None:
-        z = torch.empty((T, E), dtype=torch.bfloat16, device=x.device)
+        z = _new((T, E), torch.bfloat16, x, stream)
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=x.device)
+        tau = _new(T, torch.float32, x, stream)
     _need(z, torch.bfloat16, "z", (T, E))
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
@@ -307,9 +319,9 @@ def eqb_rank_averaged_bias(z, tau, K, shard_offsets_host, workspace, b_out=None,
     off = np.ascontiguousarray(np.asarray(shard_offsets_host), dtype=np.int64)
     P = len(off) - 1
     if b_out is None:
-        b_out = torch.empty(E, dtype=torch.float32, device=z.device)
+        b_out = _new(E, torch.float32, z, stream)
     if q_shards is None:
-        q_shards = torch.zeros((P, E), dtype=torch.bfloat16, device=z.device)
+        q_shards = _new((P, E), torch.bfloat16, z, stream, torch.zeros)
     _need(b_out, torch.float32, "b_out", (E,))
     _need(q_shards, torch.bfloat16, "q_shards", (P, E))
     _need(workspace, torch.uint8, "workspace")
@@ -328,9 +340,9 @@ def eqb_fixed_hist_bias(z, tau, K, lo, width, workspace, b_out=None, estimate=No
     _need(z, torch.bfloat16, "z")
     _need(tau, torch.float32, "tau", (T,))
     if b_out is None:
-        b_out = torch.empty(E, dtype=torch.float32, device=z.device)
+        b_out = _new(E, torch.float32, z, stream)
     if estimate is None:
-        estimate = torch.empty(E, dtype=torch.float64, device=z.device)
+        estimate = _new(E, torch.float64, z, stream)
     _need(b_out, torch.float32, "b_out", (E,))
     _need(estimate, torch.float64, "estimate", (E,))
     _need(workspace, torch.uint8, "workspace")
@@ -357,7 +369,7 @@ def eqb_maxvio(loads, mb_offsets, K, out=None, per_mb=None, stream=None):
     _need(loads, torch.int32, "loads")
     _need(mb_offsets, torch.int64, "mb_offsets", (M + 1,))
     if out is None:
-        out = torch.empty(2, dtype=torch.float64, device=loads.device)
+        out = _new(2, torch.float64, loads, stream)
     _need(out, torch.float64, "out", (2,))
     _need(per_mb, torch.float64, "per_mb", (M,) if per_mb is not None else None)
     _check(load().eqb_maxvio(_p(loads), _p(mb_offsets), M, E, K, _p(out), _p(per_mb), _stream(stream)),
@@ -385,7 +397,7 @@ def eqb_layer_step(z, b, K, mb_offsets, loads, b_next, workspace, tau=None, topk
     _need(b_next, torch.float32, "b_next", (E,))
     _need(workspace, torch.uint8, "workspace")
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=z.device)
+        tau = _new(T, torch.float32, z, stream)
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     _need(grad_s, torch.float32, "grad_s", (T, E) if grad_s is not None else None)
@@ -422,9 +434,9 @@ def eqb_router_layer_step(x, W_r, b, K, mb_offsets, loads, b_next, workspace, z=
     _need(b_next, torch.float32, "b_next", (E,))
     _need(workspace, torch.uint8, "workspace")
     if z is None:
-        z = torch.empty((T, E), dtype=torch.bfloat16, device=x.device)
+        z = _new((T, E), torch.bfloat16, x, stream)
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=x.device)
+        tau = _new(T, torch.float32, x, stream)
     _need(z, torch.bfloat16, "z", (T, E))
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
@@ -463,7 +475,7 @@ def eqb_layer_step_noalloc(z, b, K, mb_offsets, loads, b_next, tau=None, topk_id
     _need(loads, torch.int32, "loads", (M, E))
     _need(b_next, torch.float32, "b_next", (E,))
     if tau is None:
-        tau = torch.empty(T, dtype=torch.float32, device=z.device)
+        tau = _new(T, torch.float32, z, stream)
     _need(tau, torch.float32, "tau", (T,))
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     _need(grad_s, torch.float32, "grad_s", (T, E) if grad_s is not None else None)
@@ -558,17 +570,17 @@ def eqb_balance_loss(z, topk_idx, mb_offsets, alpha, zeta=0.0, score="softmax", 
     if grad_scale is not None:
         _need(grad_scale, torch.float32, "grad_scale", (1,))
     if counts is None:
-        counts = torch.empty((M, E), dtype=torch.int32, device=z.device)
+        counts = _new((M, E), torch.int32, z, stream)
     else:
         _need(counts, torch.int32, "counts", (M, E))
     if loss is None:
-        loss = torch.empty((M, 2), dtype=torch.float32, device=z.device)
+        loss = _new((M, 2), torch.float32, z, stream)
     else:
         _need(loss, torch.float32, "loss", (M, 2))
     if prob is not None:
         _need(prob, torch.float32, "prob", (M, E))
     if workspace is None:
-        workspace = torch.empty(eqb_balance_loss_workspace_bytes(T, E, M), dtype=torch.uint8, device=z.device)
+        workspace = _new(eqb_balance_loss_workspace_bytes(T, E, M), torch.uint8, z, stream)
     else:
         _need(workspace, torch.uint8, "workspace")
     if err_flag is not None:
@@ -603,7 +615,7 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
         _need(workspace, torch.uint8, "workspace")
     elif dW is not None:
         need = eqb_router_grad_workspace_bytes(T, d, E)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dz.device) if need else None
+        workspace = _new(need, torch.uint8, dz, stream) if need else None
     if err_flag is not None:
         _need(err_flag, torch.int32, "err_flag")
     rc = load().eqb_router_grad(dz.data_ptr(), x.data_ptr(), W_r.data_ptr(), T, d, E, _p(dx), bool(accumulate_dx), _p(dW),
