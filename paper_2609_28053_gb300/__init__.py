@@ -553,6 +553,7 @@ def eqb_balance_loss(z, topk_idx, mb_offsets, alpha, zeta=0.0, score="softmax", 
     T, E = z.shape
     fp32 = z.dtype is torch.float32
     _need(z, torch.float32 if fp32 else torch.bfloat16, "z")
+    _on_current_device(z, "z")
     K = topk_idx.shape[1] if topk_idx.dim() == 2 else 0
     _need(topk_idx, torch.int32, "topk_idx", (T, K))
     _need(mb_offsets, torch.int64, "mb_offsets")
@@ -605,6 +606,7 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
     T, E = dz.shape
     d = W_r.shape[1]
     _need(dz, torch.bfloat16, "dz")
+    _on_current_device(dz, "dz")
     _need(x, torch.bfloat16, "x", (T, d))
     _need(W_r, torch.bfloat16, "W_r", (E, d))
     if dx is not None:
@@ -752,6 +754,8 @@ class EqbAdamW:
             raise ValueError(f"grads must have {len(self.params)} entries, got {len(grads)}")
         if list(map(_data_ptr, self.params)) != self._ptrs:
             raise ValueError("a parameter has moved to another storage: make a new EqbAdamW")
+        if self.params:
+            _on_current_device(self.params[0], "params[0]")
         self._point_to(grads)
         _need(grad_scale, torch.float32, "grad_scale", (1,))
         _need(err_flag, torch.int32, "err_flag")
