@@ -25,6 +25,7 @@ import ctypes
 from array import array
 
 import torch
+from torch.autograd.graph import increment_version
 
 from ._lib import STATUS, AdamwTensor, EqbError, load
 
@@ -702,6 +703,9 @@ class EqbAdamW:
             raise ValueError("all tensors must be on one device")
         # aliases: what the table points to stays allocated whatever becomes of the tensors above
         self._held = [t.detach() for t in self.params + states]
+        # one tensor for every version counter: views share their base's
+        base = [t if t._base is None else t._base for t in self.params + self.copies if t is not None]
+        self._written = list({id(t): t for t in base}.values())
         self._ptrs = [p.data_ptr() for p in self.params]
         self._numels = [p.numel() for p in self.params]
         self._device = [p.get_device() for p in self.params]
@@ -719,7 +723,7 @@ class EqbAdamW:
             e.copy = _p(self.copies[i])
 
     def _point_to(self, grads):
-        """The gradients' addresses into the table, after their checks."""
+        """The gradients' addresses into the table, after their checks; whether none is missing."""
         try:  # the checks of all of them at once: hundreds of tensors take longer one by one than their step
             ptrs = list(map(_data_ptr, grads))
             dtypes = [g.dtype for g in grads]
@@ -743,6 +747,7 @@ class EqbAdamW:
                 e.grad_bf16 = t is torch.bfloat16
             self._dtypes = dtypes
         self._grad_words[:] = memoryview(array("Q", ptrs))
+        return fits
 
     def step(self, grads, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, grad_scale=None, err_flag=None,
              stream=None):
@@ -756,9 +761,13 @@ class EqbAdamW:
             raise ValueError("a parameter has moved to another storage: make a new EqbAdamW")
         if self.params:
             _on_current_device(self.params[0], "params[0]")
-        self._point_to(grads)
+        all_given = self._point_to(grads)
         _need(grad_scale, torch.float32, "grad_scale", (1,))
         _need(err_flag, torch.int32, "err_flag")
-        _check(load().eqb_adamw_step(self._table, len(self.params), self.state_bits, float(lr), int(step), float(beta1),
-                                     float(beta2), float(eps), float(weight_decay), _p(grad_scale), _p(err_flag),
-                                     _stream(stream)), "eqb_adamw_step")
+        rc = load().eqb_adamw_step(self._table, len(self.params), self.state_bits, float(lr), int(step), float(beta1),
+                                   float(beta2), float(eps), float(weight_decay), _p(grad_scale), _p(err_flag),
+                                   _stream(stream))
+        # autograd has to know that values it may have saved are gone
+        increment_version(self._written if all_given else [
+            t for p, c, g in zip(self.params, self.copies, grads) if g is not None for t in (p, c) if t is not None])
+        _check(rc, "eqb_adamw_step")
