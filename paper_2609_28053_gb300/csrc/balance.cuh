@@ -364,7 +364,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
           d += __shfl_xor_sync(kFull, d, m);
           if constexpr (GRAD) h += __shfl_xor_sync(kFull, h, m);
         }
-        if (alive && !(d < INFINITY)) raise_flag(a.err, kErrNonfinite);
+        // of a row without a finite logit too: the maxima drop NaN, and a row that
+        // is NaN throughout looks closed, but only a closed one has a sum of 0
+        if (ok && !(d < INFINITY)) raise_flag(a.err, kErrNonfinite);
         float id = rcp_approx(d);
         id = alive ? __fmaf_rn(id, __fmaf_rn(-d, id, 1.0f), id) : 0.f;
         h *= id;
