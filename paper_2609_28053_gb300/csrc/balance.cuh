@@ -317,15 +317,30 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         // sigmoids are taken relative to e^top where all are far below 0.5:
         // s e^-top = 1 / (e^top + e^(top - z))
         const float ref = !(top > -INFINITY) ? 0.f : SIG ? fminf(top, 0.f) : top;
-        const float m2 = ref * kLog2e;
-        const F2 mul = splat2(SIG ? -kLog2e : kLog2e), shift = splat2(SIG ? m2 : -m2);
+        const F2 mul = splat2(SIG ? -kLog2e : kLog2e);
+        float m2 = ref * kLog2e;
         const float em = SIG ? ex2_approx(m2) : 0.f;
         const F2 em2 = splat2(em);
+        // The power's argument is z log2(e) less m2, and m2's rounding scales all of a
+        // row alike.  Far from zero (rows closed by the type's lowest value, say) it
+        // would be off by whole powers of two, or infinite: there the reference is
+        // taken off z itself.
+        const bool wide = fabsf(ref) > 0x1p20f;
         // one reciprocal serves two sigmoids as long as the product of the two
         // denominators is finite; beyond 2^60 of the row's reference (-inf
         // among them) a sigmoid counts as zero.  Most rows are nearer than that.
         constexpr float kFar = 0x1p60f;
-        const bool far = SIG && __any_sync(kFull, low < ref - 40.f);
+        const bool rare = __any_sync(kFull, wide || (SIG && low < ref - 40.f)), far = SIG && rare;
+        if (rare && __any_sync(kFull, wide)) {
+          const F2 off = splat2(wide ? ref : 0.f);
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            e[k][0] = sub2(e[k][0], off);
+            e[k][1] = sub2(e[k][1], off);
+          }
+          if (wide) m2 = 0.f;
+        }
+        const F2 shift = splat2(SIG ? m2 : -m2);
         auto sigmoids = [&](auto FAR, F2 x) {
           const F2 xc = FAR ? f2(fmin_nan(lo2(x), kFar), fmin_nan(hi2(x), kFar)) : x;
           const F2 y = add2(em2, xc);
