@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kCountThreads) balance_count_kernel(BalanceArg
 template <int W>
 __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, uint32_t tokens_per_cta) {
   __shared__ float col[W][32];
-  __shared__ double tot[W][3];
+  __shared__ double tot[W][2];
   griddep_wait();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   for (int l = blockIdx.y; l < a.M; l += gridDim.y) {
@@ -131,17 +131,17 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
       }
     if (W > 1) col[wid][lane] = (v[0] + v[1]) + (v[2] + v[3]);
     const bool sums = blockIdx.x == 0 && a.loss;
-    double t3[3] = {0.0, 0.0, 0.0};
+    double t2[2] = {0.0, 0.0};
     if (sums) {
       for (int q = threadIdx.x; q < rows; q += 32 * W) {
-        const float4 w = __ldcg(reinterpret_cast<const float4*>(p + static_cast<int64_t>(q) * a.row));
-        t3[0] += w.x; t3[1] += w.y; t3[2] += w.z;
+        const float2 w = __ldcg(reinterpret_cast<const float2*>(p + static_cast<int64_t>(q) * a.row));
+        t2[0] += w.x; t2[1] += w.y;
       }
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) t3[i] += __shfl_xor_sync(kFull, t3[i], m);
-        if (lane == 0) tot[wid][i] = t3[i];
+        for (int m = 1; m < 32; m <<= 1) t2[i] += __shfl_xor_sync(kFull, t2[i], m);
+        if (lane == 0) tot[wid][i] = t2[i];
       }
     }
     __syncthreads();
@@ -152,15 +152,14 @@ __global__ void __launch_bounds__(32 * W) balance_finish_kernel(BalanceArgs a, u
       a.prob[static_cast<int64_t>(l) * a.E + e] = n > 0 ? x / static_cast<float>(n) : 0.f;
     }
     if (sums && threadIdx.x == 0) {
-      double h = 0.0, zz = 0.0, alive = 0.0;
+      double h = 0.0, zz = 0.0;
 #pragma unroll
       for (int q = 0; q < W; ++q) {
         h += tot[q][0];
         zz += tot[q][1];
-        alive += tot[q][2];
       }
       const float n1 = static_cast<float>(n);
-      a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * (static_cast<float>(h + alive * (1.0 / a.E)) / n1) : 0.f;
+      a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * (static_cast<float>(h) / n1) : 0.f;
       a.loss[2 * l + 1] = n > 0 ? static_cast<float>(a.zeta) * (static_cast<float>(zz) / n1) : 0.f;
     }
     __syncthreads();

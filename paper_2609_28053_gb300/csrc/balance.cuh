@@ -9,10 +9,11 @@
 // F a constant.  The counts come from the lists alone (4 K bytes a token), so
 // once they are there a single pass over z gives the loss and the gradient.
 // R_e = F_e - 1/E takes the place of F_e: p.F = p.R + 1/E, and R is formed from
-// an exact whole number, so that balanced counts give exactly 0.  The loss takes
-// the sum of p.R from the sums of p.  Without a gradient nothing else needs R,
-// and the pass runs beside the kernel that counts (T = 524,288, E = 128, sigmoid:
-// 51.4 us the call, 58.8 with p.R token by token behind the counts).
+// an exact whole number, so that balanced counts give exactly 0.  The loss is the
+// sum of p by F itself, from the sums of p: p.R + 1/E would cancel where the lists
+// name experts of little probability.  Without a gradient nothing else needs the
+// counts, and the pass runs beside the kernel that forms them (T = 524,288, E = 128,
+// sigmoid: 51.4 us the call, 58.8 with a product token by token behind the counts).
 //
 // The pass is a stream.  Rows lie one after the other, so each warp fetches its
 // groups of up to 32 tokens (z and grad_in) by bulk copies into a ring of its
@@ -66,9 +67,11 @@ constexpr int bal_blocks(bool grad, int C) { return C <= 3 || (C == 4 && !grad) 
 // rounds where a row each would take much of it.
 __host__ __device__ constexpr int bal_rows(int EM, int warps) { return EM <= 256 || warps < 2 ? warps : 2; }
 
-// Shared memory: R [EM], a cluster's counts [EM], the warps' column sums
-// [bal_rows, EM], the rings.
-__host__ __device__ constexpr int bal_fixed_bytes(int EM, int warps) { return 4 * EM * (2 + bal_rows(EM, warps)); }
+// Shared memory: F [EM], a cluster's counts [EM], with a gradient R [EM], the
+// warps' column sums [bal_rows, EM], the rings.
+__host__ __device__ constexpr int bal_fixed_bytes(int EM, int warps, bool grad) {
+  return 4 * EM * (2 + grad + bal_rows(EM, warps));
+}
 __host__ __device__ constexpr int bal_stage_bytes(int E, int group, bool f32, bool gin) {
   return group * E * ((f32 ? 4 : 2) + (gin ? 4 : 0));
 }
@@ -100,13 +103,14 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   // E = 256 takes 1,037 us where it took 665 (E = 128's value 69 with, 74 without)
   constexpr int SURE = GRAD && C > 4 ? 0 : CMIN;
   extern __shared__ __align__(128) uint8_t sm[];
-  __shared__ float sums[kBalWarps][3];
+  __shared__ float sums[kBalWarps][2];
   __shared__ __align__(8) uint64_t bars[kBalWarps * kBalMaxStages];
-  __shared__ float tot[3];
+  __shared__ float tot[2];
   __shared__ int valid_n, aborted;
-  float* Rs = reinterpret_cast<float*>(sm);
-  int* hist = reinterpret_cast<int*>(Rs + EM);
-  float* colsum = Rs + 2 * EM;
+  float* Fs = reinterpret_cast<float*>(sm);
+  int* hist = reinterpret_cast<int*>(Fs + EM);
+  float* Rs = Fs + 2 * EM;  // with a gradient
+  float* colsum = Fs + (GRAD ? 3 : 2) * EM;
   const int E = a.E, nch = E >> 2, G = cut.group, D = cut.stages;
   const int threads = static_cast<int>(blockDim.x), warps = threads >> 5;  // 8, or fewer for short microbatches
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -114,7 +118,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
   const bool gin = GRAD && a.grad_in;
   const uint32_t zrow = static_cast<uint32_t>(E) * (F32 ? 4u : 2u), grow = gin ? static_cast<uint32_t>(E) * 4u : 0u;
   const uint32_t stage_bytes = static_cast<uint32_t>(G) * (zrow + grow);
-  uint8_t* ring = sm + bal_fixed_bytes(EM, warps) + static_cast<size_t>(wid) * D * stage_bytes;
+  uint8_t* ring = sm + bal_fixed_bytes(EM, warps, GRAD) + static_cast<size_t>(wid) * D * stage_bytes;
   const uint32_t ring_s = smem_u32(ring), bar0 = smem_u32(bars + wid * kBalMaxStages);
   if (lane == 0) {
     for (int s = 0; s < D; ++s) mbar_init(bar0 + 8u * s, 1);
@@ -126,7 +130,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     for (int e = threadIdx.x; e < EM; e += threads) hist[e] = 0;
   // The counts' kernel lets this one start once what came before the call is
   // complete, so that z, grad_in, the mask and the offsets may be read; what it
-  // writes is waited for below, before R is formed.
+  // writes is waited for below, before F is formed.
   if (cut.cluster) griddep_wait();
   int l = 0;
   uint32_t rank = 0;
@@ -203,12 +207,12 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
       }
       if (hi > tb + t && hi < te) seg_end = static_cast<int>(hi - tb);
       n = hi - lo;
-      // the previous microbatch is done with R: its sums' barrier says so, if it has sums
+      // the previous microbatch is done with F and R: its sums' barrier says so, if it has sums
       if (GRAD && !a.part) __syncthreads();
     }
-    // n and R of this microbatch, from an exact whole number, so that balanced counts give 0
+    // n, F and R of this microbatch, R from an exact whole number, so that balanced counts give 0
     float rn;
-    auto put_r = [&]() {
+    auto put_f = [&]() {
       if (mb) {
         if (cut.cluster) {
           n = 0;
@@ -218,26 +222,25 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         }
       }
       rn = n > 0 ? __frcp_rn(static_cast<float>(n)) : 0.f;
-      const float rkne = rn / static_cast<float>(a.K * E);
+      const float rkn = rn / static_cast<float>(a.K), rkne = rn / static_cast<float>(a.K * E);
       if (ahead >= 0) asm volatile("cp.async.wait_all;" ::: "memory");
       for (int e = threadIdx.x; e < EM; e += threads) {
-        float r = 0.f;
+        int64_t f = 0;
         if (e < E) {
-          int64_t f = 0;
           if (cut.cluster) {
             for (int q = 0; q < cut.cluster; ++q) f += peer_word(hist + e, q);
             if (rank == 0) a.counts[static_cast<int64_t>(l) * E + e] = static_cast<int32_t>(f);
           } else {
             f = l == ahead ? hist[e] : __ldcg(a.counts + static_cast<int64_t>(l) * E + e);
           }
-          r = __ll2float_rn(f * E - a.K * n) * rkne;
         }
-        Rs[e] = r;
+        Fs[e] = __ll2float_rn(f) * rkn;
+        if constexpr (GRAD) Rs[e] = e < E ? __ll2float_rn(f * E - a.K * n) * rkne : 0.f;
       }
       __syncthreads();
     };
     if constexpr (GRAD) {
-      put_r();
+      put_f();
       if (seg_end < nt && l + 1 < a.M) {
         // The next one's counts, while this one's tokens are at work (700 sequences
         // of 286 tokens: 71.5 us for 72.8; 470 of 9, E = 256: 47.6 for 50.3).  Each
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
     for (int k = 0; k < C; ++k) acc[k][0] = acc[k][1] = f2(0.f, 0.f);
     const float ca = GRAD ? gs * (static_cast<float>(a.alpha) * rn) : 0.f;
     const float cz = GRAD ? gs * (2.0f * static_cast<float>(a.zeta) * rn) : 0.f;
-    float zsum = 0.f, alive_n = 0.f;
+    float zsum = 0.f;
 
     while (g0 < seg_end && !dead) {
       if (waited != g0) {
@@ -387,10 +390,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         h *= id;
         float lse = 0.f;
         if (!SIG && a.zeta != 0.0) lse = alive ? __fmaf_rn(lg2_approx(d), kLn2, top) : 0.f;
-        if (sub == 0) {
-          zsum = __fmaf_rn(lse, lse, zsum);
-          alive_n += alive ? 1.f : 0.f;
-        }
+        if (sub == 0) zsum = __fmaf_rn(lse, lse, zsum);
         const F2 id2 = splat2(id);
         if constexpr (!GRAD) {
 #pragma unroll
@@ -442,17 +442,16 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
       if (++stage == D) { stage = 0; phase ^= 1u; }
     }
 
-    // Without a gradient p.R is wanted of the sums alone, and R, for which the
-    // counts have to be there, only now.
+    // Without a gradient F, for which the counts have to be there, is wanted only now.
     if constexpr (!GRAD) {
       if (!cut.cluster) griddep_wait();
-      put_r();
+      put_f();
     }
     // the block's sums of this microbatch
     if (a.part || cut.cluster) {
       float* row = a.part + (static_cast<int64_t>(blockIdx.x) + l) * a.row;  // not used by a cluster
       const int ROWS = bal_rows(EM, warps);
-      float hsum = 0.f;  // of p.R: the warp's sums of p by R
+      float hsum = 0.f;  // of p.F: the warp's sums of p by F
       for (int round = 0; round < warps / ROWS; ++round) {
         if (round) __syncthreads();
         if (wid / ROWS != round) continue;
@@ -460,8 +459,8 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         for (int k = 0; k < C; ++k) {
           float4 v = make_float4(sum_slots(lo2(acc[k][0]), LPT), sum_slots(hi2(acc[k][0]), LPT),
                                  sum_slots(lo2(acc[k][1]), LPT), sum_slots(hi2(acc[k][1]), LPT));
-          const float4 rw = reinterpret_cast<const float4*>(Rs)[sub + k * LPT];
-          hsum += __fmaf_rn(v.x, rw.x, v.y * rw.y) + __fmaf_rn(v.z, rw.z, v.w * rw.w);
+          const float4 fw = reinterpret_cast<const float4*>(Fs)[sub + k * LPT];
+          hsum += __fmaf_rn(v.x, fw.x, v.y * fw.y) + __fmaf_rn(v.z, fw.z, v.w * fw.w);
           float4* col = reinterpret_cast<float4*>(colsum + wid % ROWS * EM) + sub + k * LPT;
           if (round) {
             const float4 w = *col;
@@ -474,11 +473,9 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
 #pragma unroll
       for (int m = 1; m < LPT; m <<= 1) hsum += __shfl_xor_sync(kFull, hsum, m);
       zsum = sum_slots(zsum, 1);
-      alive_n = sum_slots(alive_n, 1);
       if (lane == 0) {
         sums[wid][0] = hsum;
         sums[wid][1] = zsum;
-        sums[wid][2] = alive_n;
       }
       __syncthreads();
       for (int e = threadIdx.x; e < E; e += threads) {
@@ -487,7 +484,7 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
         if (cut.cluster) colsum[e] = v;
         else row[4 + e] = v;
       }
-      if (threadIdx.x < 3) {
+      if (threadIdx.x < 2) {
         float v = 0.f;
         for (int q = 0; q < warps; ++q) v += sums[q][threadIdx.x];
         if (cut.cluster) tot[threadIdx.x] = v;
@@ -504,11 +501,11 @@ __global__ void __launch_bounds__(kBalThreads, bal_blocks(GRAD, C)) balance_kern
           a.prob[static_cast<int64_t>(l) * E + e] = n > 0 ? v / n1 : 0.f;
         }
       if (a.loss && rank == 0 && threadIdx.x == 0) {
-        float v[3] = {0.f, 0.f, 0.f};
+        float v[2] = {0.f, 0.f};
         for (int q = 0; q < cut.cluster; ++q)
 #pragma unroll
-          for (int i = 0; i < 3; ++i) v[i] += peer_float(tot + i, q);
-        a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * ((v[0] + v[2] / static_cast<float>(E)) / n1) : 0.f;
+          for (int i = 0; i < 2; ++i) v[i] += peer_float(tot + i, q);
+        a.loss[2 * l] = n > 0 ? static_cast<float>(a.alpha) * (v[0] / n1) : 0.f;
         a.loss[2 * l + 1] = n > 0 ? static_cast<float>(a.zeta) * (v[1] / n1) : 0.f;
       }
       cluster_sync();  // no block leaves while another reads its sums
@@ -551,7 +548,7 @@ int launch_bal(const BalanceArgs& a, BalanceRun* run, cudaStream_t s) {
   const int stage1 = bal_stage_bytes(a.E, TPW, F32, gin);
   // one SM's memory over its blocks, 1 KB of each reserved and about 0.5 KB static
   int blocks = bal_blocks(GRAD, C) * kBalWarps / warps;
-  const int fixed = bal_fixed_bytes(EM, warps), two = fixed + 2 * warps * stage1 + 2048;
+  const int fixed = bal_fixed_bytes(EM, warps, GRAD), two = fixed + 2 * warps * stage1 + 2048;
   if (warps < kBalWarps && blocks > di.max_smem_optin / two) blocks = di.max_smem_optin / two;
   const int room = di.max_smem_optin / blocks - 2048 - fixed;
   int64_t grid;

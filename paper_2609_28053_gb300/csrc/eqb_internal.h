@@ -227,7 +227,7 @@ struct BalanceArgs {
   int32_t* counts;
   float* prob;  // nullable
   float* loss;  // nullable
-  float* part;  // rows of a block's sums (loss or prob): sum of p.R, of lse^2, rows alive, unused, then E of p
+  float* part;  // rows of a block's sums (loss or prob): sum of p.F, of lse^2, two unused, then E of p
   int row;      // floats in a row: E + 4
   int32_t* valid;  // [M]: valid tokens (mask)
   int32_t* err;
