@@ -520,6 +520,8 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  *              entry with n = 0 or grad = NULL is left as it is.  Tensors must
  *              not overlap.  Any element alignment; arrays aligned to 16
  *              bytes are the fast path.
+ *   eps        a normal number in fp32 (2^-126 <= eps < 2^128): where a gradient
+ *              has been 0 so far it is all of the denominator
  *   grad_scale device fp32 [1] (nullable: 1): a clipping factor or the inverse
  *              of a loss scale, formed on the device
  *   err_flag   EQB_ERR_NONFINITE if a moment became non-finite (a gradient

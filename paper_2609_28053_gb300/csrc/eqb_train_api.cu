@@ -79,8 +79,10 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t count, int32_
                           int32_t* err_flag, void* stream) {
   if (count < 0 || (count > 0 && !tensors) || (state_bits != 8 && state_bits != 32)) return EQB_ERR_INVALID_ARG;
   if (!(lr >= 0.0) || !isfinite(lr) || step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-      !(eps > 0.0) || !isfinite(eps) || !(weight_decay >= 0.0) || !isfinite(weight_decay))
+      !(weight_decay >= 0.0) || !isfinite(weight_decay))
     return EQB_ERR_INVALID_ARG;
+  // eps alone is the denominator where m = v = 0: it has to be a normal number in fp32
+  if (!isnormal(static_cast<float>(eps)) || !(eps > 0.0)) return EQB_ERR_INVALID_ARG;
   if (!aligned(grad_scale, 4) || !aligned(err_flag, 4)) return EQB_ERR_INVALID_ARG;
   const bool bits8 = state_bits == 8;
   for (int32_t i = 0; i < count; ++i) {
