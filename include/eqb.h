@@ -447,6 +447,7 @@ eqb_status eqb_router_layer_step(const eqb_bf16 *x, const eqb_bf16 *W_r, int64_t
  *   topk_idx   device int32 [T,K], e.g. from eqb_route_topk
  *   mask       device uint8 [T] (nullable)
  *   score      0 softmax, 1 normalised sigmoid (zeta must then be 0)
+ *   alpha, zeta  any sign; alpha and 2 zeta finite in fp32
  *   grad_in    device fp32 [T,E], 16-byte aligned (nullable)
  *   grad_out   device fp32 [T,E], or bf16 with grad_out_bf16 != 0 (rounded to
  *              nearest even: the operand of eqb_router_grad); 16-byte aligned
@@ -520,6 +521,8 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  *              entry with n = 0 or grad = NULL is left as it is.  Tensors must
  *              not overlap.  Any element alignment; arrays aligned to 16
  *              bytes are the fast path.
+ *   lr, weight_decay  not negative; lr / (1 - beta1^step) and 1 - lr weight_decay
+ *              finite in fp32
  *   eps        a normal number in fp32 (2^-126 <= eps < 2^128): where a gradient
  *              has been 0 so far it is all of the denominator
  *   grad_scale device fp32 [1] (nullable: 1): a clipping factor or the inverse

@@ -32,7 +32,9 @@ eqb_status eqb_balance_loss(const void* z, int32_t z_fp32, const int32_t* topk_i
                             size_t workspace_bytes, int32_t* err_flag, void* stream) {
   eqb_status st = check_shape(T, E, K, true);
   if (st != EQB_OK) return st;
-  if (M < 1 || score < 0 || score > 1 || !isfinite(alpha) || !isfinite(zeta) || (score == 1 && zeta != 0.0))
+  // the factors are used in fp32: infinite there, they would turn a zero into NaN
+  if (M < 1 || score < 0 || score > 1 || !isfinite(static_cast<float>(alpha)) || !isfinite(2.0f * static_cast<float>(zeta)) ||
+      (score == 1 && zeta != 0.0))
     return EQB_ERR_INVALID_ARG;
   if (M > (1 << 20)) return EQB_ERR_UNSUPPORTED;
   if (!mb_offsets || !counts) return EQB_ERR_INVALID_ARG;
@@ -105,6 +107,7 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor* tensors, int32_t count, int32_
   sc.eps = static_cast<float>(eps);
   sc.decay = static_cast<float>(1.0 - lr * weight_decay);
   sc.step = static_cast<float>(lr / (1.0 - pow(beta1, static_cast<double>(step))));
+  if (!isfinite(sc.decay) || !isfinite(sc.step)) return EQB_ERR_INVALID_ARG;
   sc.grad_scale = grad_scale;
   sc.err = err_flag;
   constexpr int kBatch = eqb::kAdamwBatch;
