@@ -516,6 +516,12 @@ eqb_status eqb_router_grad(const eqb_bf16 *dz, const eqb_bf16 *x, const eqb_bf16
  *   largest magnitude / 448, rounded to nearest even; a root that is not zero
  *   is not rounded to zero.  avg_scale, sq_scale: fp32 [ceil(n / 256)].  A block
  *   whose scale would be below 2^-126 is stored as zeros.
+ *   Meant for beta2 up to 0.95: three places of mantissa cannot move a root by
+ *   less than 3 to 6 % of itself against its block's scale.  Over thousands of
+ *   steps of random gradients roots then scatter by 6 to 9 % around the true ones
+ *   and stand up to 7 % above them; at 0.98 and 0.99 up to 60 and 35 % above, at
+ *   0.999 they scatter by 15 to 24 %.  Decay alone moves the scale, not the codes: a
+ *   root without gradients in a block that has some stays in step with that scale.
  * Zeroed states (and scales) are those of a first step.
  *   tensors    host array [count]; read before the call returns.  n >= 0; an
  *              entry with n = 0 or grad = NULL is left as it is.  Tensors must

@@ -640,7 +640,8 @@ class EqbAdamW:
     params  fp32 or bf16 tensors, contiguous, on one GPU
     state_bits  32: exp_avg, exp_avg_sq fp32.  8: exp_avg (m) and exp_avg_sq
             (the root of the second moment) torch.float8_e4m3fn, with an fp32
-            scale for every 256 elements in avg_scale and sq_scale.
+            scale for every 256 elements in avg_scale and sq_scale; for
+            beta2 up to 0.95 (eqb.h says what becomes of larger ones).
     exp_avg, exp_avg_sq, avg_scale, sq_scale  lists of tensors to keep the
             states in (continued from a checkpoint, say); zeros when not given
     copies  bf16 tensors (or None) that receive the new value of the fp32
