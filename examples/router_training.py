@@ -5,9 +5,14 @@ Each step projects the tokens (eqb_router_logits), routes them
 microbatch (eqb_balance_loss, the gradient in bf16), takes that gradient back
 to the router's weight and input (eqb_router_grad, accumulated over the
 microbatches of the step), and updates the fp32 master weight and the bf16 copy
-that the projection reads (EqbAdamW).  In a model, grad_in holds the score
-gradients of the experts' path, and dx is added to the gradient of the layer's
-input; here grad_in is zero and dx is only formed.
+that the projection reads (EqbAdamW).
+
+In a model the experts' path gives a gradient too, and dx is added to the gradient
+of the layer's input.  The score gradients are dL/ds, s = sigmoid(z), and LEI
+(lei_inject_grad) adds to dL/ds; the balance loss adds to dL/dz.  So they are taken
+through the sigmoid, dL/dz = dL/ds s (1 - s), before they become grad_in: step()
+does so with the grad_s that it is given.  main() trains on the loss alone, with
+grad_in zero, and dx is only formed.
 
 The tokens have a common component, as hidden states do, so a random router
 sends most of them to a few experts; the loss spreads them.
@@ -28,10 +33,10 @@ class RouterTrainer:
     """One router W_r [E, d] with its optimizer and the buffers of a step of
     `accumulate` passes over T tokens in M microbatches each."""
 
-    def __init__(self, T, d, E, K, M, accumulate=2, alpha=0.02, zeta=1e-4, lr=2e-3, state_bits=32, seed=0):
+    def __init__(self, T, d, E, K, M, accumulate=2, alpha=0.02, zeta=1e-4, lr=2e-3, state_bits=32, seed=0, eta=0.0, c=1.0):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.T, self.d, self.E, self.K, self.M, self.accumulate = T, d, E, K, M, accumulate
-        self.alpha, self.zeta, self.lr = alpha, zeta, lr
+        self.alpha, self.zeta, self.lr, self.eta, self.c = alpha, zeta, lr, eta, c
         self.master = torch.randn(E, d, generator=g, device="cuda") * d ** -0.5
         self.W_r = self.master.bfloat16()
         self.opt = eqb.EqbAdamW([self.master], state_bits=state_bits, copies=[self.W_r])
@@ -46,6 +51,7 @@ class RouterTrainer:
         # the losses of the step's microbatches are averaged
         self.scale = torch.full((1,), 1.0 / (accumulate * M), device="cuda")
         self.tau = torch.empty(T, device="cuda")
+        self.loads = torch.empty(M, E, dtype=torch.int32, device="cuda")
         self.counts = torch.empty(M, E, dtype=torch.int32, device="cuda")
         self.loss = torch.empty(M, 2, device="cuda")
         self.err = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -53,13 +59,21 @@ class RouterTrainer:
         self.ws_grad = torch.empty(eqb.eqb_router_grad_workspace_bytes(T, d, E), dtype=torch.uint8, device="cuda")
         self.steps = 0
 
-    def step(self, batches):
+    def step(self, batches, grad_s=None):
         """One optimizer step over `accumulate` batches x [T, d]; the mean
-        balance loss and the last batch's [Global, Local] MaxVio, on the device."""
+        balance loss and the last batch's [Global, Local] MaxVio, on the device.
+        grad_s: the experts' path's dL/ds of every batch, fp32 [T, E], which LEI
+        is added to (in place) with eta."""
         total = 0.0
         for i, x in enumerate(batches):
             eqb.eqb_router_logits(x, self.W_r, z=self.z, err_flag=self.err)
-            eqb.eqb_route_topk(self.z, self.bias, self.K, topk_idx=self.idx, tau=self.tau, err_flag=self.err)
+            self.loads.zero_()
+            eqb.eqb_route_topk(self.z, self.bias, self.K, self.offsets, topk_idx=self.idx, tau=self.tau, loads=self.loads,
+                               err_flag=self.err)
+            if grad_s is not None:
+                eqb.lei_inject_grad(grad_s[i], self.loads, self.offsets, self.K, self.eta, self.c)
+                zf = self.z.float()
+                torch.mul(grad_s[i], torch.sigmoid(zf) * torch.sigmoid(-zf), out=self.grad_in)  # dL/ds -> dL/dz
             eqb.eqb_balance_loss(self.z, self.idx, self.offsets, self.alpha, zeta=self.zeta, grad_in=self.grad_in,
                                  grad_out=self.dz, grad_scale=self.scale, counts=self.counts, loss=self.loss,
                                  workspace=self.ws_loss, err_flag=self.err)

@@ -448,7 +448,9 @@ eqb_status eqb_router_layer_step(const eqb_bf16 *x, const eqb_bf16 *W_r, int64_t
  *   mask       device uint8 [T] (nullable)
  *   score      0 softmax, 1 normalised sigmoid (zeta must then be 0)
  *   alpha, zeta  any sign; alpha and 2 zeta finite in fp32
- *   grad_in    device fp32 [T,E], 16-byte aligned (nullable)
+ *   grad_in    device fp32 [T,E], 16-byte aligned (nullable): a gradient with
+ *              respect to z.  The path's grad_s is one with respect to s =
+ *              sigma(z): it is multiplied by s (1 - s) before it is given here
  *   grad_out   device fp32 [T,E], or bf16 with grad_out_bf16 != 0 (rounded to
  *              nearest even: the operand of eqb_router_grad); 16-byte aligned
  *              (nullable: no gradient).  May be grad_in where both are fp32.

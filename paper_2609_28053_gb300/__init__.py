@@ -548,7 +548,9 @@ def eqb_balance_loss(z, topk_idx, mb_offsets, alpha, zeta=0.0, score="softmax", 
     their gradient, from one pass over z (see eqb.h).  z bf16 or fp32 [T,E];
     topk_idx int32 [T,K]; mask bool or uint8 [T].  With grad_out (fp32 or bf16
     [T,E]) the gradient is written as grad_in + grad_scale * d, or without
-    grad_in as grad_scale * d; grad_out may be grad_in.  prob (fp32 [M,E])
+    grad_in as grad_scale * d; grad_out may be grad_in.  grad_in is dL/dz: the
+    path's grad_s, dL/ds of s = sigmoid(z), is multiplied by s (1 - s) before it
+    is given here.  prob (fp32 [M,E])
     takes the mean probabilities when given.  Returns (loss fp32 [M,2]: balance
     loss and z-loss; counts int32 [M,E])."""
     T, E = z.shape
