@@ -435,13 +435,14 @@ eqb_status eqb_router_layer_step(const eqb_bf16 *x, const eqb_bf16 *W_r, int64_t
  *   d_{t,j} = p_j (alpha / n (F_j - sum_e p_e F_e) + 2 zeta / n lse_t)   (softmax)
  *   d_{t,j} = p_j (1 - s_j) alpha / n (F_j - sum_e p_e F_e)              (sigmoid)
  * written as grad_out = grad_in + d (grad_out = d without grad_in).  A token
- * that is masked out contributes nothing, its d is 0 and its row of z is not
- * read.  A logit of -inf closes its expert to the token (p = 0); a row that is
+ * that is masked out contributes nothing, its d is 0 and its row of z may hold
+ * anything.  A logit of -inf closes its expert to the token (p = 0); a row that is
  * -inf throughout has p = 0, lse = 0 and d = 0 and still counts in n.  An empty
  * microbatch has loss 0 and P = 0.
- * The arithmetic is fp32 (p and lse; the exponentials within a few ulps), F in
- * whole numbers and fp64; sums over tokens are formed in a fixed order, so the
- * same call gives the same bits.  The counts need no z, so one pass over it
+ * The arithmetic is fp32 (p and lse; the exponentials within a few ulps).  F, and
+ * for the gradient F - 1/E, come from whole numbers, f and f E - K n, by factors
+ * rounded to fp32; sums over tokens are formed in a fixed order, of long
+ * microbatches the last in fp64, so the same call gives the same bits.  The counts need no z, so one pass over it
  * gives loss and gradient.
  *   z          device bf16 [T,E], or fp32 with z_fp32 != 0; 16-byte aligned
  *   topk_idx   device int32 [T,K], e.g. from eqb_route_topk

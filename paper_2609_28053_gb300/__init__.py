@@ -645,7 +645,8 @@ class EqbAdamW:
             scale for every 256 elements in avg_scale and sq_scale; for
             beta2 up to 0.95 (eqb.h says what becomes of larger ones).
     exp_avg, exp_avg_sq, avg_scale, sq_scale  lists of tensors to keep the
-            states in (continued from a checkpoint, say); zeros when not given
+            states in (continued from a checkpoint, say); zeros when not given,
+            written on the stream that is current when the object is made
     copies  bf16 tensors (or None) that receive the new value of the fp32
             parameter beside them, rounded, e.g. the W_r that the projection
             reads

@@ -33,7 +33,10 @@ namespace {
 
 constexpr int kDxThreads = 224;    // two warps, four that take accumulators out, one that loads old values
 constexpr int kGradThreads = 320;  // dW: two warps, eight that take accumulators out
-constexpr int kGradCtas = 152;            // blocks of a dW grid: one an SM
+// Blocks of a dW grid: one an SM of a GB300.  Fixed, so that the workspace's size can
+// be asked for without a device; no block waits for another, so other counts only
+// take longer.
+constexpr int kGradCtas = 152;
 constexpr uint32_t kTile64 = 64 * 128;    // bytes of 64 rows of 64 bf16
 constexpr uint32_t kDxStage = 128 * 128;  // dx: 128 tokens x 64 experts of dz or columns of dx
 
