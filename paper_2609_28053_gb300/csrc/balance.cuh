@@ -13,7 +13,7 @@
 // sum of p by F itself, from the sums of p: p.R + 1/E would cancel where the lists
 // name experts of little probability.  Without a gradient nothing else needs the
 // counts, and the pass runs beside the kernel that forms them (T = 524,288, E = 128,
-// sigmoid: 51.4 us the call, 58.8 with a product token by token behind the counts).
+// sigmoid: 50.5 us the call, 7 more with a product token by token behind the counts).
 //
 // The pass is a stream.  Rows lie one after the other, so each warp fetches its
 // groups of up to 32 tokens (z and grad_in) by bulk copies into a ring of its

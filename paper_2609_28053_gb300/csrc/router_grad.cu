@@ -579,7 +579,7 @@ constexpr int64_t kFewTokens = 1024;
 // and up to this many elements of x where it is written: of two launches each
 // has its start and its end, and only the shared one reads and writes all along
 // (T = 300, d = 1,024, E = 64 8.3 us for 11.5; 7,520, 1,792, 96 19 for 31; 60,000,
-// 256, 64 26 for 50; 65,536, 4,096, 128 added to 251 for 277, without it 212 for 198).
+// 256, 64 26 for 50; 65,536, 4,096, 128 added to 255 for 280, without it 212 for 198).
 constexpr int64_t kSharedElements = int64_t(1) << 27;
 
 // The blocks of a group, of `most`: as many for every tile if that leaves no more
@@ -694,8 +694,8 @@ int launch_router_grad(const RouterGradArgs& g, cudaStream_t s) {
   // takes an SM of either side beside the other one, from the split that is
   // fastest: 64 SMs of 152 for dW (E = 32 to 128, d = 512 to 4,096; some GPUs like 56
   // and others 72 a little better), 48 where dx is added to, 80 and 62 above 128
-  // experts (T = 32,768, d = 4,096, E = 128 added to: 130 us with 48, 142 with 57,
-  // 149 with 64; T = 65,536, d = 2,048, E = 64: 98 to 108 with 64, 100 to 120 with 80).
+  // experts (T = 32,768, d = 4,096, E = 128 added to: 136 us with 48, 149 with 57,
+  // 158 with 64; T = 65,536, d = 2,048, E = 64: 98 to 108 with 64, 100 to 120 with 80).
   int sms = di.sm_count;
   const bool one = g.dx && g.dW && (g.add_dx || g.T * g.d <= kSharedElements) &&
                    (!p.direct || 4 * p.cols * p.groups <= 3 * di.sm_count);
