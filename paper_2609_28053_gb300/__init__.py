@@ -527,7 +527,11 @@ def eqb_layer_forward(z, b, K, mb_offsets, ws: EqbWorkspace, topk_idx, tau, load
     T, E = z.shape
     if r is None:
         r = eqb_target_rank(T, E, K)
-    ws.zero_()
+    if stream is None:
+        ws.zero_()
+    else:
+        with torch.cuda.stream(stream):
+            ws.zero_()
     eqb_route_topk(z, b, K, mb_offsets, topk_idx, tau, loads, ws.hist_hi, ws.err, stream)
     eqb_select_quantile(ws.hist_hi, 1, r, ws.u, ws.rho, None, ws.err, stream)
     eqb_margin_hist_pass2(z, tau, ws.u, ws.hist_lo, stream)
