@@ -3,7 +3,9 @@
  * Exact Quantile Balancing (EQB) and Load-Error Injection (LEI),
  * arXiv 2609.28053, on one NVIDIA GB300 (sm_103a), and the operators of a
  * router's training step beside it: the balance loss with its gradient, the
- * projection's gradients, and AdamW.
+ * projection's gradients, and AdamW; and of the experts behind the router: the
+ * gate's weights, the experts' rows, 8-bit values with block scales, the
+ * grouped products and the weighted sum back.
  *
  * Notation follows the paper: T tokens, E routed experts, K experts per
  * token, router logits z[T,E], expert bias b[E], cutoff tau_t = the (K+1)st
@@ -555,6 +557,199 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor *tensors, int32_t count, int32_
                           double lr, int64_t step, double beta1, double beta2, double eps,
                           double weight_decay, const float *grad_scale, int32_t *err_flag,
                           void *stream);
+
+/* ---- The experts behind the router (no counterpart in the paper, which stops
+ * at the lists: these take a list to the experts and back).
+ *
+ * Gate: experts and gate weights of every token, with experts in groups.  With
+ * the choosing score c_e = fp32(z_{t,e}) + b_e (as in eqb_route_topk; z and b may
+ * be -inf, which closes an expert):
+ *   groups   with top_groups < groups, the experts are `groups` groups of
+ *            E / groups neighbours; a group's score is its largest c, or with
+ *            group_top2 the sum (fp32) of its two largest, where a second that is
+ *            closed (or missing) counts nothing.  The top_groups best groups stay
+ *            open (ties to the lower group);
+ *   list     the K open experts of largest c > -inf, in descending order (ties to
+ *            the lower expert); where fewer are open, the rest of the list is -1;
+ *   weights  from the unbiased logits, s = sigmoid(z_t) or softmax(z_t) over all E
+ *            experts: w_k = scale s_k, or with renorm scale s_k / (sum of the
+ *            list's s).  An entry of -1 has weight 0.
+ * Choice and ties are exact (fp32 sums and comparisons); the weights are fp32,
+ * renormalised without underflow however low the logits are.
+ *   z        device bf16 [T,E], or fp32 with z_fp32 != 0; 16-byte aligned
+ *   b        device fp32 [E] (nullable: 0)
+ *   mask     device uint8 [T] (nullable): a token whose byte is 0 gets -1 and
+ *            0 throughout; its row of z is not looked at
+ *   score    0 softmax, 1 sigmoid
+ *   topk_idx device int32 [T,K] (out); weight device fp32 [T,K] (out, nullable)
+ *   err_flag EQB_ERR_NONFINITE for a NaN or +inf c (or, with softmax, z) of a
+ *            token that counts
+ * Supported: E a multiple of 8 up to 1024, 1 <= K < E, K <= 31, groups <= 32 and
+ * dividing E, 1 <= top_groups <= groups, K <= top_groups E / groups, scale
+ * finite in fp32, T as above. */
+eqb_status eqb_gate_topk(const void *z, int32_t z_fp32, const float *b, int64_t T, int32_t E, int32_t K,
+                         int32_t groups, int32_t top_groups, int32_t group_top2, int32_t score,
+                         int32_t renorm, double scale, const uint8_t *mask, int32_t *topk_idx,
+                         float *weight, int32_t *err_flag, void *stream);
+
+/* Gradient of eqb_gate_topk's weights with respect to z, the lists being
+ * constants.  With g = dL/dw, and a_k = s_k / (sum of the list's s), gb = sum_k a_k g_k:
+ *   sigmoid          d_k = scale g_k s_k (1 - s_k)
+ *   sigmoid, renorm  d_k = scale a_k (1 - s_k) (g_k - gb)
+ *   softmax, renorm  d_k = scale a_k (g_k - gb)
+ *   softmax          d_j = scale p_j ([j in list] g_j - sum_k p_k g_k), every j
+ * and 0 for experts outside the list in the first three.  grad_out = grad_in + d
+ * (d without grad_in): dL/dz as eqb_balance_loss takes it in grad_in, or, in bf16,
+ * eqb_router_grad in dz.  A list entry outside [0, E) has no part in anything, and a
+ * token without any other has d = 0, whatever its row of z holds.  An expert that a
+ * list names twice counts as two entries whose terms are added.
+ *   z, z_fp32, score, renorm, scale  as in eqb_gate_topk
+ *   topk_idx     device int32 [T,K]; grad_weight device fp32 [T,K]
+ *   grad_in      device fp32 [T,E], 16-byte aligned (nullable); of the first three
+ *                kinds only the lists' entries are touched where grad_out is grad_in
+ *   grad_out     device fp32 [T,E], or bf16 with grad_out_bf16 != 0 (rounded once);
+ *                16-byte aligned.  May be grad_in where both are fp32.
+ * Supported: sizes as in eqb_gate_topk. */
+eqb_status eqb_gate_grad(const void *z, int32_t z_fp32, const int32_t *topk_idx,
+                         const float *grad_weight, int64_t T, int32_t E, int32_t K, int32_t score,
+                         int32_t renorm, double scale, const float *grad_in, void *grad_out,
+                         int32_t grad_out_bf16, void *stream);
+
+/* The experts' rows: the entries of the lists (token t's k-th is entry t K + k)
+ * that name an expert in [0, E), sorted by expert, within an expert in ascending
+ * order.  Row r of the sorted order is what the calls below keep in row r of their
+ * buffers of R = T K rows.
+ *   offsets  device int32 [E+1] (out): expert e has rows offsets[e] .. offsets[e+1]-1
+ *   blocks   device int32 [E+1] (out): expert e has blocks[e+1] - blocks[e] =
+ *            ceil(rows / 128) blocks of 128 rows in eqb_quant_cols and eqb_expert_wgrad
+ *   slot     device int32 [T,K] (out): the row of every entry, -1 where it has none
+ *   entry    device int32 [T K] (out): the entry of every row, -1 behind the last
+ *   workspace  device buffer of eqb_expert_rows_workspace_bytes(T, K, E) bytes,
+ *            256-byte aligned (may be NULL where that is 0)
+ * Supported: 1 <= E <= 1024, 1 <= K <= 1024, T K <= 2^31 - 2^24. */
+size_t eqb_expert_rows_workspace_bytes(int64_t T, int32_t K, int32_t E);
+eqb_status eqb_expert_rows(const int32_t *topk_idx, int64_t T, int32_t K, int32_t E, int32_t *offsets,
+                           int32_t *blocks, int32_t *slot, int32_t *entry, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* Most blocks of 128 rows that R rows of E experts can have: what the buffers of
+ * eqb_quant_cols are allocated for.  Host only; -1 for invalid arguments. */
+int64_t eqb_expert_max_blocks(int64_t R, int32_t E);
+
+/* Values in 8 bits (e4m3) with an fp32 scale for each block of 128 of them:
+ *   scale = max |x| * fp32(1 / 448), 0 if below 2^-126,
+ *   code  = e4m3_rne(clamp(x * fp32(1 / scale), -448, 448)), 0 where scale is 0,
+ * operation by operation in fp32 (x = code * scale to within half a step of
+ * e4m3, 2^-4 of the value, or 2^-10 of the scale).  err_flag: EQB_ERR_NONFINITE
+ * if a value that is read is not finite; its block's codes and scale are then
+ * unspecified, and no other's.
+ *
+ * eqb_quant_rows: blocks of 128 neighbours in a row (the last of a row may be
+ * shorter).  Without slot, row t of x becomes row t of q.  With slot [T,K], row t
+ * becomes row slot[t,k] of q for every k whose slot lies in [0, T K); the others are
+ * left out, and rows of q that no slot names are left as they are.
+ *   x      device bf16 [T,d], 16-byte aligned
+ *   q      device e4m3 (one byte) [T,d], with slot [T K, d]; 16-byte aligned (out)
+ *   scale  device fp32 [rows of q, ceil(d / 128)] (out)
+ *   slot   device int32 [T,K] (nullable; then K is ignored), no row twice
+ * Supported: d a multiple of 16 up to 2^20, T and T K <= 2^31 - 2^24. */
+eqb_status eqb_quant_rows(const eqb_bf16 *x, int64_t T, int32_t d, const int32_t *slot, int32_t K,
+                          uint8_t *q, float *scale, int32_t *err_flag, void *stream);
+
+/* Blocks of 128 rows of an expert, for each column its own scale, turned: the
+ * operands of eqb_expert_wgrad.  Row i of expert e's block b' (block number
+ * b = blocks[e] + b') is the sorted row r = offsets[e] + 128 b' + i while that is
+ * below offsets[e+1], and zeros after; its values are x[r], or with entry
+ * x[entry[r] / K].
+ *   x        device bf16 [R,c], with entry [T,c]; 16-byte aligned
+ *   entry    device int32 [R] (nullable); an entry outside [0, T K) reads as zeros
+ *   offsets, blocks  device int32 [E+1], from eqb_expert_rows
+ *   q        device e4m3 [c, 128 P] (out), 16-byte aligned: q[j, 128 b + i]
+ *   scale    device fp32 [P, c] (out)
+ *   P        blocks allocated for: eqb_expert_max_blocks(R, E) is always enough.
+ *            Blocks from blocks[E] on are left as they are; blocks from P on are not
+ *            written.
+ * Supported: c a multiple of 16 up to 2^20, E <= 1024, R, T <= 2^31 - 2^24,
+ * P <= 2^24 - 2^17. */
+eqb_status eqb_quant_cols(const eqb_bf16 *x, int64_t T, int32_t c, const int32_t *entry, int64_t R,
+                          int32_t K, const int32_t *offsets, const int32_t *blocks, int32_t E,
+                          int64_t P, uint8_t *q, float *scale, int32_t *err_flag, void *stream);
+
+/* Blocks of 128 x 128 of each of E matrices, and, from the same read, of their
+ * transposes (the same codes and scales, turned): the weights of
+ * eqb_expert_matmul for the forward product and for the gradient of its input.
+ *   w        device bf16 [E,n,d], or fp32 with w_fp32 != 0; 16-byte aligned
+ *   q        device e4m3 [E,n,d]; scale device fp32 [E, ceil(n/128), ceil(d/128)]
+ *   q_t      device e4m3 [E,d,n]; scale_t device fp32 [E, ceil(d/128), ceil(n/128)]
+ *            (nullable, both together)
+ * Supported: n and d multiples of 16 up to 2^20, 0 <= E <= 1024. */
+eqb_status eqb_quant_blocks(const void *w, int32_t w_fp32, int32_t E, int32_t n, int32_t d, uint8_t *q,
+                            float *scale, uint8_t *q_t, float *scale_t, int32_t *err_flag,
+                            void *stream);
+
+/* The experts' product in 8 bits.  For every row r of expert e:
+ *   out[r, j] = sum over blocks B of 128 columns:
+ *               scale[r, B] w_scale[e, j / 128, B] sum_{i in B} q[r, i] w[e, j, i].
+ * The sum over a block is formed by the tensor cores (tcgen05, fp32), the sum
+ * over the blocks in fp32 with one fused multiply-add each, in ascending order; out
+ * is rounded once.  The same call gives the same bits.  With the transposed weights
+ * of eqb_quant_blocks it is the gradient with respect to the input.
+ *   q, scale    device e4m3 [R,d], fp32 [R, ceil(d/128)], from eqb_quant_rows; q
+ *               16-byte aligned
+ *   w, w_scale  device e4m3 [E,n,d], fp32 [E, ceil(n/128), ceil(d/128)]; w
+ *               16-byte aligned
+ *   offsets     device int32 [E+1]; read on the device, and kept within [0, R]
+ *   out         device bf16 [R,n], or fp32 with out_fp32 != 0; 32-byte aligned.
+ *               Rows from offsets[E] on are left as they are.
+ *   err_flag    EQB_ERR_CUDA if a kernel's pipeline stalled and it gave up
+ * Supported: n and d multiples of 16 up to 2^20, 1 <= E <= 1024, R <= 2^31 - 2^24. */
+eqb_status eqb_expert_matmul(const uint8_t *q, const float *scale, const uint8_t *w,
+                             const float *w_scale, const int32_t *offsets, int64_t R, int32_t n,
+                             int32_t d, int32_t E, void *out, int32_t out_fp32, int32_t *err_flag,
+                             void *stream);
+
+/* The gradient of the experts' weights in 8 bits, from two buffers of
+ * eqb_quant_cols over the same rows (a of the product's output gradient, b of its
+ * input):
+ *   dW[e, i, j] = sum over e's blocks B: a_scale[B, i] b_scale[B, j]
+ *                 sum_{r in B} a[i, r] b[j, r]
+ * with the sums of eqb_expert_matmul; with accumulate it is added to what dW
+ * holds (in fp32).  An expert without blocks gets 0 (or is left as it is).
+ *   a, a_scale  device e4m3 [n, 128 P], fp32 [P, n]; a 16-byte aligned
+ *   b, b_scale  device e4m3 [d, 128 P], fp32 [P, d]; b 16-byte aligned, b_scale too
+ *   blocks      device int32 [E+1]; read on the device, and kept within [0, P]
+ *   dW          device fp32 [E,n,d], 32-byte aligned
+ *   err_flag    as in eqb_expert_matmul
+ * Supported: as in eqb_expert_matmul; P <= 2^24 - 2^17. */
+eqb_status eqb_expert_wgrad(const uint8_t *a, const float *a_scale, const uint8_t *b,
+                            const float *b_scale, const int32_t *blocks, int64_t P, int32_t n,
+                            int32_t d, int32_t E, float *dW, int32_t accumulate, int32_t *err_flag,
+                            void *stream);
+
+/* The way back: out[t] = sum_k weight[t,k] rows[slot[t,k]] over the entries whose slot
+ * lies in [0, R), in ascending k, fp32, rounded once; without weight the plain
+ * sum (the gradient of the rows that eqb_quant_rows sent out).  Rows that no slot
+ * names are not read.
+ *   rows    device bf16 [R,n], 16-byte aligned
+ *   slot    device int32 [T,K]; weight device fp32 [T,K] (nullable: 1)
+ *   out     device bf16 [T,n], 16-byte aligned, not overlapping rows
+ * Supported: n a multiple of 16 up to 2^20, 1 <= K <= 1024, T, R and T K
+ * <= 2^31 - 2^24. */
+eqb_status eqb_expert_combine(const eqb_bf16 *rows, const int32_t *slot, const float *weight, int64_t T,
+                              int64_t R, int32_t n, int32_t K, eqb_bf16 *out, void *stream);
+
+/* Its gradients from grad = dL/dout:
+ *   grad_rows[slot[t,k]] = weight[t,k] grad[t]       (bf16, rounded once)
+ *   grad_weight[t,k] = sum_j grad[t,j] rows[slot[t,k], j]   (fp32; 0 without a slot)
+ * Either may be NULL.  Rows that no slot names are left as they are.
+ *   grad       device bf16 [T,n], 16-byte aligned
+ *   rows       as above (not read without grad_weight), weight too (nullable: 1)
+ *   slot       no row twice
+ *   grad_rows  device bf16 [R,n], 16-byte aligned; may be rows itself
+ * Supported: as in eqb_expert_combine. */
+eqb_status eqb_expert_combine_grad(const eqb_bf16 *grad, const eqb_bf16 *rows, const int32_t *slot,
+                                   const float *weight, int64_t T, int64_t R, int32_t n, int32_t K,
+                                   eqb_bf16 *grad_rows, float *grad_weight, void *stream);
 
 /* Self-test of failure detection (no GPU fault involved): every wait in the
  * library's kernels is a bounded poll of a shared-memory mbarrier, and a

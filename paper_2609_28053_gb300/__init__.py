@@ -37,7 +37,9 @@ __all__ = [
     "eqb_maxvio", "gshard_inject_grad", "eqb_rank_averaged_bias", "eqb_fixed_hist_bias",
     "eqb_rank_averaged_workspace_bytes", "eqb_selftest_stalled_wait", "lei_coefficients",
     "eqb_margin_hist_lei", "eqb_balance_loss", "eqb_balance_loss_workspace_bytes", "eqb_router_grad",
-    "eqb_router_grad_workspace_bytes", "EqbAdamW",
+    "eqb_router_grad_workspace_bytes", "EqbAdamW", "eqb_gate_topk", "eqb_gate_grad", "eqb_expert_rows",
+    "eqb_expert_rows_workspace_bytes", "eqb_expert_max_blocks", "eqb_quant_rows", "eqb_quant_cols", "eqb_quant_blocks",
+    "eqb_expert_matmul", "eqb_expert_wgrad", "eqb_expert_combine", "eqb_expert_combine_grad",
 ]
 
 
@@ -632,6 +634,326 @@ def eqb_router_grad(dz, x, W_r, dx=None, dW=None, accumulate_dx=False, accumulat
                                 _p(err_flag), _stream(stream))
     _check(rc, "eqb_router_grad")
     return dx, dW
+
+
+def _dims(t, n, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != n:
+        raise ValueError(f"{name} must have {n} dimensions, got {tuple(t.shape)}")
+    return t.shape
+
+
+def _either(t, a, b):
+    """The one of two types that t has, else the first, which _need then asks for."""
+    return b if isinstance(t, torch.Tensor) and t.dtype is b else a
+
+
+_GROUP_SCORES = {"max": 0, "top2": 1}
+
+
+def _one_of(kinds, value, name):
+    kind = kinds.get(value)
+    if kind is None:
+        raise ValueError(f"{name} must be one of {sorted(kinds)}, got {value!r}")
+    return kind
+
+
+def _mask(mask, T):
+    if mask is not None:
+        _need(mask, _either(mask, torch.bool, torch.uint8), "mask", (T,))
+
+
+def eqb_gate_topk(z, b, K, score="sigmoid", groups=1, top_groups=1, group_score="max", renorm=True, scale=1.0, mask=None,
+                  topk_idx=None, weight=None, err_flag=None, stream=None):
+    """The gate: K experts a token by z + b, from the top_groups best of `groups`
+    groups of neighbouring experts (group_score "max", or "top2": the sum of a group's two
+    largest), and their weights from z: sigmoid or softmax, renormalised over the
+    list or not, times scale (see eqb.h).  z bf16 or fp32 [T,E]; b fp32 [E] or
+    None; mask bool or uint8 [T].  A closed expert has z or b of -inf.  Returns
+    (topk_idx int32 [T,K], -1 where no expert is left, weight fp32 [T,K])."""
+    T, E = _dims(z, 2, "z")
+    dt = _either(z, torch.bfloat16, torch.float32)
+    _need(z, dt, "z")
+    _on_current_device(z, "z")
+    if b is not None:
+        _need(b, torch.float32, "b", (E,))
+    kind, two = _one_of(_SCORES, score, "score"), _one_of(_GROUP_SCORES, group_score, "group_score")
+    _mask(mask, T)
+    if topk_idx is None:
+        topk_idx = _new((T, K), torch.int32, z, stream)
+    else:
+        _need(topk_idx, torch.int32, "topk_idx", (T, K))
+    if weight is None:
+        weight = _new((T, K), torch.float32, z, stream)
+    else:
+        _need(weight, torch.float32, "weight", (T, K))
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_gate_topk(z.data_ptr(), dt is torch.float32, _p(b), T, E, K, groups, top_groups, two, kind, bool(renorm),
+                              scale, _p(mask), topk_idx.data_ptr(), weight.data_ptr(), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_gate_topk")
+    return topk_idx, weight
+
+
+def eqb_gate_grad(z, topk_idx, grad_weight, score="sigmoid", renorm=True, scale=1.0, grad_in=None, grad_out=None, stream=None):
+    """Gradient of eqb_gate_topk's weights with respect to z, from grad_weight
+    fp32 [T,K]: grad_out (fp32, or bf16 [T,E]; fp32 when not given) = grad_in + d,
+    d alone without grad_in; grad_out may be grad_in.  What eqb_balance_loss takes as
+    grad_in, and in bf16 eqb_router_grad as dz.  Returns grad_out."""
+    T, E = _dims(z, 2, "z")
+    K = _dims(topk_idx, 2, "topk_idx")[1]
+    dt = _either(z, torch.bfloat16, torch.float32)
+    _need(z, dt, "z")
+    _on_current_device(z, "z")
+    _need(topk_idx, torch.int32, "topk_idx", (T, K))
+    if grad_weight is None:
+        raise TypeError("grad_weight must be a torch.Tensor")
+    _need(grad_weight, torch.float32, "grad_weight", (T, K))
+    kind = _one_of(_SCORES, score, "score")
+    if grad_in is not None:
+        _need(grad_in, torch.float32, "grad_in", (T, E))
+    if grad_out is None:
+        grad_out = _new((T, E), torch.float32, z, stream)
+    to = _either(grad_out, torch.float32, torch.bfloat16)
+    _need(grad_out, to, "grad_out", (T, E))
+    rc = load().eqb_gate_grad(z.data_ptr(), dt is torch.float32, topk_idx.data_ptr(), grad_weight.data_ptr(), T, E, K, kind,
+                              bool(renorm), scale, _p(grad_in), grad_out.data_ptr(), to is torch.bfloat16, _stream(stream))
+    _check(rc, "eqb_gate_grad")
+    return grad_out
+
+
+def eqb_expert_rows_workspace_bytes(T: int, K: int, E: int) -> int:
+    return int(load().eqb_expert_rows_workspace_bytes(T, K, E))
+
+
+def eqb_expert_max_blocks(R: int, E: int) -> int:
+    """Most blocks of 128 rows that R rows of E experts can have."""
+    return int(load().eqb_expert_max_blocks(R, E))
+
+
+def eqb_expert_rows(topk_idx, E, offsets=None, blocks=None, slot=None, entry=None, workspace=None, stream=None):
+    """The experts' rows from the lists topk_idx int32 [T,K]: the entries sorted by
+    expert, in ascending order within one.  Returns (offsets int32 [E+1],
+    blocks int32 [E+1], slot int32 [T,K], entry int32 [T*K]); see eqb.h."""
+    T, K = _dims(topk_idx, 2, "topk_idx")
+    _need(topk_idx, torch.int32, "topk_idx")
+    _on_current_device(topk_idx, "topk_idx")
+    made = []
+    for t, name, shape in ((offsets, "offsets", (E + 1,)), (blocks, "blocks", (E + 1,)), (slot, "slot", (T, K)),
+                           (entry, "entry", (T * K,))):
+        if t is None:
+            t = _new(shape, torch.int32, topk_idx, stream)
+        else:
+            _need(t, torch.int32, name, shape)
+        made.append(t)
+    offsets, blocks, slot, entry = made
+    if workspace is None:
+        need = eqb_expert_rows_workspace_bytes(T, K, E)
+        workspace = _new(need, torch.uint8, topk_idx, stream) if need else None
+    else:
+        _need(workspace, torch.uint8, "workspace")
+    rc = load().eqb_expert_rows(topk_idx.data_ptr(), T, K, E, offsets.data_ptr(), blocks.data_ptr(), slot.data_ptr(),
+                                entry.data_ptr(), _p(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+    _check(rc, "eqb_expert_rows")
+    return offsets, blocks, slot, entry
+
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def _up(n):
+    return (n + 127) // 128
+
+
+def eqb_quant_rows(x, slot=None, q=None, scale=None, err_flag=None, stream=None):
+    """x bf16 [T,d] in 8 bits, with a scale for every 128 neighbours of a row.
+    With slot int32 [T,K] (eqb_expert_rows) row t goes to the rows slot[t] of q
+    [T*K,d], those of -1 left out.  Returns (q float8_e4m3fn, scale fp32 [rows,
+    ceil(d/128)])."""
+    T, d = _dims(x, 2, "x")
+    _need(x, torch.bfloat16, "x")
+    _on_current_device(x, "x")
+    K, R = 1, T
+    if slot is not None:
+        K = _dims(slot, 2, "slot")[1]
+        _need(slot, torch.int32, "slot", (T, K))
+        R = T * K
+    if q is None:
+        q = _new((R, d), _E4M3, x, stream)
+    else:
+        _need(q, _E4M3, "q", (R, d))
+    if scale is None:
+        scale = _new((R, _up(d)), torch.float32, x, stream)
+    else:
+        _need(scale, torch.float32, "scale", (R, _up(d)))
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_quant_rows(x.data_ptr(), T, d, _p(slot), K, q.data_ptr(), scale.data_ptr(), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_quant_rows")
+    return q, scale
+
+
+def eqb_quant_cols(x, offsets, blocks, entry=None, K=1, q=None, scale=None, err_flag=None, stream=None):
+    """The experts' rows in 8 bits, turned, with a scale for every 128 rows of an
+    expert and column: the operands of eqb_expert_wgrad.  x bf16 [R,c] in sorted
+    rows, or with entry int32 [R] and K (eqb_expert_rows) [T,c] by token.  Returns
+    (q float8_e4m3fn [c, 128 P], scale fp32 [P,c]), P = eqb_expert_max_blocks(R, E)
+    unless q says otherwise."""
+    T, c = _dims(x, 2, "x")
+    _need(x, torch.bfloat16, "x")
+    _on_current_device(x, "x")
+    E = _dims(offsets, 1, "offsets")[0] - 1
+    _need(offsets, torch.int32, "offsets")
+    if blocks is None:
+        raise TypeError("blocks must be a torch.Tensor")
+    _need(blocks, torch.int32, "blocks", (E + 1,))
+    R = T
+    if entry is not None:
+        R = _dims(entry, 1, "entry")[0]
+        _need(entry, torch.int32, "entry")
+    if q is None:
+        P = eqb_expert_max_blocks(R, E) if scale is None else _dims(scale, 2, "scale")[0]
+        q = _new((c, max(P, 0) * 128), _E4M3, x, stream)
+    else:
+        P = _dims(q, 2, "q")[1] // 128
+        _need(q, _E4M3, "q", (c, P * 128))
+    if scale is None:
+        scale = _new((max(P, 0), c), torch.float32, x, stream)
+    else:
+        _need(scale, torch.float32, "scale", (P, c))
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_quant_cols(x.data_ptr(), T, c, _p(entry), R, K, offsets.data_ptr(), blocks.data_ptr(), E, P, q.data_ptr(),
+                               scale.data_ptr(), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_quant_cols")
+    return q, scale
+
+
+def eqb_quant_blocks(w, q=None, scale=None, q_t=None, scale_t=None, turned=False, err_flag=None, stream=None):
+    """Matrices w bf16 or fp32 [E,n,d] in 8 bits with a scale for every 128 x 128,
+    and with turned (or where q_t and scale_t are given) their transposes too.
+    Returns (q, scale), or (q, scale, q_t, scale_t)."""
+    E, n, d = _dims(w, 3, "w")
+    dt = _either(w, torch.bfloat16, torch.float32)
+    _need(w, dt, "w")
+    _on_current_device(w, "w")
+    turned = turned or q_t is not None or scale_t is not None
+    made = []
+    for t, name, dtype, shape, want in ((q, "q", _E4M3, (E, n, d), True), (scale, "scale", torch.float32, (E, _up(n), _up(d)), True),
+                                        (q_t, "q_t", _E4M3, (E, d, n), turned),
+                                        (scale_t, "scale_t", torch.float32, (E, _up(d), _up(n)), turned)):
+        if t is not None:
+            _need(t, dtype, name, shape)
+        elif want:
+            t = _new(shape, dtype, w, stream)
+        made.append(t)
+    q, scale, q_t, scale_t = made
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_quant_blocks(w.data_ptr(), dt is torch.float32, E, n, d, q.data_ptr(), scale.data_ptr(), _p(q_t), _p(scale_t),
+                                 _p(err_flag), _stream(stream))
+    _check(rc, "eqb_quant_blocks")
+    return (q, scale, q_t, scale_t) if turned else (q, scale)
+
+
+def eqb_expert_matmul(q, scale, w, w_scale, offsets, out=None, err_flag=None, stream=None):
+    """Every expert's rows times its weights in 8 bits: out[r] = q_r w_e^T for the
+    rows offsets[e] .. offsets[e+1]-1.  q [R,d] and scale [R, ceil(d/128)] from
+    eqb_quant_rows, w [E,n,d] and w_scale from eqb_quant_blocks (the transposed pair
+    for the gradient of the input), offsets int32 [E+1] from eqb_expert_rows.
+    out: bf16 (when not given) or fp32 [R,n]; rows behind the last expert's are
+    left as they are.  Returns out."""
+    R, d = _dims(q, 2, "q")
+    E, n, _ = _dims(w, 3, "w")
+    _need(q, _E4M3, "q")
+    _on_current_device(q, "q")
+    _need(w, _E4M3, "w", (E, n, d))
+    for t, name, shape in ((scale, "scale", (R, _up(d))), (w_scale, "w_scale", (E, _up(n), _up(d)))):
+        if t is None:
+            raise TypeError(f"{name} must be a torch.Tensor")
+        _need(t, torch.float32, name, shape)
+    if offsets is None:
+        raise TypeError("offsets must be a torch.Tensor")
+    _need(offsets, torch.int32, "offsets", (E + 1,))
+    if out is None:
+        out = _new((R, n), torch.bfloat16, q, stream)
+    to = _either(out, torch.bfloat16, torch.float32)
+    _need(out, to, "out", (R, n))
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_expert_matmul(q.data_ptr(), scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), offsets.data_ptr(), R, n, d, E,
+                                  out.data_ptr(), to is torch.float32, _p(err_flag), _stream(stream))
+    _check(rc, "eqb_expert_matmul")
+    return out
+
+
+def eqb_expert_wgrad(a, a_scale, b, b_scale, blocks, dW=None, accumulate=False, err_flag=None, stream=None):
+    """The gradient of eqb_expert_matmul's weights in 8 bits: dW[e] = a_e b_e^T over
+    the expert's rows, a [n, 128 P] and b [d, 128 P] from eqb_quant_cols over the
+    same rows (of the output's gradient and of the input), blocks int32 [E+1] from
+    eqb_expert_rows.  dW fp32 [E,n,d], with accumulate added to.  Returns dW."""
+    n, p = _dims(a, 2, "a")
+    d = _dims(b, 2, "b")[0]
+    P = p // 128
+    E = _dims(blocks, 1, "blocks")[0] - 1
+    _need(a, _E4M3, "a", (n, P * 128))
+    _on_current_device(a, "a")
+    _need(b, _E4M3, "b", (d, P * 128))
+    for t, name, shape in ((a_scale, "a_scale", (P, n)), (b_scale, "b_scale", (P, d))):
+        if t is None:
+            raise TypeError(f"{name} must be a torch.Tensor")
+        _need(t, torch.float32, name, shape)
+    _need(blocks, torch.int32, "blocks")
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate needs dW")
+        dW = _new((E, n, d), torch.float32, a, stream)
+    else:
+        _need(dW, torch.float32, "dW", (E, n, d))
+    _need(err_flag, torch.int32, "err_flag")
+    rc = load().eqb_expert_wgrad(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), blocks.data_ptr(), P, n, d, E,
+                                 dW.data_ptr(), bool(accumulate), _p(err_flag), _stream(stream))
+    _check(rc, "eqb_expert_wgrad")
+    return dW
+
+
+def eqb_expert_combine(rows, slot, weight=None, out=None, stream=None):
+    """out[t] = sum_k weight[t,k] rows[slot[t,k]] (bf16 [T,n]) over the slots that are
+    rows, 1 for every weight when not given.  rows bf16 [R,n]; slot int32 [T,K];
+    weight fp32 [T,K].  Returns out."""
+    R, n = _dims(rows, 2, "rows")
+    T, K = _dims(slot, 2, "slot")
+    _need(rows, torch.bfloat16, "rows")
+    _on_current_device(rows, "rows")
+    _need(slot, torch.int32, "slot")
+    if weight is not None:
+        _need(weight, torch.float32, "weight", (T, K))
+    if out is None:
+        out = _new((T, n), torch.bfloat16, rows, stream)
+    else:
+        _need(out, torch.bfloat16, "out", (T, n))
+    rc = load().eqb_expert_combine(rows.data_ptr(), slot.data_ptr(), _p(weight), T, R, n, K, out.data_ptr(), _stream(stream))
+    _check(rc, "eqb_expert_combine")
+    return out
+
+
+def eqb_expert_combine_grad(grad, rows, slot, weight=None, grad_rows=None, grad_weight=None, stream=None):
+    """Gradients of eqb_expert_combine from grad bf16 [T,n]: grad_rows (bf16 [R,n],
+    rows without a slot left as they are; may be rows itself) and grad_weight
+    (fp32 [T,K]), each where it is given.  Returns (grad_rows, grad_weight)."""
+    T, n = _dims(grad, 2, "grad")
+    R = _dims(rows, 2, "rows")[0]
+    K = _dims(slot, 2, "slot")[1]
+    _need(grad, torch.bfloat16, "grad")
+    _on_current_device(grad, "grad")
+    _need(rows, torch.bfloat16, "rows", (R, n))
+    _need(slot, torch.int32, "slot", (T, K))
+    if weight is not None:
+        _need(weight, torch.float32, "weight", (T, K))
+    if grad_rows is not None:
+        _need(grad_rows, torch.bfloat16, "grad_rows", (R, n))
+    if grad_weight is not None:
+        _need(grad_weight, torch.float32, "grad_weight", (T, K))
+    rc = load().eqb_expert_combine_grad(grad.data_ptr(), rows.data_ptr(), slot.data_ptr(), _p(weight), T, R, n, K, _p(grad_rows),
+                                        _p(grad_weight), _stream(stream))
+    _check(rc, "eqb_expert_combine_grad")
+    return grad_rows, grad_weight
 
 
 _data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel

@@ -21,7 +21,9 @@ EXPORTS = (
     "eqb_rank_averaged_bias", "eqb_fixed_hist_bias", "eqb_rank_averaged_workspace_bytes",
     "eqb_selftest_stalled_wait", "lei_coefficients", "eqb_margin_hist_lei", "eqb_route_hist_fused",
     "eqb_balance_loss_workspace_bytes", "eqb_balance_loss", "eqb_router_grad_workspace_bytes",
-    "eqb_router_grad", "eqb_adamw_step",
+    "eqb_router_grad", "eqb_adamw_step", "eqb_gate_topk", "eqb_gate_grad", "eqb_expert_rows_workspace_bytes",
+    "eqb_expert_rows", "eqb_expert_max_blocks", "eqb_quant_rows", "eqb_quant_cols", "eqb_quant_blocks",
+    "eqb_expert_matmul", "eqb_expert_wgrad", "eqb_expert_combine", "eqb_expert_combine_grad",
 )
 
 STATUS = {0: "EQB_OK", 1: "EQB_ERR_INVALID_ARG", 2: "EQB_ERR_UNSUPPORTED", 3: "EQB_ERR_CUDA",
@@ -87,6 +89,16 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                  P, size, P, P],
             "eqb_router_grad": [P, P, P, i64, i32, i32, P, i32, P, i32, P, size, P, P],
             "eqb_adamw_step": [P, i32, i32, f64, i64, f64, f64, f64, f64, P, P, P],
+            "eqb_gate_topk": [P, i32, P, i64, i32, i32, i32, i32, i32, i32, i32, f64, P, P, P, P, P],
+            "eqb_gate_grad": [P, i32, P, P, i64, i32, i32, i32, i32, f64, P, P, i32, P],
+            "eqb_expert_rows": [P, i64, i32, i32, P, P, P, P, P, size, P],
+            "eqb_quant_rows": [P, i64, i32, P, i32, P, P, P, P],
+            "eqb_quant_cols": [P, i64, i32, P, i64, i32, P, P, i32, i64, P, P, P, P],
+            "eqb_quant_blocks": [P, i32, i32, i32, i32, P, P, P, P, P, P],
+            "eqb_expert_matmul": [P, P, P, P, P, i64, i32, i32, i32, P, i32, P, P],
+            "eqb_expert_wgrad": [P, P, P, P, P, i64, i32, i32, i32, P, i32, P, P],
+            "eqb_expert_combine": [P, P, P, i64, i64, i32, i32, P, P],
+            "eqb_expert_combine_grad": [P, P, P, P, i64, i64, i32, i32, P, P, P],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -104,6 +116,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eqb_balance_loss_workspace_bytes.restype = size
         lib.eqb_router_grad_workspace_bytes.argtypes = [i64, i32, i32]
         lib.eqb_router_grad_workspace_bytes.restype = size
+        lib.eqb_expert_rows_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.eqb_expert_rows_workspace_bytes.restype = size
+        lib.eqb_expert_max_blocks.argtypes = [i64, i32]
+        lib.eqb_expert_max_blocks.restype = i64
         lib.eqb_target_rank.argtypes = [i64, i32, i32]
         lib.eqb_target_rank.restype = i64
         if path is None:

@@ -290,4 +290,105 @@ struct RouterGradArgs {
 size_t router_grad_workspace(int64_t T, int d, int E);
 int launch_router_grad(const RouterGradArgs& a, cudaStream_t s);
 
+// The gate (gate.cu).
+struct GateArgs {
+  const void* z;  // bf16, or fp32 with z_fp32
+  int z_fp32;
+  const float* b;  // nullable
+  int64_t T;
+  int E, K;
+  int groups, top_groups, top2;
+  int sigmoid, renorm;
+  float scale;
+  const uint8_t* mask;  // nullable
+  int32_t* idx;
+  float* weight;  // nullable
+  int32_t* err;
+};
+int launch_gate(const GateArgs& a, cudaStream_t s);
+struct GateGradArgs {
+  const void* z;
+  int z_fp32;
+  const int32_t* idx;
+  const float* gw;
+  int64_t T;
+  int E, K;
+  int sigmoid, renorm;
+  float scale;
+  const float* grad_in;  // nullable
+  void* grad_out;        // fp32, or bf16 with grad_bf16
+  int grad_bf16;
+};
+int launch_gate_grad(const GateGradArgs& a, cudaStream_t s);
+
+// The experts' rows (expert_rows.cu): rows and blocks of 128 of a call.
+constexpr int kExpertBlock = 128;
+constexpr int kMaxExperts = 1024;
+struct ExpertRowsArgs {
+  const int32_t* idx;
+  int64_t n;  // entries: T K
+  int E;
+  int32_t* offsets;
+  int32_t* blocks;
+  int32_t* slot;
+  int32_t* entry;
+  int32_t* ws;
+};
+size_t expert_rows_workspace(int64_t n, int E);
+int launch_expert_rows(const ExpertRowsArgs& a, cudaStream_t s);
+
+// Values in 8 bits (quant.cu).
+int launch_quant_rows(const uint16_t* x, int64_t T, int d, const int32_t* slot, int K, uint8_t* q, float* scale,
+                      int32_t* err, cudaStream_t s);
+struct QuantColsArgs {
+  const uint16_t* x;
+  int64_t T;
+  int c;
+  const int32_t* entry;  // nullable
+  int64_t R;
+  int K;
+  const int32_t* offsets;
+  const int32_t* blocks;
+  int E;
+  int64_t P;
+  uint8_t* q;
+  float* scale;
+  int32_t* err;
+};
+int launch_quant_cols(const QuantColsArgs& a, cudaStream_t s);
+int launch_quant_blocks(const void* w, int w_fp32, int E, int n, int d, uint8_t* q, float* scale, uint8_t* q_t,
+                        float* scale_t, int32_t* err, cudaStream_t s);
+
+// The experts' products (expert_matmul.cu).  Rows of the first operand (m, or
+// per expert by `first`), of the second (n), and what is summed over (k).
+struct ExpertMatmulArgs {
+  const uint8_t* a;
+  const float* a_scale;
+  const uint8_t* b;
+  const float* b_scale;
+  const int32_t* first;  // offsets, or for the weights' gradient blocks
+  int64_t R;             // rows of a, or blocks
+  int n, d, E;
+  void* out;
+  int out_fp32;
+  int add;
+  int32_t* err;
+};
+int launch_expert_matmul(const ExpertMatmulArgs& a, cudaStream_t s);
+int launch_expert_wgrad(const ExpertMatmulArgs& a, cudaStream_t s);
+
+// The way back (expert_combine.cu).
+struct CombineArgs {
+  const uint16_t* grad;  // backward
+  const uint16_t* rows;
+  const int32_t* slot;
+  const float* weight;  // nullable
+  int64_t T, R;
+  int n, K;
+  uint16_t* out;  // or grad_rows (nullable)
+  float* gw;      // nullable
+};
+int launch_combine(const CombineArgs& a, cudaStream_t s);
+int launch_combine_grad(const CombineArgs& a, cudaStream_t s);
+
 }  // namespace eqb

@@ -1,0 +1,190 @@
+// expert_rows.cu -- the experts' rows from the tokens' lists: a stable counting
+// sort of the list entries by expert.
+//
+// The entries are cut into chunks, one a block.  One kernel counts every chunk's
+// entries of each expert, one forms each expert's running sums over the chunks (a
+// warp an expert), and one gives every entry its row: the rows of the experts
+// before, of the chunks before, of the block's warps before, and of the entries
+// before it in the warp's 32, which __match_any_sync counts.  Every step counts in
+// a fixed order, so rows are in ascending order of entry.  Few entries are one
+// chunk, whose block needs no other kernel.
+#include "eqb_device.cuh"
+
+namespace eqb {
+
+namespace {
+
+constexpr int kRowsWarps = 16;
+constexpr int kRowsThreads = kRowsWarps * 32;
+constexpr int kRowsChunk = 4096;  // least entries of a chunk
+constexpr int kRowsChunks = 608;  // most chunks
+
+struct RowsPlan {
+  int chunks, per;  // per: entries of a chunk, a multiple of kRowsThreads
+};
+RowsPlan plan_rows(int64_t n) {
+  RowsPlan p;
+  const int64_t want = (n + kRowsChunks - 1) / kRowsChunks;
+  const int64_t per = want > kRowsChunk ? want : kRowsChunk;
+  p.per = static_cast<int>((per + kRowsThreads - 1) / kRowsThreads * kRowsThreads);
+  p.chunks = static_cast<int>((n + p.per - 1) / p.per);
+  if (p.chunks < 1) p.chunks = 1;
+  return p;
+}
+
+__device__ __forceinline__ int expert_of(const ExpertRowsArgs& a, int64_t i, int64_t end) {
+  if (i >= end) return -1;
+  const int e = __ldg(a.idx + i);
+  return e >= 0 && e < a.E ? e : -1;
+}
+
+__global__ void __launch_bounds__(kRowsThreads) rows_count_kernel(const ExpertRowsArgs a, int per, int chunks) {
+  __shared__ int cnt[kMaxExperts];
+  for (int e = threadIdx.x; e < a.E; e += kRowsThreads) cnt[e] = 0;
+  __syncthreads();
+  griddep_wait();
+  const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per, end = min(a.n, i0 + per);
+  for (int64_t i = i0 + threadIdx.x; i < end; i += kRowsThreads) {
+    const int e = expert_of(a, i, end);
+    if (e >= 0) atomicAdd(cnt + e, 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kRowsThreads) a.ws[static_cast<int64_t>(e) * chunks + blockIdx.x] = cnt[e];
+}
+
+// Running sums over the chunks, exclusive, and each expert's total behind them.
+__global__ void __launch_bounds__(256) rows_scan_kernel(const ExpertRowsArgs a, int chunks) {
+  const int e = static_cast<int>(blockIdx.x) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  griddep_wait();
+  if (e >= a.E) return;
+  int* row = a.ws + static_cast<int64_t>(e) * chunks;
+  int run = 0;
+  for (int c0 = 0; c0 < chunks; c0 += 32) {
+    const int v = c0 + lane < chunks ? row[c0 + lane] : 0;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    if (c0 + lane < chunks) row[c0 + lane] = run + x - v;
+    run += __shfl_sync(kFull, x, 31);
+  }
+  if (lane == 0) a.ws[static_cast<int64_t>(a.E) * chunks + e] = run;
+}
+
+__global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRowsArgs a, int per, int chunks) {
+  extern __shared__ int cnt[];  // [warps][E], then the experts' totals and first rows [E] each
+  __shared__ int part[2][kRowsWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
+  int* total = cnt + kRowsWarps * E;
+  int* first = total + E;
+  for (int i = threadIdx.x; i < kRowsWarps * E; i += kRowsThreads) cnt[i] = 0;
+  __syncthreads();
+  griddep_wait();
+  // a warp's entries: a contiguous part of the chunk
+  const int64_t w0 = static_cast<int64_t>(blockIdx.x) * per + warp * (per / kRowsWarps);
+  const int64_t end = min(a.n, w0 + per / kRowsWarps);
+  int* mine = cnt + warp * E;
+  for (int64_t i = w0; i < end; i += 32) {
+    const int e = expert_of(a, i + lane, end);
+    const uint32_t same = __match_any_sync(kFull, e);
+    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  // what the chunk's warps before have, and the experts' totals
+  for (int e = threadIdx.x; e < E; e += kRowsThreads) {
+    int run = 0;
+    for (int w = 0; w < kRowsWarps; ++w) {
+      const int v = cnt[w * E + e];
+      cnt[w * E + e] = run;
+      run += v;
+    }
+    total[e] = chunks == 1 ? run : a.ws[static_cast<int64_t>(E) * chunks + e];
+  }
+  __syncthreads();
+  // first rows and blocks of the experts: two neighbours a thread
+  {
+    const int e0 = 2 * threadIdx.x;
+    const int n0 = e0 < E ? total[e0] : 0, n1 = e0 + 1 < E ? total[e0 + 1] : 0;
+    const int b0 = (n0 + kExpertBlock - 1) / kExpertBlock, b1 = (n1 + kExpertBlock - 1) / kExpertBlock;
+    int x = n0 + n1, y = b0 + b1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int p = __shfl_up_sync(kFull, x, o), q = __shfl_up_sync(kFull, y, o);
+      if (lane >= o) {
+        x += p;
+        y += q;
+      }
+    }
+    if (lane == 31) {
+      part[0][warp] = x;
+      part[1][warp] = y;
+    }
+    __syncthreads();
+    int rows = x - n0 - n1, blks = y - b0 - b1;
+    for (int w = 0; w < warp; ++w) {
+      rows += part[0][w];
+      blks += part[1][w];
+    }
+    if (e0 < E) first[e0] = rows;
+    if (e0 + 1 < E) first[e0 + 1] = rows + n0;
+    if (blockIdx.x == 0) {
+      if (e0 < E) {
+        a.offsets[e0 + 1] = rows + n0;
+        a.blocks[e0 + 1] = blks + b0;
+      }
+      if (e0 + 1 < E) {
+        a.offsets[e0 + 2] = rows + n0 + n1;
+        a.blocks[e0 + 2] = blks + b0 + b1;
+      }
+      if (threadIdx.x == 0) a.offsets[0] = a.blocks[0] = 0;
+    }
+  }
+  __syncthreads();
+  const int all = first[E - 1] + total[E - 1];
+  for (int e = threadIdx.x; e < E; e += kRowsThreads) {
+    const int base = first[e] + (chunks == 1 ? 0 : a.ws[static_cast<int64_t>(e) * chunks + blockIdx.x]);
+    for (int w = 0; w < kRowsWarps; ++w) cnt[w * E + e] += base;
+  }
+  __syncthreads();
+  for (int64_t i = w0; i < end; i += 32) {
+    const int e = expert_of(a, i + lane, end);
+    const uint32_t same = __match_any_sync(kFull, e);
+    const int row = e >= 0 ? mine[e] + __popc(same & ((1u << lane) - 1u)) : -1;
+    __syncwarp();
+    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    __syncwarp();
+    if (i + lane < end) {
+      a.slot[i + lane] = row;
+      if (row >= 0) a.entry[row] = static_cast<int32_t>(i + lane);
+    }
+  }
+  // the rows of this chunk's numbers that no entry has
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * per, r1 = min(a.n, r0 + per);
+  for (int64_t r = max(r0, static_cast<int64_t>(all)) + threadIdx.x; r < r1; r += kRowsThreads) a.entry[r] = -1;
+}
+
+}  // namespace
+
+size_t expert_rows_workspace(int64_t n, int E) {
+  const RowsPlan p = plan_rows(n);
+  return p.chunks == 1 ? 0 : carve_round((static_cast<size_t>(p.chunks) + 1) * static_cast<size_t>(E) * 4);
+}
+
+int launch_expert_rows(const ExpertRowsArgs& a, cudaStream_t s) {
+  const RowsPlan p = plan_rows(a.n);
+  const int smem = (kRowsWarps + 2) * a.E * 4;
+  if (!allow_smem(rows_place_kernel, (kRowsWarps + 2) * kMaxExperts * 4)) return kErrCuda;
+  if (p.chunks > 1) {
+    if (launch_dependent(rows_count_kernel, dim3(p.chunks), dim3(kRowsThreads), 0, s, a, p.per, p.chunks) != cudaSuccess ||
+        launch_dependent(rows_scan_kernel, dim3((a.E + 7) / 8), dim3(256), 0, s, a, p.chunks) != cudaSuccess)
+      return kErrCuda;
+  }
+  return launch_dependent(rows_place_kernel, dim3(p.chunks), dim3(kRowsThreads), smem, s, a, p.per, p.chunks) == cudaSuccess
+             ? kOk
+             : kErrCuda;
+}
+
+}  // namespace eqb

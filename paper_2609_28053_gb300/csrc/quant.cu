@@ -1,0 +1,281 @@
+// quant.cu -- values in 8 bits (e4m3) with an fp32 scale for each block of 128:
+//   scale = max |x| * fp32(1 / 448),   code = e4m3(x * fp32(1 / scale)),
+// along a row (rows), along 128 rows (cols, turned), and over 128 x 128 (blocks).
+//
+// All three stream: two or four bytes a value in, one a copy out.  A block's values
+// stay in registers between its maximum and its codes, so x is read once.  The
+// maximum is taken of the patterns without their signs, as whole numbers: they
+// order as the magnitudes do, and infinities and NaN come out on top, so that one
+// comparison a block finds them.
+#include "eqb_device.cuh"
+
+namespace eqb {
+
+namespace {
+
+constexpr uint32_t kAbs2 = 0x7fff7fffu;
+
+struct Scale {
+  float scale, inv;
+};
+// From the largest magnitude of a block.
+__device__ __forceinline__ Scale scale_of(float top) {
+  Scale s;
+  s.scale = __fmul_rn(top, 1.0f / 448.0f);
+  if (s.scale < 0x1p-126f) s.scale = 0.f;
+  s.inv = s.scale > 0.f ? __fdiv_rn(1.0f, s.scale) : 0.f;
+  return s;
+}
+// Two codes, lo in the low byte.  The conversion rounds to nearest even and keeps
+// what is above 448 there, so that the clamp is its own.
+__device__ __forceinline__ uint32_t code2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) { return code2(a, b) | code2(c, d) << 16; }
+
+// ---- rows.  A lane has 16 neighbours, eight lanes a block.
+constexpr int kRowWarps = 8;
+
+template <bool SLOT>
+__global__ void __launch_bounds__(kRowWarps * 32)
+    quant_rows_kernel(const uint16_t* __restrict__ x, int64_t T, int d, int strips, const int32_t* __restrict__ slot, int K,
+                      uint8_t* __restrict__ q, float* __restrict__ scale, int32_t* err) {
+  const int lane = threadIdx.x & 31, nb = (d + 127) / 128;
+  const int64_t items = T * strips, R = T * K;
+  griddep_wait();
+  for (int64_t it = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); it < items;
+       it += static_cast<int64_t>(gridDim.x) * kRowWarps) {
+    const int64_t t = it / strips;
+    const int j = static_cast<int>(it % strips) * 512 + lane * 16;
+    if (SLOT) {  // a token that no expert has is not looked at
+      bool any = false;
+      for (int k = lane; k < K; k += 32) {
+        const int r = __ldg(slot + t * K + k);
+        any |= r >= 0 && r < R;
+      }
+      if (!__any_sync(kFull, any)) continue;
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 0u;
+    if (j < d) {
+      const uint4* p = reinterpret_cast<const uint4*>(x + t * d + j);
+      const uint4 a = __ldg(p), b = __ldg(p + 1);
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+      w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & kAbs2);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(kFull, m, o));
+    const uint32_t top = max(m & 0xffffu, m >> 16);
+    if (top >= 0x7f80u) raise_flag(err, kErrNonfinite);
+    const Scale sc = scale_of(bf16_bits_to_f32(top));
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c[i] = code4(bf16_lo(w[2 * i]) * sc.inv, bf16_hi(w[2 * i]) * sc.inv, bf16_lo(w[2 * i + 1]) * sc.inv,
+                   bf16_hi(w[2 * i + 1]) * sc.inv);
+    if (j >= d) continue;
+    const uint4 out = make_uint4(c[0], c[1], c[2], c[3]);
+    if (!SLOT) {
+      *reinterpret_cast<uint4*>(q + t * d + j) = out;
+      if ((lane & 7) == 0) scale[t * nb + j / 128] = sc.scale;
+    } else {
+      for (int k = 0; k < K; ++k) {
+        const int64_t r = __ldg(slot + t * K + k);
+        if (r < 0 || r >= R) continue;
+        *reinterpret_cast<uint4*>(q + r * d + j) = out;
+        if ((lane & 7) == 0) scale[r * nb + j / 128] = sc.scale;
+      }
+    }
+  }
+}
+
+// The expert whose blocks contain block b (E if none): blocks[e] <= b < blocks[e + 1].
+// A warp looks at 32 experts at a time.
+__device__ __forceinline__ int expert_of_block(const int32_t* __restrict__ blocks, int E, int64_t b, int lane) {
+  for (int e0 = 0; e0 < E; e0 += 32) {
+    const int e = e0 + lane;
+    const uint32_t hit = __ballot_sync(kFull, e < E && b < __ldg(blocks + min(e, E - 1) + 1));
+    if (hit) return e0 + __ffs(hit) - 1;
+  }
+  return E;
+}
+
+// ---- cols.  A block of 256 threads takes 128 rows x 64 columns, a thread four
+// neighbouring rows x eight columns: four codes of a column are a word of the
+// output's line, which is turned in shared memory.
+constexpr int kColThreads = 256;
+
+__global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantColsArgs a) {
+  __shared__ uint32_t tops[8][32];     // of every warp: the largest patterns of 64 columns, two a word
+  __shared__ uint32_t tile[64][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int strips = (a.c + 63) / 64;
+  const int64_t b = blockIdx.x / strips;
+  const int cg = threadIdx.x & 7, rg = threadIdx.x >> 3, j0 = static_cast<int>(blockIdx.x % strips) * 64, j = j0 + cg * 8;
+  griddep_wait();
+  const int e = expert_of_block(a.blocks, a.E, b, lane);
+  if (e >= a.E) return;
+  const int64_t r0 = static_cast<int64_t>(__ldg(a.offsets + e)) + (b - __ldg(a.blocks + e)) * kExpertBlock;
+  const int64_t r1 = min(static_cast<int64_t>(__ldg(a.offsets + e + 1)), a.R);
+  uint32_t w[4][4];  // [row][pair of columns]
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    int64_t r = r0 + rg * 4 + i;
+    bool there = j < a.c && r >= 0 && r < r1;
+    if (there && a.entry) {
+      r = __ldg(a.entry + r);
+      there = r >= 0;
+      r /= a.K;
+    }
+    if (there && r < a.T) v = __ldg(reinterpret_cast<const uint4*>(a.x + r * a.c + j));
+    w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+  }
+  uint32_t m[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    m[p] = __vmaxu2(__vmaxu2(w[0][p] & kAbs2, w[1][p] & kAbs2), __vmaxu2(w[2][p] & kAbs2, w[3][p] & kAbs2));
+    m[p] = __vmaxu2(m[p], __shfl_xor_sync(kFull, m[p], 8));
+    m[p] = __vmaxu2(m[p], __shfl_xor_sync(kFull, m[p], 16));
+    if (lane < 8) tops[warp][cg * 4 + p] = m[p];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    uint32_t t = tops[0][cg * 4 + p];
+#pragma unroll
+    for (int v = 1; v < 8; ++v) t = __vmaxu2(t, tops[v][cg * 4 + p]);
+    const uint32_t lo = t & 0xffffu, hi = t >> 16;
+    if (max(lo, hi) >= 0x7f80u) raise_flag(a.err, kErrNonfinite);
+    const Scale s0 = scale_of(bf16_bits_to_f32(lo)), s1 = scale_of(bf16_bits_to_f32(hi));
+    tile[cg * 8 + 2 * p][rg] = code4(bf16_lo(w[0][p]) * s0.inv, bf16_lo(w[1][p]) * s0.inv, bf16_lo(w[2][p]) * s0.inv,
+                                     bf16_lo(w[3][p]) * s0.inv);
+    tile[cg * 8 + 2 * p + 1][rg] = code4(bf16_hi(w[0][p]) * s1.inv, bf16_hi(w[1][p]) * s1.inv, bf16_hi(w[2][p]) * s1.inv,
+                                         bf16_hi(w[3][p]) * s1.inv);
+    if (rg == 0 && j < a.c) {
+      a.scale[b * a.c + j + 2 * p] = s0.scale;
+      a.scale[b * a.c + j + 2 * p + 1] = s1.scale;
+    }
+  }
+  __syncthreads();
+  const int64_t pitch = a.P * kExpertBlock;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int col = i * 8 + warp;
+    if (j0 + col < a.c)
+      reinterpret_cast<uint32_t*>(a.q + (j0 + col) * pitch + b * kExpertBlock)[lane] = tile[col][lane];
+  }
+}
+
+// ---- blocks of 128 x 128.  A block of 256 threads takes one, a thread eight
+// rows x eight columns.
+template <bool F32>
+__global__ void __launch_bounds__(256)
+    quant_blocks_kernel(const void* __restrict__ w, int n, int d, uint8_t* __restrict__ q, float* __restrict__ scale,
+                        uint8_t* __restrict__ q_t, float* __restrict__ scale_t, int32_t* err) {
+  __shared__ uint32_t tops[8];
+  __shared__ uint32_t tile[128][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
+  const int jb = blockIdx.x, ib = blockIdx.y, e = blockIdx.z, nb = (n + 127) / 128, db = (d + 127) / 128;
+  const int j = jb * 128 + cg * 8, i0 = ib * 128 + rg * 8;
+  const int64_t base = static_cast<int64_t>(e) * n * d;
+  griddep_wait();
+  float v[8][8];
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool there = i0 + i < n && j < d;
+    const int64_t at = base + static_cast<int64_t>(i0 + i) * d + j;
+    if (F32) {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+      if (there) {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(w) + at);
+        x = __ldg(p);
+        y = __ldg(p + 1);
+      }
+      const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        m = max(m, u[k] & 0x7fffffffu);
+        v[i][k] = __uint_as_float(u[k]);
+      }
+    } else {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (there) x = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + at));
+      const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        m = max(m, max((u[k] << 16) & 0x7fffffffu, u[k] & 0x7fff0000u));
+        v[i][2 * k] = bf16_lo(u[k]);
+        v[i][2 * k + 1] = bf16_hi(u[k]);
+      }
+    }
+  }
+  m = __reduce_max_sync(kFull, m);
+  if (lane == 0) tops[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, tops[i]);
+  if (m >= 0x7f800000u && threadIdx.x == 0) raise_flag(err, kErrNonfinite);
+  const Scale sc = scale_of(__uint_as_float(m));
+  if (threadIdx.x == 0) {
+    scale[(static_cast<int64_t>(e) * nb + ib) * db + jb] = sc.scale;
+    if (scale_t) scale_t[(static_cast<int64_t>(e) * db + jb) * nb + ib] = sc.scale;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[i][k] = __fmul_rn(v[i][k], sc.inv);
+    if (i0 + i < n && j < d)
+      *reinterpret_cast<uint2*>(q + base + static_cast<int64_t>(i0 + i) * d + j) =
+          make_uint2(code4(v[i][0], v[i][1], v[i][2], v[i][3]), code4(v[i][4], v[i][5], v[i][6], v[i][7]));
+  }
+  if (!q_t) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    tile[cg * 8 + k][rg * 2] = code4(v[0][k], v[1][k], v[2][k], v[3][k]);
+    tile[cg * 8 + k][rg * 2 + 1] = code4(v[4][k], v[5][k], v[6][k], v[7][k]);
+  }
+  __syncthreads();
+  // a column of the block: 128 codes, 16 of them at least are there
+  for (int col = warp; col < 128; col += 8)
+    if (jb * 128 + col < d && ib * 128 + lane * 4 < n)
+      reinterpret_cast<uint32_t*>(q_t + base + static_cast<int64_t>(jb * 128 + col) * n + ib * 128)[lane] = tile[col][lane];
+}
+
+int status_of(cudaError_t e) { return e == cudaSuccess ? kOk : kErrCuda; }
+
+}  // namespace
+
+int launch_quant_rows(const uint16_t* x, int64_t T, int d, const int32_t* slot, int K, uint8_t* q, float* scale, int32_t* err,
+                      cudaStream_t s) {
+  DeviceInfo di;
+  if (int rc = device_info(&di)) return rc;
+  const int strips = (d + 511) / 512;
+  const int64_t blocks = (T * strips + kRowWarps - 1) / kRowWarps, most = static_cast<int64_t>(di.sm_count) * 64;
+  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most)), block(kRowWarps * 32);
+  return status_of(slot ? launch_dependent(quant_rows_kernel<true>, grid, block, 0, s, x, T, d, strips, slot, K, q, scale, err)
+                        : launch_dependent(quant_rows_kernel<false>, grid, block, 0, s, x, T, d, strips, slot, K, q, scale, err));
+}
+
+int launch_quant_cols(const QuantColsArgs& a, cudaStream_t s) {
+  const int64_t grid = a.P * ((a.c + 63) / 64);
+  if (grid > 0x7fffffff) return kErrUnsupported;
+  return status_of(launch_dependent(quant_cols_kernel, dim3(static_cast<unsigned>(grid)), dim3(kColThreads), 0, s, a));
+}
+
+int launch_quant_blocks(const void* w, int w_fp32, int E, int n, int d, uint8_t* q, float* scale, uint8_t* q_t, float* scale_t,
+                        int32_t* err, cudaStream_t s) {
+  const dim3 grid((d + 127) / 128, (n + 127) / 128, E);
+  return status_of(w_fp32 ? launch_dependent(quant_blocks_kernel<true>, grid, dim3(256), 0, s, w, n, d, q, scale, q_t, scale_t, err)
+                          : launch_dependent(quant_blocks_kernel<false>, grid, dim3(256), 0, s, w, n, d, q, scale, q_t, scale_t, err));
+}
+
+}  // namespace eqb
