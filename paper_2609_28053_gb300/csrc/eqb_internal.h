@@ -306,6 +306,9 @@ struct GateArgs {
   int32_t* err;
 };
 int launch_gate(const GateArgs& a, cudaStream_t s);
+// Many tokens, a thread each (gate_tile.cu).
+bool gate_tile_supported(const GateArgs& a);
+int launch_gate_tile(const GateArgs& a, cudaStream_t s);
 struct GateGradArgs {
   const void* z;
   int z_fp32;

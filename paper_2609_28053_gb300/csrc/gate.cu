@@ -10,12 +10,14 @@
 // selection is one maximum over the warp and one minimum over the experts that
 // have it.
 #include "eqb_device.cuh"
+#include "f32x2.cuh"
 
 namespace eqb {
 
 namespace {
 
 constexpr int kGateWarps = 4;
+constexpr int64_t kFewGateTokens = 8192;  // up to here a warp a token
 constexpr uint32_t kClosed = 0x007fffffu;  // the key of -inf: an open expert's is larger
 
 // Order-preserving key of a float; -0 as +0.
@@ -200,120 +202,156 @@ __global__ void __launch_bounds__(kGateWarps * 32) gate_warp_kernel(const GateAr
   }
 }
 
-// A warp a token.  The row is written from eight neighbouring experts a lane, then
-// the list's entries once more by the lanes that hold them (the barrier of the warp
-// between the two orders the stores).
-template <bool F32, bool BF16>
+// Sums and maxima over the LPT lanes of a token.
+template <int LPT, class F>
+__device__ __forceinline__ float lanes_all(float v, F f) {
+#pragma unroll
+  for (int o = LPT >> 1; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(kFull, v, o));
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float lanes_max(float v) {
+  return lanes_all<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LPT>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return lanes_all<LPT>(v, [](float a, float b) { return __fadd_rn(a, b); });
+}
+
+// The gradient.  LPT lanes take a token, eight neighbouring experts each and pass
+// (NC of them), and one entry of its list each.  The row is written from the
+// lanes' experts, then the list's entries once more by the lanes that hold them; the
+// barrier of the warp between the two orders the stores.
+template <int LPT, int NC, bool F32, bool BF16>
 __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGradArgs a) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E, K = a.K;
+  constexpr int kTokens = 32 / LPT;  // of a warp
+  constexpr float kLog2e = 1.4426950408889634f;
+  const int lane = threadIdx.x & 31, sub = lane % LPT, E = a.E, K = a.K;
   const bool dense = !a.sigmoid && !a.renorm;
   const bool in_place = a.grad_in && a.grad_out == static_cast<const void*>(a.grad_in);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGateWarps * kTokens;
   griddep_wait();
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kGateWarps + warp; t < a.T; t += static_cast<int64_t>(gridDim.x) * kGateWarps) {
+  // a warp's tokens leave the loop together
+  for (int64_t w0 = (static_cast<int64_t>(blockIdx.x) * kGateWarps + (threadIdx.x >> 5)) * kTokens; w0 < a.T; w0 += step) {
+    const int64_t t = w0 + lane / LPT;
+    const bool live = t < a.T;
+    float v[NC][8];
+    if (dense) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int e0 = (c * LPT + sub) * 8;
+        if (live && e0 < E) {
+          load8<F32>(a.z, t * E + e0, v[c]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[c][j] = -INFINITY;
+        }
+      }
+    }
     int e = -1;
     float g = 0.f, z = -INFINITY, old = 0.f;
-    if (lane < K) {
-      e = a.idx[t * K + lane];
+    if (live && sub < K) {
+      e = a.idx[t * K + sub];
       if (e < 0 || e >= E) e = -1;
     }
     if (e >= 0) {
-      g = a.gw[t * K + lane];
+      g = a.gw[t * K + sub];
       z = load1<F32>(a.z, t * E + e);
       if (a.grad_in) old = a.grad_in[t * E + e];
     }
-    const bool any = __any_sync(kFull, e >= 0);
-    float d = 0.f, zmax = -INFINITY, rest = 0.f;  // rest: -scale gb / sum, the factor of exp(z_j - zmax) for every j
-    if (any) {
-      if (dense) {
-        float sum = 0.f;
-        for (int e0 = lane * 8; e0 < E; e0 += 256) {
-          float v[8];
-          load8<F32>(a.z, t * E + e0, v);
-          float top = v[0];
+    const uint32_t mine = LPT == 32 ? kFull : ((1u << (LPT & 31)) - 1u) << (lane / LPT * LPT);
+    const bool any = (__ballot_sync(kFull, e >= 0) & mine) != 0u;
+    // lanes of the token with the same expert: its terms are added, in the list's order, by the first
+    const uint32_t same = __match_any_sync(kFull, e >= 0 ? e * kTokens + lane / LPT : -1 - lane);
+    float d = 0.f;
+    if (dense) {
+      float top = -INFINITY;
 #pragma unroll
-          for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j]);
-          const float m = fmaxf(zmax, top);
-          if (m > -INFINITY) {
-            sum = sum * expf(zmax - m);
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = sum + expf(v[j] - m);
-            zmax = m;
-          }
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, v[c][j]);
+      top = lanes_max<LPT>(top);
+      const float ref = top > -INFINITY ? top : 0.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[c][j] = ex2_approx((v[c][j] - ref) * kLog2e);
+          sum = sum + v[c][j];
         }
-        const float m = warp_max(zmax);
-        sum = warp_sum(zmax > -INFINITY ? sum * expf(zmax - m) : 0.f);
-        zmax = m;
-        const float p = e >= 0 && m > -INFINITY ? expf(z - m) / sum : 0.f;
-        const float gb = warp_sum(p * g);
-        rest = m > -INFINITY ? -(gb * a.scale) / sum : 0.f;
-        // an expert named twice: its g's added, gb taken off once
-        float both = g;
-        bool first = true;
-        for (int k = 0; k < K; ++k) {
-          const int ek = __shfl_sync(kFull, e, k);
+      sum = lanes_sum<LPT>(sum);
+      const float f = sum > 0.f ? __fdiv_rn(1.f, sum) : 0.f;
+      const float p = e >= 0 ? ex2_approx((z - ref) * kLog2e) * f : 0.f;
+      const float gb = lanes_sum<LPT>(e >= 0 ? p * g : 0.f);
+      const float rest = any ? -(gb * a.scale) * f : 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[c][j] = any ? v[c][j] * rest : 0.f;
+      d = g;
+      if (__any_sync(kFull, same & (same - 1u))) {
+        d = 0.f;
+        for (int k = 0; k < 32; ++k) {
           const float gk = __shfl_sync(kFull, g, k);
-          if (k != lane && ek == e && e >= 0) {
-            both = both + gk;
-            first &= k > lane;
-          }
+          if (same >> k & 1u) d = d + gk;
         }
-        d = p * (both - gb) * a.scale;
-        if (!first) e = -1;
+      }
+      d = p * (d - gb) * a.scale;
+    } else {
+      const float s1 = 1.f / (1.f + expf(z));  // 1 - s
+      if (!a.renorm) {
+        d = e >= 0 ? g * (1.f / (1.f + expf(-z))) * s1 * a.scale : 0.f;
       } else {
-        if (!a.renorm) {
-          const float s = 1.f / (1.f + expf(-z));
-          d = e >= 0 ? g * s * (1.f / (1.f + expf(z))) * a.scale : 0.f;
-        } else {
-          const float w = a.sigmoid ? sigmoid_share(z) : softmax_share(z);
-          const float gb = warp_sum(w * g);
-          d = e >= 0 ? w * (g - gb) * a.scale : 0.f;
-          if (a.sigmoid) d = d * (1.f / (1.f + expf(z)));
-        }
-        float both = d;
-        bool first = true;
-        for (int k = 0; k < K; ++k) {
-          const int ek = __shfl_sync(kFull, e, k);
+        const float m = lanes_max<LPT>(z), ref = a.sigmoid ? fminf(m, 0.f) : m;
+        float u = 0.f;
+        if (e >= 0 && m > -INFINITY) u = !a.sigmoid ? expf(z - ref) : z > 0.f ? 1.f / (1.f + expf(-z)) : expf(z - ref) * s1;
+        const float sum = lanes_sum<LPT>(u);
+        const float w = sum > 0.f ? u / sum : 0.f;
+        const float gb = lanes_sum<LPT>(e >= 0 ? w * g : 0.f);
+        d = e >= 0 ? w * (g - gb) * a.scale : 0.f;
+        if (a.sigmoid) d = d * s1;
+      }
+      if (__any_sync(kFull, same & (same - 1u))) {
+        float both = 0.f;
+        for (int k = 0; k < 32; ++k) {
           const float dk = __shfl_sync(kFull, d, k);
-          if (k != lane && ek == e && e >= 0) {
-            both = both + dk;
-            first &= k > lane;
-          }
+          if (same >> k & 1u) both = both + dk;
         }
         d = both;
-        if (!first) e = -1;
       }
     }
-    if (!(in_place && (!dense || !any))) {
-      for (int e0 = lane * 8; e0 < E; e0 += 256) {
-        float v[8];
+    if (!in_place || dense) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        if (dense && any) {
-          load8<F32>(a.z, t * E + e0, v);
+      for (int c = 0; c < NC; ++c) {
+        const int e0 = (c * LPT + sub) * 8;
+        if (!live || e0 >= E) continue;
+        if (!dense) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = v[j] > -INFINITY ? expf(v[j] - zmax) * rest : 0.f;
+          for (int j = 0; j < 8; ++j) v[c][j] = 0.f;
         }
         if (a.grad_in) {
           const float4* p = reinterpret_cast<const float4*>(a.grad_in + t * E + e0);
           const float4 x = p[0], y = p[1];
-          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-          v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+          v[c][0] += x.x; v[c][1] += x.y; v[c][2] += x.z; v[c][3] += x.w;
+          v[c][4] += y.x; v[c][5] += y.y; v[c][6] += y.z; v[c][7] += y.w;
         }
         if (BF16) {
           *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.grad_out) + t * E + e0) =
-              make_uint4(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]), pack_bf16x2_rn(v[4], v[5]), pack_bf16x2_rn(v[6], v[7]));
+              make_uint4(pack_bf16x2_rn(v[c][0], v[c][1]), pack_bf16x2_rn(v[c][2], v[c][3]), pack_bf16x2_rn(v[c][4], v[c][5]),
+                         pack_bf16x2_rn(v[c][6], v[c][7]));
         } else {
           float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.grad_out) + t * E + e0);
-          p[0] = make_float4(v[0], v[1], v[2], v[3]);
-          p[1] = make_float4(v[4], v[5], v[6], v[7]);
+          p[0] = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
+          p[1] = make_float4(v[c][4], v[c][5], v[c][6], v[c][7]);
         }
       }
       __syncwarp();
     }
-    if (e >= 0) {
-      const float v = old + d;
-      if (BF16) static_cast<uint16_t*>(a.grad_out)[t * E + e] = static_cast<uint16_t>(pack_bf16x2_rn(v, 0.f));
-      else static_cast<float*>(a.grad_out)[t * E + e] = v;
+    if (e >= 0 && lane == __ffs(same) - 1) {
+      const float x = old + d;
+      if (BF16) static_cast<uint16_t*>(a.grad_out)[t * E + e] = static_cast<uint16_t>(pack_bf16x2_rn(x, 0.f));
+      else static_cast<float*>(a.grad_out)[t * E + e] = x;
     }
   }
 }
@@ -330,11 +368,25 @@ int warp_grid(int64_t T, const DeviceInfo& di) {
   return static_cast<int>(blocks < most ? blocks : most);
 }
 
+template <int LPT, int NC>
+int launch_gate_grad_t(const GateGradArgs& a, const DeviceInfo& di, cudaStream_t s) {
+  const dim3 grid(warp_grid((a.T + 32 / LPT - 1) / (32 / LPT), di)), block(kGateWarps * 32);
+  cudaError_t e;
+  if (a.z_fp32)
+    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, true, true>, grid, block, 0, s, a)
+                    : launch_dependent(gate_grad_kernel<LPT, NC, true, false>, grid, block, 0, s, a);
+  else
+    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, false, true>, grid, block, 0, s, a)
+                    : launch_dependent(gate_grad_kernel<LPT, NC, false, false>, grid, block, 0, s, a);
+  return e == cudaSuccess ? kOk : kErrCuda;
+}
+
 }  // namespace
 
 int launch_gate(const GateArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
+  if (a.T > kFewGateTokens && gate_tile_supported(a)) return launch_gate_tile(a, s);
   const int grid = warp_grid(a.T, di);
   if (a.E <= 256) return launch_gate_warp<1>(a, grid, s);
   if (a.E <= 512) return launch_gate_warp<2>(a, grid, s);
@@ -344,15 +396,13 @@ int launch_gate(const GateArgs& a, cudaStream_t s) {
 int launch_gate_grad(const GateGradArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  const dim3 grid(warp_grid(a.T, di)), block(kGateWarps * 32);
-  cudaError_t e;
-  if (a.z_fp32)
-    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<true, true>, grid, block, 0, s, a)
-                    : launch_dependent(gate_grad_kernel<true, false>, grid, block, 0, s, a);
-  else
-    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<false, true>, grid, block, 0, s, a)
-                    : launch_dependent(gate_grad_kernel<false, false>, grid, block, 0, s, a);
-  return e == cudaSuccess ? kOk : kErrCuda;
+  int lanes = 8;  // of a token: as many as its list has entries, and a pass for its experts
+  while (lanes < 32 && (lanes * 8 < a.E || lanes < a.K)) lanes *= 2;
+  if (lanes == 8) return launch_gate_grad_t<8, 1>(a, di, s);
+  if (lanes == 16) return launch_gate_grad_t<16, 1>(a, di, s);
+  if (a.E <= 256) return launch_gate_grad_t<32, 1>(a, di, s);
+  if (a.E <= 512) return launch_gate_grad_t<32, 2>(a, di, s);
+  return launch_gate_grad_t<32, 4>(a, di, s);
 }
 
 }  // namespace eqb

@@ -1,0 +1,396 @@
+// gate_tile.cu -- the gate of many tokens (see gate.cu): a thread takes a token
+// whose row of z lies in shared memory, a warp a tile of 32 tokens.
+//
+// The row is cut into eight parts, each within a group:
+//   1. the two largest c = z + b of every part, in pairs: exact (fp32), so the
+//      groups' scores and their ranking are too;
+//   2. of the parts that stay open, the eighth largest of their two largest is a
+//      lower bound of the K-th largest c (K <= 8): two sorts of eight and a merge;
+//   3. a bit for every open expert at or above the bound (about 13 of 128 for K = 8);
+//   4. those are inserted in ascending order into a sorted list.
+// Phases 1 and 3 take four to five instructions a value, phase 4 about fifty a
+// candidate of the lane that has most.  A thread a token needs about a tenth of
+// the instructions of a warp a token (gate.cu), which waits for every maximum of
+// the warp.
+//
+// Lanes bring their rows with bulk copies (a barrier a warp), at a stride of 4
+// (mod 8) words so that the lanes' 16-byte reads of one column hit distinct banks.
+#include <float.h>
+
+#include "f32x2.cuh"
+#include "route_wide.cuh"
+
+namespace eqb {
+
+namespace {
+
+constexpr int kParts = 8;
+constexpr int kMaxGateWarps = 16;
+
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// The two largest of two pairs of the two largest.  NaN stays in the first.
+__device__ __forceinline__ void merge2(float& m1, float& m2, float h, float l) {
+  const float lo = fminf(m1, h);
+  m2 = max3(lo, m2, l);
+  m1 = fmax_nan(m1, h);
+}
+
+template <bool F32>
+__device__ __forceinline__ void row8(const uint8_t* row, int chunk, F2 (&v)[4]) {
+  if (F32) {
+    const float4 x = *reinterpret_cast<const float4*>(row + 32 * chunk), y = *reinterpret_cast<const float4*>(row + 32 * chunk + 16);
+    v[0] = f2(x.x, x.y);
+    v[1] = f2(x.z, x.w);
+    v[2] = f2(y.x, y.y);
+    v[3] = f2(y.z, y.w);
+  } else {
+    const uint4 x = lds128(row + 16 * chunk);
+    v[0] = f2(bf16_lo(x.x), bf16_hi(x.x));
+    v[1] = f2(bf16_lo(x.y), bf16_hi(x.y));
+    v[2] = f2(bf16_lo(x.z), bf16_hi(x.z));
+    v[3] = f2(bf16_lo(x.w), bf16_hi(x.w));
+  }
+}
+template <bool F32>
+__device__ __forceinline__ float row1(const uint8_t* row, int e) {
+  return F32 ? *reinterpret_cast<const float*>(row + 4 * e) : bf16_bits_to_f32(lds_u16(row + 2 * e));
+}
+__device__ __forceinline__ void add_bias(F2 (&v)[4], const float* bs, int chunk) {
+  const float4 x = *reinterpret_cast<const float4*>(bs + 8 * chunk), y = *reinterpret_cast<const float4*>(bs + 8 * chunk + 4);
+  v[0] = add2(v[0], f2(x.x, x.y));
+  v[1] = add2(v[1], f2(x.z, x.w));
+  v[2] = add2(v[2], f2(y.x, y.y));
+  v[3] = add2(v[3], f2(y.z, y.w));
+}
+
+struct GateTile {
+  int stride;  // bytes of a staged row
+  int warp_bytes, words;  // words: mask words of a part
+  int64_t tiles_per_warp;
+};
+
+// First chunk (of eight experts) of part s, with groups of gc chunks in SP parts.
+template <int SP>
+__device__ __forceinline__ int part_chunk(int s, int gc) {
+  return s / SP * gc + s % SP * gc / SP;
+}
+
+template <bool F32, int G, int KP>
+__global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const GateArgs a, const GateTile g) {
+  constexpr int SP = kParts / G;  // parts of a group
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const int E = a.E, K = a.K, gc = E / 8 / G, cmax = (gc + SP - 1) / SP;
+  float* bs = reinterpret_cast<float*>(smem);
+  uint8_t* mine = smem + 4 * E + wid * g.warp_bytes;
+  uint32_t* mw = reinterpret_cast<uint32_t*>(mine + 32 * g.stride) + lane;  // [part][words][32 lanes]
+  const uint32_t bar = saddr(mine + 32 * g.stride + kParts * g.words * 128);
+  const uint8_t* row = mine + lane * g.stride;
+  const int row_bytes = E * (F32 ? 4 : 2);
+  if (lane == 0) {
+    bar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  griddep_wait();
+  for (int e = threadIdx.x; e < E; e += blockDim.x) bs[e] = a.b ? a.b[e] : 0.f;
+  __syncthreads();
+  const int64_t ntiles = (a.T + 31) >> 5;
+  const int64_t tb = (static_cast<int64_t>(blockIdx.x) * nw + wid) * g.tiles_per_warp, te = min(tb + g.tiles_per_warp, ntiles);
+  if (tb >= te) return;
+  const uint8_t* z = static_cast<const uint8_t*>(a.z);
+  auto load_tile = [&](int64_t tl) {
+    const int64_t t0 = tl << 5;
+    const int rows = static_cast<int>(min(static_cast<int64_t>(32), a.T - t0));
+    if (lane == 0) bar_expect_tx(bar, static_cast<uint32_t>(rows * row_bytes));
+    __syncwarp();
+    if (lane < rows) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bulk_copy(saddr(mine + lane * g.stride), z + (t0 + lane) * row_bytes, row_bytes, bar);
+    }
+  };
+  auto prefetch = [&](int64_t tl) {
+    if (lane == 0 && tl < te) {
+      const int64_t t0 = tl << 5;
+      const uint32_t bytes = static_cast<uint32_t>(min(static_cast<int64_t>(32), a.T - t0) * row_bytes);
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(z + t0 * row_bytes), "r"(bytes) : "memory");
+    }
+  };
+  uint32_t phase = 0;
+  load_tile(tb);
+  prefetch(tb + 1);
+  for (int64_t tl = tb; tl < te; ++tl) {
+    if (!__all_sync(kFull, bar_wait_bounded(bar, phase, kRouteWaitLimit))) {
+      raise_flag(a.err, kErrCuda);
+      bar_wait_bounded(bar, phase, kRouteWaitLimit);
+      return;
+    }
+    phase ^= 1u;
+    const int64_t t = (tl << 5) + lane;
+    const bool valid = t < a.T && (!a.mask || a.mask[t]);
+
+    // ---- 1: the parts' two largest
+    float m1[kParts], m2[kParts];
+    bool bad = false;
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+      m1[s] = m2[s] = -INFINITY;
+      const int c1 = part_chunk<SP>(s + 1, gc);
+      for (int c = part_chunk<SP>(s, gc); c < c1; ++c) {
+        F2 v[4];
+        row8<F32>(row, c, v);
+        add_bias(v, bs, c);
+        float h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[i] = fmax_nan(lo2(v[i]), hi2(v[i]));
+          l[i] = fminf(lo2(v[i]), hi2(v[i]));
+        }
+        merge2(h[0], l[0], h[1], l[1]);
+        merge2(h[2], l[2], h[3], l[3]);
+        merge2(h[0], l[0], h[2], l[2]);
+        merge2(m1[s], m2[s], h[0], l[0]);
+      }
+      bad |= !(m1[s] < INFINITY);
+    }
+    if (valid && bad) raise_flag(a.err, kErrNonfinite);
+
+    // ---- the groups' ranking: bits of the open parts
+    uint32_t open = (1u << kParts) - 1u;
+    if (G > 1 && a.top_groups < G) {
+      float score[G];
+      int ahead[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        float h = m1[i * SP], l = m2[i * SP];
+#pragma unroll
+        for (int j = 1; j < SP; ++j) merge2(h, l, m1[i * SP + j], m2[i * SP + j]);
+        score[i] = a.top2 && l > -INFINITY ? __fadd_rn(h, l) : h;
+        ahead[i] = 0;
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int j = i + 1; j < G; ++j) {
+          const bool later = score[j] > score[i];
+          ahead[i] += later;
+          ahead[j] += !later;
+        }
+      open = 0u;
+#pragma unroll
+      for (int i = 0; i < G; ++i) open |= ahead[i] < a.top_groups ? ((1u << SP) - 1u) << (i * SP) : 0u;
+    }
+
+    // ---- 2: a lower bound of the K-th largest
+    float bound = INFINITY;
+    {
+#pragma unroll
+      for (int s = 0; s < kParts; ++s)
+        if (!(open >> s & 1u)) m1[s] = m2[s] = -INFINITY;
+      sort_desc<kParts>(m1);
+      sort_desc<kParts>(m2);
+#pragma unroll
+      for (int i = 0; i < KP; ++i) bound = fminf(bound, fmaxf(m1[i], m2[KP - 1 - i]));
+      bound = fmaxf(bound, -FLT_MAX);  // a closed expert is never chosen
+    }
+
+    // ---- 3: who is at or above it; the sign of c - bound, eight chunks' bits a word
+    uint32_t hits = 0u;
+    if (!valid) open = 0u;
+    {
+      const F2 less = splat2(-bound);
+      const int parts = a.top_groups < G ? a.top_groups * SP : kParts;
+      uint32_t left = open;
+      for (int j = 0; j < parts; ++j) {
+        const int s = left ? __ffs(left) - 1 : 0;
+        const bool there = left != 0u;
+        left &= left - 1u;
+        const int c0 = part_chunk<SP>(s, gc), c1 = part_chunk<SP>(s + 1, gc);
+        for (int w = 0; w < g.words; ++w) {
+          uint32_t word = 0u;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int c = c0 + 4 * w + u;
+            uint32_t bits = 0xffu;  // signs: set where it is below
+            if (4 * w + u < cmax && c < c1 && there) {
+              F2 v[4];
+              row8<F32>(row, c, v);
+              add_bias(v, bs, c);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const F2 d = add2(v[i], less);
+                bits = __funnelshift_l(__float_as_uint(lo2(d)), bits, 1);
+                bits = __funnelshift_l(__float_as_uint(hi2(d)), bits, 1);
+              }
+            }
+            word = word << 8 | (~bits & 0xffu);
+          }
+          if (there) mw[(s * g.words + w) << 5] = word;
+          hits |= there && word != 0u ? 0x80000000u >> (s * g.words + w) : 0u;
+        }
+      }
+    }
+    // ---- 4: the candidates in ascending order
+    float v[KP];
+    int id[KP];
+#pragma unroll
+    for (int j = 0; j < KP; ++j) {
+      v[j] = -INFINITY;
+      id[j] = -1;
+    }
+    uint32_t m = 0u;
+    int wb = 0;
+    auto fetch = [&]() -> int {
+      if (m == 0u && hits != 0u) {
+        const int k = __clz(hits);
+        hits ^= 0x80000000u >> k;
+        m = mw[k << 5];
+        const int s = g.words == 1 ? k : k >> 1;
+        wb = (part_chunk<SP>(s, gc) + (g.words == 1 ? 0 : (k & 1) * 4)) * 8;
+      }
+      const int p = __clz(m);
+      const int e = m != 0u ? wb + p : -1;
+      m &= shr_clamp(0x7fffffffu, p);
+      return e;
+    };
+    int e0 = fetch();
+    while (__any_sync(kFull, e0 >= 0)) {
+      const int e1 = fetch();
+      const int at = max(e0, 0);
+      insert_sorted<KP>(v, id, e0 >= 0 ? __fadd_rn(row1<F32>(row, at), bs[at]) : -INFINITY, e0);
+      e0 = e1;
+    }
+    // after a NaN (flagged) a finished lane's entry can stand before others; it is -1
+
+    // ---- the weights
+    float w[KP];
+    if (a.weight) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < KP; ++j) {
+        w[j] = id[j] >= 0 && j < K ? row1<F32>(row, id[j]) : -INFINITY;
+        top = fmaxf(top, w[j]);
+      }
+      float sum = 0.f;
+      if (a.sigmoid) {
+        // relative to exp(min(0, top)) where they are renormalised: see gate.cu
+        const float ref = a.renorm && top > -INFINITY ? fminf(top, 0.f) : 0.f;
+#pragma unroll
+        for (int j = 0; j < KP; ++j) {
+          const float n = expf(-fabsf(w[j])), r = __fdividef(1.f, 1.f + n);
+          w[j] = w[j] > 0.f ? r : (a.renorm ? expf(w[j] - ref) : n) * r;
+          sum = sum + w[j];
+        }
+      } else if (a.renorm) {
+#pragma unroll
+        for (int j = 0; j < KP; ++j) {
+          w[j] = w[j] > -INFINITY ? expf(w[j] - top) : 0.f;
+          sum = sum + w[j];
+        }
+      } else {
+        // the sum over the whole row, relative to its largest logit
+        float zm = -INFINITY;
+        for (int c = 0; c < E / 8; ++c) {
+          F2 x[4];
+          row8<F32>(row, c, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) zm = max3(zm, lo2(x[i]), hi2(x[i]));
+        }
+        constexpr float kLog2e = 1.4426950408889634f;
+        const float ref = zm > -INFINITY ? zm : 0.f;
+        F2 acc[4] = {splat2(0.f), splat2(0.f), splat2(0.f), splat2(0.f)};
+        for (int c = 0; c < E / 8; ++c) {
+          F2 x[4];
+          row8<F32>(row, c, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const F2 d = mul2(sub2(x[i], splat2(ref)), splat2(kLog2e));
+            acc[i] = add2(acc[i], f2(ex2_approx(lo2(d)), ex2_approx(hi2(d))));
+          }
+        }
+        const F2 all = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
+        sum = lo2(all) + hi2(all);
+#pragma unroll
+        for (int j = 0; j < KP; ++j) w[j] = w[j] > -INFINITY ? expf(w[j] - ref) : 0.f;
+      }
+      const float f = a.sigmoid && !a.renorm ? a.scale : sum > 0.f ? __fdiv_rn(a.scale, sum) : 0.f;
+#pragma unroll
+      for (int j = 0; j < KP; ++j) w[j] = w[j] * f;
+    }
+    __syncwarp();  // every lane is done with the tile
+    if (tl + 1 < te) {
+      load_tile(tl + 1);
+      prefetch(tl + 2);
+    }
+    if (t < a.T) {
+      int32_t* idx = a.idx + t * K;
+      float* out = a.weight ? a.weight + t * K : nullptr;
+      if (K == 8 && KP == 8 && (reinterpret_cast<uintptr_t>(a.idx) & 15u) == 0 && (reinterpret_cast<uintptr_t>(a.weight) & 15u) == 0) {
+        reinterpret_cast<int4*>(idx)[0] = make_int4(id[0], id[1], id[2], id[3]);
+        reinterpret_cast<int4*>(idx)[1] = make_int4(id[4], id[5], id[6], id[7]);
+        if (out) {
+          reinterpret_cast<float4*>(out)[0] = make_float4(w[0], w[1], w[2], w[3]);
+          reinterpret_cast<float4*>(out)[1] = make_float4(w[4], w[5], w[6], w[7]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < KP; ++j)
+          if (j < K) {
+            idx[j] = id[j];
+            if (out) out[j] = w[j];
+          }
+      }
+    }
+  }
+}
+
+template <bool F32, int G>
+int launch_tile(const GateArgs& a, cudaStream_t s) {
+  DeviceInfo di;
+  if (int rc = device_info(&di)) return rc;
+  GateTile g;
+  const int words = a.E * (F32 ? 4 : 2) / 4;
+  g.stride = 4 * (words + ((4 - words) & 7));
+  const int gc = a.E / 8 / G, sp = kParts / G, cmax = (gc + sp - 1) / sp;
+  g.words = (cmax + 3) / 4;
+  g.warp_bytes = 32 * g.stride + kParts * g.words * 128 + 16;
+  const int head = 4 * a.E;
+  int most = (di.max_smem_optin - head) / g.warp_bytes;
+  if (most > kMaxGateWarps) most = kMaxGateWarps;
+  if (most < 1 || g.words > 2) return kErrUnsupported;
+  const int64_t ntiles = (a.T + 31) / 32;
+  int64_t nw = (ntiles + di.sm_count - 1) / di.sm_count;
+  if (nw > most) nw = most;
+  int64_t grid = (ntiles + nw - 1) / nw;
+  if (grid > di.sm_count) grid = di.sm_count;
+  g.tiles_per_warp = (ntiles + grid * nw - 1) / (grid * nw);
+  auto kern = gate_tile_kernel<F32, G, 8>;
+  if (!allow_smem(kern, di.max_smem_optin)) return kErrCuda;
+  return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(static_cast<unsigned>(nw) * 32),
+                          head + static_cast<int>(nw) * g.warp_bytes, s, a, g) == cudaSuccess
+             ? kOk
+             : kErrCuda;
+}
+
+template <bool F32>
+int launch_tile_groups(const GateArgs& a, cudaStream_t s) {
+  const int G = a.top_groups < a.groups ? a.groups : 1;
+  if (G == 1) return launch_tile<F32, 1>(a, s);
+  if (G == 2) return launch_tile<F32, 2>(a, s);
+  if (G == 4) return launch_tile<F32, 4>(a, s);
+  return launch_tile<F32, 8>(a, s);
+}
+
+}  // namespace
+
+bool gate_tile_supported(const GateArgs& a) {
+  const int G = a.top_groups < a.groups ? a.groups : 1;
+  return a.K <= 8 && a.E <= 512 && a.E >= 64 && (G == 1 || G == 2 || G == 4 || G == 8) && a.E / 8 % G == 0;
+}
+
+int launch_gate_tile(const GateArgs& a, cudaStream_t s) {
+  return a.z_fp32 ? launch_tile_groups<true>(a, s) : launch_tile_groups<false>(a, s);
+}
+
+}  // namespace eqb
