@@ -1,0 +1,454 @@
+// expert_mm.cuh -- what the kernels of the experts' products share
+// (expert_matmul.cu, expert_pair.cu): tiles and whose they are, the instruction of
+// 8-bit operands, the way from tensor memory into the sums, and the tensor maps.
+#pragma once
+
+#include "f32x2.cuh"
+#include "tcgen05.cuh"
+
+namespace eqb {
+
+namespace {
+
+// Warps 0 and 1 load and issue the MMAs, 2 and 3 bring the scales, 4 to 11 take
+// accumulators out.
+constexpr int kMmThreads = 384;
+// Registers a thread at the launch, and of both kinds of warpgroups after the
+// split of the widest tiles (which keep 128 sums a thread): what the launch has.
+constexpr int kMmRegs = 168, kMmFew = 72, kMmMany = 216;
+static_assert(128 * kMmFew + 256 * kMmMany <= kMmThreads * kMmRegs, "more registers than the launch has");
+constexpr uint32_t kATile = 128 * 128;  // bytes of A's part of a stage
+constexpr int kMmWarps = 8;             // that take accumulators out
+
+// Instruction descriptor, kind::f8f6f4: fp32 accumulator, A and B e4m3 (0), both K-major.
+__host__ __device__ constexpr uint32_t umma_idesc_e4m3(int M, int N) {
+  return (1u << 4) | ((static_cast<uint32_t>(N) >> 3) << 17) | ((static_cast<uint32_t>(M) >> 4) << 24);
+}
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void store_sector8(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+struct MmArgs {
+  const float* a_scale;
+  const float* b_scale;
+  const int32_t* first;  // [E+1]: rows (forward) or blocks (weights)
+  int64_t limit;         // rows of A, or blocks
+  int E, n, k;           // columns of the output; forward: of K
+  int rows;              // weights: rows of a tile's matrix
+  int nt, mt;            // tiles along the columns; weights: along the rows
+  int S;
+  int most;              // tiles that there can be
+  void* out;
+  int out_fp32, add;
+  int32_t* err;
+};
+
+// A tile: expert, first row, rows, first block of K and blocks of it.
+struct Tile {
+  int e, m, rows, n0, b0, kb;
+};
+
+// What the tiles of a call are, in shared memory: read from `first` once, so that a
+// tile's start waits for no memory.
+struct Table {
+  int tiles[kMaxExperts + 1];  // forward: tiles of the experts before
+  int lo[kMaxExperts], n[kMaxExperts];  // first row and rows, or blocks
+};
+
+// Tile t; *e moves on to the tile's expert (tiles come in ascending order).
+template <int BM, int BN, bool WG>
+__device__ __forceinline__ Tile tile_of(const MmArgs& a, const Table& table, int t, int* e) {
+  Tile x;
+  if (WG) {
+    const int per = a.nt * a.mt;
+    x.e = t / per;
+    const int rest = t - x.e * per, mt = rest / a.nt;
+    x.m = mt * BM;
+    x.n0 = (rest - mt * a.nt) * BN;
+    x.rows = min(BM, a.rows - x.m);
+    x.b0 = table.lo[x.e];
+    x.kb = table.n[x.e];
+  } else {
+    const int mt = t / a.nt;
+    while (table.tiles[*e + 1] <= mt) ++*e;
+    x.e = *e;
+    x.n0 = (t - mt * a.nt) * BN;
+    const int first = (mt - table.tiles[x.e]) * BM;
+    x.m = table.lo[x.e] + first;
+    x.rows = min(BM, table.n[x.e] - first);
+    x.b0 = 0;
+    x.kb = (a.k + 127) / 128;
+  }
+  return x;
+}
+
+// Fills the table by the block's threads: `first` is kept within [0, limit] and in order
+// whatever it says; tiles add up to at most 2^30.
+template <int BM>
+__device__ __forceinline__ void fill_table(const MmArgs& a, Table& table) {
+  constexpr int kMost = 1 << 30;
+  const int lane = threadIdx.x & 31, limit = static_cast<int>(a.limit);
+  for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
+    const int lo = min(max(__ldg(a.first + e), 0), limit), n = min(max(__ldg(a.first + e + 1), lo), limit) - lo;
+    table.lo[e] = lo;
+    table.n[e] = n;
+    table.tiles[e + 1] = (n + BM - 1) / BM;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    int run = 0;
+    if (lane == 0) table.tiles[0] = 0;
+    for (int e0 = 0; e0 < a.E; e0 += 32) {
+      int v = e0 + lane < a.E ? table.tiles[e0 + lane + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, v, o);
+        if (lane >= o) v = min(v + y, kMost);
+      }
+      if (e0 + lane < a.E) table.tiles[e0 + lane + 1] = min(run + v, kMost);
+      run = min(run + __shfl_sync(kFull, v, 31), kMost);
+    }
+  }
+}
+// The tiles of a table.
+__device__ __forceinline__ int tiles_of(const MmArgs& a, const Table& table) {
+  const int64_t n = static_cast<int64_t>(table.tiles[a.E]) * a.nt;
+  return n < a.most ? static_cast<int>(n) : a.most;
+}
+
+// 32 or 16 columns of the warp's lanes, on their way until tmem_wait has returned.
+// The registers pass through it, or through tmem_here after it, so that no use of them
+// moves before it; and the loads that come again into the same registers take
+// their old values along, so that no use of those moves behind.
+__device__ __forceinline__ void tmem_start(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_again(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+        "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+        "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+        "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_start(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_again(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+        "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                 "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_here(uint32_t (&r)[16]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+
+// N columns of a stage, times f (and times the columns' own factors in cs), added to the sums.
+template <bool kColScale, int N>
+__device__ __forceinline__ void add_columns(const uint32_t (&r)[N], const F2& ff, const float* cs, F2* acc) {
+#pragma unroll
+  for (int v = 0; v < N / 2; ++v) {
+    F2 d = f2(__uint_as_float(r[2 * v]), __uint_as_float(r[2 * v + 1]));
+    if (kColScale) {
+      const float2 s = *reinterpret_cast<const float2*>(cs + 2 * v);
+      d = mul2(d, f2(s.x, s.y));
+    }
+    acc[v] = fma2(d, ff, acc[v]);
+  }
+}
+
+// Takes kCols columns of the warp's lanes out of tensor memory and adds them to the
+// sums; `release` runs as soon as the last of them are in registers.  A wait is for
+// all loads on their way and takes about 130 cycles however much was asked for, so 48
+// columns share one (64 do not fit in registers beside 128 sums).
+template <int kCols, bool kColScale, class Release>
+__device__ __forceinline__ void add_stage(uint32_t taddr, float f, const float* cs, F2 (&acc)[kCols / 2], Release release) {
+  static_assert(kCols == 32 || kCols == 128, "columns of a warp");
+  const F2 ff = splat2(f);
+  uint32_t r[32];
+  tmem_start(taddr, r);
+  if constexpr (kCols == 32) {
+    tmem_wait(r);
+    release();
+    add_columns<kColScale>(r, ff, cs, acc);
+  } else {
+    uint32_t s[16];
+    tmem_start(taddr + 32u, s);
+    tmem_wait(r);
+    tmem_here(s);
+    add_columns<kColScale>(r, ff, cs, acc);
+    tmem_again(taddr + 48u, r);
+    add_columns<kColScale>(s, ff, cs + 32, acc + 16);
+    tmem_again(taddr + 80u, s);
+    tmem_wait(r);
+    tmem_here(s);
+    add_columns<kColScale>(r, ff, cs + 48, acc + 24);
+    tmem_again(taddr + 96u, r);
+    add_columns<kColScale>(s, ff, cs + 80, acc + 40);
+    tmem_wait(r);
+    release();
+    add_columns<kColScale>(r, ff, cs + 96, acc + 48);
+  }
+}
+
+// Up to 64 polls of at most ~1 us for the phase of parity `parity`, in one loop of
+// three instructions: where a step of the pipeline hangs on a phase that is there
+// already, what follows the poll counts.
+__device__ __forceinline__ uint32_t mbar_try64(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, more;\n\t.reg .u32 left;\n\t"
+      "mov.u32 left, 64;\n"
+      "again_%=:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "@p bra there_%=;\n\t"
+      "sub.u32 left, left, 1;\n\t"
+      "setp.ne.u32 more, left, 0;\n\t"
+      "@more bra again_%=;\n"
+      "there_%=:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(1000u)
+      : "memory");
+  return ok;
+}
+// Bounded wait of a whole warp, false when it ran out or another role aborted.  The
+// abort word by its address in shared memory: it takes fewer registers.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_word) {
+  if (__all_sync(kFull, mbar_try64(bar, parity))) return true;
+  for (uint32_t i = 0; i < kSpinLimit / 64; ++i) {
+    int gone;
+    asm volatile("ld.volatile.shared.s32 %0, [%1];" : "=r"(gone) : "r"(abort_word) : "memory");
+    if (__any_sync(kFull, gone)) return false;
+    if (__all_sync(kFull, mbar_try64(bar, parity))) return true;
+  }
+  asm volatile("st.volatile.shared.s32 [%0], %1;" ::"r"(abort_word), "r"(1) : "memory");
+  return false;
+}
+// One lane of a whole warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ float lds_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// The warp's lanes' sums, a row a lane, to its kCols columns of the output from
+// `col` on, a whole sector a store.
+template <int kCols, bool WG>
+__device__ __forceinline__ void store_row(const MmArgs& a, int64_t row, int col, F2 (&acc)[kCols / 2]) {
+  const int64_t at = row * a.n + col;
+  if (!WG && !a.out_fp32) {
+    uint16_t* o = static_cast<uint16_t*>(a.out) + at;
+#pragma unroll
+    for (int i = 0; i < kCols / 16; ++i)
+      if (col + i * 16 < a.n) {
+        uint32_t p[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) p[v] = pack_bf16x2_rn(lo2(acc[i * 8 + v]), hi2(acc[i * 8 + v]));
+        store_sector8(o + i * 16, p);
+      }
+    return;
+  }
+  float* o = static_cast<float*>(a.out) + at;
+#pragma unroll
+  for (int i = 0; i < kCols / 8; ++i)
+    if (col + i * 8 < a.n) {
+      uint32_t p[8];
+      if (WG && a.add) {
+        const float4 u = *reinterpret_cast<const float4*>(o + i * 8), v = *reinterpret_cast<const float4*>(o + i * 8 + 4);
+        acc[i * 4] = add2(acc[i * 4], f2(u.x, u.y));
+        acc[i * 4 + 1] = add2(acc[i * 4 + 1], f2(u.z, u.w));
+        acc[i * 4 + 2] = add2(acc[i * 4 + 2], f2(v.x, v.y));
+        acc[i * 4 + 3] = add2(acc[i * 4 + 3], f2(v.z, v.w));
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        p[2 * v] = __float_as_uint(lo2(acc[i * 4 + v]));
+        p[2 * v + 1] = __float_as_uint(hi2(acc[i * 4 + v]));
+      }
+      store_sector8(o + i * 8, p);
+    }
+}
+
+// The factors of a stage, in shared memory: of each half of the columns, of every
+// row (forward: both scales' product), or of the rows and of the columns (weights).
+template <int BN, bool WG>
+struct Factors {
+  static_assert(!WG || BN == 256, "a warp brings the factors of 2 x 128 columns");
+  float row[WG ? 1 : 2][kBM];
+  float col[WG ? BN : 4];
+};
+
+// Warps 2 (h = 0) and 3 (h = 1): the factors of one tile's stages into `ring`, two
+// stages deep, each loaded from memory two stages before it is written.  ring[buf]
+// may be written once `freed(buf)` has a phase for it, and adds its arrival to what
+// `ready(buf)` waits for.  False when a wait ran out.
+template <int BN, bool WG, class Freed, class Ready>
+__device__ __forceinline__ bool bring_factors(const MmArgs& a, const Tile& x, int row0, int h, int lane, Factors<BN, WG>* ring,
+                                              int* chunk, Freed freed, Ready ready, uint32_t gone) {
+  // forward: rows lane, lane + 32, ... of a, and half h's scale of b;
+  // weights: the same rows of a (h = 0), or 2 x 4 columns of b (h = 1)
+  const float* pa[4];
+  bool la[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = row0 + i * 32 + lane;
+    la[i] = row < x.rows && (!WG || h == 0);
+    pa[i] = WG ? a.a_scale + static_cast<int64_t>(x.b0) * a.rows + x.m + row : a.a_scale + (static_cast<int64_t>(x.m) + row) * x.kb;
+  }
+  const int nb = (a.n + 127) / 128, col = x.n0 + h * (BN / 2);
+  const float* pb = WG ? a.b_scale + static_cast<int64_t>(x.b0) * a.n + x.n0 + lane * 4
+                       : a.b_scale + (static_cast<int64_t>(x.e) * nb + min(col / 128, nb - 1)) * x.kb;
+  const bool l0 = WG && h == 1 && x.n0 + lane * 4 < a.n, l1 = WG && h == 1 && x.n0 + 128 + lane * 4 < a.n;
+  float va[2][4], vb[2];
+  float4 q0[2], q1[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    vb[s] = 0.f;
+    q0[s] = q1[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) va[s][i] = 0.f;
+  }
+  auto fetch = [&](int i, int s) {
+    if (i >= x.kb) return;
+    const int64_t oa = WG ? static_cast<int64_t>(i) * a.rows : i;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (la[k]) va[s][k] = __ldg(pa[k] + oa);
+    if (!WG) vb[s] = __ldg(pb + i);
+    if (l0) q0[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n));
+    if (l1) q1[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n + 128));
+  };
+  fetch(0, 0);
+  fetch(1, 1);
+  for (int i0 = 0; i0 < x.kb; i0 += 2) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (i0 + s >= x.kb) break;
+      const int buf = *chunk & 1;
+      if (!mbar_wait_warp(freed(buf), (static_cast<uint32_t>(*chunk >> 1) & 1u) ^ 1u, gone)) return false;
+      Factors<BN, WG>& f = ring[buf];
+      if (!WG || h == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f.row[WG ? 0 : h][k * 32 + lane] = WG ? va[s][k] : va[s][k] * vb[s];
+      } else if constexpr (WG) {
+        *reinterpret_cast<float4*>(f.col + lane * 4) = q0[s];
+        *reinterpret_cast<float4*>(f.col + 128 + lane * 4) = q1[s];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ready(buf));
+      ++*chunk;
+      fetch(i0 + s + 2, s);
+    }
+  }
+  return true;
+}
+
+// Tensor map of [depth, rows, cols] bytes, box [1, box_rows, 128].
+bool make_map8(CUtensorMap* m, const void* ptr, uint64_t depth, uint64_t rows, uint64_t cols, uint32_t box_rows, int dims) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t size[3] = {cols, rows, depth};
+  const cuuint64_t strides[2] = {cols, cols * rows};
+  const cuuint32_t box[3] = {128, box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, static_cast<cuuint32_t>(dims), const_cast<void*>(ptr), size, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// false: more tiles than the kernels count (no output of that size fits a GPU).
+template <int BM, int BN, bool WG>
+bool mm_args(const ExpertMatmulArgs& g, MmArgs* out) {
+  MmArgs& a = *out;
+  a.a_scale = g.a_scale;
+  a.b_scale = g.b_scale;
+  a.first = g.first;
+  a.limit = g.R;
+  a.E = g.E;
+  a.rows = g.n;
+  a.n = WG ? g.d : g.n;
+  a.k = g.d;
+  a.nt = (a.n + BN - 1) / BN;
+  a.mt = (g.n + BM - 1) / BM;
+  a.S = 0;
+  const int64_t most = WG ? static_cast<int64_t>(g.E) * a.nt * a.mt : (g.R / BM + (g.R < g.E ? g.R : g.E)) * a.nt;
+  a.most = static_cast<int>(most);
+  a.out = g.out;
+  a.out_fp32 = g.out_fp32;
+  a.add = g.add;
+  a.err = g.err;
+  return most <= 1 << 30;
+}
+
+// The split of the registers would wait for ever where the launch has fewer.
+template <typename... KArgs>
+int check_registers(void (*kern)(KArgs...), std::atomic<int>* checked) {
+  if (checked->load(std::memory_order_relaxed)) return kOk;
+  cudaFuncAttributes at;
+  if (cudaFuncGetAttributes(&at, kern) != cudaSuccess) return kErrCuda;
+  if (at.numRegs < kMmRegs) return kErrUnsupported;
+  checked->store(1, std::memory_order_relaxed);
+  return kOk;
+}
+
+}  // namespace
+
+}  // namespace eqb
