@@ -195,13 +195,16 @@ __device__ __forceinline__ void tmem_here(uint32_t (&r)[16]) {
 template <bool kColScale, int N>
 __device__ __forceinline__ void add_columns(const uint32_t (&r)[N], const F2& ff, const float* cs, F2* acc) {
 #pragma unroll
-  for (int v = 0; v < N / 2; ++v) {
+  for (int v = 0; v < N / 2; v += 2) {
     F2 d = f2(__uint_as_float(r[2 * v]), __uint_as_float(r[2 * v + 1]));
+    F2 e = f2(__uint_as_float(r[2 * v + 2]), __uint_as_float(r[2 * v + 3]));
     if (kColScale) {
-      const float2 s = *reinterpret_cast<const float2*>(cs + 2 * v);
+      const float4 s = *reinterpret_cast<const float4*>(cs + 2 * v);
       d = mul2(d, f2(s.x, s.y));
+      e = mul2(e, f2(s.z, s.w));
     }
     acc[v] = fma2(d, ff, acc[v]);
+    acc[v + 1] = fma2(e, ff, acc[v + 1]);
   }
 }
 
