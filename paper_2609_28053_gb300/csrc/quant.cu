@@ -8,6 +8,7 @@
 // order as the magnitudes do, and infinities and NaN come out on top, so that one
 // comparison a block finds them.
 #include "eqb_device.cuh"
+#include "f32x2.cuh"
 
 namespace eqb {
 
@@ -114,16 +115,17 @@ __device__ __forceinline__ int expert_of_block(const int32_t* __restrict__ block
 // different times, and kColStrips * 128 bytes of every token stay in L2 in between
 // (T = 16,384, c = 4,096, K = 8 339 us, 444 with a row of blocks at a time).
 constexpr int kColThreads = 256;
-constexpr int kColStrips = 8;
+constexpr int kColStrips = 16;  // at most
 
-__global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantColsArgs a) {
+__global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantColsArgs a, int strips) {
   __shared__ uint32_t tops[8][32];  // of every warp: the largest patterns of 64 columns, two a word
-  __shared__ uint32_t tile[64][33];
+  __shared__ __align__(16) float inv[64];
+  __shared__ __align__(16) uint32_t tile[64 * 32];  // [column][word]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t b = blockIdx.x % a.P;
   const int cg = threadIdx.x & 7, rg = threadIdx.x >> 3;
-  int j0 = static_cast<int>(blockIdx.x / a.P) * (kColStrips * 64);
-  const int j1 = min(j0 + kColStrips * 64, a.c);
+  int j0 = static_cast<int>(blockIdx.x / a.P) * (strips * 64);
+  const int j1 = min(j0 + strips * 64, a.c);
   griddep_wait();
   const int e = expert_of_block(a.blocks, a.E, b, lane);
   if (e >= a.E) return;
@@ -147,6 +149,7 @@ __global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantCols
       v[i] = from[i] && j + cg * 8 < j1 ? __ldg(reinterpret_cast<const uint4*>(from[i] + j)) : make_uint4(0u, 0u, 0u, 0u);
   };
   const int64_t pitch = a.P * kExpertBlock;
+  uint8_t* out = a.q + b * kExpertBlock + (lane & 7) * 16;
   uint4 next[4];
   load(j0, next);
   for (; j0 < j1; j0 += 64) {
@@ -165,29 +168,39 @@ __global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantCols
       if (lane < 8) tops[warp][cg * 4 + p] = m;
     }
     __syncthreads();
+    if (threadIdx.x < 64) {  // a column's scale, once
+      const int col = threadIdx.x;
+      uint32_t t = tops[0][col >> 1];
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      uint32_t t = tops[0][cg * 4 + p];
+      for (int v = 1; v < 8; ++v) t = __vmaxu2(t, tops[v][col >> 1]);
+      t = col & 1 ? t >> 16 : t & 0xffffu;
+      if (t >= 0x7f80u) raise_flag(a.err, kErrNonfinite);
+      const Scale sc = scale_of(bf16_bits_to_f32(t));
+      inv[col] = sc.inv;
+      if (j0 + col < a.c) a.scale[b * a.c + j0 + col] = sc.scale;
+    }
+    __syncthreads();
+    {
+      // a word is four rows of a column; groups of four words are turned by the
+      // column's eight, so that neither these stores nor the loads below meet in a bank
+      const float4 x = *reinterpret_cast<const float4*>(inv + cg * 8), y = *reinterpret_cast<const float4*>(inv + cg * 8 + 4);
+      const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      uint32_t* to = tile + cg * 256 + ((warp ^ cg) << 2) + (lane >> 3);
 #pragma unroll
-      for (int v = 1; v < 8; ++v) t = __vmaxu2(t, tops[v][cg * 4 + p]);
-      const uint32_t lo = t & 0xffffu, hi = t >> 16;
-      if (max(lo, hi) >= 0x7f80u) raise_flag(a.err, kErrNonfinite);
-      const Scale s0 = scale_of(bf16_bits_to_f32(lo)), s1 = scale_of(bf16_bits_to_f32(hi));
-      tile[cg * 8 + 2 * p][rg] = code4(bf16_lo(w[0][p]) * s0.inv, bf16_lo(w[1][p]) * s0.inv, bf16_lo(w[2][p]) * s0.inv,
-                                       bf16_lo(w[3][p]) * s0.inv);
-      tile[cg * 8 + 2 * p + 1][rg] = code4(bf16_hi(w[0][p]) * s1.inv, bf16_hi(w[1][p]) * s1.inv, bf16_hi(w[2][p]) * s1.inv,
-                                           bf16_hi(w[3][p]) * s1.inv);
-      if (rg == 0 && j < a.c) {
-        a.scale[b * a.c + j + 2 * p] = s0.scale;
-        a.scale[b * a.c + j + 2 * p + 1] = s1.scale;
+      for (int p = 0; p < 4; ++p) {
+        const F2 f0 = splat2(f[2 * p]), f1 = splat2(f[2 * p + 1]);
+        const F2 a0 = mul2(f2(bf16_lo(w[0][p]), bf16_lo(w[1][p])), f0), a1 = mul2(f2(bf16_lo(w[2][p]), bf16_lo(w[3][p])), f0);
+        const F2 b0 = mul2(f2(bf16_hi(w[0][p]), bf16_hi(w[1][p])), f1), b1 = mul2(f2(bf16_hi(w[2][p]), bf16_hi(w[3][p])), f1);
+        to[(2 * p) * 32] = code4(lo2(a0), hi2(a0), lo2(a1), hi2(a1));
+        to[(2 * p + 1) * 32] = code4(lo2(b0), hi2(b0), lo2(b1), hi2(b1));
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int col = i * 8 + warp;
+    for (int i = 0; i < 2; ++i) {
+      const int col = i * 32 + warp * 4 + (lane >> 3);
       if (j0 + col < a.c)
-        reinterpret_cast<uint32_t*>(a.q + (j0 + col) * pitch + b * kExpertBlock)[lane] = tile[col][lane];
+        *reinterpret_cast<uint4*>(out + (j0 + col) * pitch) = *reinterpret_cast<const uint4*>(tile + col * 32 + (((lane & 7) ^ (col >> 3)) << 2));
     }
   }
 }
@@ -285,9 +298,14 @@ int launch_quant_rows(const uint16_t* x, int64_t T, int d, const int32_t* slot, 
 }
 
 int launch_quant_cols(const QuantColsArgs& a, cudaStream_t s) {
-  const int64_t grid = a.P * ((a.c + kColStrips * 64 - 1) / (kColStrips * 64));
+  DeviceInfo di;
+  if (int rc = device_info(&di)) return rc;
+  // as many strips a block as leave every SM some blocks
+  int strips = kColStrips;
+  while (strips > 1 && a.P * ((a.c + strips * 64 - 1) / (strips * 64)) < 16 * di.sm_count) strips /= 2;
+  const int64_t grid = a.P * ((a.c + strips * 64 - 1) / (strips * 64));
   if (grid > 0x7fffffff) return kErrUnsupported;
-  return status_of(launch_dependent(quant_cols_kernel, dim3(static_cast<unsigned>(grid)), dim3(kColThreads), 0, s, a));
+  return status_of(launch_dependent(quant_cols_kernel, dim3(static_cast<unsigned>(grid)), dim3(kColThreads), 0, s, a, strips));
 }
 
 int launch_quant_blocks(const void* w, int w_fp32, int E, int n, int d, uint8_t* q, float* scale, uint8_t* q_t, float* scale_t,
