@@ -24,7 +24,7 @@ __device__ __forceinline__ Scale scale_of(float top) {
   Scale s;
   s.scale = __fmul_rn(top, 1.0f / 448.0f);
   if (s.scale < 0x1p-126f) s.scale = 0.f;
-  s.inv = s.scale > 0.f ? __fdiv_rn(1.0f, s.scale) : 0.f;
+  s.inv = s.scale > 0.f ? __frcp_rn(s.scale) : 0.f;
   return s;
 }
 // Two codes, lo in the low byte.  The conversion rounds to nearest even and keeps
@@ -117,7 +117,7 @@ __device__ __forceinline__ int expert_of_block(const int32_t* __restrict__ block
 constexpr int kColThreads = 256;
 constexpr int kColStrips = 16;  // at most
 
-__global__ void __launch_bounds__(kColThreads) quant_cols_kernel(const QuantColsArgs a, int strips) {
+__global__ void __launch_bounds__(kColThreads, 4) quant_cols_kernel(const QuantColsArgs a, int strips) {
   __shared__ uint32_t tops[8][32];  // of every warp: the largest patterns of 64 columns, two a word
   __shared__ __align__(16) float inv[64];
   __shared__ __align__(16) uint32_t tile[64 * 32];  // [column][word]
