@@ -1,14 +1,17 @@
 // gate_tile.cu -- the gate of many tokens (see gate.cu): a thread takes a token
 // whose row of z lies in shared memory, a warp a tile of 32 tokens.
 //
-// The row is cut into eight parts, each within a group:
+// The row is cut into 16 parts (8 where its chunks of 8 experts do not make 16 equal
+// ones), each within a group:
 //   1. the two largest c = z + b of every part, in pairs: exact (fp32), so the
 //      groups' scores and their ranking are too;
 //   2. of the parts that stay open, the eighth largest of their two largest is a
-//      lower bound of the K-th largest c (K <= 8): two sorts of eight and a merge;
-//   3. a bit for every open expert at or above the bound (about 13 of 128 for K = 8);
-//   4. those are inserted in ascending order into a sorted list.
-// Phases 1 and 3 take four to five instructions a value, phase 4 about fifty a
+//      lower bound of the K-th largest c (K <= 8): from the eight largest of either;
+//   3. a bit for every open expert at or above the bound;
+//   4. those are inserted in ascending order into a sorted list: with 4 of 8 groups of
+//      32 open and K = 8 there are 8.1 a token and 9.0 in the lane of a warp that has
+//      most, which is how often the warp inserts (with eight parts 11.0 and 18.6).
+// Phases 1 and 3 take four to five instructions a value, phase 4 about seventy a
 // candidate of the lane that has most.  A thread a token needs about a tenth of
 // the instructions of a warp a token (gate.cu), which waits for every maximum of
 // the warp.
@@ -24,10 +27,35 @@ namespace eqb {
 
 namespace {
 
-constexpr int kParts = 8;
 constexpr int kMaxGateWarps = 16;
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// The eight largest of 8 or 16 values, descending, in a[0..7].
+__device__ __forceinline__ void top8(float (&a)[8]) { sort_desc<8>(a); }
+__device__ __forceinline__ void top8(float (&a)[16]) {
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = a[i];
+    y[i] = a[8 + i];
+  }
+  sort_desc<8>(x);
+  sort_desc<8>(y);
+  // the larger of the i-th of one and the i-th from behind of the other: the eight
+  // largest, first falling, then rising
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = fmaxf(x[i], y[7 - i]);
+#pragma unroll
+  for (int j = 4; j > 0; j >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!(i & j)) {
+        const float h = fmaxf(a[i], a[i | j]), l = fminf(a[i], a[i | j]);
+        a[i] = h;
+        a[i | j] = l;
+      }
+}
 
 // The two largest of two pairs of the two largest.  NaN stays in the first.
 __device__ __forceinline__ void merge2(float& m1, float& m2, float h, float l) {
@@ -70,22 +98,24 @@ struct GateTile {
   int64_t tiles_per_warp;
 };
 
-// First chunk (of eight experts) of part s, with groups of gc chunks in SP parts.
-template <int SP>
+// First chunk (of eight experts) of part s: C chunks a part, or (C = 0) groups of gc
+// chunks in SP parts.
+template <int SP, int C>
 __device__ __forceinline__ int part_chunk(int s, int gc) {
-  return s / SP * gc + s % SP * gc / SP;
+  return C ? s * C : s / SP * gc + s % SP * gc / SP;
 }
 
-template <bool F32, int G, int KP>
+// C: chunks of each of 16 parts; 0: eight parts of any size.
+template <bool F32, int G, int KP, int C>
 __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const GateArgs a, const GateTile g) {
-  constexpr int SP = kParts / G;  // parts of a group
+  constexpr int kParts = C ? 16 : 8, SP = kParts / G;  // SP: parts of a group
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int E = a.E, K = a.K, gc = E / 8 / G, cmax = (gc + SP - 1) / SP;
+  const int E = C ? 128 * C : a.E, K = a.K, gc = E / 8 / G, cmax = C ? C : (gc + SP - 1) / SP, words = C ? 1 : g.words;
   float* bs = reinterpret_cast<float*>(smem);
   uint8_t* mine = smem + 4 * E + wid * g.warp_bytes;
   uint32_t* mw = reinterpret_cast<uint32_t*>(mine + 32 * g.stride) + lane;  // [part][words][32 lanes]
-  const uint32_t bar = saddr(mine + 32 * g.stride + kParts * g.words * 128);
+  const uint32_t bar = saddr(mine + 32 * g.stride + kParts * words * 128);
   const uint8_t* row = mine + lane * g.stride;
   const int row_bytes = E * (F32 ? 4 : 2);
   if (lane == 0) {
@@ -136,8 +166,9 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 #pragma unroll
     for (int s = 0; s < kParts; ++s) {
       m1[s] = m2[s] = -INFINITY;
-      const int c1 = part_chunk<SP>(s + 1, gc);
-      for (int c = part_chunk<SP>(s, gc); c < c1; ++c) {
+      const int c1 = part_chunk<SP, C>(s + 1, gc);
+#pragma unroll
+      for (int c = part_chunk<SP, C>(s, gc); c < c1; ++c) {
         F2 v[4];
         row8<F32>(row, c, v);
         add_bias(v, bs, c);
@@ -188,8 +219,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 #pragma unroll
       for (int s = 0; s < kParts; ++s)
         if (!(open >> s & 1u)) m1[s] = m2[s] = -INFINITY;
-      sort_desc<kParts>(m1);
-      sort_desc<kParts>(m2);
+      top8(m1);
+      top8(m2);
 #pragma unroll
       for (int i = 0; i < KP; ++i) bound = fminf(bound, fmaxf(m1[i], m2[KP - 1 - i]));
       bound = fmaxf(bound, -FLT_MAX);  // a closed expert is never chosen
@@ -206,8 +237,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
         const int s = left ? __ffs(left) - 1 : 0;
         const bool there = left != 0u;
         left &= left - 1u;
-        const int c0 = part_chunk<SP>(s, gc), c1 = part_chunk<SP>(s + 1, gc);
-        for (int w = 0; w < g.words; ++w) {
+        const int c0 = part_chunk<SP, C>(s, gc), c1 = part_chunk<SP, C>(s + 1, gc);
+        for (int w = 0; w < words; ++w) {
           uint32_t word = 0u;
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
@@ -226,8 +257,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
             }
             word = word << 8 | (~bits & 0xffu);
           }
-          if (there) mw[(s * g.words + w) << 5] = word;
-          hits |= there && word != 0u ? 0x80000000u >> (s * g.words + w) : 0u;
+          if (there) mw[(s * words + w) << 5] = word;
+          hits |= there && word != 0u ? 0x80000000u >> (s * words + w) : 0u;
         }
       }
     }
@@ -246,8 +277,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
         const int k = __clz(hits);
         hits ^= 0x80000000u >> k;
         m = mw[k << 5];
-        const int s = g.words == 1 ? k : k >> 1;
-        wb = (part_chunk<SP>(s, gc) + (g.words == 1 ? 0 : (k & 1) * 4)) * 8;
+        const int s = words == 1 ? k : k >> 1;
+        wb = (part_chunk<SP, C>(s, gc) + (words == 1 ? 0 : (k & 1) * 4)) * 8;
       }
       const int p = __clz(m);
       const int e = m != 0u ? wb + p : -1;
@@ -345,13 +376,14 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
   }
 }
 
-template <bool F32, int G>
+template <bool F32, int G, int C>
 int launch_tile(const GateArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
   GateTile g;
   const int words = a.E * (F32 ? 4 : 2) / 4;
   g.stride = 4 * (words + ((4 - words) & 7));
+  constexpr int kParts = C ? 16 : 8;
   const int gc = a.E / 8 / G, sp = kParts / G, cmax = (gc + sp - 1) / sp;
   g.words = (cmax + 3) / 4;
   g.warp_bytes = 32 * g.stride + kParts * g.words * 128 + 16;
@@ -365,7 +397,7 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
   int64_t grid = (ntiles + nw - 1) / nw;
   if (grid > di.sm_count) grid = di.sm_count;
   g.tiles_per_warp = (ntiles + grid * nw - 1) / (grid * nw);
-  auto kern = gate_tile_kernel<F32, G, 8>;
+  auto kern = gate_tile_kernel<F32, G, 8, C>;
   if (!allow_smem(kern, di.max_smem_optin)) return kErrCuda;
   return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(static_cast<unsigned>(nw) * 32),
                           head + static_cast<int>(nw) * g.warp_bytes, s, a, g) == cudaSuccess
@@ -373,13 +405,21 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
              : kErrCuda;
 }
 
+template <bool F32, int G>
+int launch_tile_width(const GateArgs& a, cudaStream_t s) {
+  if (a.E == 128) return launch_tile<F32, G, 1>(a, s);
+  if (a.E == 256) return launch_tile<F32, G, 2>(a, s);
+  if (a.E == 512) return launch_tile<F32, G, 4>(a, s);
+  return launch_tile<F32, G, 0>(a, s);
+}
+
 template <bool F32>
 int launch_tile_groups(const GateArgs& a, cudaStream_t s) {
   const int G = a.top_groups < a.groups ? a.groups : 1;
-  if (G == 1) return launch_tile<F32, 1>(a, s);
-  if (G == 2) return launch_tile<F32, 2>(a, s);
-  if (G == 4) return launch_tile<F32, 4>(a, s);
-  return launch_tile<F32, 8>(a, s);
+  if (G == 1) return launch_tile_width<F32, 1>(a, s);
+  if (G == 2) return launch_tile_width<F32, 2>(a, s);
+  if (G == 4) return launch_tile_width<F32, 4>(a, s);
+  return launch_tile_width<F32, 8>(a, s);
 }
 
 }  // namespace
