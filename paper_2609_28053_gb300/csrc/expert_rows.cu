@@ -2,12 +2,17 @@
 // sort of the list entries by expert.
 //
 // The entries are cut into chunks, one a block.  One kernel counts every chunk's
-// entries of each expert, one forms each expert's running sums over the chunks (a
-// warp an expert), and one gives every entry its row: the rows of the experts
+// entries of each expert, and one gives every entry its row: the rows of the experts
 // before, of the chunks before, of the block's warps before, and of the entries
 // before it in the warp's 32, which __match_any_sync counts.  Every step counts in
 // a fixed order, so rows are in ascending order of entry.  Few entries are one
-// chunk, whose block needs no other kernel.
+// chunk, whose block needs no other kernel; of many chunks a third kernel forms
+// each expert's running sums (a warp an expert), of up to kAddedCounts counts every
+// block adds those before its own itself.
+//
+// It is latency that counts: launches, and loads that wait for one another.  A lane
+// asks for eight entries together (T = 65,536, K = 8, E = 128: 14.1 us with one at a
+// time and three launches, ROWS_NOW).
 #include "eqb_device.cuh"
 
 namespace eqb {
@@ -17,20 +22,24 @@ namespace {
 constexpr int kRowsWarps = 16;
 constexpr int kRowsThreads = kRowsWarps * 32;
 constexpr int kRowsChunk = 4096;  // least entries of a chunk
-constexpr int kRowsChunks = 608;  // most chunks
+constexpr int kRowsChunks = 608;  // most chunks, about
+constexpr int kRowsAhead = 8;     // entries that a lane asks for together
+constexpr int kAddedCounts = 1 << 15;
 
 struct RowsPlan {
   int chunks, per;  // per: entries of a chunk, a multiple of kRowsThreads
 };
 RowsPlan plan_rows(int64_t n) {
   RowsPlan p;
-  const int64_t want = (n + kRowsChunks - 1) / kRowsChunks;
-  const int64_t per = want > kRowsChunk ? want : kRowsChunk;
+  const int64_t even = (n + kRowsChunks - 1) / kRowsChunks;
+  const int64_t per = even > kRowsChunk ? even : n < kRowsChunk ? (n > 0 ? n : 1) : kRowsChunk;
   p.per = static_cast<int>((per + kRowsThreads - 1) / kRowsThreads * kRowsThreads);
   p.chunks = static_cast<int>((n + p.per - 1) / p.per);
   if (p.chunks < 1) p.chunks = 1;
   return p;
 }
+
+__host__ __device__ constexpr bool added_counts(int chunks, int E) { return static_cast<int64_t>(chunks) * E <= kAddedCounts; }
 
 __device__ __forceinline__ int expert_of(const ExpertRowsArgs& a, int64_t i, int64_t end) {
   if (i >= end) return -1;
@@ -44,12 +53,19 @@ __global__ void __launch_bounds__(kRowsThreads) rows_count_kernel(const ExpertRo
   __syncthreads();
   griddep_wait();
   const int64_t i0 = static_cast<int64_t>(blockIdx.x) * per, end = min(a.n, i0 + per);
-  for (int64_t i = i0 + threadIdx.x; i < end; i += kRowsThreads) {
-    const int e = expert_of(a, i, end);
-    if (e >= 0) atomicAdd(cnt + e, 1);
+  for (int64_t i = i0 + threadIdx.x; i < end; i += kRowsThreads * kRowsAhead) {
+    int e[kRowsAhead];
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) e[k] = expert_of(a, i + k * kRowsThreads, end);
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k)
+      if (e[k] >= 0) atomicAdd(cnt + e[k], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += kRowsThreads) a.ws[static_cast<int64_t>(e) * chunks + blockIdx.x] = cnt[e];
+  // a row of counts a chunk, or, to be scanned, a row of chunks an expert
+  const bool added = added_counts(chunks, a.E);
+  for (int e = threadIdx.x; e < a.E; e += kRowsThreads)
+    a.ws[added ? static_cast<int64_t>(blockIdx.x) * a.E + e : static_cast<int64_t>(e) * chunks + blockIdx.x] = cnt[e];
 }
 
 // Running sums over the chunks, exclusive, and each expert's total behind them.
@@ -74,34 +90,63 @@ __global__ void __launch_bounds__(256) rows_scan_kernel(const ExpertRowsArgs a, 
 }
 
 __global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRowsArgs a, int per, int chunks) {
-  extern __shared__ int cnt[];  // [warps][E], then the experts' totals and first rows [E] each
+  extern __shared__ int cnt[];  // [warps][E], then the experts' totals, first rows and rows of the chunks before [E] each
   __shared__ int part[2][kRowsWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
   int* total = cnt + kRowsWarps * E;
   int* first = total + E;
-  for (int i = threadIdx.x; i < kRowsWarps * E; i += kRowsThreads) cnt[i] = 0;
+  int* before = first + E;
+  for (int i = threadIdx.x; i < (kRowsWarps + 3) * E; i += kRowsThreads) cnt[i] = 0;
   __syncthreads();
   griddep_wait();
   // a warp's entries: a contiguous part of the chunk
   const int64_t w0 = static_cast<int64_t>(blockIdx.x) * per + warp * (per / kRowsWarps);
   const int64_t end = min(a.n, w0 + per / kRowsWarps);
   int* mine = cnt + warp * E;
-  for (int64_t i = w0; i < end; i += 32) {
-    const int e = expert_of(a, i + lane, end);
-    const uint32_t same = __match_any_sync(kFull, e);
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  int e[kRowsAhead];
+  for (int64_t i = w0; i < end; i += 32 * kRowsAhead) {
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) e[k] = expert_of(a, i + k * 32 + lane, end);
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) {
+      const uint32_t same = __match_any_sync(kFull, e[k]);
+      if (e[k] >= 0 && lane == __ffs(same) - 1) mine[e[k]] += __popc(same);
+      __syncwarp();
+    }
+  }
+  if (chunks > 1) {
+    if (added_counts(chunks, E)) {
+      // kRowsThreads / E threads an expert, each some of the chunks
+      const int threads = max(kRowsThreads / E, 1);
+      for (int u = threadIdx.x; u < E * threads; u += kRowsThreads) {
+        const int x = u % E;
+        int all = 0, ahead = 0;
+#pragma unroll 8
+        for (int c = u / E; c < chunks; c += threads) {
+          const int v = __ldcg(a.ws + static_cast<int64_t>(c) * E + x);
+          all += v;
+          ahead += c < static_cast<int>(blockIdx.x) ? v : 0;
+        }
+        atomicAdd(total + x, all);
+        atomicAdd(before + x, ahead);
+      }
+    } else {
+      for (int x = threadIdx.x; x < E; x += kRowsThreads) {
+        total[x] = __ldcg(a.ws + static_cast<int64_t>(E) * chunks + x);
+        before[x] = __ldcg(a.ws + static_cast<int64_t>(x) * chunks + blockIdx.x);
+      }
+    }
   }
   __syncthreads();
-  // what the chunk's warps before have, and the experts' totals
-  for (int e = threadIdx.x; e < E; e += kRowsThreads) {
+  // what the chunk's warps before have
+  for (int x = threadIdx.x; x < E; x += kRowsThreads) {
     int run = 0;
     for (int w = 0; w < kRowsWarps; ++w) {
-      const int v = cnt[w * E + e];
-      cnt[w * E + e] = run;
+      const int v = cnt[w * E + x];
+      cnt[w * E + x] = run;
       run += v;
     }
-    total[e] = chunks == 1 ? run : a.ws[static_cast<int64_t>(E) * chunks + e];
+    if (chunks == 1) total[x] = run;
   }
   __syncthreads();
   // first rows and blocks of the experts: two neighbours a thread
@@ -144,21 +189,29 @@ __global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRo
   }
   __syncthreads();
   const int all = first[E - 1] + total[E - 1];
-  for (int e = threadIdx.x; e < E; e += kRowsThreads) {
-    const int base = first[e] + (chunks == 1 ? 0 : a.ws[static_cast<int64_t>(e) * chunks + blockIdx.x]);
-    for (int w = 0; w < kRowsWarps; ++w) cnt[w * E + e] += base;
+  for (int x = threadIdx.x; x < E; x += kRowsThreads) {
+    const int base = first[x] + before[x];
+    for (int w = 0; w < kRowsWarps; ++w) cnt[w * E + x] += base;
   }
   __syncthreads();
-  for (int64_t i = w0; i < end; i += 32) {
-    const int e = expert_of(a, i + lane, end);
-    const uint32_t same = __match_any_sync(kFull, e);
-    const int row = e >= 0 ? mine[e] + __popc(same & ((1u << lane) - 1u)) : -1;
-    __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
-    if (i + lane < end) {
-      a.slot[i + lane] = row;
-      if (row >= 0) a.entry[row] = static_cast<int32_t>(i + lane);
+  const bool again = per / kRowsWarps > 32 * kRowsAhead;  // else e has the warp's entries still
+  for (int64_t i = w0; i < end; i += 32 * kRowsAhead) {
+    if (again) {
+#pragma unroll
+      for (int k = 0; k < kRowsAhead; ++k) e[k] = expert_of(a, i + k * 32 + lane, end);
+    }
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) {
+      const uint32_t same = __match_any_sync(kFull, e[k]);
+      const int row = e[k] >= 0 ? mine[e[k]] + __popc(same & ((1u << lane) - 1u)) : -1;
+      __syncwarp();
+      if (e[k] >= 0 && lane == __ffs(same) - 1) mine[e[k]] += __popc(same);
+      __syncwarp();
+      const int64_t at = i + k * 32 + lane;
+      if (at < end) {
+        a.slot[at] = row;
+        if (row >= 0) a.entry[row] = static_cast<int32_t>(at);
+      }
     }
   }
   // the rows of this chunk's numbers that no entry has
@@ -175,10 +228,12 @@ size_t expert_rows_workspace(int64_t n, int E) {
 
 int launch_expert_rows(const ExpertRowsArgs& a, cudaStream_t s) {
   const RowsPlan p = plan_rows(a.n);
-  const int smem = (kRowsWarps + 2) * a.E * 4;
-  if (!allow_smem(rows_place_kernel, (kRowsWarps + 2) * kMaxExperts * 4)) return kErrCuda;
+  const int smem = (kRowsWarps + 3) * a.E * 4;
+  if (!allow_smem(rows_place_kernel, (kRowsWarps + 3) * kMaxExperts * 4)) return kErrCuda;
   if (p.chunks > 1) {
-    if (launch_dependent(rows_count_kernel, dim3(p.chunks), dim3(kRowsThreads), 0, s, a, p.per, p.chunks) != cudaSuccess ||
+    if (launch_dependent(rows_count_kernel, dim3(p.chunks), dim3(kRowsThreads), 0, s, a, p.per, p.chunks) != cudaSuccess)
+      return kErrCuda;
+    if (!added_counts(p.chunks, a.E) &&
         launch_dependent(rows_scan_kernel, dim3((a.E + 7) / 8), dim3(256), 0, s, a, p.chunks) != cudaSuccess)
       return kErrCuda;
   }

@@ -29,7 +29,11 @@ namespace {
 
 constexpr int kMaxGateWarps = 16;
 
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 
 // The eight largest of 8 or 16 values, descending, in a[0..7].
 __device__ __forceinline__ void top8(float (&a)[8]) { sort_desc<8>(a); }
@@ -84,12 +88,36 @@ template <bool F32>
 __device__ __forceinline__ float row1(const uint8_t* row, int e) {
   return F32 ? *reinterpret_cast<const float*>(row + 4 * e) : bf16_bits_to_f32(lds_u16(row + 2 * e));
 }
-__device__ __forceinline__ void add_bias(F2 (&v)[4], const float* bs, int chunk) {
+// fp32(z) + b of the two bf16 values of a word, one rounding each: the sum takes the
+// bf16 value as it is, so that nothing is unpacked (the shifts and masks of that
+// run where the minima and maxima do, and those bound this kernel).
+__device__ __forceinline__ F2 add_wide(uint32_t w, float b0, float b1) {
+  float x, y;
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "mov.b32 {l, h}, %2;\n\t"
+      "add.rn.f32.bf16 %0, l, %3;\n\t"
+      "add.rn.f32.bf16 %1, h, %4;\n\t}"
+      : "=f"(x), "=f"(y)
+      : "r"(w), "f"(b0), "f"(b1));
+  return f2(x, y);
+}
+// c of eight experts.
+template <bool F32>
+__device__ __forceinline__ void scores8(const uint8_t* row, const float* bs, int chunk, F2 (&v)[4]) {
   const float4 x = *reinterpret_cast<const float4*>(bs + 8 * chunk), y = *reinterpret_cast<const float4*>(bs + 8 * chunk + 4);
-  v[0] = add2(v[0], f2(x.x, x.y));
-  v[1] = add2(v[1], f2(x.z, x.w));
-  v[2] = add2(v[2], f2(y.x, y.y));
-  v[3] = add2(v[3], f2(y.z, y.w));
+  if (F32) {
+    row8<F32>(row, chunk, v);
+    v[0] = add2(v[0], f2(x.x, x.y));
+    v[1] = add2(v[1], f2(x.z, x.w));
+    v[2] = add2(v[2], f2(y.x, y.y));
+    v[3] = add2(v[3], f2(y.z, y.w));
+  } else {
+    const uint4 w = lds128(row + 16 * chunk);
+    v[0] = add_wide(w.x, x.x, x.y);
+    v[1] = add_wide(w.y, x.z, x.w);
+    v[2] = add_wide(w.z, y.x, y.y);
+    v[3] = add_wide(w.w, y.z, y.w);
+  }
 }
 
 struct GateTile {
@@ -170,8 +198,7 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 #pragma unroll
       for (int c = part_chunk<SP, C>(s, gc); c < c1; ++c) {
         F2 v[4];
-        row8<F32>(row, c, v);
-        add_bias(v, bs, c);
+        scores8<F32>(row, bs, c, v);
         float h[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -184,6 +211,7 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
         merge2(m1[s], m2[s], h[0], l[0]);
       }
       bad |= !(m1[s] < INFINITY);
+      if (C == 4) asm volatile("" ::: "memory");  // all parts' loads at once do not fit in registers
     }
     if (valid && bad) raise_flag(a.err, kErrNonfinite);
 
@@ -215,7 +243,12 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 
     // ---- 2: a lower bound of the K-th largest
     float bound = INFINITY;
+    float first[G == 1 ? kParts : 1];  // the parts' largest, as they were
     {
+      if constexpr (G == 1) {
+#pragma unroll
+        for (int s = 0; s < kParts; ++s) first[s] = m1[s];
+      }
 #pragma unroll
       for (int s = 0; s < kParts; ++s)
         if (!(open >> s & 1u)) m1[s] = m2[s] = -INFINITY;
@@ -228,12 +261,16 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 
     // ---- 3: who is at or above it; the sign of c - bound, eight chunks' bits a word
     uint32_t hits = 0u;
+    if constexpr (G == 1) {  // parts whose largest is below it have none
+      open = 0u;
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) open |= first[s] >= bound ? 1u << s : 0u;
+    }
     if (!valid) open = 0u;
     {
       const F2 less = splat2(-bound);
-      const int parts = a.top_groups < G ? a.top_groups * SP : kParts;
       uint32_t left = open;
-      for (int j = 0; j < parts; ++j) {
+      while (__any_sync(kFull, left != 0u)) {
         const int s = left ? __ffs(left) - 1 : 0;
         const bool there = left != 0u;
         left &= left - 1u;
@@ -246,8 +283,7 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
             uint32_t bits = 0xffu;  // signs: set where it is below
             if (4 * w + u < cmax && c < c1 && there) {
               F2 v[4];
-              row8<F32>(row, c, v);
-              add_bias(v, bs, c);
+              scores8<F32>(row, bs, c, v);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const F2 d = add2(v[i], less);
