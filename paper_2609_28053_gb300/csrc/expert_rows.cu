@@ -12,7 +12,7 @@
 //
 // It is latency that counts: launches, and loads that wait for one another.  A lane
 // asks for eight entries together (T = 65,536, K = 8, E = 128: 14.1 us with one at a
-// time and three launches, ROWS_NOW).
+// time and three launches, 10.8 us).
 #include "eqb_device.cuh"
 
 namespace eqb {
@@ -103,29 +103,32 @@ __global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRo
   const int64_t w0 = static_cast<int64_t>(blockIdx.x) * per + warp * (per / kRowsWarps);
   const int64_t end = min(a.n, w0 + per / kRowsWarps);
   int* mine = cnt + warp * E;
+  const bool again = per / kRowsWarps > 32 * kRowsAhead;  // the warp's entries do not stay in e
   int e[kRowsAhead];
-  for (int64_t i = w0; i < end; i += 32 * kRowsAhead) {
+  auto load = [&](int64_t i) {
 #pragma unroll
     for (int k = 0; k < kRowsAhead; ++k) e[k] = expert_of(a, i + k * 32 + lane, end);
-#pragma unroll
-    for (int k = 0; k < kRowsAhead; ++k) {
-      const uint32_t same = __match_any_sync(kFull, e[k]);
-      if (e[k] >= 0 && lane == __ffs(same) - 1) mine[e[k]] += __popc(same);
-      __syncwarp();
-    }
-  }
+  };
+  load(w0);
   if (chunks > 1) {
     if (added_counts(chunks, E)) {
-      // kRowsThreads / E threads an expert, each some of the chunks
+      // kRowsThreads / E threads an expert, each some of the chunks, 32 asked for together
       const int threads = max(kRowsThreads / E, 1);
       for (int u = threadIdx.x; u < E * threads; u += kRowsThreads) {
         const int x = u % E;
         int all = 0, ahead = 0;
-#pragma unroll 8
-        for (int c = u / E; c < chunks; c += threads) {
-          const int v = __ldcg(a.ws + static_cast<int64_t>(c) * E + x);
-          all += v;
-          ahead += c < static_cast<int>(blockIdx.x) ? v : 0;
+        for (int c0 = u / E; c0 < chunks; c0 += 32 * threads) {
+          int v[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const int c = c0 + k * threads;
+            v[k] = c < chunks ? __ldcg(a.ws + static_cast<int64_t>(c) * E + x) : 0;
+          }
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            all += v[k];
+            ahead += c0 + k * threads < static_cast<int>(blockIdx.x) ? v[k] : 0;
+          }
         }
         atomicAdd(total + x, all);
         atomicAdd(before + x, ahead);
@@ -137,14 +140,22 @@ __global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRo
       }
     }
   }
+  for (int64_t i = w0; i < end; i += 32 * kRowsAhead) {
+    if (i > w0) load(i);
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k)
+      if (e[k] >= 0) atomicAdd(mine + e[k], 1);
+  }
   __syncthreads();
   // what the chunk's warps before have
   for (int x = threadIdx.x; x < E; x += kRowsThreads) {
-    int run = 0;
+    int run = 0, v[kRowsWarps];
+#pragma unroll
+    for (int w = 0; w < kRowsWarps; ++w) v[w] = cnt[w * E + x];
+#pragma unroll
     for (int w = 0; w < kRowsWarps; ++w) {
-      const int v = cnt[w * E + x];
       cnt[w * E + x] = run;
-      run += v;
+      run += v[w];
     }
     if (chunks == 1) total[x] = run;
   }
@@ -191,15 +202,12 @@ __global__ void __launch_bounds__(kRowsThreads) rows_place_kernel(const ExpertRo
   const int all = first[E - 1] + total[E - 1];
   for (int x = threadIdx.x; x < E; x += kRowsThreads) {
     const int base = first[x] + before[x];
+#pragma unroll
     for (int w = 0; w < kRowsWarps; ++w) cnt[w * E + x] += base;
   }
   __syncthreads();
-  const bool again = per / kRowsWarps > 32 * kRowsAhead;  // else e has the warp's entries still
   for (int64_t i = w0; i < end; i += 32 * kRowsAhead) {
-    if (again) {
-#pragma unroll
-      for (int k = 0; k < kRowsAhead; ++k) e[k] = expert_of(a, i + k * 32 + lane, end);
-    }
+    if (again) load(i);
 #pragma unroll
     for (int k = 0; k < kRowsAhead; ++k) {
       const uint32_t same = __match_any_sync(kFull, e[k]);
@@ -229,7 +237,8 @@ size_t expert_rows_workspace(int64_t n, int E) {
 int launch_expert_rows(const ExpertRowsArgs& a, cudaStream_t s) {
   const RowsPlan p = plan_rows(a.n);
   const int smem = (kRowsWarps + 3) * a.E * 4;
-  if (!allow_smem(rows_place_kernel, (kRowsWarps + 3) * kMaxExperts * 4)) return kErrCuda;
+  // above what every launch may have
+  if (smem > 48 * 1024 && !allow_smem(rows_place_kernel, (kRowsWarps + 3) * kMaxExperts * 4)) return kErrCuda;
   if (p.chunks > 1) {
     if (launch_dependent(rows_count_kernel, dim3(p.chunks), dim3(kRowsThreads), 0, s, a, p.per, p.chunks) != cudaSuccess)
       return kErrCuda;

@@ -4,11 +4,9 @@
 //
 // All three stream: two or four bytes a value in, one a copy out.  A block's values
 // stay in registers between its maximum and its codes, so x is read once.  The
-// maximum is taken of the patterns without their signs, as whole numbers: they
-// order as the magnitudes do, and infinities and NaN come out on top, so that one
-// comparison a block finds them.
+// maximum is one of magnitudes that NaN stays in, so that one comparison a block
+// finds infinities and NaN.
 #include "eqb_device.cuh"
-#include "f32x2.cuh"
 
 namespace eqb {
 
@@ -27,14 +25,24 @@ __device__ __forceinline__ Scale scale_of(float top) {
   s.inv = s.scale > 0.f ? __frcp_rn(s.scale) : 0.f;
   return s;
 }
-// Two codes, lo in the low byte.  The conversion rounds to nearest even and keeps
+// Four codes, a's in the lowest byte.  The conversion rounds to nearest even and keeps
 // what is above 448 there, so that the clamp is its own.
-__device__ __forceinline__ uint32_t code2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\t"
+      "mov.b32 %0, {l, h};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
-__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) { return code2(a, b) | code2(c, d) << 16; }
+// The larger magnitudes of two bf16 pairs (their signs are anything; NaN stays).
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 
 // ---- rows.  A lane has 16 neighbours, eight lanes a block.
 constexpr int kRowWarps = 8;
@@ -67,11 +75,12 @@ __global__ void __launch_bounds__(kRowWarps * 32)
       w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
       w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
-    uint32_t m = 0u;
+    uint32_t m = w[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & kAbs2);
+    for (int i = 1; i < 8; ++i) m = larger2(m, w[i]);
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(kFull, m, o));
+    for (int o = 1; o < 8; o <<= 1) m = larger2(m, __shfl_xor_sync(kFull, m, o));
+    m &= kAbs2;
     const uint32_t top = max(m & 0xffffu, m >> 16);
     if (top >= 0x7f80u) raise_flag(err, kErrNonfinite);
     const Scale sc = scale_of(bf16_bits_to_f32(top));
@@ -107,100 +116,107 @@ __device__ __forceinline__ int expert_of_block(const int32_t* __restrict__ block
   return E;
 }
 
-// ---- cols.  A block of 256 threads takes 128 rows x kColStrips strips of 64
-// columns, a thread four neighbouring rows x eight columns of each: four codes of a
-// column are a word of the output's line, which is turned in shared memory.  The
-// next strip's values are on their way while this one's are turned.  The grid goes
-// over all rows of a group of strips first: a gathered row is wanted by K experts at
-// different times, and kColStrips * 128 bytes of every token stay in L2 in between
-// (T = 16,384, c = 4,096, K = 8 339 us, 444 with a row of blocks at a time).
-constexpr int kColThreads = 256;
-constexpr int kColStrips = 16;  // at most
+// ---- cols.  A warp takes 128 rows x 32 columns, a lane 16 neighbouring rows x eight
+// columns: 16 codes of a column are 16 bytes of the output's line, so that nothing
+// is turned in shared memory and no warp waits for another; and of the 32 scales
+// every lane forms one.  The next step's values are copied into the warp's own part of
+// shared memory meanwhile (the lanes' registers have no room for them).  Blocks go over all rows of a group of columns first: a
+// gathered row is wanted by K experts at different times, and the group's columns of
+// every token stay in L2 in between.  T = 16,384, c = 4,096, K = 8, 128 experts:
+// 208 us; 218 with 128 x 64 a block, turned in shared memory, 444 with all of a
+// row of blocks at a time and a scale formed by every thread that needs it.
+constexpr int kColWarps = 8;
+constexpr int kColSteps = 4;  // of kColWarps * 32 columns a block, at most
+// 64 bytes of every row; 16 rows and 64 bytes apart, so that two lanes' rows lie in different banks
+constexpr int kColGroup = 16 * 64 + 64, kColWarpBytes = 8 * kColGroup;
 
-__global__ void __launch_bounds__(kColThreads, 4) quant_cols_kernel(const QuantColsArgs a, int strips) {
-  __shared__ uint32_t tops[8][32];  // of every warp: the largest patterns of 64 columns, two a word
-  __shared__ __align__(16) float inv[64];
-  __shared__ __align__(16) uint32_t tile[64 * 32];  // [column][word]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(kColWarps * 32, 2) quant_cols_kernel(const QuantColsArgs a, int steps) {
+  extern __shared__ __align__(16) uint8_t ahead[];
+  __shared__ __align__(16) int tokens[128];  // rows of x (-1: zeros)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = lane & 3, rg = lane >> 2;
+  uint8_t* mine = ahead + warp * kColWarpBytes + rg * kColGroup + q * 16;
   const int64_t b = blockIdx.x % a.P;
-  const int cg = threadIdx.x & 7, rg = threadIdx.x >> 3;
-  int j0 = static_cast<int>(blockIdx.x / a.P) * (strips * 64);
-  const int j1 = min(j0 + strips * 64, a.c);
+  const int c0 = static_cast<int>(blockIdx.x / a.P) * (steps * kColWarps * 32), c1 = min(c0 + steps * kColWarps * 32, a.c);
   griddep_wait();
   const int e = expert_of_block(a.blocks, a.E, b, lane);
   if (e >= a.E) return;
   const int64_t r0 = static_cast<int64_t>(__ldg(a.offsets + e)) + (b - __ldg(a.blocks + e)) * kExpertBlock;
   const int64_t r1 = min(static_cast<int64_t>(__ldg(a.offsets + e + 1)), a.R);
-  const uint16_t* from[4];  // the thread's rows (null: zeros)
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    int64_t r = r0 + rg * 4 + i;
-    bool there = r >= 0 && r < r1;
-    if (there && a.entry) {
-      const int n = __ldg(a.entry + r);
-      there = n >= 0;
-      r = static_cast<uint32_t>(n) / static_cast<uint32_t>(a.K);
-    }
-    from[i] = there && r < a.T ? a.x + r * a.c + cg * 8 : nullptr;
-  }
-  auto load = [&](int j, uint4 (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[i] = from[i] && j + cg * 8 < j1 ? __ldg(reinterpret_cast<const uint4*>(from[i] + j)) : make_uint4(0u, 0u, 0u, 0u);
-  };
-  const int64_t pitch = a.P * kExpertBlock;
-  uint8_t* out = a.q + b * kExpertBlock + (lane & 7) * 16;
-  uint4 next[4];
-  load(j0, next);
-  for (; j0 < j1; j0 += 64) {
-    uint32_t w[4][4];  // [row][pair of columns]
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i][0] = next[i].x; w[i][1] = next[i].y; w[i][2] = next[i].z; w[i][3] = next[i].w;
-    }
-    load(j0 + 64, next);
-    const int j = j0 + cg * 8;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      uint32_t m = __vmaxu2(__vmaxu2(w[0][p] & kAbs2, w[1][p] & kAbs2), __vmaxu2(w[2][p] & kAbs2, w[3][p] & kAbs2));
-      m = __vmaxu2(m, __shfl_xor_sync(kFull, m, 8));
-      m = __vmaxu2(m, __shfl_xor_sync(kFull, m, 16));
-      if (lane < 8) tops[warp][cg * 4 + p] = m;
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {  // a column's scale, once
-      const int col = threadIdx.x;
-      uint32_t t = tops[0][col >> 1];
-#pragma unroll
-      for (int v = 1; v < 8; ++v) t = __vmaxu2(t, tops[v][col >> 1]);
-      t = col & 1 ? t >> 16 : t & 0xffffu;
-      if (t >= 0x7f80u) raise_flag(a.err, kErrNonfinite);
-      const Scale sc = scale_of(bf16_bits_to_f32(t));
-      inv[col] = sc.inv;
-      if (j0 + col < a.c) a.scale[b * a.c + j0 + col] = sc.scale;
-    }
-    __syncthreads();
-    {
-      // a word is four rows of a column; groups of four words are turned by the
-      // column's eight, so that neither these stores nor the loads below meet in a bank
-      const float4 x = *reinterpret_cast<const float4*>(inv + cg * 8), y = *reinterpret_cast<const float4*>(inv + cg * 8 + 4);
-      const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-      uint32_t* to = tile + cg * 256 + ((warp ^ cg) << 2) + (lane >> 3);
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const F2 f0 = splat2(f[2 * p]), f1 = splat2(f[2 * p + 1]);
-        const F2 a0 = mul2(f2(bf16_lo(w[0][p]), bf16_lo(w[1][p])), f0), a1 = mul2(f2(bf16_lo(w[2][p]), bf16_lo(w[3][p])), f0);
-        const F2 b0 = mul2(f2(bf16_hi(w[0][p]), bf16_hi(w[1][p])), f1), b1 = mul2(f2(bf16_hi(w[2][p]), bf16_hi(w[3][p])), f1);
-        to[(2 * p) * 32] = code4(lo2(a0), hi2(a0), lo2(a1), hi2(a1));
-        to[(2 * p + 1) * 32] = code4(lo2(b0), hi2(b0), lo2(b1), hi2(b1));
+  if (threadIdx.x < 128) {
+    const int64_t r = r0 + threadIdx.x;
+    int n = -1;
+    if (r >= 0 && r < r1) {
+      n = static_cast<int>(r);
+      if (a.entry) {
+        n = __ldg(a.entry + r);
+        if (n >= 0) n = static_cast<int>(static_cast<uint32_t>(n) / static_cast<uint32_t>(a.K));
       }
     }
-    __syncthreads();
+    tokens[threadIdx.x] = n < a.T ? n : -1;
+  }
+  __syncthreads();
+  int from[16];  // the lane's rows; where there is none, zeros stay in their place
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int col = i * 32 + warp * 4 + (lane >> 3);
-      if (j0 + col < a.c)
-        *reinterpret_cast<uint4*>(out + (j0 + col) * pitch) = *reinterpret_cast<const uint4*>(tile + col * 32 + (((lane & 7) ^ (col >> 3)) << 2));
+  for (int i = 0; i < 4; ++i) {
+    const int4 t = *reinterpret_cast<const int4*>(tokens + rg * 16 + 4 * i);
+    from[4 * i] = t.x; from[4 * i + 1] = t.y; from[4 * i + 2] = t.z; from[4 * i + 3] = t.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (from[i] < 0) *reinterpret_cast<uint4*>(mine + i * 64) = make_uint4(0u, 0u, 0u, 0u);
+  const int64_t pitch = a.P * kExpertBlock;
+  auto fetch = [&](int j) {  // a lane copies what it reads itself
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
+    if (j < c1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (from[i] >= 0)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 64), "l"(a.x + static_cast<int64_t>(from[i]) * a.c + j)
+                       : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  fetch(c0 + warp * 32 + q * 8);
+  for (int j0 = c0 + warp * 32; j0 < c1; j0 += kColWarps * 32) {
+    const int j = j0 + q * 8;
+    uint32_t w[16][4];  // [row][pair of columns]
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint4 v = *reinterpret_cast<const uint4*>(mine + i * 64);
+      w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+    }
+    if (j0 + kColWarps * 32 < c1) fetch(j + kColWarps * 32);
+    uint32_t m[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      m[p] = w[0][p];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) m[p] = larger2(m[p], w[i][p]);
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) m[p] = larger2(m[p], __shfl_xor_sync(kFull, m[p], o));
+      m[p] &= kAbs2;
+    }
+    // this lane's column of the 32: the rg-th of its eight
+    uint32_t t = rg & 4 ? (rg & 2 ? m[3] : m[2]) : (rg & 2 ? m[1] : m[0]);
+    t = rg & 1 ? t >> 16 : t & 0xffffu;
+    if (t >= 0x7f80u && j < c1) raise_flag(a.err, kErrNonfinite);
+    const Scale sc = scale_of(bf16_bits_to_f32(t));
+    if (j < c1) a.scale[b * a.c + j + rg] = sc.scale;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float f0 = __shfl_sync(kFull, sc.inv, (2 * p) * 4 + q), f1 = __shfl_sync(kFull, sc.inv, (2 * p + 1) * 4 + q);
+      uint32_t lo[4], hi[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        lo[g] = code4(bf16_lo(w[4 * g][p]) * f0, bf16_lo(w[4 * g + 1][p]) * f0, bf16_lo(w[4 * g + 2][p]) * f0, bf16_lo(w[4 * g + 3][p]) * f0);
+        hi[g] = code4(bf16_hi(w[4 * g][p]) * f1, bf16_hi(w[4 * g + 1][p]) * f1, bf16_hi(w[4 * g + 2][p]) * f1, bf16_hi(w[4 * g + 3][p]) * f1);
+      }
+      if (j < c1) {
+        uint8_t* out = a.q + (j + 2 * p) * pitch + b * kExpertBlock + rg * 16;
+        *reinterpret_cast<uint4*>(out) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<uint4*>(out + pitch) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      }
     }
   }
 }
@@ -300,12 +316,15 @@ int launch_quant_rows(const uint16_t* x, int64_t T, int d, const int32_t* slot, 
 int launch_quant_cols(const QuantColsArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  // as many strips a block as leave every SM some blocks
-  int strips = kColStrips;
-  while (strips > 1 && a.P * ((a.c + strips * 64 - 1) / (strips * 64)) < 16 * di.sm_count) strips /= 2;
-  const int64_t grid = a.P * ((a.c + strips * 64 - 1) / (strips * 64));
+  // as many steps a block as leave every SM some blocks
+  constexpr int kStep = kColWarps * 32;
+  int steps = kColSteps;
+  while (steps > 1 && a.P * ((a.c + steps * kStep - 1) / (steps * kStep)) < 16 * di.sm_count) steps /= 2;
+  const int64_t grid = a.P * ((a.c + steps * kStep - 1) / (steps * kStep));
   if (grid > 0x7fffffff) return kErrUnsupported;
-  return status_of(launch_dependent(quant_cols_kernel, dim3(static_cast<unsigned>(grid)), dim3(kColThreads), 0, s, a, strips));
+  if (!allow_smem(quant_cols_kernel, kColWarps * kColWarpBytes)) return kErrCuda;
+  return status_of(launch_dependent(quant_cols_kernel, dim3(static_cast<unsigned>(grid)), dim3(kColWarps * 32),
+                                    kColWarps * kColWarpBytes, s, a, steps));
 }
 
 int launch_quant_blocks(const void* w, int w_fp32, int E, int n, int d, uint8_t* q, float* scale, uint8_t* q_t, float* scale_t,
