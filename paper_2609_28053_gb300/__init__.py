@@ -97,8 +97,8 @@ def _need(t, dtype, name, shape=None):
 def _on_current_device(t, name):
     """The library takes its scratch and streams from the CUDA device that is
     current when it is called: the tensors must live on that device."""
-    cur = torch.cuda.current_device() if _raw_device is None else _raw_device()
-    if t.get_device() != cur:
+    cur = torch.cuda.current_device()
+    if t.device.index != cur:
         raise ValueError(f"{name} is on cuda:{t.device.index} but cuda:{cur} is the current device; "
                          f"call inside torch.cuda.device({t.device})")
 

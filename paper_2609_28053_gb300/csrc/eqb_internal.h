@@ -306,9 +306,10 @@ struct GateArgs {
   int32_t* err;
 };
 int launch_gate(const GateArgs& a, cudaStream_t s);
-// Many tokens, a thread each (gate_tile.cu).
-bool gate_tile_supported(const GateArgs& a);
-int launch_gate_tile(const GateArgs& a, cudaStream_t s);
+// Many tokens, a thread each (gate_tile.cuh): K <= 8, E <= 512, groups that parts of
+// a row lie within.
+int launch_gate_tile_bf16(const GateArgs& a, cudaStream_t s);
+int launch_gate_tile_fp32(const GateArgs& a, cudaStream_t s);
 struct GateGradArgs {
   const void* z;
   int z_fp32;

@@ -11,7 +11,7 @@ namespace eqb {
 namespace {
 
 constexpr int kCombineWarps = 8;
-constexpr int kRowsAhead = 8;  // rows of a token that are asked for together
+constexpr int kRowsAhead = 8;  // rows, or parts of rows, of a token that are asked for together
 
 __device__ __forceinline__ void unpack8(const uint4& x, float* v) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -72,53 +72,66 @@ __global__ void __launch_bounds__(kCombineWarps * 32) combine_kernel(const Combi
   }
 }
 
-// A warp a token, eight of its rows at a time: their dot products stay in the
-// lanes' registers over all columns.
+// A warp a token, N of its rows and M parts of 256 columns at a time (N M = 8): the rows' dot
+// products stay in the lanes' registers over all columns.
+template <int N>
 __global__ void __launch_bounds__(kCombineWarps * 32, 2) combine_grad_kernel(const CombineArgs a) {
+  constexpr int M = kRowsAhead / N;
   const int lane = threadIdx.x & 31;
   griddep_wait();
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * kCombineWarps + (threadIdx.x >> 5); t < a.T;
        t += static_cast<int64_t>(gridDim.x) * kCombineWarps) {
-    for (int k0 = 0; k0 < a.K; k0 += kRowsAhead) {
+    for (int k0 = 0; k0 < a.K; k0 += N) {
       float w;
       const int r = slots_of(a, t, k0, lane, &w);
-      int rk[kRowsAhead];
-      float wk[kRowsAhead], dot[kRowsAhead];
+      int rk[N];
+      float wk[N], dot[N];
 #pragma unroll
-      for (int k = 0; k < kRowsAhead; ++k) {
+      for (int k = 0; k < N; ++k) {
         rk[k] = __shfl_sync(kFull, r, k);
         wk[k] = __shfl_sync(kFull, w, k);
         dot[k] = 0.f;
       }
 #pragma unroll 1
-      for (int j = lane * 8; j < a.n; j += 256) {
-        uint4 x[kRowsAhead];
-        if (a.gw) {
+      for (int j0 = lane * 8; j0 < a.n; j0 += 256 * M) {
+        uint4 x[N][M], gr[M];
 #pragma unroll
-          for (int k = 0; k < kRowsAhead; ++k)
-            x[k] = rk[k] >= 0 ? *reinterpret_cast<const uint4*>(a.rows + static_cast<int64_t>(rk[k]) * a.n + j) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        float g[8];
-        unpack8(__ldg(reinterpret_cast<const uint4*>(a.grad + t * a.n + j)), g);
-#pragma unroll
-        for (int k = 0; k < kRowsAhead; ++k) {
+        for (int m = 0; m < M; ++m) {
+          const int j = j0 + 256 * m;
+          const bool in = M == 1 || j < a.n;
+          gr[m] = in ? __ldg(reinterpret_cast<const uint4*>(a.grad + t * a.n + j)) : make_uint4(0u, 0u, 0u, 0u);
           if (a.gw) {
-            float v[8];
-            unpack8(x[k], v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dot[k] = __fmaf_rn(g[i], v[i], dot[k]);
+            for (int k = 0; k < N; ++k)
+              x[k][m] = in && rk[k] >= 0 ? *reinterpret_cast<const uint4*>(a.rows + static_cast<int64_t>(rk[k]) * a.n + j)
+                                         : make_uint4(0u, 0u, 0u, 0u);
           }
-          if (a.out && rk[k] >= 0) {
-            float v[8];
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = g[i] * wk[k];
-            *reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(rk[k]) * a.n + j) = pack8(v);
+        for (int m = 0; m < M; ++m) {
+          const int j = j0 + 256 * m;
+          float g[8];
+          unpack8(gr[m], g);
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            if (a.gw) {
+              float v[8];
+              unpack8(x[k][m], v);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) dot[k] = __fmaf_rn(g[i], v[i], dot[k]);
+            }
+            if (a.out && rk[k] >= 0 && (M == 1 || j < a.n)) {
+              float v[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = g[i] * wk[k];
+              *reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(rk[k]) * a.n + j) = pack8(v);
+            }
           }
         }
       }
       if (a.gw) {
 #pragma unroll
-        for (int k = 0; k < kRowsAhead; ++k) {
+        for (int k = 0; k < N; ++k) {
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) dot[k] = __fadd_rn(dot[k], __shfl_xor_sync(kFull, dot[k], o));
           if (lane == 0 && k0 + k < a.K) a.gw[t * a.K + k0 + k] = rk[k] >= 0 ? dot[k] : 0.f;
@@ -147,8 +160,11 @@ int launch_combine(const CombineArgs& a, cudaStream_t s) {
 int launch_combine_grad(const CombineArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  return launch_dependent(combine_grad_kernel, dim3(grid_of(a.T, di)), dim3(kCombineWarps * 32), 0, s, a) == cudaSuccess ? kOk
-                                                                                                                          : kErrCuda;
+  const dim3 grid(grid_of(a.T, di)), block(kCombineWarps * 32);
+  const cudaError_t e = a.K <= 2   ? launch_dependent(combine_grad_kernel<2>, grid, block, 0, s, a)
+                        : a.K <= 4 ? launch_dependent(combine_grad_kernel<4>, grid, block, 0, s, a)
+                                   : launch_dependent(combine_grad_kernel<8>, grid, block, 0, s, a);
+  return e == cudaSuccess ? kOk : kErrCuda;
 }
 
 }  // namespace eqb

@@ -7,8 +7,8 @@
 // for few rows an expert; expert_pair.cu has the one for many, by pairs of SMs.
 //
 // A scale belongs to 128 values of K, so the tensor cores' sums end with each
-// stage: the accumulators of a stage (two of BN columns of tensor memory
-// alternate) are read by eight warps, multiplied by the stage's scales and added to
+// stage: the accumulators of a stage (BN columns of tensor memory, two to four of
+// them in turn) are read by eight warps, multiplied by the stage's scales and added to
 // fp32 sums in registers.  That also keeps the tensor cores' own sums, which cut
 // off instead of rounding, 128 products long.
 //
@@ -25,16 +25,23 @@ namespace eqb {
 
 namespace {
 
+// Accumulators of BN columns: what tensor memory holds, at most four.  Few rows are a
+// chain of stages, each of which waits for its MMAs, its way out and the next's
+// barriers: with more stages in between they overlap.
+constexpr int kMaxBufs = 4;
+constexpr int mm_buffers(int BN) { return 512 / BN < kMaxBufs ? 512 / BN : kMaxBufs; }
+
 template <int BN, bool WG>
 __global__ void __launch_bounds__(kMmThreads, 1)
     expert_matmul_kernel(const __grid_constant__ CUtensorMap tma128, const __grid_constant__ CUtensorMap tma32,
                          const __grid_constant__ CUtensorMap tmb, const MmArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * 8 + 7];  // full, empty, accumulators full and empty, drain, factors read
+  __shared__ __align__(8) uint64_t bars[2 * 8 + 3 * kMaxBufs + 1];  // full, empty, accumulators full, empty and factors read, drain
   __shared__ uint32_t tmem_holder;
   __shared__ int abort_word, issued;
   __shared__ Table table;
-  __shared__ __align__(16) Factors<BN, WG> ring[2];
+  constexpr int kBufs = mm_buffers(BN);
+  __shared__ __align__(16) Factors<BN, WG> ring[kBufs];
   constexpr uint32_t kStage = kATile + BN * 128u;
   constexpr int kCols = BN / 2;  // columns of a warp that takes accumulators out
   volatile int* abort_flag = &abort_word;
@@ -44,9 +51,9 @@ __global__ void __launch_bounds__(kMmThreads, 1)
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (8 + s); };
   auto accf = [&](uint32_t b) { return bar0 + 8u * (16 + b); };
-  auto acce = [&](uint32_t b) { return bar0 + 8u * (18 + b); };
-  const uint32_t drain = bar0 + 8u * 20;
-  auto read = [&](uint32_t b) { return bar0 + 8u * (21 + b); };
+  auto acce = [&](uint32_t b) { return bar0 + 8u * (16 + kMaxBufs + b); };
+  auto read = [&](uint32_t b) { return bar0 + 8u * (16 + 2 * kMaxBufs + b); };
+  const uint32_t drain = bar0 + 8u * (16 + 3 * kMaxBufs);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -54,7 +61,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kBufs; ++b) {
       mbar_init(accf(b), 3);  // the MMAs, and both warps that bring factors
       mbar_init(read(b), kMmWarps);
       mbar_init(acce(b), kMmWarps);
@@ -120,15 +127,15 @@ __global__ void __launch_bounds__(kMmThreads, 1)
       for (int t = first; t < total && ok; t += step) {
         const int kb = tile_of<kBM, BN, WG>(a, table, t, &e).kb;
         for (int i = 0; i < kb; ++i, ++chunk) {
-          const uint32_t buf = static_cast<uint32_t>(chunk & 1);
-          ok = mbar_wait_warp(full(stage), phase, gone) && mbar_wait_warp(acce(buf), (static_cast<uint32_t>(chunk >> 1) & 1u) ^ 1u, gone);
+          const uint32_t buf = static_cast<uint32_t>(chunk % kBufs), phase_acc = static_cast<uint32_t>(chunk / kBufs) & 1u;
+          ok = mbar_wait_warp(full(stage), phase, gone) && mbar_wait_warp(acce(buf), phase_acc ^ 1u, gone);
           if (!ok) break;
           tc_fence_after();
           const uint64_t at = static_cast<uint64_t>(stage) * (kStage >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)  // 32 of K an MMA: 32 bytes
-              umma_e4m3(tmem + buf * 256u, ad0 + at + 2u * kk, bd0 + at + 2u * kk, idesc, kk > 0 ? 1u : 0u);
+              umma_e4m3(tmem + buf * BN, ad0 + at + 2u * kk, bd0 + at + 2u * kk, idesc, kk > 0 ? 1u : 0u);
             umma_commit(empty(stage));
             umma_commit(accf(buf));
           }
@@ -146,7 +153,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
       int chunk = 0, e = 0;
       for (int t = first; t < total; t += step) {
         const Tile x = tile_of<kBM, BN, WG>(a, table, t, &e);
-        if (!bring_factors<BN, WG>(a, x, 0, warp - 2, lane, ring, &chunk, read, accf, smem_u32(&abort_word))) break;
+        if (!bring_factors<BN, WG, kBufs>(a, x, 0, warp - 2, lane, ring, &chunk, read, accf, smem_u32(&abort_word))) break;
       }
     }
   } else {
@@ -171,8 +178,8 @@ __global__ void __launch_bounds__(kMmThreads, 1)
         some = q * 32 < x.rows;
       }
       for (; kb > 0; --kb, ++chunk) {
-        const uint32_t buf = static_cast<uint32_t>(chunk & 1);
-        ok = mbar_wait_warp(accf(buf), static_cast<uint32_t>(chunk >> 1) & 1u, gone);
+        const uint32_t buf = static_cast<uint32_t>(chunk % kBufs), phase_acc = static_cast<uint32_t>(chunk / kBufs) & 1u;
+        ok = mbar_wait_warp(accf(buf), phase_acc, gone);
         if (!ok) break;
         tc_fence_after();
         const float f = lds_f32(factor + buf * static_cast<uint32_t>(sizeof(Factors<BN, WG>)));
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
             if (!WG) mbar_arrive(read(buf));
           }
         };
-        if (some) add_stage<kCols, WG>(mine + buf * 256u, f, ring[buf].col + (WG ? h * kCols : 0), acc, release);
+        if (some) add_stage<kCols, WG>(mine + buf * BN, f, ring[buf].col + (WG ? h * kCols : 0), acc, release);
         else release();
         if (WG) {
           __syncwarp();  // the columns' factors are read
@@ -218,7 +225,7 @@ __global__ void __launch_bounds__(256) zero_weights_kernel(float4* p, int64_t n)
 template <int BN, bool WG>
 int launch_mm(const ExpertMatmulArgs& g, const DeviceInfo& di, cudaStream_t s) {
   constexpr int kStage = static_cast<int>(kATile) + BN * 128;
-  constexpr int kStatic = 24 * 8 + 64 + sizeof(Table) + 2 * sizeof(Factors<BN, WG>) + 512;  // shared memory beside the stages
+  constexpr int kStatic = (17 + 3 * kMaxBufs) * 8 + 64 + sizeof(Table) + mm_buffers(BN) * sizeof(Factors<BN, WG>) + 512;  // shared memory beside the stages
   MmArgs a;
   if (!mm_args<kBM, BN, WG>(g, &a)) return kErrUnsupported;
   const int room = di.max_smem_optin - kStatic - 1024;

@@ -70,6 +70,7 @@ struct Tile {
 struct Table {
   int tiles[kMaxExperts + 1];  // forward: tiles of the experts before
   int lo[kMaxExperts], n[kMaxExperts];  // first row and rows, or blocks
+  int group[kMaxExperts / 32];
 };
 
 // Tile t; *e moves on to the tile's expert (tiles come in ascending order).
@@ -87,7 +88,15 @@ __device__ __forceinline__ Tile tile_of(const MmArgs& a, const Table& table, int
     x.kb = table.n[x.e];
   } else {
     const int mt = t / a.nt;
-    while (table.tiles[*e + 1] <= mt) ++*e;
+    if (table.tiles[*e + 1] <= mt) {  // the first expert behind it whose tiles end after mt
+      int lo = *e + 1, hi = a.E - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (table.tiles[mid + 1] <= mt) lo = mid + 1;
+        else hi = mid;
+      }
+      *e = lo;
+    }
     x.e = *e;
     x.n0 = (t - mt * a.nt) * BN;
     const int first = (mt - table.tiles[x.e]) * BM;
@@ -105,27 +114,40 @@ template <int BM>
 __device__ __forceinline__ void fill_table(const MmArgs& a, Table& table) {
   constexpr int kMost = 1 << 30;
   const int lane = threadIdx.x & 31, limit = static_cast<int>(a.limit);
-  for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
-    const int lo = min(max(__ldg(a.first + e), 0), limit), n = min(max(__ldg(a.first + e + 1), lo), limit) - lo;
-    table.lo[e] = lo;
-    table.n[e] = n;
-    table.tiles[e + 1] = (n + BM - 1) / BM;
+  // running sums within 32 experts, then over the sums of the 32 groups
+  for (int e0 = static_cast<int>(threadIdx.x) & ~31; e0 < a.E; e0 += blockDim.x) {
+    const int e = e0 + lane;
+    int v = 0;
+    if (e < a.E) {
+      const int lo = min(max(__ldg(a.first + e), 0), limit), n = min(max(__ldg(a.first + e + 1), lo), limit) - lo;
+      table.lo[e] = lo;
+      table.n[e] = n;
+      v = (n + BM - 1) / BM;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(kFull, v, o);
+      if (lane >= o) v = min(v + y, kMost);
+    }
+    if (e < a.E) table.tiles[e + 1] = v;
+    if (lane == 31) table.group[e0 >> 5] = v;
   }
   __syncthreads();
   if (threadIdx.x < 32) {
-    int run = 0;
     if (lane == 0) table.tiles[0] = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 32) {
-      int v = e0 + lane < a.E ? table.tiles[e0 + lane + 1] : 0;
+    const int own = lane * 32 < a.E ? table.group[lane] : 0;
+    int v = own;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(kFull, v, o);
-        if (lane >= o) v = min(v + y, kMost);
-      }
-      if (e0 + lane < a.E) table.tiles[e0 + lane + 1] = min(run + v, kMost);
-      run = min(run + __shfl_sync(kFull, v, 31), kMost);
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(kFull, v, o);
+      if (lane >= o) v = min(v + y, kMost);
     }
+    const int before = __shfl_up_sync(kFull, v, 1);
+    __syncwarp();
+    table.group[lane] = lane ? before : 0;
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += blockDim.x) table.tiles[e + 1] = min(table.tiles[e + 1] + table.group[e >> 5], kMost);
 }
 // The tiles of a table.
 __device__ __forceinline__ int tiles_of(const MmArgs& a, const Table& table) {
@@ -339,11 +361,11 @@ struct Factors {
   float col[WG ? BN : 4];
 };
 
-// Warps 2 (h = 0) and 3 (h = 1): the factors of one tile's stages into `ring`, two
+// Warps 2 (h = 0) and 3 (h = 1): the factors of one tile's stages into `ring`, kBufs
 // stages deep, each loaded from memory two stages before it is written.  ring[buf]
 // may be written once `freed(buf)` has a phase for it, and adds its arrival to what
 // `ready(buf)` waits for.  False when a wait ran out.
-template <int BN, bool WG, class Freed, class Ready>
+template <int BN, bool WG, int kBufs, class Freed, class Ready>
 __device__ __forceinline__ bool bring_factors(const MmArgs& a, const Tile& x, int row0, int h, int lane, Factors<BN, WG>* ring,
                                               int* chunk, Freed freed, Ready ready, uint32_t gone) {
   // forward: rows lane, lane + 32, ... of a, and half h's scale of b;
@@ -385,8 +407,8 @@ __device__ __forceinline__ bool bring_factors(const MmArgs& a, const Tile& x, in
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if (i0 + s >= x.kb) break;
-      const int buf = *chunk & 1;
-      if (!mbar_wait_warp(freed(buf), (static_cast<uint32_t>(*chunk >> 1) & 1u) ^ 1u, gone)) return false;
+      const int buf = *chunk % kBufs;
+      if (!mbar_wait_warp(freed(buf), (static_cast<uint32_t>(*chunk / kBufs) & 1u) ^ 1u, gone)) return false;
       Factors<BN, WG>& f = ring[buf];
       if (!WG || h == 0) {
 #pragma unroll

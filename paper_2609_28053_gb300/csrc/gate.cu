@@ -241,12 +241,11 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // (NC of them), and one entry of its list each.  The row is written from the
 // lanes' experts, then the list's entries once more by the lanes that hold them; the
 // barrier of the warp between the two orders the stores.
-template <int LPT, int NC, bool F32, bool BF16>
+template <int LPT, int NC, bool dense, bool F32, bool BF16>
 __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGradArgs a) {
   constexpr int kTokens = 32 / LPT;  // of a warp
   constexpr float kLog2e = 1.4426950408889634f;
   const int lane = threadIdx.x & 31, sub = lane % LPT, E = a.E, K = a.K;
-  const bool dense = !a.sigmoid && !a.renorm;
   const bool in_place = a.grad_in && a.grad_out == static_cast<const void*>(a.grad_in);
   const int64_t step = static_cast<int64_t>(gridDim.x) * kGateWarps * kTokens;
   griddep_wait();
@@ -277,7 +276,7 @@ __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGr
     const int64_t t = w0 + lane / LPT;
     const bool live = t < a.T;
     float v[NC][8];
-    if (dense) {
+    if constexpr (dense) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) row[c].unpack(v[c]);
     }
@@ -398,17 +397,28 @@ int warp_grid(int64_t T, const DeviceInfo& di) {
   return static_cast<int>(blocks < most ? blocks : most);
 }
 
-template <int LPT, int NC>
+template <int LPT, int NC, bool dense>
 int launch_gate_grad_t(const GateGradArgs& a, const DeviceInfo& di, cudaStream_t s) {
   const dim3 grid(warp_grid((a.T + 32 / LPT - 1) / (32 / LPT), di)), block(kGateWarps * 32);
   cudaError_t e;
   if (a.z_fp32)
-    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, true, true>, grid, block, 0, s, a)
-                    : launch_dependent(gate_grad_kernel<LPT, NC, true, false>, grid, block, 0, s, a);
+    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, dense, true, true>, grid, block, 0, s, a)
+                    : launch_dependent(gate_grad_kernel<LPT, NC, dense, true, false>, grid, block, 0, s, a);
   else
-    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, false, true>, grid, block, 0, s, a)
-                    : launch_dependent(gate_grad_kernel<LPT, NC, false, false>, grid, block, 0, s, a);
+    e = a.grad_bf16 ? launch_dependent(gate_grad_kernel<LPT, NC, dense, false, true>, grid, block, 0, s, a)
+                    : launch_dependent(gate_grad_kernel<LPT, NC, dense, false, false>, grid, block, 0, s, a);
   return e == cudaSuccess ? kOk : kErrCuda;
+}
+
+template <bool dense>
+int launch_gate_grad_d(const GateGradArgs& a, const DeviceInfo& di, cudaStream_t s) {
+  int lanes = 8;  // of a token: as many as its list has entries, and a pass for its experts
+  while (lanes < 32 && (lanes * 8 < a.E || lanes < a.K)) lanes *= 2;
+  if (lanes == 8) return launch_gate_grad_t<8, 1, dense>(a, di, s);
+  if (lanes == 16) return launch_gate_grad_t<16, 1, dense>(a, di, s);
+  if (a.E <= 256) return launch_gate_grad_t<32, 1, dense>(a, di, s);
+  if (a.E <= 512) return launch_gate_grad_t<32, 2, dense>(a, di, s);
+  return launch_gate_grad_t<32, 4, dense>(a, di, s);
 }
 
 }  // namespace
@@ -416,7 +426,9 @@ int launch_gate_grad_t(const GateGradArgs& a, const DeviceInfo& di, cudaStream_t
 int launch_gate(const GateArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  if (a.T > kFewGateTokens && gate_tile_supported(a)) return launch_gate_tile(a, s);
+  const int G = a.top_groups < a.groups ? a.groups : 1;
+  if (a.T > kFewGateTokens && a.K <= 8 && a.E <= 512 && (G == 1 || G == 2 || G == 4 || G == 8) && a.E / 8 % G == 0)
+    return a.z_fp32 ? launch_gate_tile_fp32(a, s) : launch_gate_tile_bf16(a, s);
   const int grid = warp_grid(a.T, di);
   if (a.E <= 256) return launch_gate_warp<1>(a, grid, s);
   if (a.E <= 512) return launch_gate_warp<2>(a, grid, s);
@@ -426,13 +438,7 @@ int launch_gate(const GateArgs& a, cudaStream_t s) {
 int launch_gate_grad(const GateGradArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
-  int lanes = 8;  // of a token: as many as its list has entries, and a pass for its experts
-  while (lanes < 32 && (lanes * 8 < a.E || lanes < a.K)) lanes *= 2;
-  if (lanes == 8) return launch_gate_grad_t<8, 1>(a, di, s);
-  if (lanes == 16) return launch_gate_grad_t<16, 1>(a, di, s);
-  if (a.E <= 256) return launch_gate_grad_t<32, 1>(a, di, s);
-  if (a.E <= 512) return launch_gate_grad_t<32, 2>(a, di, s);
-  return launch_gate_grad_t<32, 4>(a, di, s);
+  return !a.sigmoid && !a.renorm ? launch_gate_grad_d<true>(a, di, s) : launch_gate_grad_d<false>(a, di, s);
 }
 
 }  // namespace eqb

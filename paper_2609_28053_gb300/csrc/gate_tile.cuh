@@ -1,8 +1,8 @@
-// gate_tile.cu -- the gate of many tokens (see gate.cu): a thread takes a token
+// gate_tile.cuh -- the gate of many tokens (see gate.cu): a thread takes a token
 // whose row of z lies in shared memory, a warp a tile of 32 tokens.
 //
-// The row is cut into 16 parts (8 where its chunks of 8 experts do not make 16 equal
-// ones), each within a group:
+// The row is cut into 16, 12 or 8 equal parts (8 of different size where its chunks of
+// 8 experts do not make equal ones), each within a group:
 //   1. the two largest c = z + b of every part, in pairs: exact (fp32), so the
 //      groups' scores and their ranking are too;
 //   2. of the parts that stay open, the eighth largest of their two largest is a
@@ -18,6 +18,8 @@
 //
 // Lanes bring their rows with bulk copies (a barrier a warp), at a stride of 4
 // (mod 8) words so that the lanes' 16-byte reads of one column hit distinct banks.
+#pragma once
+
 #include <float.h>
 
 #include "f32x2.cuh"
@@ -35,14 +37,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// The eight largest of 8 or 16 values, descending, in a[0..7].
+// The eight largest of 8 to 16 values, descending, in a[0..7].
 __device__ __forceinline__ void top8(float (&a)[8]) { sort_desc<8>(a); }
-__device__ __forceinline__ void top8(float (&a)[16]) {
+template <int N>
+__device__ __forceinline__ void top8(float (&a)[N]) {
   float x[8], y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     x[i] = a[i];
-    y[i] = a[8 + i];
+    y[i] = 8 + i < N ? a[8 + i] : -INFINITY;
   }
   sort_desc<8>(x);
   sort_desc<8>(y);
@@ -133,13 +136,13 @@ __device__ __forceinline__ int part_chunk(int s, int gc) {
   return C ? s * C : s / SP * gc + s % SP * gc / SP;
 }
 
-// C: chunks of each of 16 parts; 0: eight parts of any size.
-template <bool F32, int G, int KP, int C>
+// P parts of C chunks each; C = 0: eight parts of any size.
+template <bool F32, int G, int KP, int P, int C>
 __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const GateArgs a, const GateTile g) {
-  constexpr int kParts = C ? 16 : 8, SP = kParts / G;  // SP: parts of a group
+  constexpr int kParts = P, SP = kParts / G;  // SP: parts of a group
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int E = C ? 128 * C : a.E, K = a.K, gc = E / 8 / G, cmax = C ? C : (gc + SP - 1) / SP, words = C ? 1 : g.words;
+  const int E = C ? 8 * P * C : a.E, K = a.K, gc = E / 8 / G, cmax = C ? C : (gc + SP - 1) / SP, words = C ? 1 : g.words;
   float* bs = reinterpret_cast<float*>(smem);
   uint8_t* mine = smem + 4 * E + wid * g.warp_bytes;
   uint32_t* mw = reinterpret_cast<uint32_t*>(mine + 32 * g.stride) + lane;  // [part][words][32 lanes]
@@ -412,14 +415,14 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
   }
 }
 
-template <bool F32, int G, int C>
+template <bool F32, int G, int P, int C>
 int launch_tile(const GateArgs& a, cudaStream_t s) {
   DeviceInfo di;
   if (int rc = device_info(&di)) return rc;
   GateTile g;
   const int words = a.E * (F32 ? 4 : 2) / 4;
   g.stride = 4 * (words + ((4 - words) & 7));
-  constexpr int kParts = C ? 16 : 8;
+  constexpr int kParts = P;
   const int gc = a.E / 8 / G, sp = kParts / G, cmax = (gc + sp - 1) / sp;
   g.words = (cmax + 3) / 4;
   g.warp_bytes = 32 * g.stride + kParts * g.words * 128 + 16;
@@ -433,7 +436,7 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
   int64_t grid = (ntiles + nw - 1) / nw;
   if (grid > di.sm_count) grid = di.sm_count;
   g.tiles_per_warp = (ntiles + grid * nw - 1) / (grid * nw);
-  auto kern = gate_tile_kernel<F32, G, 8, C>;
+  auto kern = gate_tile_kernel<F32, G, 8, P, C>;
   if (!allow_smem(kern, di.max_smem_optin)) return kErrCuda;
   return launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(static_cast<unsigned>(nw) * 32),
                           head + static_cast<int>(nw) * g.warp_bytes, s, a, g) == cudaSuccess
@@ -443,10 +446,12 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
 
 template <bool F32, int G>
 int launch_tile_width(const GateArgs& a, cudaStream_t s) {
-  if (a.E == 128) return launch_tile<F32, G, 1>(a, s);
-  if (a.E == 256) return launch_tile<F32, G, 2>(a, s);
-  if (a.E == 512) return launch_tile<F32, G, 4>(a, s);
-  return launch_tile<F32, G, 0>(a, s);
+  if (a.E == 64) return launch_tile<F32, G, 8, 1>(a, s);
+  if (a.E == 96 && G < 8) return launch_tile<F32, G, G < 8 ? 12 : 8, 1>(a, s);
+  if (a.E == 128) return launch_tile<F32, G, 16, 1>(a, s);
+  if (a.E == 256) return launch_tile<F32, G, 16, 2>(a, s);
+  if (a.E == 512) return launch_tile<F32, G, 16, 4>(a, s);
+  return launch_tile<F32, G, 8, 0>(a, s);
 }
 
 template <bool F32>
@@ -459,14 +464,5 @@ int launch_tile_groups(const GateArgs& a, cudaStream_t s) {
 }
 
 }  // namespace
-
-bool gate_tile_supported(const GateArgs& a) {
-  const int G = a.top_groups < a.groups ? a.groups : 1;
-  return a.K <= 8 && a.E <= 512 && a.E >= 64 && (G == 1 || G == 2 || G == 4 || G == 8) && a.E / 8 % G == 0;
-}
-
-int launch_gate_tile(const GateArgs& a, cudaStream_t s) {
-  return a.z_fp32 ? launch_tile_groups<true>(a, s) : launch_tile_groups<false>(a, s);
-}
 
 }  // namespace eqb
