@@ -5,8 +5,9 @@
 // 8 experts do not make equal ones), each within a group:
 //   1. the two largest c = z + b of every part, in pairs: exact (fp32), so the
 //      groups' scores and their ranking are too;
-//   2. of the parts that stay open, the eighth largest of their two largest is a
-//      lower bound of the K-th largest c (K <= 8): from the eight largest of either;
+//   2. of the parts that stay open, the K-th largest of their two largest is a lower
+//      bound of the K-th largest c (K <= 8): from the eight largest of either, sorted, the
+//      smallest over i of the larger of one's i-th and the other's (K + 1 - i)-th;
 //   3. a bit for every open expert at or above the bound;
 //   4. those are inserted in ascending order into a sorted list: with 4 of 8 groups of
 //      32 open and K = 8 there are 8.1 a token and 9.0 in the lane of a warp that has
@@ -258,7 +259,11 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
       top8(m1);
       top8(m2);
 #pragma unroll
-      for (int i = 0; i < KP; ++i) bound = fminf(bound, fmaxf(m1[i], m2[KP - 1 - i]));
+      for (int k = 1; k <= KP; ++k)
+        if (k == K) {
+#pragma unroll
+          for (int i = 0; i < k; ++i) bound = fminf(bound, fmaxf(m1[i], m2[k - 1 - i]));
+        }
       bound = fmaxf(bound, -FLT_MAX);  // a closed expert is never chosen
     }
 
