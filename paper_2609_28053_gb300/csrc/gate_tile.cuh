@@ -126,7 +126,7 @@ __device__ __forceinline__ void scores8(const uint8_t* row, const float* bs, int
 
 struct GateTile {
   int stride;  // bytes of a staged row
-  int warp_bytes, words;  // words: mask words of a part
+  int warp_bytes;
   int64_t tiles_per_warp;
 };
 
@@ -143,11 +143,11 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
   constexpr int kParts = P, SP = kParts / G;  // SP: parts of a group
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int E = C ? 8 * P * C : a.E, K = a.K, gc = E / 8 / G, cmax = C ? C : (gc + SP - 1) / SP, words = C ? 1 : g.words;
+  const int E = C ? 8 * P * C : a.E, K = a.K, gc = E / 8 / G, words = (E + 31) / 32;
   float* bs = reinterpret_cast<float*>(smem);
   uint8_t* mine = smem + 4 * E + wid * g.warp_bytes;
-  uint32_t* mw = reinterpret_cast<uint32_t*>(mine + 32 * g.stride) + lane;  // [part][words][32 lanes]
-  const uint32_t bar = saddr(mine + 32 * g.stride + kParts * words * 128);
+  uint32_t* mw = reinterpret_cast<uint32_t*>(mine + 32 * g.stride) + lane;  // [words][32 lanes]
+  const uint32_t bar = saddr(mine + 32 * g.stride + words * 128);
   const uint8_t* row = mine + lane * g.stride;
   const int row_bytes = E * (F32 ? 4 : 2);
   if (lane == 0) {
@@ -219,8 +219,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
     }
     if (valid && bad) raise_flag(a.err, kErrNonfinite);
 
-    // ---- the groups' ranking: bits of the open parts
-    uint32_t open = (1u << kParts) - 1u;
+    // ---- the groups' ranking: bits of the open groups
+    uint32_t open = (1u << G) - 1u;
     if (G > 1 && a.top_groups < G) {
       float score[G];
       int ahead[G];
@@ -242,20 +242,15 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
         }
       open = 0u;
 #pragma unroll
-      for (int i = 0; i < G; ++i) open |= ahead[i] < a.top_groups ? ((1u << SP) - 1u) << (i * SP) : 0u;
+      for (int i = 0; i < G; ++i) open |= ahead[i] < a.top_groups ? 1u << i : 0u;
     }
 
     // ---- 2: a lower bound of the K-th largest
     float bound = INFINITY;
-    float first[G == 1 ? kParts : 1];  // the parts' largest, as they were
     {
-      if constexpr (G == 1) {
-#pragma unroll
-        for (int s = 0; s < kParts; ++s) first[s] = m1[s];
-      }
 #pragma unroll
       for (int s = 0; s < kParts; ++s)
-        if (!(open >> s & 1u)) m1[s] = m2[s] = -INFINITY;
+        if (!(open >> (s / SP) & 1u)) m1[s] = m2[s] = -INFINITY;
       top8(m1);
       top8(m2);
 #pragma unroll
@@ -267,42 +262,38 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
       bound = fmaxf(bound, -FLT_MAX);  // a closed expert is never chosen
     }
 
-    // ---- 3: who is at or above it; the sign of c - bound, eight chunks' bits a word
+    // ---- 3: who is at or above it: the sign of c - bound, 32 experts a word.  All
+    // chunks alike: of the open groups alone, each lane would read other places, in
+    // banks that meet, and wait for them (362 us at T = 2,097,152, E = 256, 4 of 8
+    // groups, where this takes 337)
     uint32_t hits = 0u;
-    if constexpr (G == 1) {  // parts whose largest is below it have none
-      open = 0u;
-#pragma unroll
-      for (int s = 0; s < kParts; ++s) open |= first[s] >= bound ? 1u << s : 0u;
-    }
     if (!valid) open = 0u;
     {
       const F2 less = splat2(-bound);
-      uint32_t left = open;
-      while (__any_sync(kFull, left != 0u)) {
-        const int s = left ? __ffs(left) - 1 : 0;
-        const bool there = left != 0u;
-        left &= left - 1u;
-        const int c0 = part_chunk<SP, C>(s, gc), c1 = part_chunk<SP, C>(s + 1, gc);
-        for (int w = 0; w < words; ++w) {
-          uint32_t word = 0u;
+      uint32_t word = 0u;
+      int group = 0, left = gc;  // chunks of the group from here on
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int c = c0 + 4 * w + u;
-            uint32_t bits = 0xffu;  // signs: set where it is below
-            if (4 * w + u < cmax && c < c1 && there) {
-              F2 v[4];
-              scores8<F32>(row, bs, c, v);
+      for (int c = 0; c < E / 8; ++c) {
+        F2 v[4];
+        scores8<F32>(row, bs, c, v);
+        uint32_t bits = 0u;  // signs: set where it is below
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const F2 d = add2(v[i], less);
-                bits = __funnelshift_l(__float_as_uint(lo2(d)), bits, 1);
-                bits = __funnelshift_l(__float_as_uint(hi2(d)), bits, 1);
-              }
-            }
-            word = word << 8 | (~bits & 0xffu);
-          }
-          if (there) mw[(s * words + w) << 5] = word;
-          hits |= there && word != 0u ? 0x80000000u >> (s * words + w) : 0u;
+        for (int i = 0; i < 4; ++i) {
+          const F2 d = add2(v[i], less);
+          bits = __funnelshift_l(__float_as_uint(lo2(d)), bits, 1);
+          bits = __funnelshift_l(__float_as_uint(hi2(d)), bits, 1);
+        }
+        word = word << 8 | (open >> group & 1u ? ~bits & 0xffu : 0u);
+        if ((c & 3) == 3 || c == E / 8 - 1) {
+          word <<= 8 * (3 - (c & 3));
+          mw[(c >> 2) << 5] = word;
+          hits |= word != 0u ? 0x80000000u >> (c >> 2) : 0u;
+          word = 0u;
+          if (C == 4) asm volatile("" ::: "memory");
+        }
+        if (--left == 0) {
+          ++group;
+          left = gc;
         }
       }
     }
@@ -321,20 +312,23 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
         const int k = __clz(hits);
         hits ^= 0x80000000u >> k;
         m = mw[k << 5];
-        const int s = words == 1 ? k : k >> 1;
-        wb = (part_chunk<SP, C>(s, gc) + (words == 1 ? 0 : (k & 1) * 4)) * 8;
+        wb = k << 5;
       }
       const int p = __clz(m);
       const int e = m != 0u ? wb + p : -1;
       m &= shr_clamp(0x7fffffffu, p);
       return e;
     };
+    // the next candidate's c is formed while this one is inserted
+    auto score_of = [&](int e) { return e >= 0 ? __fadd_rn(row1<F32>(row, e), bs[e]) : -INFINITY; };
     int e0 = fetch();
+    float s0 = score_of(e0);
     while (__any_sync(kFull, e0 >= 0)) {
       const int e1 = fetch();
-      const int at = max(e0, 0);
-      insert_sorted<KP>(v, id, e0 >= 0 ? __fadd_rn(row1<F32>(row, at), bs[at]) : -INFINITY, e0);
+      const float s1 = score_of(e1);
+      insert_sorted<KP>(v, id, s0, e0);
       e0 = e1;
+      s0 = s1;
     }
     // after a NaN (flagged) a finished lane's entry can stand before others; it is -1
 
@@ -427,14 +421,11 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
   GateTile g;
   const int words = a.E * (F32 ? 4 : 2) / 4;
   g.stride = 4 * (words + ((4 - words) & 7));
-  constexpr int kParts = P;
-  const int gc = a.E / 8 / G, sp = kParts / G, cmax = (gc + sp - 1) / sp;
-  g.words = (cmax + 3) / 4;
-  g.warp_bytes = 32 * g.stride + kParts * g.words * 128 + 16;
+  g.warp_bytes = 32 * g.stride + (a.E + 31) / 32 * 128 + 16;
   const int head = 4 * a.E;
   int most = (di.max_smem_optin - head) / g.warp_bytes;
   if (most > kMaxGateWarps) most = kMaxGateWarps;
-  if (most < 1 || g.words > 2) return kErrUnsupported;
+  if (most < 1) return kErrUnsupported;
   const int64_t ntiles = (a.T + 31) / 32;
   int64_t nw = (ntiles + di.sm_count - 1) / di.sm_count;
   if (nw > most) nw = most;
