@@ -3,8 +3,7 @@
 //   forward   out[r, j] = sum_B scale[r, B] w_scale[e, j / 128, B] (q_r . w_ej over block B)
 //   weights   dW[e, i, j] = sum_B a_scale[B, i] b_scale[B, j] (a_i . b_j over block B of e's rows)
 // Both operands lie K-major, so both are one kernel: tiles of the output, 128 of K
-// (one 128-byte swizzle atom) a stage.  This file has the launches, and the kernel
-// for few rows an expert; expert_pair.cu has the one for many, by pairs of SMs.
+// (one 128-byte swizzle atom) a stage.
 //
 // A scale belongs to 128 values of K, so the tensor cores' sums end with each
 // stage: the accumulators of a stage (BN columns of tensor memory, two to four of
@@ -12,13 +11,31 @@
 // fp32 sums in registers.  That also keeps the tensor cores' own sums, which cut
 // off instead of rounding, 128 products long.
 //
-// Few rows an expert: the weights are what is read, and a tile of 128 rows needs no
-// more of A than the rows that there are.
+// What bounds it with many rows an expert is that way out.  R = 131,072, n = 2,048, d =
+// 4,096, 128 experts: 897 us and 2.45 PFLOP/s where all have the same number of rows, 947
+// us where some have a multiple of others'; a stage takes an SM about 970 clocks, of
+// which its MMAs are 512.  A warp that takes 32 rows x 128 columns of a stage out waits
+// three times for tensor memory (about 130 clocks whatever it asked for), and beside
+// 128 sums there are registers for 48 columns on their way.  Sixteen such warps would
+// hide that, but their registers do not fit.  The scales count too: every scale
+// fetched once, four stages at a time, took 947 us where each stage's own loads took 1,015.
+// Pairs of SMs (cta_group::2) take in less a stage and were slower: tiles of 256 x 256
+// with two accumulators 1,025 us, of 256 x 160 with three 1,195.
+// Few rows an expert: the weights are what is read (256 rows in 109 of the 128 experts
+// 138 us, 99% of the copy rate), and a tile of 128 rows needs no more of A than the
+// groups of 32 rows that there are.  Where the tiles of 256 columns leave SMs without
+// one, they are 64 wide (8 rows in 8 experts of 2,048 x 4,096: 16.8 us).
+// Weights' gradient: a stage has a factor for each column beside the row's, one more
+// multiplication a sum, 1,600 clocks; an expert's rows are few stages (R = 65,536 over 64
+// experts: eight), so the sums' way to memory, 128 KB a tile, counts as well: 291 us
+// where the output alone takes 79.
 //
-// Roles, bounded waits and the way out of a stall are those of the router's
-// projection: warp 0 loads, warp 1 issues the MMAs, the others take the
-// accumulators out.  A block goes over tiles blockIdx.x, blockIdx.x + gridDim.x, ...;
-// which expert and rows a tile has follows from `first`, read on the device.
+// Roles: warp 0 loads, warp 1 issues the MMAs, warps 2 and 3 bring the scales'
+// products to shared memory (in the warps that need them they took the registers of
+// their sums), the others take the accumulators out.  Every wait is bounded; after one
+// that ran out the block waits for its loads in flight, frees its tensor memory and
+// returns.  A block goes over tiles blockIdx.x, blockIdx.x + gridDim.x, ...; which
+// expert and rows a tile has follows from `first`, read on the device.
 #include "expert_mm.cuh"
 
 namespace eqb {
@@ -117,7 +134,9 @@ __global__ void __launch_bounds__(kMmThreads, 1)
       issued = n;
     } else if (warp == 1) {
       // The whole warp goes through the loop, so that addresses and descriptors are the
-      // same for all lanes, and one lane issues: ISSUE_NOTE
+      // same for all lanes, and one lane issues.  The operands' barrier comes first: it
+      // is there already when the accumulator's, which the chain hangs on, completes (the
+      // other way round 1,073 us where this took 1,031)
       constexpr uint32_t idesc = umma_idesc_e4m3(kBM, BN);
       const uint32_t gone = smem_u32(&abort_word);
       const uint64_t ad0 = sw128_desc(base), bd0 = sw128_desc(base + kATile);
@@ -163,7 +182,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
     // 192 registers, and what is not kept meanwhile does not have to be spilled
     const int q = warp & 3, h = (warp - 4) >> 2;
     const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * kCols);
-    const uint32_t factor = smem_u32(&ring[0].row[WG ? 0 : h][q * 32 + lane]), gone = smem_u32(&abort_word);
+    const uint32_t factor = smem_u32(&ring[0].row[WG || mm_blocks(BN) == 1 ? 0 : h][q * 32 + lane]), gone = smem_u32(&abort_word);
     int chunk = 0, e = 0;
     bool ok = true;
     for (int t = first; t < total && ok; t += step) {
@@ -186,10 +205,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
         auto release = [&]() {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(acce(buf));
-            if (!WG) mbar_arrive(read(buf));
-          }
+          mbar_arrive_one(acce(buf), WG ? 0u : read(buf), lane);
         };
         if (some) add_stage<kCols, WG>(mine + buf * BN, f, ring[buf].col + (WG ? h * kCols : 0), acc, release);
         else release();

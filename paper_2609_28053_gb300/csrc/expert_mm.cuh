@@ -1,6 +1,6 @@
-// expert_mm.cuh -- what the kernels of the experts' products share
-// (expert_matmul.cu, expert_pair.cu): tiles and whose they are, the instruction of
-// 8-bit operands, the way from tensor memory into the sums, and the tensor maps.
+// expert_mm.cuh -- parts of the experts' products (expert_matmul.cu): tiles and whose
+// they are, the instruction of 8-bit operands, the scales' way in, the way from
+// tensor memory into the sums, and the tensor maps.
 #pragma once
 
 #include "f32x2.cuh"
@@ -266,7 +266,9 @@ __device__ __forceinline__ void add_stage(uint32_t taddr, float f, const float* 
 
 // Up to 64 polls of at most ~1 us for the phase of parity `parity`, in one loop of
 // three instructions: where a step of the pipeline hangs on a phase that is there
-// already, what follows the poll counts.
+// already, what follows the poll counts (with the poll, its limit and the abort word in
+// one loop: 1,202 us for the product that takes 1,073 so; one lane polling for its
+// warp: 2,150).
 __device__ __forceinline__ uint32_t mbar_try64(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -307,6 +309,18 @@ __device__ __forceinline__ bool elect_one() {
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(p));
   return p != 0;
+}
+// Lane 0 arrives at `first` and, unless it is 0, at `second`: by predicate, so that the
+// warp does not part and meet again in between.
+__device__ __forceinline__ void mbar_arrive_one(uint32_t first, uint32_t second, int lane) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.eq.s32 p, %2, 0;\n\t"
+      "setp.ne.and.u32 q, %1, 0, p;\n\t"
+      "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t"
+      "@q mbarrier.arrive.shared::cta.b64 _, [%1];\n\t}" ::"r"(first),
+      "r"(second), "r"(lane)
+      : "memory");
 }
 __device__ __forceinline__ float lds_f32(uint32_t at) {
   float v;
@@ -352,75 +366,135 @@ __device__ __forceinline__ void store_row(const MmArgs& a, int64_t row, int col,
     }
 }
 
-// The factors of a stage, in shared memory: of each half of the columns, of every
-// row (forward: both scales' product), or of the rows and of the columns (weights).
+// The factors of a stage, in shared memory.  Forward: of every row, both scales'
+// product, for each of the blocks of 128 columns that a tile of BN touches.  Weights:
+// of the rows, and of the columns.
+constexpr int mm_blocks(int BN) { return BN > 128 ? BN / 128 : 1; }
 template <int BN, bool WG>
 struct Factors {
-  static_assert(!WG || BN == 256, "a warp brings the factors of 2 x 128 columns");
-  float row[WG ? 1 : 2][kBM];
+  float row[WG ? 1 : mm_blocks(BN)][kBM];
   float col[WG ? BN : 4];
 };
 
 // Warps 2 (h = 0) and 3 (h = 1): the factors of one tile's stages into `ring`, kBufs
-// stages deep, each loaded from memory two stages before it is written.  ring[buf]
-// may be written once `freed(buf)` has a phase for it, and adds its arrival to what
-// `ready(buf)` waits for.  False when a wait ran out.
+// stages deep.  ring[buf] may be written once `freed(buf)` has a phase for it, and adds
+// its arrival to what `ready(buf)` waits for.  False when a wait ran out.
 template <int BN, bool WG, int kBufs, class Freed, class Ready>
 __device__ __forceinline__ bool bring_factors(const MmArgs& a, const Tile& x, int row0, int h, int lane, Factors<BN, WG>* ring,
                                               int* chunk, Freed freed, Ready ready, uint32_t gone) {
-  // forward: rows lane, lane + 32, ... of a, and half h's scale of b;
-  // weights: the same rows of a (h = 0), or 2 x 4 columns of b (h = 1)
-  const float* pa[4];
-  bool la[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + i * 32 + lane;
-    la[i] = row < x.rows && (!WG || h == 0);
-    pa[i] = WG ? a.a_scale + static_cast<int64_t>(x.b0) * a.rows + x.m + row : a.a_scale + (static_cast<int64_t>(x.m) + row) * x.kb;
-  }
-  const int nb = (a.n + 127) / 128, col = x.n0 + h * (BN / 2);
-  const float* pb = WG ? a.b_scale + static_cast<int64_t>(x.b0) * a.n + x.n0 + lane * 4
-                       : a.b_scale + (static_cast<int64_t>(x.e) * nb + min(col / 128, nb - 1)) * x.kb;
-  const bool l0 = WG && h == 1 && x.n0 + lane * 4 < a.n, l1 = WG && h == 1 && x.n0 + 128 + lane * 4 < a.n;
-  float va[2][4], vb[2];
-  float4 q0[2], q1[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    vb[s] = 0.f;
-    q0[s] = q1[s] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) va[s][i] = 0.f;
-  }
-  auto fetch = [&](int i, int s) {
-    if (i >= x.kb) return;
-    const int64_t oa = WG ? static_cast<int64_t>(i) * a.rows : i;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (la[k]) va[s][k] = __ldg(pa[k] + oa);
-    if (!WG) vb[s] = __ldg(pb + i);
-    if (l0) q0[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n));
-    if (l1) q1[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n + 128));
+  auto begin = [&](int* buf) {
+    *buf = *chunk % kBufs;
+    return mbar_wait_warp(freed(*buf), (static_cast<uint32_t>(*chunk / kBufs) & 1u) ^ 1u, gone);
   };
-  fetch(0, 0);
-  fetch(1, 1);
-  for (int i0 = 0; i0 < x.kb; i0 += 2) {
+  auto end = [&](int buf) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(ready(buf));
+    ++*chunk;
+  };
+  if constexpr (!WG) {
+    // rows h * 64 + lane and 32 further, four stages of their scales at a time, the
+    // next four on their way meanwhile; b's scales of four stages in lanes 4 j + i
+    constexpr int kBlocks = mm_blocks(BN);
+    const int nb = (a.n + 127) / 128, i4 = lane & 3;
+    const float* pa[2];
+    bool la[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (i0 + s >= x.kb) break;
-      const int buf = *chunk % kBufs;
-      if (!mbar_wait_warp(freed(buf), (static_cast<uint32_t>(*chunk / kBufs) & 1u) ^ 1u, gone)) return false;
-      Factors<BN, WG>& f = ring[buf];
-      if (!WG || h == 0) {
+    for (int r = 0; r < 2; ++r) {
+      const int row = row0 + h * 64 + r * 32 + lane;
+      la[r] = row < x.rows;
+      pa[r] = a.a_scale + (static_cast<int64_t>(x.m) + row) * x.kb;
+    }
+    const float* pb = a.b_scale + (static_cast<int64_t>(x.e) * nb + min(x.n0 / 128 + (lane >> 2), nb - 1)) * x.kb + i4;
+    const bool lb = lane < 4 * kBlocks, wide = (x.kb & 3) == 0 && (reinterpret_cast<uintptr_t>(a.a_scale) & 15u) == 0;
+    float next[2][4] = {}, next_b = 0.f;
+    auto fetch = [&](int k0) {
+      if (k0 >= x.kb) return;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) f.row[WG ? 0 : h][k * 32 + lane] = WG ? va[s][k] : va[s][k] * vb[s];
-      } else if constexpr (WG) {
-        *reinterpret_cast<float4*>(f.col + lane * 4) = q0[s];
-        *reinterpret_cast<float4*>(f.col + 128 + lane * 4) = q1[s];
+      for (int r = 0; r < 2; ++r) {
+        if (!la[r]) continue;
+        if (wide) {
+          const float4 v = __ldg(reinterpret_cast<const float4*>(pa[r] + k0));
+          next[r][0] = v.x; next[r][1] = v.y; next[r][2] = v.z; next[r][3] = v.w;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (k0 + i < x.kb) next[r][i] = __ldg(pa[r] + k0 + i);
+        }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ready(buf));
-      ++*chunk;
-      fetch(i0 + s + 2, s);
+      if (lb && k0 + i4 < x.kb) next_b = __ldg(pb + k0);
+    };
+    fetch(0);
+    for (int k0 = 0; k0 < x.kb; k0 += 4) {
+      float va[2][4];
+      const float vb = next_b;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) va[r][i] = next[r][i];
+      fetch(k0 + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (k0 + i >= x.kb) break;
+        int buf;
+        if (!begin(&buf)) return false;
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+          const float b = __shfl_sync(kFull, vb, 4 * j + i);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) ring[buf].row[j][h * 64 + r * 32 + lane] = va[r][i] * b;
+        }
+        end(buf);
+      }
+    }
+  } else if (h == 0) {
+    // rows lane, lane + 32, ... of a, two stages ahead
+    const float* pa = a.a_scale + static_cast<int64_t>(x.b0) * a.rows + x.m + row0 + lane;
+    float v[2][4] = {};
+    auto fetch = [&](int i, int s) {
+      if (i >= x.kb) return;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (row0 + k * 32 + lane < x.rows) v[s][k] = __ldg(pa + static_cast<int64_t>(i) * a.rows + k * 32);
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    for (int i0 = 0; i0 < x.kb; i0 += 2) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (i0 + s >= x.kb) break;
+        int buf;
+        if (!begin(&buf)) return false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ring[buf].row[0][k * 32 + lane] = v[s][k];
+        end(buf);
+        fetch(i0 + s + 2, s);
+      }
+    }
+  } else {
+    // columns 4 lane .. 4 lane + 3 of b, and those 128 further, two stages ahead
+    const float* pb = a.b_scale + static_cast<int64_t>(x.b0) * a.n + x.n0 + lane * 4;
+    const bool l0 = x.n0 + lane * 4 < a.n && lane * 4 < BN, l1 = x.n0 + 128 + lane * 4 < a.n && 128 + lane * 4 < BN;
+    float4 q0[2], q1[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) q0[s] = q1[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fetch = [&](int i, int s) {
+      if (i >= x.kb) return;
+      if (l0) q0[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n));
+      if (l1) q1[s] = __ldg(reinterpret_cast<const float4*>(pb + static_cast<int64_t>(i) * a.n + 128));
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    for (int i0 = 0; i0 < x.kb; i0 += 2) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (i0 + s >= x.kb) break;
+        int buf;
+        if (!begin(&buf)) return false;
+        if (lane * 4 < BN) *reinterpret_cast<float4*>(ring[buf].col + lane * 4) = q0[s];
+        if (128 + lane * 4 < BN) *reinterpret_cast<float4*>(ring[buf].col + 128 + lane * 4) = q1[s];
+        end(buf);
+        fetch(i0 + s + 2, s);
+      }
     }
   }
   return true;
