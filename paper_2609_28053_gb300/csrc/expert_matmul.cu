@@ -182,7 +182,9 @@ __global__ void __launch_bounds__(kMmThreads, 1)
     // 192 registers, and what is not kept meanwhile does not have to be spilled
     const int q = warp & 3, h = (warp - 4) >> 2;
     const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(h * kCols);
-    const uint32_t factor = smem_u32(&ring[0].row[WG || mm_blocks(BN) == 1 ? 0 : h][q * 32 + lane]), gone = smem_u32(&abort_word);
+    const int line = q * 32 + (WG ? lane >> 2 : lane), quad = WG ? 2 * (lane & 3) : 0;  // the thread's first row and column
+    const uint32_t factor = smem_u32(&ring[0].row[WG || mm_blocks(BN) == 1 ? 0 : h][line]), gone = smem_u32(&abort_word);
+    const uint32_t factor_col = smem_u32(&ring[0].col[WG ? h * kCols + quad : 0]);
     int chunk = 0, e = 0;
     bool ok = true;
     for (int t = first; t < total && ok; t += step) {
@@ -201,23 +203,24 @@ __global__ void __launch_bounds__(kMmThreads, 1)
         ok = mbar_wait_warp(accf(buf), phase_acc, gone);
         if (!ok) break;
         tc_fence_after();
-        const float f = lds_f32(factor + buf * static_cast<uint32_t>(sizeof(Factors<BN, WG>)));
+        const uint32_t there = buf * static_cast<uint32_t>(sizeof(Factors<BN, WG>));
+        float f[WG ? 4 : 1];
+#pragma unroll
+        for (int k = 0; k < (WG ? 4 : 1); ++k) f[k] = lds_f32(factor + there + 32u * k);
         auto release = [&]() {
           tc_fence_before();
           __syncwarp();
-          mbar_arrive_one(acce(buf), WG ? 0u : read(buf), lane);
+          mbar_arrive_one(acce(buf), read(buf), lane);
         };
-        if (some) add_stage<kCols, WG>(mine + buf * BN, f, ring[buf].col + (WG ? h * kCols : 0), acc, release);
-        else release();
-        if (WG) {
-          __syncwarp();  // the columns' factors are read
-          if (lane == 0) mbar_arrive(read(buf));
-        }
+        if (!some) release();
+        else if constexpr (WG) add_stage_columns<kCols>(mine + buf * BN, f, factor_col + there, acc, release);
+        else add_stage<kCols>(mine + buf * BN, f[0], acc, release);
       }
       if (!ok) break;
       const Tile x = tile_of<kBM, BN, WG>(a, table, t, &e);
-      const int row = q * 32 + lane;
-      if (row < x.rows) store_row<kCols, WG>(a, (WG ? static_cast<int64_t>(x.e) * a.rows : 0) + x.m + row, x.n0 + h * kCols, acc);
+      const int col = x.n0 + h * kCols + quad;
+      if constexpr (WG) store_quads<kCols>(a, static_cast<int64_t>(x.e) * a.rows + x.m + line, x.rows - line, col, acc);
+      else if (line < x.rows) store_row<kCols>(a, static_cast<int64_t>(x.m) + line, col, acc);
     }
   }
   tc_fence_before();

@@ -155,6 +155,17 @@ __device__ __forceinline__ int tiles_of(const MmArgs& a, const Table& table) {
   return n < a.most ? static_cast<int>(n) : a.most;
 }
 
+__device__ __forceinline__ float lds_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ F2 lds_f2(uint32_t at) {
+  float x, y;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(at) : "memory");
+  return f2(x, y);
+}
+
 // 32 or 16 columns of the warp's lanes, on their way until tmem_wait has returned.
 // The registers pass through it, or through tmem_here after it, so that no use of them
 // moves before it; and the loads that come again into the same registers take
@@ -213,29 +224,19 @@ __device__ __forceinline__ void tmem_here(uint32_t (&r)[16]) {
                  "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
 }
 
-// N columns of a stage, times f (and times the columns' own factors in cs), added to the sums.
-template <bool kColScale, int N>
-__device__ __forceinline__ void add_columns(const uint32_t (&r)[N], const F2& ff, const float* cs, F2* acc) {
+// N columns of a stage, times f, added to the sums.
+template <int N>
+__device__ __forceinline__ void add_columns(const uint32_t (&r)[N], const F2& ff, F2* acc) {
 #pragma unroll
-  for (int v = 0; v < N / 2; v += 2) {
-    F2 d = f2(__uint_as_float(r[2 * v]), __uint_as_float(r[2 * v + 1]));
-    F2 e = f2(__uint_as_float(r[2 * v + 2]), __uint_as_float(r[2 * v + 3]));
-    if (kColScale) {
-      const float4 s = *reinterpret_cast<const float4*>(cs + 2 * v);
-      d = mul2(d, f2(s.x, s.y));
-      e = mul2(e, f2(s.z, s.w));
-    }
-    acc[v] = fma2(d, ff, acc[v]);
-    acc[v + 1] = fma2(e, ff, acc[v + 1]);
-  }
+  for (int v = 0; v < N / 2; ++v) acc[v] = fma2(f2(__uint_as_float(r[2 * v]), __uint_as_float(r[2 * v + 1])), ff, acc[v]);
 }
 
 // Takes kCols columns of the warp's lanes out of tensor memory and adds them to the
 // sums; `release` runs as soon as the last of them are in registers.  A wait is for
 // all loads on their way and takes about 130 cycles however much was asked for, so 48
 // columns share one (64 do not fit in registers beside 128 sums).
-template <int kCols, bool kColScale, class Release>
-__device__ __forceinline__ void add_stage(uint32_t taddr, float f, const float* cs, F2 (&acc)[kCols / 2], Release release) {
+template <int kCols, class Release>
+__device__ __forceinline__ void add_stage(uint32_t taddr, float f, F2 (&acc)[kCols / 2], Release release) {
   static_assert(kCols == 32 || kCols == 128, "columns of a warp");
   const F2 ff = splat2(f);
   uint32_t r[32];
@@ -243,24 +244,75 @@ __device__ __forceinline__ void add_stage(uint32_t taddr, float f, const float* 
   if constexpr (kCols == 32) {
     tmem_wait(r);
     release();
-    add_columns<kColScale>(r, ff, cs, acc);
+    add_columns(r, ff, acc);
   } else {
     uint32_t s[16];
     tmem_start(taddr + 32u, s);
     tmem_wait(r);
     tmem_here(s);
-    add_columns<kColScale>(r, ff, cs, acc);
+    add_columns(r, ff, acc);
     tmem_again(taddr + 48u, r);
-    add_columns<kColScale>(s, ff, cs + 32, acc + 16);
+    add_columns(s, ff, acc + 16);
     tmem_again(taddr + 80u, s);
     tmem_wait(r);
     tmem_here(s);
-    add_columns<kColScale>(r, ff, cs + 48, acc + 24);
+    add_columns(r, ff, acc + 24);
     tmem_again(taddr + 96u, r);
-    add_columns<kColScale>(s, ff, cs + 80, acc + 40);
+    add_columns(s, ff, acc + 40);
     tmem_wait(r);
     release();
-    add_columns<kColScale>(r, ff, cs + 96, acc + 48);
+    add_columns(r, ff, acc + 48);
+  }
+}
+// 32 columns of 16 lanes: of every 8 columns, a thread gets columns 2 (lane % 4) and the
+// next of lanes lane / 4 and 8 further.
+__device__ __forceinline__ void tmem_quads(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+        "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+// The same where each column has a factor of its own.  A row a lane, every lane would
+// need every column's factor, and 128 of them to each lane of eight warps are 1,024
+// clocks of shared memory a stage; in quads of lanes a thread has four rows and a
+// quarter of the columns.  acc[c / 8 * 4 + r]: columns c + 2 (lane % 4) and the next of
+// row lane / 4 + 8 r; f: the rows' factors, cs: those of columns 2 (lane % 4) and on.
+template <int kCols, class Release>
+__device__ __forceinline__ void add_stage_columns(uint32_t taddr, const float (&f)[4], uint32_t cs, F2 (&acc)[kCols / 2], Release release) {
+  uint32_t r[2][16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[0][i] = r[1][i] = 0u;
+  tmem_quads(taddr, r[0]);
+  tmem_quads(taddr + (16u << 16), r[1]);
+#pragma unroll
+  for (int c = 0; c < kCols; c += 32) {
+    F2 p[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) p[g] = lds_f2(cs + static_cast<uint32_t>(c + 8 * g) * 4u);
+    tmem_wait(r[0]);
+    tmem_here(r[1]);
+    if (c + 32 == kCols) release();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          F2& sum = acc[(c / 8 + g) * 4 + 2 * h + k];
+          const F2 d = f2(__uint_as_float(r[h][4 * g + 2 * k]), __uint_as_float(r[h][4 * g + 2 * k + 1]));
+          sum = fma2(mul2(d, p[g]), splat2(f[2 * h + k]), sum);
+        }
+      if (c + 32 < kCols) tmem_quads(taddr + (static_cast<uint32_t>(16 * h) << 16) + c + 32u, r[h]);
+    }
   }
 }
 
@@ -310,30 +362,23 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(p));
   return p != 0;
 }
-// Lane 0 arrives at `first` and, unless it is 0, at `second`: by predicate, so that the
-// warp does not part and meet again in between.
+// Lane 0 arrives at both: by predicate, so that the warp does not part and meet again
+// in between.
 __device__ __forceinline__ void mbar_arrive_one(uint32_t first, uint32_t second, int lane) {
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
+      "{\n\t.reg .pred p;\n\t"
       "setp.eq.s32 p, %2, 0;\n\t"
-      "setp.ne.and.u32 q, %1, 0, p;\n\t"
       "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t"
-      "@q mbarrier.arrive.shared::cta.b64 _, [%1];\n\t}" ::"r"(first),
+      "@p mbarrier.arrive.shared::cta.b64 _, [%1];\n\t}" ::"r"(first),
       "r"(second), "r"(lane)
       : "memory");
 }
-__device__ __forceinline__ float lds_f32(uint32_t at) {
-  float v;
-  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-
 // The warp's lanes' sums, a row a lane, to its kCols columns of the output from
 // `col` on, a whole sector a store.
-template <int kCols, bool WG>
+template <int kCols>
 __device__ __forceinline__ void store_row(const MmArgs& a, int64_t row, int col, F2 (&acc)[kCols / 2]) {
   const int64_t at = row * a.n + col;
-  if (!WG && !a.out_fp32) {
+  if (!a.out_fp32) {
     uint16_t* o = static_cast<uint16_t*>(a.out) + at;
 #pragma unroll
     for (int i = 0; i < kCols / 16; ++i)
@@ -350,13 +395,6 @@ __device__ __forceinline__ void store_row(const MmArgs& a, int64_t row, int col,
   for (int i = 0; i < kCols / 8; ++i)
     if (col + i * 8 < a.n) {
       uint32_t p[8];
-      if (WG && a.add) {
-        const float4 u = *reinterpret_cast<const float4*>(o + i * 8), v = *reinterpret_cast<const float4*>(o + i * 8 + 4);
-        acc[i * 4] = add2(acc[i * 4], f2(u.x, u.y));
-        acc[i * 4 + 1] = add2(acc[i * 4 + 1], f2(u.z, u.w));
-        acc[i * 4 + 2] = add2(acc[i * 4 + 2], f2(v.x, v.y));
-        acc[i * 4 + 3] = add2(acc[i * 4 + 3], f2(v.z, v.w));
-      }
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         p[2 * v] = __float_as_uint(lo2(acc[i * 4 + v]));
@@ -364,6 +402,27 @@ __device__ __forceinline__ void store_row(const MmArgs& a, int64_t row, int col,
       }
       store_sector8(o + i * 8, p);
     }
+}
+// The same of sums in quads of lanes, `row` and `col` being the lane's first: a quad
+// writes a sector.  `rows`: how many there are behind row.
+template <int kCols>
+__device__ __forceinline__ void store_quads(const MmArgs& a, int64_t row, int rows, int col, F2 (&acc)[kCols / 2]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (8 * k >= rows) break;
+    float* o = static_cast<float*>(a.out) + (row + 8 * k) * a.n + col;
+#pragma unroll
+    for (int g = 0; g < kCols / 8; ++g)
+      if (col + g * 8 < a.n) {
+        F2 v = acc[g * 4 + k];
+        float2* to = reinterpret_cast<float2*>(o + g * 8);
+        if (a.add) {
+          const float2 u = *to;
+          v = add2(v, f2(u.x, u.y));
+        }
+        *to = make_float2(lo2(v), hi2(v));
+      }
+  }
 }
 
 // The factors of a stage, in shared memory.  Forward: of every row, both scales'
