@@ -26,9 +26,11 @@
 // groups of 32 rows that there are.  Where the tiles of 256 columns leave SMs without
 // one, they are 64 wide (8 rows in 8 experts of 2,048 x 4,096: 16.8 us).
 // Weights' gradient: a stage has a factor for each column beside the row's, one more
-// multiplication a sum, 1,600 clocks; an expert's rows are few stages (R = 65,536 over 64
-// experts: eight), so the sums' way to memory, 128 KB a tile, counts as well: 291 us
-// where the output alone takes 79.
+// multiplication a sum, and takes about 1,400 clocks; an expert's rows are few stages (R =
+// 65,536 over 64 experts, n = 1,024, d = 2,048: eight and a half), so the sums' way to
+// memory, 128 KB a tile, counts as well: 245 us where the output alone takes 79.  Whole lines
+// instead of sectors a store (248 where sectors took 253) and the two halves of a
+// tile as blocks of their own on one SM (282) did not change that.
 //
 // Roles: warp 0 loads, warp 1 issues the MMAs, warps 2 and 3 bring the scales'
 // products to shared memory (in the warps that need them they took the registers of
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   griddep_wait();
-  fill_table<kBM>(a, table);
+  fill_table<kBM, WG>(a, table);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

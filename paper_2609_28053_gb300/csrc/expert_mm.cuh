@@ -70,6 +70,7 @@ struct Tile {
 struct Table {
   int tiles[kMaxExperts + 1];  // forward: tiles of the experts before
   int lo[kMaxExperts], n[kMaxExperts];  // first row and rows, or blocks
+  uint32_t order[kMaxExperts];  // weights: the tiles' experts, min(blocks, 2^22 - 1) and 1023 - expert
   int group[kMaxExperts / 32];
 };
 
@@ -79,8 +80,8 @@ __device__ __forceinline__ Tile tile_of(const MmArgs& a, const Table& table, int
   Tile x;
   if (WG) {
     const int per = a.nt * a.mt;
-    x.e = t / per;
-    const int rest = t - x.e * per, mt = rest / a.nt;
+    const int i = t / per, rest = t - i * per, mt = rest / a.nt;
+    x.e = kMaxExperts - 1 - static_cast<int>(table.order[i] % kMaxExperts);
     x.m = mt * BM;
     x.n0 = (rest - mt * a.nt) * BN;
     x.rows = min(BM, a.rows - x.m);
@@ -109,8 +110,14 @@ __device__ __forceinline__ Tile tile_of(const MmArgs& a, const Table& table, int
 }
 
 // Fills the table by the block's threads: `first` is kept within [0, limit] and in order
-// whatever it says; tiles add up to at most 2^30.
-template <int BM>
+// whatever it says; tiles add up to at most 2^30.  Weights: the experts by falling
+// number of blocks (then by number; a bitonic sort), so that what every SM gets, each 152nd
+// tile, differs by no more than one tile's blocks.  R = 65,536 over 64 experts, n = 1,024, d =
+// 2,048: 245 us, in the experts' order 253, with rows an expert whose logarithm deviates
+// by 0.5 from its mean; by 1.5, 262 and 295.  Experts of few tiles keep their order:
+// sorting takes 8 us of 1,024 (n = 128, d = 256, one tile an expert: 36 us, sorted 44).
+constexpr int kOrderTiles = 8;
+template <int BM, bool WG>
 __device__ __forceinline__ void fill_table(const MmArgs& a, Table& table) {
   constexpr int kMost = 1 << 30;
   const int lane = threadIdx.x & 31, limit = static_cast<int>(a.limit);
@@ -131,6 +138,25 @@ __device__ __forceinline__ void fill_table(const MmArgs& a, Table& table) {
     }
     if (e < a.E) table.tiles[e + 1] = v;
     if (lane == 31) table.group[e0 >> 5] = v;
+  }
+  if (WG) {
+    int size = 1;
+    while (size < a.E) size *= 2;
+    for (int e = threadIdx.x; e < size; e += blockDim.x)
+      table.order[e] = e < a.E ? static_cast<uint32_t>(min(table.n[e], (1 << 22) - 1)) * kMaxExperts + (kMaxExperts - 1 - e) : 0u;
+    for (int run = 2; run <= size && a.nt * a.mt >= kOrderTiles; run *= 2)
+      for (int apart = run / 2; apart; apart /= 2) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < size / 2; i += blockDim.x) {
+          const int lo = 2 * i - (i & (apart - 1)), hi = lo + apart;
+          const uint32_t x = table.order[lo], y = table.order[hi];
+          if (((lo & run) == 0) == (x < y)) {
+            table.order[lo] = y;
+            table.order[hi] = x;
+          }
+        }
+      }
+    return;
   }
   __syncthreads();
   if (threadIdx.x < 32) {

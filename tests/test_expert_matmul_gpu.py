@@ -177,6 +177,18 @@ def test_wgrad_exact_on_whole_numbers(blk, n, d, add):
     assert torch.equal(got, (want + dW0.double() if add else want).float())
 
 
+def test_wgrad_of_many_unlike_experts():
+    """Tiles go by the experts' sizes, not by their numbers; equal and empty ones are among them."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    blk, n, d = [(7 * e) % 5 if e % 3 else 0 for e in range(100)], 144, 1040
+    P = sum(blk)
+    a, b = codes((n, P * 128), g, 2), codes((d, P * 128), g, 3)
+    sa, sb = powers((P, n), g), powers((P, d), g)
+    blocks = offsets_of(blk)
+    want, _ = wgrad(a, sa, b, sb, blocks)
+    assert torch.equal(run_wgrad(a, sa, b, sb, blocks).double(), want)
+
+
 @pytest.mark.parametrize("blk,n,d", [([3, 0, 9], 272, 144), ([20, 4], 128, 1040)])
 def test_wgrad_against_64_bits(blk, n, d):
     g = torch.Generator(device="cuda").manual_seed(n)
