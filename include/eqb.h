@@ -638,7 +638,7 @@ int64_t eqb_expert_max_blocks(int64_t R, int32_t E);
 
 /* Values in 8 bits (e4m3) with an fp32 scale for each block of 128 of them:
  *   scale = max |x| * fp32(1 / 448), 0 if below 2^-126,
- *   code  = e4m3_rne(clamp(x * fp32(1 / scale), -448, 448)), 0 where scale is 0,
+ *   code  = e4m3_rne(clamp(x * fp32(1 / scale), -448, 448)), x's zero where scale is 0,
  * operation by operation in fp32 (x = code * scale to within half a step of
  * e4m3, 2^-4 of the value, or 2^-10 of the scale).  err_flag: EQB_ERR_NONFINITE
  * if a value that is read is not finite; its block's codes and scale are then

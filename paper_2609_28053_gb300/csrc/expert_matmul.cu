@@ -13,12 +13,13 @@
 //
 // What bounds it with many rows an expert is that way out.  R = 131,072, n = 2,048, d =
 // 4,096, 128 experts: 897 us and 2.45 PFLOP/s where all have the same number of rows, 947
-// us where some have a multiple of others'; a stage takes an SM about 970 clocks, of
-// which its MMAs are 512.  A warp that takes 32 rows x 128 columns of a stage out waits
-// three times for tensor memory (about 130 clocks whatever it asked for), and beside
-// 128 sums there are registers for 48 columns on their way.  Sixteen such warps would
-// hide that, but their registers do not fit.  The scales count too: every scale
-// fetched once, four stages at a time, took 947 us where each stage's own loads took 1,015.
+// where some have a multiple of others' (ten calls in a row; over seconds the power limit
+// lowers the clock, and the second takes 1,040 to 1,090).  A stage takes an SM about 970
+// clocks, of which its MMAs are 512.  A warp that takes 32 rows x 128 columns of a stage out
+// waits three times for tensor memory (about 130 clocks whatever it asked for), and
+// beside 128 sums there are registers for 48 columns on their way.  Sixteen such warps
+// would hide that, but their registers do not fit.  The scales count too: every scale
+// fetched once, four stages at a time, took 947 us where each stage's own loads took 1,030.
 // Pairs of SMs (cta_group::2) take in less a stage and were slower: tiles of 256 x 256
 // with two accumulators 1,025 us, of 256 x 160 with three 1,195.
 // Few rows an expert: the weights are what is read (256 rows in 109 of the 128 experts
