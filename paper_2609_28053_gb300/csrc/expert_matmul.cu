@@ -15,13 +15,17 @@
 // 4,096, 128 experts: 897 us and 2.45 PFLOP/s where all have the same number of rows, 947
 // where some have a multiple of others' (ten calls in a row; over seconds the power limit
 // lowers the clock, and the second takes 1,040 to 1,090).  A stage takes an SM about 970
-// clocks, of which its MMAs are 512.  A warp that takes 32 rows x 128 columns of a stage out
-// waits three times for tensor memory (about 130 clocks whatever it asked for), and
-// beside 128 sums there are registers for 48 columns on their way.  Sixteen such warps
-// would hide that, but their registers do not fit.  The scales count too: every scale
-// fetched once, four stages at a time, took 947 us where each stage's own loads took 1,030.
-// Pairs of SMs (cta_group::2) take in less a stage and were slower: tiles of 256 x 256
-// with two accumulators 1,025 us, of 256 x 160 with three 1,195.
+// clocks, of which its MMAs are 512: an accumulator goes round in 1,900, of which there
+// are two.  By clock stamps: 330 from the last warp's release to the first MMA, 800 until
+// the last is done and its barrier says so, 245 until the takers see it, 530 until
+// their loads are done: a warp waits three times for tensor memory (about 130 clocks
+// whatever it asked for), and beside 128 sums there are registers for 48 columns on
+// their way (64 with 24 bytes spilled: 1,120 us).  Tiles 192 wide, whose 96 columns a warp
+// come with one wait, took 1,140: a stage costs what it costs, and does less.  Polls
+// that do not suspend, 975.  The scales count too: every scale fetched once, four
+// stages at a time, took 947 us where each stage's own loads took 1,030.  Pairs of SMs
+// (cta_group::2) take in less a stage and were slower: tiles of 256 x 256 with two
+// accumulators 1,025 us, of 256 x 160 with three 1,195.
 // Few rows an expert: the weights are what is read (256 rows in 109 of the 128 experts
 // 138 us, 99% of the copy rate), and a tile of 128 rows needs no more of A than the
 // groups of 32 rows that there are.  Where the tiles of 256 columns leave SMs without
