@@ -12,7 +12,7 @@
 // off instead of rounding, 128 products long.
 //
 // What bounds it with many rows an expert is that way out.  R = 131,072, n = 2,048, d =
-// 4,096, 128 experts: 897 us and 2.45 PFLOP/s where all have the same number of rows, 947
+// 4,096, 128 experts: 897 us and 2.45 PFLOP/s where all have the same number of rows, 943
 // where some have a multiple of others' (ten calls in a row; over seconds the power limit
 // lowers the clock, and the second takes 1,040 to 1,090).  A stage takes an SM about 970
 // clocks, of which its MMAs are 512: an accumulator goes round in 1,900, of which there
@@ -162,8 +162,8 @@ __global__ void __launch_bounds__(kMmThreads, 1)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)  // 32 of K an MMA: 32 bytes
               umma_e4m3(tmem + buf * BN, ad0 + at + 2u * kk, bd0 + at + 2u * kk, idesc, kk > 0 ? 1u : 0u);
+            umma_commit(accf(buf));  // first: it is waited for (943 us, the other way round 947)
             umma_commit(empty(stage));
-            umma_commit(accf(buf));
           }
           __syncwarp();
           if (++stage == S) { stage = 0; phase ^= 1u; }

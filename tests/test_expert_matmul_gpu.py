@@ -177,10 +177,11 @@ def test_wgrad_exact_on_whole_numbers(blk, n, d, add):
     assert torch.equal(got, (want + dW0.double() if add else want).float())
 
 
-def test_wgrad_of_many_unlike_experts():
+@pytest.mark.parametrize("E,n,d", [(100, 144, 1040), (1024, 16, 2064), (1000, 16, 1808)])
+def test_wgrad_of_many_unlike_experts(E, n, d):
     """Tiles go by the experts' sizes, not by their numbers; equal and empty ones are among them."""
     g = torch.Generator(device="cuda").manual_seed(5)
-    blk, n, d = [(7 * e) % 5 if e % 3 else 0 for e in range(100)], 144, 1040
+    blk = [(7 * e) % 5 if e % 3 else 0 for e in range(E)]
     P = sum(blk)
     a, b = codes((n, P * 128), g, 2), codes((d, P * 128), g, 3)
     sa, sb = powers((P, n), g), powers((P, d), g)
