@@ -120,11 +120,15 @@ __device__ __forceinline__ int expert_of_block(const int32_t* __restrict__ block
 // columns: 16 codes of a column are 16 bytes of the output's line, so that nothing
 // is turned in shared memory and no warp waits for another; and of the 32 scales
 // every lane forms one.  The next step's values are copied into the warp's own part of
-// shared memory meanwhile (the lanes' registers have no room for them).  Blocks go over all rows of a group of columns first: a
-// gathered row is wanted by K experts at different times, and the group's columns of
-// every token stay in L2 in between.  T = 16,384, c = 4,096, K = 8, 128 experts:
-// 208 us; 218 with 128 x 64 a block, turned in shared memory, 444 with all of a
-// row of blocks at a time and a scale formed by every thread that needs it.
+// shared memory meanwhile (the lanes' registers have no room for them, nor for the
+// numbers of their rows: 208 us where they were kept and others spilled).  Blocks go over
+// all rows of a group of columns first: a gathered row is wanted by K experts at
+// different times, and the group's columns of every token stay in L2 in between.
+// T = 16,384, c = 4,096, K = 8, 128 experts: 194 us; 235 where 24 warps an SM read their
+// values twice instead of keeping them, 218 with 128 x 64 a block, turned in shared memory,
+// 444 with all of a row of blocks at a time and a scale formed by every thread that needs
+// it.  What bounds it is the instructions of 131,072 rows, not their memory: rows that are
+// read once (K = 1) come at 94% of the copy rate.
 constexpr int kColWarps = 8;
 constexpr int kColSteps = 4;  // of kColWarps * 32 columns a block, at most
 // 64 bytes of every row; 16 rows and 64 bytes apart, so that two lanes' rows lie in different banks
@@ -155,24 +159,24 @@ __global__ void __launch_bounds__(kColWarps * 32, 2) quant_cols_kernel(const Qua
     tokens[threadIdx.x] = n < a.T ? n : -1;
   }
   __syncthreads();
-  int from[16];  // the lane's rows; where there is none, zeros stay in their place
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int4 t = *reinterpret_cast<const int4*>(tokens + rg * 16 + 4 * i);
-    from[4 * i] = t.x; from[4 * i + 1] = t.y; from[4 * i + 2] = t.z; from[4 * i + 3] = t.w;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (from[i] < 0) *reinterpret_cast<uint4*>(mine + i * 64) = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = 0; i < 16; ++i)  // where there is no row, zeros stay in its place
+    if (tokens[rg * 16 + i] < 0) *reinterpret_cast<uint4*>(mine + i * 64) = make_uint4(0u, 0u, 0u, 0u);
   const int64_t pitch = a.P * kExpertBlock;
   auto fetch = [&](int j) {  // a lane copies what it reads itself
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
     if (j < c1) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (from[i] >= 0)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 64), "l"(a.x + static_cast<int64_t>(from[i]) * a.c + j)
-                       : "memory");
+      for (int g = 0; g < 4; ++g) {
+        const int4 t = *reinterpret_cast<const int4*>(tokens + rg * 16 + 4 * g);
+        const int from[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (from[i] >= 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (4 * g + i) * 64),
+                         "l"(a.x + static_cast<int64_t>(from[i]) * a.c + j)
+                         : "memory");
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
