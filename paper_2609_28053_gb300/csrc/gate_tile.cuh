@@ -269,7 +269,8 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
     uint32_t hits = 0u;
     if (!valid) open = 0u;
     {
-      const F2 less = splat2(-bound);
+      // +0 from a bound of either zero: -0 + -0 would be below, though the two are equal
+      const F2 less = splat2(__fsub_rn(0.f, bound));
       uint32_t word = 0u;
       int group = 0, left = gc;  // chunks of the group from here on
 #pragma unroll
