@@ -384,9 +384,11 @@ __global__ void __launch_bounds__(32 * kMaxGateWarps, 1) gate_tile_kernel(const 
 #pragma unroll
         for (int j = 0; j < KP; ++j) w[j] = w[j] > -INFINITY ? expf(w[j] - ref) : 0.f;
       }
-      const float f = a.sigmoid && !a.renorm ? a.scale : sum > 0.f ? __fdiv_rn(a.scale, sum) : 0.f;
+      // a sum of sigmoids is half at least: over twice the sum the factor becomes no larger
+      const bool plain = a.sigmoid && !a.renorm;
+      const float f = plain ? a.scale : sum > 0.f ? __fdiv_rn(a.scale, sum + sum) : 0.f;
 #pragma unroll
-      for (int j = 0; j < KP; ++j) w[j] = w[j] * f;
+      for (int j = 0; j < KP; ++j) w[j] = (plain ? w[j] : w[j] + w[j]) * f;
     }
     __syncwarp();  // every lane is done with the tile
     if (tl + 1 < te) {
