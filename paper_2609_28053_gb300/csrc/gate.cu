@@ -81,6 +81,13 @@ __device__ __forceinline__ float load1(const void* z, int64_t at) {
   return F32 ? __ldg(static_cast<const float*>(z) + at) : bf16_bits_to_f32(__ldg(static_cast<const uint16_t*>(z) + at));
 }
 
+// 1 / (1 + exp(-z)).  From -88.7 down exp(-z) is infinite, where exp(z) is still a number
+// (from -17 down the two are equal in fp32).
+__device__ __forceinline__ float sigmoid_of(float z) {
+  const bool low = z < -80.f;
+  const float n = expf(low ? z : -z);
+  return low ? n : 1.f / (1.f + n);
+}
 // sigmoid(z) of the entries that are there (z = -inf: not), each divided by their
 // sum.  The sigmoids are taken relative to exp(m), m = min(0, largest z), so that
 // however low the logits are the largest one does not underflow.
@@ -214,7 +221,7 @@ __global__ void __launch_bounds__(kGateWarps * 32) gate_warp_kernel(const GateAr
       const float z = mine >= 0 ? load1<F32>(a.z, t * E + mine) : -INFINITY;
       float w;
       if (a.renorm) w = a.sigmoid ? sigmoid_share(z) : softmax_share(z);
-      else if (a.sigmoid) w = 1.f / (1.f + expf(-z));
+      else if (a.sigmoid) w = sigmoid_of(z);
       else w = mine >= 0 ? expf(z - zmax) / zsum : 0.f;
       if (lane < K) a.weight[t * K + lane] = w * a.scale;
     }
@@ -328,9 +335,9 @@ __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGr
       }
       d = p * (d - gb) * a.scale;
     } else {
-      const float s1 = 1.f / (1.f + expf(z));  // 1 - s
+      const float s1 = sigmoid_of(-z);  // 1 - s
       if (!a.renorm) {
-        d = e >= 0 ? g * (1.f / (1.f + expf(-z))) * s1 * a.scale : 0.f;
+        d = e >= 0 ? g * sigmoid_of(z) * s1 * a.scale : 0.f;
       } else {
         const float m = lanes_max<LPT>(z), ref = a.sigmoid ? fminf(m, 0.f) : m;
         float u = 0.f;
