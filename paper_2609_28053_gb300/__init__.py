@@ -792,12 +792,16 @@ def eqb_quant_rows(x, slot=None, q=None, scale=None, err_flag=None, stream=None)
     return q, scale
 
 
-def eqb_quant_cols(x, offsets, blocks, entry=None, K=1, q=None, scale=None, err_flag=None, stream=None):
+def eqb_quant_cols(x, offsets, blocks, entry=None, K=None, q=None, scale=None, err_flag=None, stream=None):
     """The experts' rows in 8 bits, turned, with a scale for every 128 rows of an
     expert and column: the operands of eqb_expert_wgrad.  x bf16 [R,c] in sorted
-    rows, or with entry int32 [R] and K (eqb_expert_rows) [T,c] by token.  Returns
-    (q float8_e4m3fn [c, 128 P], scale fp32 [P,c]), P = eqb_expert_max_blocks(R, E)
-    unless q says otherwise."""
+    rows, or with entry int32 [R] (eqb_expert_rows) and K, the length of the lists,
+    [T,c] by token: entry i is of token i // K.  Returns (q float8_e4m3fn [c, 128 P],
+    scale fp32 [P,c]), P = eqb_expert_max_blocks(R, E) unless q says otherwise."""
+    if K is None:
+        if entry is not None:
+            raise ValueError("entry needs K: the lists' length says which token an entry is of")
+        K = 1
     T, c = _dims(x, 2, "x")
     _need(x, torch.bfloat16, "x")
     _on_current_device(x, "x")
