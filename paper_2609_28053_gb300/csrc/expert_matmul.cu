@@ -226,8 +226,9 @@ __global__ void __launch_bounds__(kMmThreads, 1)
       if (!ok) break;
       const Tile x = tile_of<kBM, BN, WG>(a, table, t, &e);
       const int col = x.n0 + h * kCols + quad;
-      if constexpr (WG) store_quads<kCols>(a, static_cast<int64_t>(x.e) * a.rows + x.m + line, x.rows - line, col, acc);
-      else if (line < x.rows) store_row<kCols>(a, static_cast<int64_t>(x.m) + line, col, acc);
+      if constexpr (WG) {  // nothing is added to an expert without blocks
+        if (x.kb > 0 || !a.add) store_quads<kCols>(a, static_cast<int64_t>(x.e) * a.rows + x.m + line, x.rows - line, col, acc);
+      } else if (line < x.rows) store_row<kCols>(a, static_cast<int64_t>(x.m) + line, col, acc);
     }
   }
   tc_fence_before();
