@@ -247,7 +247,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // The gradient.  LPT lanes take a token, eight neighbouring experts each and pass
 // (NC of them), and one entry of its list each.  The row is written from the
 // lanes' experts, then the list's entries once more by the lanes that hold them; the
-// barrier of the warp between the two orders the stores.
+// barrier of the warp between the two orders the stores, and one before them what
+// the entries' lanes have read of a row that is added to in place.
 template <int LPT, int NC, bool dense, bool F32, bool BF16>
 __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGradArgs a) {
   constexpr int kTokens = 32 / LPT;  // of a warp
@@ -358,6 +359,7 @@ __global__ void __launch_bounds__(kGateWarps * 32) gate_grad_kernel(const GateGr
       }
     }
     if (!in_place || dense) {
+      if (dense) __syncwarp();
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const int e0 = (c * LPT + sub) * 8;
