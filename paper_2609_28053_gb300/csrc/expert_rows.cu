@@ -25,6 +25,7 @@ constexpr int kRowsChunk = 4096;  // least entries of a chunk
 constexpr int kRowsChunks = 608;  // most chunks, about
 constexpr int kRowsAhead = 8;     // entries that a lane asks for together
 constexpr int kAddedCounts = 1 << 15;
+constexpr int kRowsFree = 47 * 1024;  // what every launch may have, less room for the kernel's static part
 
 struct RowsPlan {
   int chunks, per;  // per: entries of a chunk, a multiple of kRowsThreads
@@ -237,8 +238,7 @@ size_t expert_rows_workspace(int64_t n, int E) {
 int launch_expert_rows(const ExpertRowsArgs& a, cudaStream_t s) {
   const RowsPlan p = plan_rows(a.n);
   const int smem = (kRowsWarps + 3) * a.E * 4;
-  // above what every launch may have
-  if (smem > 48 * 1024 && !allow_smem(rows_place_kernel, (kRowsWarps + 3) * kMaxExperts * 4)) return kErrCuda;
+  if (smem > kRowsFree && !allow_smem(rows_place_kernel, (kRowsWarps + 3) * kMaxExperts * 4)) return kErrCuda;
   if (p.chunks > 1) {
     if (launch_dependent(rows_count_kernel, dim3(p.chunks), dim3(kRowsThreads), 0, s, a, p.per, p.chunks) != cudaSuccess)
       return kErrCuda;
