@@ -647,7 +647,11 @@ int64_t eqb_expert_max_blocks(int64_t R, int32_t E);
  * eqb_quant_rows: blocks of 128 neighbours in a row (the last of a row may be
  * shorter).  Without slot, row t of x becomes row t of q.  With slot [T,K], row t
  * becomes row slot[t,k] of q for every k whose slot lies in [0, T K); the others are
- * left out, and rows of q that no slot names are left as they are.
+ * left out, and rows of q that no slot names are left as they are; a token without a
+ * slot is not looked at.  Without slot all T rows are, and raise err_flag: of sorted rows
+ * those behind the last expert's too, which the calls below do not write.  They hold finite
+ * values (a buffer cleared when it is made), or are left out by a slot [R,1] of r, and -1
+ * where entry[r] is.
  *   x      device bf16 [T,d], 16-byte aligned
  *   q      device e4m3 (one byte) [T,d], with slot [T K, d]; 16-byte aligned (out)
  *   scale  device fp32 [rows of q, ceil(d / 128)] (out)

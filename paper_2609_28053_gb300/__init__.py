@@ -768,8 +768,9 @@ def _up(n):
 def eqb_quant_rows(x, slot=None, q=None, scale=None, err_flag=None, stream=None):
     """x bf16 [T,d] in 8 bits, with a scale for every 128 neighbours of a row.
     With slot int32 [T,K] (eqb_expert_rows) row t goes to the rows slot[t] of q
-    [T*K,d], those of -1 left out.  Returns (q float8_e4m3fn, scale fp32 [rows,
-    ceil(d/128)])."""
+    [T*K,d], those of -1 left out.  Without, every row of x is read: sorted rows
+    behind the last expert's have to hold something finite, or be left out by a slot
+    [R,1] (see eqb.h).  Returns (q float8_e4m3fn, scale fp32 [rows, ceil(d/128)])."""
     T, d = _dims(x, 2, "x")
     _need(x, torch.bfloat16, "x")
     _on_current_device(x, "x")
