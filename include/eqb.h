@@ -574,8 +574,10 @@ eqb_status eqb_adamw_step(const eqb_adamw_tensor *tensors, int32_t count, int32_
  *   weights  from the unbiased logits, s = sigmoid(z_t) or softmax(z_t) over all E
  *            experts: w_k = scale s_k, or with renorm scale s_k / (sum of the
  *            list's s).  An entry of -1 has weight 0.
- * Choice and ties are exact (fp32 sums and comparisons); the weights are fp32,
- * renormalised without underflow however low the logits are.
+ * Choice and ties are exact (fp32 sums and comparisons; -0 and +0 are equal); the
+ * weights are fp32, renormalised without underflow however low the logits are.  Calls
+ * of up to 4,096 tokens and calls of more divide and sum exponentials in other ways,
+ * so the last places of a token's weights can differ between them; its list does not.
  *   z        device bf16 [T,E], or fp32 with z_fp32 != 0; 16-byte aligned
  *   b        device fp32 [E] (nullable: 0)
  *   mask     device uint8 [T] (nullable): a token whose byte is 0 gets -1 and
@@ -602,7 +604,8 @@ eqb_status eqb_gate_topk(const void *z, int32_t z_fp32, const float *b, int64_t 
  * (d without grad_in): dL/dz as eqb_balance_loss takes it in grad_in, or, in bf16,
  * eqb_router_grad in dz.  A list entry outside [0, E) has no part in anything, and a
  * token without any other has d = 0, whatever its row of z holds.  An expert that a
- * list names twice counts as two entries whose terms are added.
+ * list names twice counts as two entries whose terms are added.  In the last kind a p
+ * below 2^-126 counts as 0.
  *   z, z_fp32, score, renorm, scale  as in eqb_gate_topk
  *   topk_idx     device int32 [T,K]; grad_weight device fp32 [T,K]
  *   grad_in      device fp32 [T,E], 16-byte aligned (nullable); of the first three

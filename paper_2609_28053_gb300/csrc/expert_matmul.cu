@@ -35,7 +35,10 @@
 // 65,536 over 64 experts, n = 1,024, d = 2,048: eight and a half), so the sums' way to
 // memory, 128 KB a tile, counts as well: 245 us where the output alone takes 79.  Whole lines
 // instead of sectors a store (248 where sectors took 253) and the two halves of a
-// tile as blocks of their own on one SM (282) did not change that.
+// tile as blocks of their own on one SM (282) did not change that.  Added to what is there
+// it takes 776 us (190 by the bytes; where they go is not measured).  A tile's stages are one
+// block's, so few tiles leave SMs idle: 131,072 rows, n = d = 64, 8 experts 88 us on 8 of them
+// (2.5 by the bytes).
 //
 // Roles: warp 0 loads, warp 1 issues the MMAs, warps 2 and 3 bring the scales'
 // products to shared memory (in the warps that need them they took the registers of
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(kMmThreads, 1)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)  // 32 of K an MMA: 32 bytes
               umma_e4m3(tmem + buf * BN, ad0 + at + 2u * kk, bd0 + at + 2u * kk, idesc, kk > 0 ? 1u : 0u);
-            umma_commit(accf(buf));  // first: it is waited for (943 us, the other way round 947)
+            umma_commit(accf(buf));  // first: it is waited for (the other way round no slower than runs differ)
             umma_commit(empty(stage));
           }
           __syncwarp();

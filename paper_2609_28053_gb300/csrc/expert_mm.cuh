@@ -115,7 +115,10 @@ __device__ __forceinline__ Tile tile_of(const MmArgs& a, const Table& table, int
 // tile, differs by no more than one tile's blocks.  R = 65,536 over 64 experts, n = 1,024, d =
 // 2,048: 245 us, in the experts' order 253, with rows an expert whose logarithm deviates
 // by 0.5 from its mean; by 1.5, 262 and 295.  Experts of few tiles keep their order:
-// sorting takes 8 us of 1,024 (n = 128, d = 256, one tile an expert: 36 us, sorted 44).
+// sorting takes 2 us of 128 experts and 8 of 1,024.  us sorted / in order, by 0.5 and by 1.5:
+// 128 experts, 512 rows each on the mean, of 1 tile 18.5 / 16.2 and 51 / 49, of 4 38 / 35 and 67 /
+// 60, of 8 54 / 54 and 82 / 84, of 16 95 / 93 and 118 / 129; 1,024 experts, 128 rows, of 1 tile 48 /
+// 40 and 63 / 54, of 8 239 / 219 and 247 / 242; 64 experts, 2,048 rows, of 8 79 / 74 and 177 / 172.
 constexpr int kOrderTiles = 8;
 template <int BM, bool WG>
 __device__ __forceinline__ void fill_table(const MmArgs& a, Table& table) {

@@ -17,8 +17,12 @@ namespace eqb {
 namespace {
 
 constexpr int kGateWarps = 4;
-// Up to here a warp a token (E = 256 in groups, T = 4,096: 11.1 us, 8,192: 16.6, where
-// a thread a token takes 12.5).
+// Up to here a warp a token.  us of a warp / of a thread a token (bf16, K = 8, sigmoids
+// renormalised, launches in a graph) at T = 2,048, 4,096 and 8,192: E = 40 4.0 / 7.1, 5.6 /
+// 7.2, 9.2 / 7.3; E = 128 4.2 / 5.9, 5.8 / 6.0, 9.5 / 6.2; E = 256 4.3 / 7.8, 6.3 / 8.1, 10.0 /
+// 7.9, in 8 groups 6.6 / 8.2, 9.7 / 8.7, 15.4 / 8.4; E = 512 6.3 / 10.7, 9.3 / 11.2, 15.2 / 11.3,
+// in 8 groups 9.6 / 11.0, 15.2 / 12.0, 24.3 / 11.8.  fp32 and softmax over all are alike: the
+// two meet between 2,048 and about 8,192 tokens at every width from 8 to 512.
 constexpr int64_t kFewGateTokens = 4096;
 constexpr uint32_t kClosed = 0x007fffffu;  // the key of -inf: an open expert's is larger
 
