@@ -444,9 +444,9 @@ int launch_tile(const GateArgs& a, cudaStream_t s) {
 }
 
 // The widths of the workloads are known at compile time; others take eight parts and
-// loops of their length.  T = 524,288, K = 8, bf16, sigmoids renormalised: E = 128 58.8 us (42%
-// of the time its bytes need at the copy rate), 256 88.1 (51%), 512 210 (40%); E = 40 54.0 (21%),
-// 160 80.1 (37%), 320 142 (38%), 384 165 (39%).
+// loops of their length.  T = 524,288, K = 8, bf16, sigmoids renormalised: E = 128 58.8 us (the
+// bytes at the copy rate are 42% of that), 256 88.1 (51%), 512 210 (40%); E = 40 54.0 (21%), 160
+// 80.1 (37%), 320 142 (38%), 384 165 (39%).
 template <bool F32, int G>
 int launch_tile_width(const GateArgs& a, cudaStream_t s) {
   if (a.E == 64) return launch_tile<F32, G, 8, 1>(a, s);
